@@ -73,7 +73,8 @@ enum { ARMOR_AB_EXACT = 0, ARMOR_AB_GD = 1, ARMOR_AB_ADAM = 2 };
  *            with the block-diagonal wrappers are the same in both modes. */
 enum { ARMOR_PREC_FP32X3 = 0, ARMOR_PREC_TF32 = 1, ARMOR_PREC_SIMT = 2, ARMOR_PREC_FP16X3 = 3 };
 enum { ARMOR_PHASE_A = 1, ARMOR_PHASE_B = 2, ARMOR_PHASE_S = 4, ARMOR_PHASE_MASK = 8 };
-enum { ARMOR_DTYPE_F32 = 0, ARMOR_DTYPE_BF16 = 1, ARMOR_DTYPE_BF16_SPARSE = 2 };
+enum { ARMOR_DTYPE_F32 = 0, ARMOR_DTYPE_BF16 = 1, ARMOR_DTYPE_BF16_SPARSE = 2,
+       ARMOR_DTYPE_F16 = 3, ARMOR_DTYPE_I8 = 4 /* the 8-bit products and the norms only */ };
 
 typedef struct {
   int64_t d_out, d_in;
@@ -228,6 +229,42 @@ armor_status armor_pack_layer(armor_ctx* ctx, const float* d_A, const float* d_B
                               const float* d_r1, const float* d_r2, void* d_packed, armor_stream_t stream);
 armor_status armor_apply_layer(armor_ctx* ctx, const void* d_packed, const void* d_x, void* d_y, int64_t n_tokens,
                                armor_stream_t stream);
+
+/* ---- 8-bit products -------------------------------------------------------------------------------------------
+ * Rows as int8 with a scale each: a_t = max_c |x[t][c]|, d_scale[t] = a_t / 127 (rounded to fp32), d_q[t][c] = 127 x[t][c] / a_t
+ * rounded to the nearest integer, ties to even -- the exact quotient's, whatever the type of x.  A row of zeros gets scale 0 and
+ * zeros; a row that holds a NaN or an infinity gets scale NaN and zeros, so that what is made of it is NaN.
+ * x [n_rows, n_cols] of x_dtype (F32, BF16, F16) with leading dimension ldx (elements, any alignment of its rows); d_q [n_rows, ldq],
+ * 16-byte aligned, ldq a multiple of 16 and at least n_cols (columns behind n_cols may be written with zeros).  n_rows == 0 is a
+ * no-op.  Errors: INVALID_ARG, SHAPE (sizes, leading dimensions), UNSUPPORTED (x_dtype).  Any sizes: none of the calls of this section
+ * but armor_*_layer_i8 depends on the context's shape. */
+armor_status armor_quantize_rows(armor_ctx* ctx, const void* d_x, int32_t x_dtype, int64_t ldx, int64_t n_rows, int64_t n_cols,
+                                 int8_t* d_q, int64_t ldq, float* d_scale, armor_stream_t stream);
+
+/* A linear layer in 8 bits: y[t][m] = x_scale[t] w_scale[m] sum_k xq[t][k] wq[m][k] (+ bias[m]), the sum exact in int32.
+ *   x_dtype I8: d_x holds xq [n_tokens, n_in] (leading dimension ldx) and d_x_scale [n_tokens] its scales;
+ *   x_dtype F32, BF16, F16: x is rounded by armor_quantize_rows into the context's workspace first (d_x_scale NULL).
+ * wq [n_out, n_in] with leading dimension ldw, w_scale [n_out], bias [n_out] fp32 or NULL; y [n_tokens, n_out] with leading dimension
+ * ldy in y_dtype (F32, BF16, F16), rounded once from fp32.  wq (and xq where given) are 16-byte aligned with leading dimensions that are
+ * multiples of 16; any n_out, n_in and n_tokens; columns behind n_in are not read.  y must not overlap x.  Errors: INVALID_ARG,
+ * SHAPE (sizes below one, leading dimensions, alignment), UNSUPPORTED (types), TOO_LARGE (n_in above 131,071, where a sum
+ * of products of -128 would leave int32; n_out or n_tokens above 2^30), WORKSPACE (not even one token fits the workspace). */
+armor_status armor_linear_i8(armor_ctx* ctx, const void* d_x, int32_t x_dtype, int64_t ldx, const float* d_x_scale, const int8_t* d_wq,
+                             int64_t ldw, const float* d_w_scale, const float* d_bias, void* d_y, int32_t y_dtype, int64_t ldy,
+                             int64_t n_tokens, int64_t n_out, int64_t n_in, armor_stream_t stream);
+
+/* The packed layer of armor_pack_layer with its core in 8 bits: kept values as int8 with a scale for each row of S (rounded as
+ * armor_quantize_rows has it, over what the row keeps), 0.625 bytes for an entry of S where the bf16 core has 1.125; the wrappers are
+ * bf16 as there.  armor_apply_layer_i8: bf16 x [n_tokens, d_in] -> bf16 y [n_tokens, d_out] (both 16-byte aligned):
+ *   z1 = (r1 . x) B^T, rounded from fp32 to int8 with a scale for each token; z2 = z1 S^T on the sparse tensor cores, exact int32
+ *   sums, scaled and rounded to bf16; y = r2 . (z2 A^T).
+ * Same shapes and errors as armor_pack_layer and armor_apply_layer; a group of d_M with more than two kept positions raises
+ * device status word 4 and contributes its first two. */
+armor_status armor_packed_layer_i8_bytes(const armor_config* cfg, size_t* out_bytes);
+armor_status armor_pack_layer_i8(armor_ctx* ctx, const float* d_A, const float* d_B, const float* d_S, const uint8_t* d_M,
+                                 const float* d_r1, const float* d_r2, void* d_packed, armor_stream_t stream);
+armor_status armor_apply_layer_i8(armor_ctx* ctx, const void* d_packed, const void* d_x, void* d_y, int64_t n_tokens,
+                                  armor_stream_t stream);
 
 /* Copies up to n (at most 16) device status words to h_codes (host).
  *   word 0: Cholesky failures since the context was created; word 1: first failing block id + 1;

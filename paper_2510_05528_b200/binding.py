@@ -22,11 +22,14 @@ S_EXACT, S_BETA = 0, 1
 AB_EXACT, AB_GD, AB_ADAM = 0, 1, 2
 PREC_FP32X3, PREC_TF32, PREC_SIMT, PREC_FP16X3 = 0, 1, 2, 3
 PHASE_A, PHASE_B, PHASE_S, PHASE_MASK = 1, 2, 4, 8
-DTYPE_F32, DTYPE_BF16, DTYPE_BF16_SPARSE = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_BF16_SPARSE, DTYPE_F16, DTYPE_I8 = 0, 1, 2, 3, 4
+# element types of the 8-bit products and of the norms
+ROW_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 EXPORTS = ["armor_workspace_bytes", "armor_create", "armor_destroy", "armor_gram", "armor_init",
            "armor_bcd_step", "armor_proxy_loss", "armor_apply", "armor_packed_core_bytes", "armor_pack_core", "armor_apply_packed",
            "armor_packed_layer_bytes", "armor_pack_layer", "armor_apply_layer",
+           "armor_quantize_rows", "armor_linear_i8", "armor_packed_layer_i8_bytes", "armor_pack_layer_i8", "armor_apply_layer_i8",
            "armor_get_device_status",
            "armor_status_string", "armor_launch_count", "armor_gemm_timing_enable", "armor_gemm_timing",
            "armor_normalize_noalloc", "armor_block_product", "armor_block_product_dual", "armor_block_product_two_sided", "armor_selftest_wait_timeout", "armor_kernel_timing_enable", "armor_use_graphs", "armor_fuse_grams",
@@ -77,6 +80,11 @@ def lib() -> C.CDLL:
         L.armor_packed_layer_bytes.argtypes = [C.POINTER(armor_config), C.POINTER(C.c_size_t)]
         L.armor_pack_layer.argtypes = [vp] + [vp] * 7 + [vp]
         L.armor_apply_layer.argtypes = [vp, vp, vp, vp, i64, vp]
+        L.armor_quantize_rows.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, vp, vp]
+        L.armor_linear_i8.argtypes = [vp, vp, i32, i64, vp, vp, i64, vp, vp, vp, i32, i64, i64, i64, i64, vp]
+        L.armor_packed_layer_i8_bytes.argtypes = [C.POINTER(armor_config), C.POINTER(C.c_size_t)]
+        L.armor_pack_layer_i8.argtypes = [vp] + [vp] * 7 + [vp]
+        L.armor_apply_layer_i8.argtypes = [vp, vp, vp, vp, i64, vp]
         L.armor_get_device_status.argtypes = [vp, C.POINTER(i32), i32]
         L.armor_status_string.argtypes = [C.c_int]
         L.armor_status_string.restype = C.c_char_p
@@ -240,6 +248,85 @@ def armor_apply_layer(ctx, packed, x, y) -> None:
         _check(code, "armor_apply_layer")
 
 
+def _row_ptr(t: torch.Tensor | None, dtype, name: str, cols: int | None = None) -> tuple[int | None, int]:
+    """(address, leading dimension) of rows [n, cols] with unit column stride; (None, 0) of None."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor (this library has no CPU path)")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    shape = t.shape
+    if len(shape) != 2 or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name} must be [rows, {'cols' if cols is None else cols}], got {list(shape)}")
+    n, c = shape
+    ld, one = t.stride()
+    if n <= 1 and ld < c:                            # a single row's stride says nothing
+        ld = c
+    if (one != 1 and c > 1) or ld < c:
+        raise ValueError(f"{name} must have unit column stride and rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _row_dtype(t: torch.Tensor, name: str) -> int:
+    code = ROW_DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def armor_quantize_rows(ctx, x, q, scale) -> None:
+    """q [n, c] int8 (rows on 16-byte boundaries) and scale [n] fp32 of x [n, c] (see armor.h)."""
+    code = _row_dtype(x, "x")
+    xp, ldx = _row_ptr(x, x.dtype, "x")
+    n, c = x.shape
+    qp, ldq = _row_ptr(q, torch.int8, "q", c)
+    if q.shape[0] != n or scale.numel() != n:
+        raise ValueError(f"q and scale must have the {n} rows of x")
+    _check(lib().armor_quantize_rows(ctx, xp, code, ldx, n, c, qp, ldq, _ptr(scale, torch.float32, "scale"), _stream()),
+           "armor_quantize_rows")
+
+
+def armor_linear_i8(ctx, x, x_scale, wq, w_scale, bias, y) -> None:
+    """y [n, n_out] = x [n, n_in] wq^T with the scales of both (see armor.h); x_scale None: x is rounded on the way."""
+    f = torch.float32
+    code = DTYPE_I8 if x.dtype is torch.int8 else _row_dtype(x, "x")
+    xp, ldx = _row_ptr(x, x.dtype, "x")
+    n, n_in = x.shape
+    wp, ldw = _row_ptr(wq, torch.int8, "wq", n_in)
+    n_out = wq.shape[0]
+    yp, ldy = _row_ptr(y, y.dtype, "y", n_out)
+    if y.shape[0] != n or w_scale.numel() != n_out or (bias is not None and bias.numel() != n_out) or \
+            (x_scale is not None and x_scale.numel() != n):
+        raise ValueError(f"y and x_scale must have the {n} rows of x, w_scale and bias the {n_out} of wq")
+    code = lib().armor_linear_i8(ctx, xp, code, ldx, _ptr(x_scale, f, "x_scale"), wp, ldw, _ptr(w_scale, f, "w_scale"),
+                                 _ptr(bias, f, "bias"), yp, _row_dtype(y, "y"), ldy, n, n_out, n_in, _stream())
+    if code:
+        _check(code, "armor_linear_i8")
+
+
+def armor_packed_layer_i8_bytes(cfg: armor_config) -> int:
+    n = C.c_size_t(0)
+    _check(lib().armor_packed_layer_i8_bytes(C.byref(cfg), C.byref(n)), "armor_packed_layer_i8_bytes")
+    return int(n.value)
+
+
+def armor_pack_layer_i8(ctx, A, B, S, M, r1, r2, packed) -> None:
+    f = torch.float32
+    _check(lib().armor_pack_layer_i8(ctx, _ptr(A, f, "A"), _ptr(B, f, "B"), _ptr(S, f, "S"), _ptr(M, torch.uint8, "M"),
+                                     _ptr(r1, f, "r1"), _ptr(r2, f, "r2"), _ptr(packed, torch.uint8, "packed"), _stream()),
+           "armor_pack_layer_i8")
+
+
+def armor_apply_layer_i8(ctx, packed, x, y) -> None:
+    bf16 = torch.bfloat16
+    if x.dtype is not bf16 or y.dtype is not bf16:
+        raise ValueError("the packed layer takes bf16 x and y")
+    code = lib().armor_apply_layer_i8(ctx, _ptr(packed, torch.uint8, "packed"), _ptr(x, None, "x"), _ptr(y, None, "y"), x.shape[0], _stream())
+    if code:
+        _check(code, "armor_apply_layer_i8")
+
+
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
     buf = (C.c_int32 * n)()
     _check(lib().armor_get_device_status(ctx, buf, n), "armor_get_device_status")
@@ -347,6 +434,8 @@ class ArmorContext:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("ArmorContext needs a CUDA device")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.cfg = make_config(d_out, d_in, d_block, **kw)
         self.d_out, self.d_in, self.d_block = d_out, d_in, d_block
         nbytes = armor_workspace_bytes(self.cfg)
@@ -433,6 +522,52 @@ class ArmorContext:
     def apply_layer(self, packed: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
         y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
         armor_apply_layer(self.ctx, packed, x, y)
+        return y
+
+    # -- 8-bit products
+    def _here(self, *tensors) -> None:
+        """The context's device is the current one and holds every tensor given: the calls enqueue on its current stream."""
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"the context is on {self.device}, a tensor on {t.device}")
+        if torch._C._cuda_getDevice() != self.device.index:
+            raise ValueError(f"{self.device} must be the current device")
+
+    def new_int8_rows(self, n: int, cols: int) -> torch.Tensor:
+        """[n, cols] int8 whose rows start on 16-byte boundaries."""
+        return torch.empty(n, (cols + 15) // 16 * 16, dtype=torch.int8, device=self.device)[:, :cols]
+
+    def quantize_rows(self, x: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+        """The rows of x (tokens, or the output channels of a weight) as int8 with an fp32 scale each."""
+        self._here(x)
+        q = self.new_int8_rows(x.shape[0], x.shape[1])
+        scale = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
+        armor_quantize_rows(self.ctx, x, q, scale)
+        return q, scale
+
+    def linear_i8(self, x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, *, bias: torch.Tensor | None = None,
+                  x_scale: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
+        """y = x W^T (+ bias) in 8 bits with W = w_scale wq as quantize_rows gives it.  x: fp32, bf16 or fp16 (rounded to int8 here), or
+        int8 with its x_scale; out_dtype: x's by default, bf16 for int8."""
+        self._here(x, wq, w_scale, bias, x_scale)
+        if out_dtype is None:
+            out_dtype = torch.bfloat16 if x.dtype is torch.int8 else x.dtype
+        y = torch.empty(x.shape[0], wq.shape[0], dtype=out_dtype, device=self.device)
+        armor_linear_i8(self.ctx, x, x_scale, wq, w_scale, bias, y)
+        return y
+
+    def pack_layer_i8(self, st: LayerState, denormalize: bool = False) -> torch.Tensor:
+        """Core in 8 bits (a scale for each row) and bf16 wrappers, packed for apply_layer_i8."""
+        self._here(st.A, st.B, st.S, st.M)
+        packed = torch.empty(armor_packed_layer_i8_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+        r1, r2 = (st.r1, st.r2) if denormalize else (None, None)
+        armor_pack_layer_i8(self.ctx, st.A, st.B, st.S, st.M, r1, r2, packed)
+        return packed
+
+    def apply_layer_i8(self, packed: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
+        self._here(packed, x)
+        y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
+        armor_apply_layer_i8(self.ctx, packed, x, y)
         return y
 
     def device_status(self) -> list[int]:

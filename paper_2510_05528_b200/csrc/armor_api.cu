@@ -280,13 +280,13 @@ const char* armor_status_string(armor_status st) {
   switch (st) {
     case ARMOR_OK: return "ok";
     case ARMOR_ERR_INVALID_ARG: return "invalid argument";
-    case ARMOR_ERR_SHAPE: return "shape error: d_block must divide d_out and d_in, m_group must divide d_block";
+    case ARMOR_ERR_SHAPE: return "shape error: sizes, leading dimensions or alignment (d_block must divide d_out and d_in, m_group must divide d_block)";
     case ARMOR_ERR_WORKSPACE: return "workspace too small or misaligned";
     case ARMOR_ERR_CUDA: return "CUDA runtime error";
     case ARMOR_ERR_NOT_SPD: return "block not positive definite";
     case ARMOR_ERR_TIMEOUT: return "bounded device wait ran out";
     case ARMOR_ERR_UNSUPPORTED: return "configuration not supported";
-    case ARMOR_ERR_TOO_LARGE: return "size exceeds the built-in scratch of the no-allocation entry point";
+    case ARMOR_ERR_TOO_LARGE: return "size exceeds a limit of the entry point";
   }
   return "unknown status";
 }
@@ -971,6 +971,137 @@ armor_status armor_apply_layer(armor_ctx* c, const void* d_packed, const void* d
     st = launch_tc_sparse(c, buf, buf + tc_sparse_values_bytes(c), c->T, c->V, true, n, s);   // z2 = z1 S^T
     if (st != ARMOR_OK) return st;
     st = launch_fwd_block(c, c->V, buf + layer_off_A(c), yc, n, d_out, s);                    // y = r2 . (z2 A^T)
+    if (st != ARMOR_OK) return st;
+  }
+  return finish_call(c);
+}
+
+// ---- 8-bit products (their sizes and types are looked at before the context) -------------------------------------
+armor_status armor_quantize_rows(armor_ctx* c, const void* d_x, int32_t x_dtype, int64_t ldx, int64_t n_rows, int64_t n_cols, int8_t* d_q,
+                                 int64_t ldq, float* d_scale, armor_stream_t stream) {
+  if (n_rows < 0) return ARMOR_ERR_INVALID_ARG;
+  if (!rows_dtype_bytes(x_dtype)) return ARMOR_ERR_UNSUPPORTED;
+  if (n_cols < 1 || ldx < n_cols || ldq < n_cols || ldq % 16 || reinterpret_cast<uintptr_t>(d_q) % 16) return ARMOR_ERR_SHAPE;
+  if (!c) return ARMOR_ERR_INVALID_ARG;
+  if (n_rows == 0) return ARMOR_OK;
+  if (!d_x || !d_q || !d_scale) return ARMOR_ERR_INVALID_ARG;
+  const armor_status st = launch_quantize_rows(c, d_x, x_dtype, ldx, n_rows, n_cols, d_q, ldq, d_scale, cs(stream));
+  return st == ARMOR_OK ? finish_call(c) : st;
+}
+
+armor_status armor_linear_i8(armor_ctx* c, const void* d_x, int32_t x_dtype, int64_t ldx, const float* d_x_scale, const int8_t* d_wq,
+                             int64_t ldw, const float* d_w_scale, const float* d_bias, void* d_y, int32_t y_dtype, int64_t ldy,
+                             int64_t n_tokens, int64_t n_out, int64_t n_in, armor_stream_t stream) {
+  if (n_tokens < 0) return ARMOR_ERR_INVALID_ARG;
+  const bool given = x_dtype == ARMOR_DTYPE_I8;
+  const int64_t xb = given ? 1 : rows_dtype_bytes(x_dtype), yb = rows_dtype_bytes(y_dtype);
+  if (!xb || !yb) return ARMOR_ERR_UNSUPPORTED;
+  if (n_out < 1 || n_in < 1 || ldx < n_in || ldw < n_in || ldy < n_out || ldw % 16 || (given && ldx % 16)) return ARMOR_ERR_SHAPE;
+  if (n_in > 131071 || n_out > (1 << 30) || n_tokens > (1 << 30)) return ARMOR_ERR_TOO_LARGE;
+  if (reinterpret_cast<uintptr_t>(d_wq) % 16 || (given && reinterpret_cast<uintptr_t>(d_x) % 16)) return ARMOR_ERR_SHAPE;
+  if (!c) return ARMOR_ERR_INVALID_ARG;
+  if (n_tokens == 0) return ARMOR_OK;
+  if (!d_x || !d_wq || !d_w_scale || !d_y || given != (d_x_scale != nullptr)) return ARMOR_ERR_INVALID_ARG;
+  cudaStream_t s = cs(stream);
+  if (given) {
+    const armor_status st = launch_linear_i8(c, static_cast<const int8_t*>(d_x), ldx, d_x_scale, d_wq, ldw, d_w_scale, d_bias, d_y, y_dtype, ldy,
+                                             n_tokens, n_out, n_in, false, s);
+    return st == ARMOR_OK ? finish_call(c) : st;
+  }
+  // the tokens' int8 rows, then their scales, in the workspace; more tokens than it holds in chunks
+  const int64_t ldq = (n_in + 15) / 16 * 16;
+  int64_t chunk = (ws_scratch_bytes(c) - 256) / (ldq + 4);
+  if (chunk < 1) return ARMOR_ERR_WORKSPACE;
+  if (chunk > n_tokens) chunk = n_tokens;
+  int8_t* const xq = reinterpret_cast<int8_t*>(c->T);
+  float* const xs = reinterpret_cast<float*>(xq + (chunk * ldq + 255) / 256 * 256);
+  for (int64_t t0 = 0; t0 < n_tokens; t0 += chunk) {
+    const int64_t n = n_tokens - t0 < chunk ? n_tokens - t0 : chunk;
+    armor_status st = launch_quantize_rows(c, static_cast<const char*>(d_x) + t0 * ldx * xb, x_dtype, ldx, n, n_in, xq, ldq, xs, s);
+    if (st == ARMOR_OK)
+      st = launch_linear_i8(c, xq, ldq, xs, d_wq, ldw, d_w_scale, d_bias, static_cast<char*>(d_y) + t0 * ldy * yb, y_dtype, ldy, n, n_out, n_in, true, s);
+    if (st != ARMOR_OK) return st;
+  }
+  return finish_call(c);
+}
+
+// The layer with its core in 8 bits: kept values, positions, B blocks, A blocks, the core's scales
+struct LayerI8 { size_t e, b, a, scale, total; };
+static LayerI8 layer_i8(int64_t d_out, int64_t d_in, int64_t db) {
+  LayerI8 l;
+  l.e = (size_t)(d_out * d_in) / 2;
+  l.b = l.e + packed_core_i8_e_bytes(d_out, d_in);
+  l.a = l.b + (size_t)(d_in * db) * 2;
+  l.scale = l.a + (size_t)(d_out * db) * 2;
+  l.total = l.scale + (size_t)d_out * sizeof(float);
+  return l;
+}
+
+armor_status armor_packed_layer_i8_bytes(const armor_config* cfg, size_t* out_bytes) {
+  size_t bf16 = 0;
+  const armor_status st = armor_packed_layer_bytes(cfg, &bf16);    // the same shapes
+  if (st != ARMOR_OK || !out_bytes) return st != ARMOR_OK ? st : ARMOR_ERR_INVALID_ARG;
+  *out_bytes = layer_i8(cfg->d_out, cfg->d_in, cfg->d_block).total;
+  return ARMOR_OK;
+}
+
+armor_status armor_pack_layer_i8(armor_ctx* c, const float* A, const float* B, const float* S, const uint8_t* M, const float* r1,
+                                 const float* r2, void* d_packed, armor_stream_t stream) {
+  if (!c || !A || !B || !S || !M || !d_packed) return ARMOR_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(d_packed) % 128 || (r1 == nullptr) != (r2 == nullptr)) return ARMOR_ERR_INVALID_ARG;
+  if (!tc_sparse_ok(c) || !fwd_block_ok(c)) return ARMOR_ERR_UNSUPPORTED;
+  cudaStream_t s = cs(stream);
+  char* buf = static_cast<char*>(d_packed);
+  const LayerI8 l = layer_i8(c->d_out, c->d_in, c->db);
+  const armor_status st = launch_pack_core_i8(c, S, M, reinterpret_cast<int8_t*>(buf), buf + l.e, reinterpret_cast<float*>(buf + l.scale), s);
+  if (st != ARMOR_OK) return st;
+  launch_pack_blocks(c, B, nullptr, r1, buf + l.b, c->nbi, s);
+  launch_pack_blocks(c, A, r2, nullptr, buf + l.a, c->nbo, s);
+  return finish_call(c);
+}
+
+armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void* d_x, void* d_y, int64_t n_tokens, armor_stream_t stream) {
+  if (!c || !d_packed || n_tokens < 0) return ARMOR_ERR_INVALID_ARG;
+  if (n_tokens == 0) return ARMOR_OK;
+  if (!d_x || !d_y || reinterpret_cast<uintptr_t>(d_packed) % 128) return ARMOR_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(d_x) % 16 || reinterpret_cast<uintptr_t>(d_y) % 16) return ARMOR_ERR_INVALID_ARG;
+  if (!tc_sparse_ok(c) || !fwd_block_ok(c)) return ARMOR_ERR_UNSUPPORTED;
+  cudaStream_t s = cs(stream);
+  const char* buf = static_cast<const char*>(d_packed);
+  const int64_t d_out = c->d_out, d_in = c->d_in;
+  const LayerI8 l = layer_i8(d_out, d_in, c->db);
+  const int8_t* const core = reinterpret_cast<const int8_t*>(buf);
+  const float* const core_scale = reinterpret_cast<const float*>(buf + l.scale);
+  char* const scratch = reinterpret_cast<char*>(c->T);
+  auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
+  if (n_tokens <= ARMOR_SMALL_TOKENS) {
+    // z1 and z2 in fp32 (z2 is rounded to bf16 by the product with A): 5 d_in n + 4 d_out n bytes, n at most d_in and d_out
+    float* const z1 = reinterpret_cast<float*>(scratch);
+    int8_t* const zq = reinterpret_cast<int8_t*>(scratch + up(4 * n_tokens * d_in));
+    float* const zs = reinterpret_cast<float*>(zq + up(n_tokens * d_in));
+    float* const z2 = reinterpret_cast<float*>(reinterpret_cast<char*>(zs) + up(4 * n_tokens));
+    armor_status st = launch_fwd_small(c, d_x, 0, buf + l.b, z1, n_tokens, d_in, s, true);
+    if (st == ARMOR_OK) st = launch_quantize_rows(c, z1, ARMOR_DTYPE_F32, d_in, n_tokens, d_in, zq, d_in, zs, s);
+    if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_F32, n_tokens, true, s);
+    if (st == ARMOR_OK) st = launch_fwd_small(c, z2, 1, buf + l.a, d_y, n_tokens, d_out, s);
+    return st == ARMOR_OK ? finish_call(c) : st;
+  }
+  // a chunk: int8 z1 [chunk, d_in], its maxima and scales, bf16 z2 [chunk, d_out], 24 of the workspace's 40 bytes an entry of S at most
+  const int64_t least = d_out < d_in ? d_out : d_in;
+  const int64_t chunk = 8 * least < n_tokens ? 8 * least : n_tokens;
+  int8_t* const zq = reinterpret_cast<int8_t*>(scratch);
+  unsigned* const top = reinterpret_cast<unsigned*>(scratch + up(chunk * d_in));
+  float* const zs = reinterpret_cast<float*>(reinterpret_cast<char*>(top) + up(4 * chunk));
+  char* const z2 = reinterpret_cast<char*>(zs) + up(4 * chunk);
+  for (int64_t t0 = 0; t0 < n_tokens; t0 += chunk) {
+    const int64_t n = n_tokens - t0 < chunk ? n_tokens - t0 : chunk;
+    const char* xc = static_cast<const char*>(d_x) + (size_t)(t0 * d_in) * 2;
+    char* yc = static_cast<char*>(d_y) + (size_t)(t0 * d_out) * 2;
+    ARMOR_CUDA_OK(cudaMemsetAsync(top, 0, (size_t)n * 4, s));
+    armor_status st = launch_fwd_block_top(c, xc, buf + l.b, top, n, d_in, s);
+    if (st == ARMOR_OK) st = launch_fwd_block_i8(c, xc, buf + l.b, top, zq, zs, n, d_in, s);
+    if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_BF16, n, false, s);
+    if (st == ARMOR_OK) st = launch_fwd_block(c, z2, buf + l.a, yc, n, d_out, s);
     if (st != ARMOR_OK) return st;
   }
   return finish_call(c);

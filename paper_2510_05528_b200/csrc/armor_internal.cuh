@@ -510,10 +510,30 @@ void launch_pack_blocks(armor_ctx* c, const float* P, const float* rowscale, con
                         cudaStream_t s);
 armor_status launch_fwd_block(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d,
                               cudaStream_t s);
+// The same product rounded to int8 rows with a scale each, in two passes: the rows' maxima (bits of |.|, added to what top holds), then
+// the values.  The product itself is in no memory.
+armor_status launch_fwd_block_top(armor_ctx* c, const void* X, const void* Q, unsigned* top, int64_t rows, int64_t d, cudaStream_t s);
+armor_status launch_fwd_block_i8(armor_ctx* c, const void* X, const void* Q, const unsigned* top, int8_t* q, float* scale, int64_t rows,
+                                 int64_t d, cudaStream_t s);
 // Few tokens (decoding): up to this many, and beyond while the layer is small (fwd_is_small), the three products of the bf16 forward
 // run as latency-bound kernels whose contraction over d_in is split over the chip; the tiles of the persistent kernels fill it themselves.
 static const int64_t ARMOR_SMALL_TOKENS = 128;
 armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const void* Q, void* out, int64_t rows, int64_t d,
-                              cudaStream_t s);
+                              cudaStream_t s, bool out_f32 = false);
 armor_status launch_tc_sparse_small(armor_ctx* c, const void* Sc, const void* E, const void* z1_bf16, float* Zp, int64_t n,
                                     int* pieces, cudaStream_t s);
+
+// ---------------------------------------------------------------- 8-bit products (quant_i8.cu, i8_tcgen05.cu)
+// bytes of an element of an ARMOR_DTYPE_* that rows are given in; 0: none of them
+int rows_dtype_bytes(int32_t dtype);
+armor_status launch_quantize_rows(armor_ctx* c, const void* x, int32_t dtype, int64_t ldx, int64_t n, int64_t cols, int8_t* q,
+                                  int64_t ldq, float* scale, cudaStream_t s);
+armor_status launch_linear_i8(armor_ctx* c, const int8_t* xq, int64_t ldx, const float* xs, const int8_t* wq, int64_t ldw, const float* ws,
+                              const float* bias, void* y, int32_t y_dtype, int64_t ldy, int64_t n, int64_t n_out, int64_t n_in, bool ahead,
+                              cudaStream_t s);
+size_t packed_core_i8_e_bytes(int64_t d_out, int64_t d_in);
+armor_status launch_pack_core_i8(armor_ctx* c, const float* S, const uint8_t* M, int8_t* V, void* E, float* scale, cudaStream_t s);
+armor_status launch_core_i8(armor_ctx* c, const int8_t* zq, const float* zs, const int8_t* V, const void* E, const float* scale, void* z2,
+                            int32_t z2_dtype, int64_t n, bool ahead, cudaStream_t s);
+// The W-shaped buffers that lie side by side from T, as scratch of a call that optimises nothing: at least so many bytes
+inline int64_t ws_scratch_bytes(const armor_ctx* c) { return 10 * c->wn * (int64_t)sizeof(float); }

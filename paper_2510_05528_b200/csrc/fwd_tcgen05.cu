@@ -17,6 +17,7 @@
 // bandwidth; now 85 and 27.)  Two accumulators.  Every wait is bounded.
 #include <cuda_bf16.h>
 
+#include "rows_io.cuh"
 #include "tc_common.cuh"
 
 namespace {
@@ -39,7 +40,14 @@ struct FParams {
   int64_t rows;                      // tokens
   int m_tiles, n_groups;             // groups of N columns
   int32_t* status;
+  unsigned* top;                     // TOP writes and INT8 reads the rows' maxima, as bits
+  int8_t* q; int64_t ldq;            // INT8: the rounded rows and their scales
+  float* scale;
 };
+// What becomes of the product: bf16; the rows' largest |.|; int8 with the scale that this gives.  The last two together round the
+// product to int8 without having it in memory: the rows' maxima are known only when all their columns are, so it is formed twice
+// (x is read twice, 2 B an element, instead of fp32 sums being written and read, 8 B).
+enum { OUT_BF16 = 0, OUT_TOP = 1, OUT_INT8 = 2 };
 
 __device__ __forceinline__ uint64_t smem_desc_k(uint32_t addr) {
   uint64_t d = 0;
@@ -66,7 +74,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int DB, int N>
+template <int DB, int N, int OUT>
 __global__ void __launch_bounds__(NTHREADS, 1)
 fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapC,
                  const FParams p) {
@@ -195,6 +203,12 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
       if (!mbar_wait(tfull0 + 8 * as, aphase, abortp, p.status)) { ok = false; break; }
       tc_fence_after();
       const int64_t row0 = (int64_t)mt * BM + q * 32;
+      unsigned top = 0;
+      rows::RowScale rs;
+      if (OUT == OUT_INT8 && row0 + lane < p.rows) {
+        rs = rows::row_scale(p.top[row0 + lane]);
+        if (b == 0 && half == 0) p.scale[row0 + lane] = rs.s;
+      }
 #pragma unroll 1
       for (int ch = 0; ch < N / 128; ++ch) {
         // 64 columns of the lane's row as bf16: 16-byte unit c of the box's row sits at unit c ^ (row % 8)
@@ -206,6 +220,28 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(tempty0 + 8 * as);
+        }
+        if (OUT == OUT_TOP) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) top = max(top, max(r0[k] & 0x7fffffffu, r1[k] & 0x7fffffffu));
+          continue;
+        }
+        if (OUT == OUT_INT8) {
+          if (row0 + lane < p.rows) {
+            int8_t* const at = p.q + (row0 + lane) * p.ldq + (int64_t)b * N + col;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              float v[8], w[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                v[k] = __uint_as_float(u < 2 ? r0[(u & 1) * 16 + k] : r1[(u & 1) * 16 + k]);
+                w[k] = __uint_as_float(u < 2 ? r0[(u & 1) * 16 + 8 + k] : r1[(u & 1) * 16 + 8 + k]);
+              }
+              const uint2 lo = rows::row_round8(v, rs), hi = rows::row_round8(w, rs);
+              *reinterpret_cast<uint4*>(at + 16 * u) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+          }
+          continue;
         }
         if (lane == 0) tma_store_wait_read();       // the previous store has read the box
         __syncwarp();
@@ -227,6 +263,7 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
           tma_store_commit();
         }
       }
+      if (OUT == OUT_TOP && row0 + lane < p.rows) atomicMax(p.top + row0 + lane, top);   // (a maximum: any order)
     }
     if (lane == 0) tma_store_wait_read();           // shared memory stays valid until the stores have read it
   }
@@ -245,6 +282,7 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
 // does the rest.  The order of k inside an instruction is free as long as both operands agree, so a lane takes eight
 // consecutive k (16 bytes) of its rows as the operands of two instructions; the columns of the two n-tiles are dealt out so
 // that a lane ends with four neighbouring ones.
+// out32 non-null: the product is written there in fp32 instead.
 // SUM: the tokens come as `pieces` arrays of fp32 partial sums [rows][d], added in order and rounded to bf16 once.
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -256,7 +294,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 template <int DB, bool SUM>
 __global__ void __launch_bounds__(256)
 fwd_small_kernel(const void* X, int pieces, const __nv_bfloat16* Q, __nv_bfloat16* __restrict__ out,
-                 int rows, int64_t d) {
+                 int rows, int64_t d, float* out32) {
   constexpr int LD = DB * 2 + 64;                     // bytes per staged token: eight lanes of a phase hit eight banks
   __shared__ __align__(16) uint8_t tok[16 * LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -309,6 +347,14 @@ fwd_small_kernel(const void* X, int pieces, const __nv_bfloat16* Q, __nv_bfloat1
       mma_bf16(acc[nt], a0.z, a1.z, a0.w, a1.w, w[nt][ch].z, w[nt][ch].w);
     }
   }
+  if (!SUM && out32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (r0 + g + 8 * h < rows)
+        *reinterpret_cast<float4*>(out32 + (int64_t)(r0 + g + 8 * h) * d + n0 + 4 * t) =
+            make_float4(acc[0][2 * h], acc[0][2 * h + 1], acc[1][2 * h], acc[1][2 * h + 1]);
+    return;
+  }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     if (r0 + g + 8 * h < rows)
@@ -343,18 +389,19 @@ bool make_map_bf16(CUtensorMap* map, const void* base, int64_t rows, int64_t col
   return r == CUDA_SUCCESS;
 }
 
-template <int DB, int N>
-armor_status launch_block(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d, cudaStream_t s) {
+template <int DB, int N, int OUT>
+armor_status launch_block(armor_ctx* c, const void* X, const void* Q, void* out, FParams p, int64_t rows, int64_t d, cudaStream_t s) {
   CUtensorMap mX, mQ, mC;
-  if (!make_map_bf16(&mX, X, rows, d, d, BM) || !make_map_bf16(&mQ, Q, d, DB, DB, N) || !make_map_bf16(&mC, out, rows, d, d, 32)) return ARMOR_ERR_CUDA;
-  FParams p{};
+  if (!make_map_bf16(&mX, X, rows, d, d, BM) || !make_map_bf16(&mQ, Q, d, DB, DB, N)) return ARMOR_ERR_CUDA;
+  if (OUT != OUT_BF16) mC = mX;                      // (nothing is stored through it)
+  else if (!make_map_bf16(&mC, out, rows, d, d, 32)) return ARMOR_ERR_CUDA;
   p.rows = rows; p.m_tiles = (int)((rows + BM - 1) / BM); p.n_groups = (int)(d / N);
   p.status = c->status;
   static PerDeviceOnce attr;
-  if (ensure_dynamic_smem(attr, c->device, fwd_block_kernel<DB, N>, Geo<DB, N>::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  if (ensure_dynamic_smem(attr, c->device, fwd_block_kernel<DB, N, OUT>, Geo<DB, N>::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
   const int64_t tiles = (int64_t)p.m_tiles * p.n_groups;
-  KTimer kt(c, ARMOR_KC_FORWARD, 4.0 * (double)rows * (double)d, s);
-  launch_dependent(fwd_block_kernel<DB, N>, (unsigned)(tiles < c->n_sm ? tiles : c->n_sm), NTHREADS, Geo<DB, N>::SMEM, s, mX, mQ, mC, p);
+  KTimer kt(c, ARMOR_KC_FORWARD, (OUT == OUT_BF16 ? 4.0 : (OUT == OUT_TOP ? 2.0 : 3.0)) * (double)rows * (double)d, s);
+  launch_dependent(fwd_block_kernel<DB, N, OUT>, (unsigned)(tiles < c->n_sm ? tiles : c->n_sm), NTHREADS, Geo<DB, N>::SMEM, s, mX, mQ, mC, p);
   c->launches++;
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }
@@ -373,22 +420,38 @@ void launch_pack_blocks(armor_ctx* c, const float* P, const float* rowscale, con
   c->launches++;
 }
 
+template <int OUT>
+static armor_status block_product(armor_ctx* c, const void* X, const void* Q, void* out, const FParams& p, int64_t rows, int64_t d, cudaStream_t s) {
+  if (!fwd_block_ok(c) || rows <= 0 || d % c->db) return ARMOR_ERR_UNSUPPORTED;
+  if (c->db == 128) return launch_block<128, 128, OUT>(c, X, Q, out, p, rows, d, s);
+  // a block of 256 in halves while an SM has no more than one: 4096 columns x 400 tokens 28.1 us a forward in halves, 30.4 whole;
+  // x 640 31.8 and 30.9; x 1,000 34.3 and 31.9
+  return 2 * ((rows + BM - 1) / BM) * (d / 256) <= c->n_sm ? launch_block<256, 128, OUT>(c, X, Q, out, p, rows, d, s)
+                                                          : launch_block<256, 256, OUT>(c, X, Q, out, p, rows, d, s);
+}
+
 // out[rows][d] (bf16) = X[rows][d] (bf16) times the block-diagonal matrix whose stacked blocks are Q[d][db] (bf16):
 // out[t][n] = sum_k X[t][j*db + k] Q[n][k], j = n / db
 armor_status launch_fwd_block(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d,
                               cudaStream_t s) {
-  if (!fwd_block_ok(c) || rows <= 0 || d % c->db) return ARMOR_ERR_UNSUPPORTED;
-  if (c->db == 128) return launch_block<128, 128>(c, X, Q, out, rows, d, s);
-  // a block of 256 in halves while an SM has no more than one: 4096 columns x 400 tokens 28.1 us a forward in halves, 30.4 whole;
-  // x 640 31.8 and 30.9; x 1,000 34.3 and 31.9
-  return 2 * ((rows + BM - 1) / BM) * (d / 256) <= c->n_sm ? launch_block<256, 128>(c, X, Q, out, rows, d, s)
-                                                          : launch_block<256, 256>(c, X, Q, out, rows, d, s);
+  return block_product<OUT_BF16>(c, X, Q, out, FParams{}, rows, d, s);
+}
+armor_status launch_fwd_block_top(armor_ctx* c, const void* X, const void* Q, unsigned* top, int64_t rows, int64_t d, cudaStream_t s) {
+  FParams p{};
+  p.top = top;
+  return block_product<OUT_TOP>(c, X, Q, nullptr, p, rows, d, s);
+}
+armor_status launch_fwd_block_i8(armor_ctx* c, const void* X, const void* Q, const unsigned* top, int8_t* q, float* scale, int64_t rows,
+                                 int64_t d, cudaStream_t s) {
+  FParams p{};
+  p.top = const_cast<unsigned*>(top); p.q = q; p.ldq = d; p.scale = scale;
+  return block_product<OUT_INT8>(c, X, Q, nullptr, p, rows, d, s);
 }
 
 // The same for few rows.  pieces == 0: X is bf16 [rows][d]; otherwise X holds that many fp32 arrays
-// [rows][d] whose sum, rounded to bf16, is the operand.  Either way a dependent launch.
+// [rows][d] whose sum, rounded to bf16, is the operand.  Either way a dependent launch.  out_f32 (pieces == 0): out is fp32.
 armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const void* Q, void* out, int64_t rows, int64_t d,
-                              cudaStream_t s) {
+                              cudaStream_t s, bool out_f32) {
   if (!fwd_block_ok(c) || rows <= 0 || d % 128) return ARMOR_ERR_UNSUPPORTED;
   KTimer kt(c, ARMOR_KC_FORWARD, 4.0 * (double)rows * (double)d, s);
   cudaLaunchConfig_t cfg{};
@@ -399,12 +462,13 @@ armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const voi
   cfg.attrs = at; cfg.numAttrs = 1;
   const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(Q);
   __nv_bfloat16* o = static_cast<__nv_bfloat16*>(out);
+  float* o32 = out_f32 ? static_cast<float*>(out) : nullptr;   // (not with pieces)
   const int n = (int)rows;
   cudaError_t e;
-  if (c->db == 128) e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, true>, X, pieces, q, o, n, d)
-                                   : cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, false>, X, 0, q, o, n, d);
-  else e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, true>, X, pieces, q, o, n, d)
-                      : cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, false>, X, 0, q, o, n, d);
+  if (c->db == 128) e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, true>, X, pieces, q, o, n, d, o32)
+                                   : cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, false>, X, 0, q, o, n, d, o32);
+  else e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, true>, X, pieces, q, o, n, d, o32)
+                      : cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, false>, X, 0, q, o, n, d, o32);
   c->launches++;
   return e == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }

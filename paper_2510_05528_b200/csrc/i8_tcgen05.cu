@@ -1,0 +1,651 @@
+// Products of int8 rows with a scale each on the tensor cores (tcgen05.mma kind::i8, int32 sums in tensor memory):
+//   Y[t][m] = xs[t] ws[m] sum_k Xq[t][k] Wq[m][k] (+ b[m])
+// with W dense, or the 2:4 core of a factorised layer given as its kept values (int8, two of every four along k) and their
+// positions (tcgen05.mma.sp).  The sums are exact: |q| <= 128, so 131,071 products fit an int32.  The one rounding is that of the sum to
+// fp32 on its way out, a further one where Y is bf16 or fp16.
+//
+// W is the A operand, lanes of an accumulator are its rows and columns are tokens, from one token to many.  One instruction
+// multiplies 32 k (dense; 32 bytes of each operand) or 64 (sparse; 32 bytes of kept values, 64 of tokens).  A stage is 128 bytes of W's
+// rows: 128 k, or 256.
+//
+// Positions for one sparse instruction: lane l holds the 64 bits of row l, a nibble for each group of four k in order (the lower
+// kept position in bits 0-1, the higher in bits 2-3), in two columns of tensor memory; the selector field is 0.  pack_core_i8_kernel
+// writes a stage's positions as two blocks of 128 lanes x 16 bytes, which two tcgen05.cp take to eight columns ahead of the stage's
+// four instructions, in order with them.
+//
+// Every wait is bounded.
+#include "rows_io.cuh"
+#include "tc_common.cuh"
+
+namespace {
+
+using namespace tc;
+
+constexpr int BM = 128;                             // rows of W a CTA
+constexpr int A_BYTES = BM * 128;                   // a stage of W
+constexpr int E_BYTES = 128 * 32;                   // positions of a sparse stage
+
+struct I8P {
+  void* Y; int64_t ldy; int out;                    // ARMOR_DTYPE_* of Y
+  int pairs;                                        // two neighbouring rows of W may be stored at once
+  const float *xs, *ws, *bias;
+  int64_t M, N;                                     // rows of W, tokens
+  int m_tiles, n_tiles, k_tiles, tile_n;
+  int per;                                          // few tokens: k tiles a CTA
+  int ahead;                                        // few tokens: W may be fetched before the wait for the kernel before
+  int32_t* status;
+};
+
+// K-major rows of 128 bytes, 128-byte swizzle
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) { return smem_desc_sw128(addr, 16, 1024); }
+// 128 rows of 16 bytes, groups of eight rows 128 bytes apart, no swizzle
+__device__ __forceinline__ uint64_t desc_e(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(128 >> 4) << 16;
+  d |= (uint64_t)(128 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  return d;
+}
+// signed int8 operands, both K-major, int32 sums
+__device__ __forceinline__ uint32_t idesc_i8(int m, int n, bool sparse) {
+  uint32_t d = sparse ? 1u << 2 : 0u;
+  d |= 2u << 4;                   // D format: S32
+  d |= 1u << 7;                   // A format: S8
+  d |= 1u << 10;                  // B format: S8
+  d |= (uint32_t)(n >> 3) << 17;
+  d |= (uint32_t)(m >> 4) << 24;
+  return d;
+}
+template <int CTAS, bool SP>
+__device__ __forceinline__ void umma_i8(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t tmem_e, uint32_t idesc, uint32_t acc) {
+  if (SP && CTAS == 1)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+                 "tcgen05.mma.sp.cta_group::1.kind::i8 [%0], %1, %2, [%3], %4, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(tmem_e), "r"(idesc), "r"(acc) : "memory");
+  else if (SP)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+                 "tcgen05.mma.sp.cta_group::2.kind::i8 [%0], %1, %2, [%3], %4, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(tmem_e), "r"(idesc), "r"(acc) : "memory");
+  else if (CTAS == 1)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void copy_e(uint32_t taddr, uint64_t sdesc) {
+  if (CTAS == 1) asm volatile("tcgen05.cp.cta_group::1.128x128b [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.128x128b [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+
+__device__ __forceinline__ void store_one(const I8P& p, int64_t tok, int64_t row, float v) {
+  const int64_t o = tok * p.ldy + row;
+  if (p.out == ARMOR_DTYPE_F32) static_cast<float*>(p.Y)[o] = v;
+  else if (p.out == ARMOR_DTYPE_BF16) static_cast<__nv_bfloat16*>(p.Y)[o] = __float2bfloat16_rn(v);
+  else static_cast<__half*>(p.Y)[o] = __float2half_rn(v);
+}
+// rows row, row + 1 (row even) of one token
+__device__ __forceinline__ void store_two(const I8P& p, int64_t tok, int64_t row, float a, float b) {
+  if (p.pairs && row + 1 < p.M) {
+    const int64_t o = tok * p.ldy + row;
+    if (p.out == ARMOR_DTYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(p.Y) + o) = make_float2(a, b);
+    else if (p.out == ARMOR_DTYPE_BF16)
+      *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.Y) + o) = rows::pack2(static_cast<const __nv_bfloat16*>(nullptr), a, b);
+    else *reinterpret_cast<uint32_t*>(static_cast<__half*>(p.Y) + o) = rows::pack2(static_cast<const __half*>(nullptr), a, b);
+    return;
+  }
+  if (row < p.M) store_one(p, tok, row, a);
+  if (row + 1 < p.M) store_one(p, tok, row + 1, b);
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Few tokens: reading W is the cost.  A CTA takes a row tile, BN tokens and a piece of the contraction; the pieces of a tile are
+// a cluster, which adds its int32 sums through distributed shared memory (exact in any order): each CTA has a share of the rows and
+// writes their outputs.  W is fetched before the wait for the kernel that rounds the tokens.
+template <int BN, bool SP>
+struct Few {
+  static constexpr int B_BYTES = BN * 128 * (SP ? 2 : 1);
+  static constexpr int STAGE = A_BYTES + B_BYTES + (SP ? E_BYTES : 0);
+  static constexpr int SUMS = BN * BM * 4;                                    // a CTA's sums, in the place of the stages
+  static constexpr int FIT = 110 * 1024 / STAGE;                              // two CTAs share an SM
+  static constexpr int STAGES = FIT * STAGE >= SUMS ? FIT : (SUMS + STAGE - 1) / STAGE;
+  static constexpr int NEED = BN + (SP ? 8 * STAGES : 0);
+  static constexpr uint32_t COLS = NEED <= 32 ? 32 : (NEED <= 64 ? 64 : (NEED <= 128 ? 128 : 256));
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024;
+};
+constexpr int FEW_THREADS = 192;
+// the same place in shared memory of another piece's CTA
+__device__ __forceinline__ uint32_t in_piece(uint32_t addr, uint32_t piece) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(piece));
+  return r;
+}
+
+template <int BN, bool SP>
+__global__ void __launch_bounds__(FEW_THREADS, 2)
+i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+              const __grid_constant__ CUtensorMap mapE, const I8P p) {
+  using T = Few<BN, SP>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ __align__(8) uint64_t bars[2 * T::STAGES + 1];
+  __shared__ uint32_t tmem_base_holder;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[T::STAGES]), tfull = smem_u32(&bars[2 * T::STAGES]);
+  const int mt = blockIdx.x, piece = blockIdx.y, pieces = gridDim.y;
+  const int k0 = piece * p.per, k1 = min(p.k_tiles, k0 + p.per);
+  const int64_t tok0 = (int64_t)blockIdx.z * BN;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < T::STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+    mbar_init(tfull, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_holder)),
+                 "r"(T::COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const bool ahead = p.ahead != 0;
+  if (!ahead) grid_dependency_wait();
+  grid_launch_dependents();
+  const uint32_t tmem_base = tmem_base_holder;
+  volatile int* abortp = &abort_flag;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      auto load_w = [&](int kt, int stage) {
+        const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE), fb = full0 + 8 * stage;
+        mbar_expect_tx(fb, T::STAGE);
+        tma_load_2d(dst, &mapA, kt * 128, mt * BM, fb);
+        if (SP) tma_load_2d(dst + A_BYTES + T::B_BYTES, &mapE, 0, (mt * p.k_tiles + kt) * 256, fb);
+      };
+      auto load_x = [&](int kt, int stage) {
+        const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE) + A_BYTES, fb = full0 + 8 * stage;
+        tma_load_2d(dst, &mapB, kt * (SP ? 256 : 128), (int)tok0, fb);
+        if (SP) tma_load_2d(dst + BN * 128, &mapB, kt * 256 + 128, (int)tok0, fb);
+      };
+      const int pre = min(T::STAGES, k1 - k0);
+      for (int i = 0; i < pre; ++i) load_w(k0 + i, i);
+      if (ahead) grid_dependency_wait();
+      for (int i = 0; i < pre; ++i) load_x(k0 + i, i);
+      int stage = pre % T::STAGES; uint32_t phase = pre == T::STAGES ? 1 : 0;
+      long long issued = pre;
+      bool ok = true;
+      for (int kt = k0 + pre; kt < k1; ++kt) {
+        if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abortp, p.status)) { ok = false; break; }
+        load_w(kt, stage);
+        load_x(kt, stage);
+        ++issued;
+        if (++stage == T::STAGES) { stage = 0; phase ^= 1; }
+      }
+      if (!ok) {
+        for (int back = 1; back <= T::STAGES && back <= issued; ++back) {
+          int s = stage - back; uint32_t ph = phase;
+          if (s < 0) { s += T::STAGES; ph ^= 1; }
+          const long long t0 = clock64();
+          while (!mbar_try(full0 + 8 * s, ph) && clock64() - t0 < 20000000ll) {}
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = idesc_i8(BM, BN, SP);
+      int stage = 0; uint32_t phase = 0;
+      bool ok = true;
+      for (int kt = k0; kt < k1; ++kt) {
+        if (!mbar_wait(full0 + 8 * stage, phase, abortp, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sa = smem_u32(smem + (size_t)stage * T::STAGE), sb = sa + A_BYTES;
+        const uint32_t meta = tmem_base + BN + (uint32_t)(8 * stage);
+        if (SP) {
+          copy_e<1>(meta, desc_e(sb + T::B_BYTES));
+          copy_e<1>(meta + 4, desc_e(sb + T::B_BYTES + 2048));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          umma_i8<1, SP>(tmem_base, desc_k(sa + j * 32), desc_k(SP ? sb + (j >> 1) * (BN * 128) + (j & 1) * 64 : sb + j * 32), meta + 2 * j, idesc,
+                         (uint32_t)((kt > k0) | (j != 0)));
+        umma_commit(empty0 + 8 * stage);
+        if (++stage == T::STAGES) { stage = 0; phase ^= 1; }
+      }
+      if (ok) umma_commit(tfull);
+    }
+  } else {
+    // the CTA's sums to shared memory, [token][row]: all stages have been read when they are complete
+    if (mbar_wait_warp(tfull, 0, abortp, p.status)) {
+      tc_fence_after();
+      const int q = warp & 3;
+      int32_t* const sums = reinterpret_cast<int32_t*>(smem);
+#pragma unroll 1
+      for (int ch = 0; ch < BN / 16; ++ch) {
+        if (tok0 + ch * 16 >= p.N) break;
+        uint32_t r[16];
+        tmem_ld16(tmem_base + (uint32_t)(ch * 16) + ((uint32_t)(q * 32) << 16), r);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[(ch * 16 + i) * BM + q * 32 + lane] = (int32_t)r[i];
+      }
+      tc_fence_before();
+    }
+  }
+  __syncwarp();
+  if (pieces > 1) cluster_sync_all(); else __syncthreads();
+  if (!*abortp) {
+    grid_dependency_wait();                                 // (every thread that reads the tokens' scales)
+    // row pairs [u0, u1) of every token
+    const int u0 = 64 * piece / pieces, u1 = 64 * (piece + 1) / pieces, w = u1 - u0;
+    const int nv = (int)(p.N - tok0 < BN ? p.N - tok0 : BN);
+    const uint32_t base = smem_u32(smem);
+    for (int u = threadIdx.x; u < nv * w; u += FEW_THREADS) {
+      const int t = u / w, r2 = u0 + u - t * w;
+      int32_t a = 0, b = 0;
+      const uint32_t at = base + (uint32_t)(t * BM + 2 * r2) * 4;
+      for (int k = 0; k < pieces; ++k) {
+        int32_t x, y;
+        const uint32_t from = pieces > 1 ? in_piece(at, (uint32_t)k) : at;
+        asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(from) : "memory");
+        a += x; b += y;
+      }
+      const int64_t row = (int64_t)mt * BM + 2 * r2, tok = tok0 + t;
+      if (row >= p.M) continue;
+      const bool two = row + 1 < p.M;
+      const float xs = p.xs[tok];
+      float va = (float)a * (xs * p.ws[row]), vb = two ? (float)b * (xs * p.ws[row + 1]) : 0.f;
+      if (p.bias) { va += p.bias[row]; if (two) vb += p.bias[row + 1]; }
+      store_two(p, tok, row, va, vb);
+    }
+  }
+  __syncwarp();
+  if (pieces > 1) cluster_sync_all(); else __syncthreads(); // nobody leaves while its sums are being read
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(T::COLS) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Many tokens: pairs of CTAs (cta_group::2), a tile of 256 rows of W by up to 256 tokens (sparse: 224), persistent, the next tile's
+// products beside the last one's way out (two accumulators).  Each CTA holds 128 rows of W (and their positions, in its tensor
+// memory) and half of the tile's tokens.
+//   full[s]   (even CTA): armed for the bytes of both CTAs, whose loads complete on it
+//   empty[s], tfull[2] (both CTAs): tcgen05.commit to the pair
+//   tempty[2] (even CTA): an arrival of every epilogue warp of either CTA
+template <bool SP>
+struct Many {
+  static constexpr int MAX_N = SP ? 224 : 256;                                // two accumulators and the positions fit tensor memory
+  static constexpr int BH = MAX_N / 2 * 128;                                  // 128 bytes of half the tile's tokens
+  static constexpr int E_AT = A_BYTES + BH * (SP ? 2 : 1);
+  static constexpr int STAGE = E_AT + (SP ? E_BYTES : 0);
+  static constexpr int STAGES = 220 * 1024 / STAGE;
+  static constexpr uint32_t META = 2 * MAX_N;
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024;
+  static_assert(!SP || META + 8 * STAGES <= 512, "tensor memory");
+};
+constexpr int MANY_THREADS = 192;
+constexpr uint32_t MANY_COLS = 512;
+
+constexpr int GROUP_M = 8;                          // row tiles that run side by side: see sparse_tcgen05.cu
+__device__ __forceinline__ void tile_to_mn(int tile, int m_tiles, int n_tiles, int& mt, int& nt) {
+  const int per_group = GROUP_M * n_tiles;
+  const int g = tile / per_group, r = tile - g * per_group;
+  const int gm = min(GROUP_M, m_tiles - g * GROUP_M);
+  mt = g * GROUP_M + r % gm;
+  nt = r / gm;
+}
+
+template <bool SP>
+__global__ void __launch_bounds__(MANY_THREADS, 1)
+i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+               const __grid_constant__ CUtensorMap mapE, const I8P p) {
+  using T = Many<SP>;
+  constexpr int STAGES = T::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ __align__(8) uint64_t bars[2 * STAGES + 4];
+  __shared__ uint32_t tmem_base_holder;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[STAGES]);
+  const uint32_t tfull0 = smem_u32(&bars[2 * STAGES]), tempty0 = smem_u32(&bars[2 * STAGES + 2]);
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const int n_tiles_total = p.m_tiles * p.n_tiles;          // row tiles of 256
+  const int half_n = p.tile_n / 2;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(tfull0 + 8 * s, 1); mbar_init(tempty0 + 8 * s, 8); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_holder)),
+                 "r"(MANY_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                       // both CTAs' barriers exist before anyone signals them
+  tc_fence_after();
+  grid_begin();                                             // (tensor memory is this CTA's before the next kernel's CTAs start)
+  const uint32_t tmem_base = tmem_base_holder;
+  volatile int* abortp = &abort_flag;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer (both CTAs)
+    if (lane == 0) {
+      int stage = 0; uint32_t phase = 0; long long issued = 0;
+      bool ok = true;
+      for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs) {
+        int mt, nt;
+        tile_to_mn(tile, p.m_tiles, p.n_tiles, mt, nt);
+        const int row0 = mt * 256 + (int)rank * 128, tok0 = nt * p.tile_n + (int)rank * half_n;
+        for (int kt = 0; kt < p.k_tiles; ++kt) {
+          if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abortp, p.status)) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * (A_BYTES + half_n * 128 * (SP ? 2 : 1) + (SP ? E_BYTES : 0)));
+          const uint32_t fb = map_to_cta(full0 + 8 * stage, 0);
+          const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE);
+          tma_load_2d_pair(dst, &mapA, kt * 128, row0, fb);
+          tma_load_2d_pair(dst + A_BYTES, &mapB, kt * (SP ? 256 : 128), tok0, fb);
+          if (SP) {
+            tma_load_2d_pair(dst + A_BYTES + T::BH, &mapB, kt * 256 + 128, tok0, fb);
+            tma_load_2d_pair(dst + T::E_AT, &mapE, 0, ((2 * mt + (int)rank) * p.k_tiles + kt) * 256, fb);
+          }
+          ++issued;
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+      }
+      // tail: the MMAs that read the stages issued last have finished (their commits reach both CTAs), so
+      // nothing is in flight towards this CTA's shared memory when it leaves
+      for (int back = 1; back <= STAGES && back <= issued; ++back) {
+        int s = stage - back; uint32_t ph = phase;
+        if (s < 0) { s += STAGES; ph ^= 1; }
+        const long long t0 = clock64();
+        while (!mbar_try(empty0 + 8 * s, ph) && clock64() - t0 < (ok ? WAIT_CYCLES : 20000000ll)) {}
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer (even CTA only)
+    if (lane == 0 && rank == 0) {
+      const uint64_t da0 = desc_k(smem_u32(smem)), db0 = desc_k(smem_u32(smem) + A_BYTES), de0 = desc_e(smem_u32(smem) + T::E_AT);
+      const uint32_t idesc = idesc_i8(256, p.tile_n, SP);
+      int stage = 0; uint32_t phase = 0;
+      int local = 0;
+      bool ok = true;
+      for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs, ++local) {
+        const int as = local & 1;
+        if (!mbar_wait_cluster(tempty0 + 8 * as, ((uint32_t)(local >> 1) & 1u) ^ 1u, abortp, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t tacc = tmem_base + (uint32_t)(as * T::MAX_N);
+        for (int kt = 0; kt < p.k_tiles; ++kt) {
+          if (!mbar_wait_cluster(full0 + 8 * stage, phase, abortp, p.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t off = (uint64_t)(uint32_t)(stage * (T::STAGE >> 4));
+          const uint32_t meta = tmem_base + T::META + (uint32_t)(8 * stage);
+          if (SP) {
+            copy_e<2>(meta, de0 + off);
+            copy_e<2>(meta + 4, de0 + off + (2048 >> 4));
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            umma_i8<2, SP>(tacc, da0 + off + 2 * j, db0 + off + (SP ? (uint64_t)((j >> 1) * (T::BH >> 4) + 4 * (j & 1)) : (uint64_t)(2 * j)), meta + 2 * j, idesc,
+                           (uint32_t)((kt > 0) | (j != 0)));
+          umma_commit_pair(empty0 + 8 * stage);
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (ok) umma_commit_pair(tfull0 + 8 * as);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue warps (both CTAs)
+    const int q = warp & 3;
+    int local = 0;
+    bool ok = true;
+    for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs, ++local) {
+      int mt, nt;
+      tile_to_mn(tile, p.m_tiles, p.n_tiles, mt, nt);
+      const int as = local & 1;
+      const int64_t row = (int64_t)mt * 256 + rank * 128 + q * 32 + lane;
+      const float ws = row < p.M ? p.ws[row] : 0.f, bias = p.bias && row < p.M ? p.bias[row] : 0.f;
+      if (!mbar_wait_warp(tfull0 + 8 * as, (uint32_t)(local >> 1) & 1u, abortp, p.status)) { ok = false; break; }
+      tc_fence_after();
+      const bool odd = lane & 1;
+#pragma unroll 1
+      for (int ch = 0; ch < p.tile_n / 32; ++ch) {
+        const int64_t tok0 = (int64_t)nt * p.tile_n + ch * 32;
+        if (tok0 >= p.N) break;
+        const float xs = tok0 + lane < p.N ? p.xs[tok0 + lane] : 0.f;
+        uint32_t r[32];
+        tmem_ld32(tmem_base + (uint32_t)(as * T::MAX_N + ch * 32) + ((uint32_t)(q * 32) << 16), r);
+        // neighbouring lanes swap one value of every pair of tokens: a lane stores two rows of one token
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float v0 = fmaf((float)(int32_t)r[i], __shfl_sync(0xffffffffu, xs, i) * ws, bias);
+          const float v1 = fmaf((float)(int32_t)r[i + 1], __shfl_sync(0xffffffffu, xs, i + 1) * ws, bias);
+          const float got = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
+          const int64_t tok = tok0 + i + (odd ? 1 : 0);
+          if (tok < p.N) store_two(p, tok, row & ~int64_t(1), odd ? got : v0, odd ? v1 : got);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty0 + 8 * as, 0));
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                       // neither CTA leaves while its partner may still signal it
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(MANY_COLS) : "memory");
+  }
+}
+
+// int8 rows [rows][cols], box of 128 bytes x box_rows, 128-byte swizzle, zeros outside
+bool make_map_i8(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld};
+  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// positions: rows of 16 bytes, a stage's 256 a box
+bool make_map_e(CUtensorMap* map, const void* base, int64_t rows) {
+  PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {4, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {16};
+  cuuint32_t box[2] = {4, 256};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// One thread for 32 k of a row: their kept values (of eight groups of four) as int8 and the word of their positions.  Places behind
+// the core (k of a last stage that is half full, rows of a last tile of 256) keep positions 0 and 1, which meet zeros.
+__global__ void __launch_bounds__(256)
+pack_core_i8_kernel(const float* __restrict__ S, const uint8_t* __restrict__ Mk, const float* __restrict__ top, int8_t* __restrict__ V,
+                    uint32_t* __restrict__ E, float* __restrict__ scale, int64_t d_out, int64_t d_in, int32_t* status) {
+  const int64_t k_tiles = (d_in + 255) / 256, words = k_tiles * 8;
+  const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = w / words, kw = w - row * words;      // 32 k from 32 kw on
+  if (row >= (d_out + 255) / 256 * 256) return;
+  uint32_t word = 0x44444444u;
+  if (row < d_out && kw * 32 < d_in) {
+    const rows::RowScale r = rows::row_scale(__float_as_uint(top[row]));
+    if (kw == 0) scale[row] = r.s;
+    word = 0;
+    uint32_t out[4] = {0u, 0u, 0u, 0u};
+    int bad = 0;
+    for (int g = 0; g < 8; ++g) {
+      const int64_t at = row * (d_in / 4) + kw * 8 + g;
+      const unsigned m = Mk[at] & 15u;
+      const float4 v = *reinterpret_cast<const float4*>(S + 4 * at);
+      const float vals[4] = {v.x, v.y, v.z, v.w};
+      int i0 = -1, i1 = -1, cnt = 0;
+      for (int i = 0; i < 4; ++i)
+        if ((m >> i) & 1u) { if (cnt == 0) i0 = i; else if (cnt == 1) i1 = i; ++cnt; }
+      if (cnt > 2) bad = 1;
+      if (cnt < 2) {                                        // padded with positions that are not kept, i0 < i1
+        if (cnt == 0) { i0 = 0; i1 = 1; }
+        else if (i0 < 3) i1 = i0 + 1;
+        else { i1 = 3; i0 = 2; }
+      }
+      float a = 0.f, b = 0.f;
+      for (int i = 0; i < 4; ++i) {
+        if (i == i0 && ((m >> i) & 1u)) a = vals[i];
+        if (i == i1 && ((m >> i) & 1u)) b = vals[i];
+      }
+      word |= (uint32_t)(i0 | (i1 << 2)) << (4 * g);
+      const uint32_t two = (uint32_t)(rows::row_round(a, r) & 255) | ((uint32_t)(rows::row_round(b, r) & 255) << 8);
+      out[g >> 1] |= two << (16 * (g & 1));
+    }
+    *reinterpret_cast<uint4*>(V + row * (d_in / 2) + kw * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+    if (bad) atomicAdd(&status[ST_SPARSE_BAD_GROUPS], 1);
+  }
+  // stage kt of row tile mt: two blocks (128 k each) of 128 lanes x 16 bytes
+  const int64_t mt = row / 128, kt = kw / 8;
+  E[((mt * k_tiles + kt) * 2 + (kw % 8) / 4) * 512 + (row % 128) * 4 + kw % 4] = word;
+}
+// the largest kept |S| of a row, as bits in top (row_scale); of a group that keeps more than two, the first two
+__global__ void __launch_bounds__(256)
+core_top_kernel(const float* __restrict__ S, const uint8_t* __restrict__ Mk, float* __restrict__ top, int64_t d_in) {
+  __shared__ float red[1][32];
+  const int64_t row = blockIdx.x;
+  unsigned m = 0;
+  for (int64_t g = threadIdx.x; g < d_in / 4; g += 256) {
+    const unsigned k = Mk[row * (d_in / 4) + g] & 15u;
+    const float4 v = *reinterpret_cast<const float4*>(S + row * d_in + 4 * g);
+    const float vals[4] = {v.x, v.y, v.z, v.w};
+    int cnt = 0;
+    for (int i = 0; i < 4; ++i)
+      if (((k >> i) & 1u) && cnt++ < 2) m = max(m, __float_as_uint(vals[i]) & 0x7fffffffu);
+  }
+  m = rows::cta_max(m, red);
+  if (threadIdx.x == 0) top[row] = __uint_as_float(m);
+}
+
+// a dependent launch whose CTAs along y are a cluster
+template <typename K>
+armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStream_t s, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mE,
+                        const I8P& p) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid; cfg.blockDim = dim3(FEW_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 1; at[1].val.clusterDim.y = grid.y; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = grid.y > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, mA, mB, mE, p) != cudaSuccess) return ARMOR_ERR_CUDA;
+  c->launches++;
+  return ARMOR_OK;
+}
+
+template <int BN, bool SP>
+armor_status run_few(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
+  using T = Few<BN, SP>;
+  CUtensorMap mB;
+  if (!make_map_i8(&mB, xq, p.N, K, ldx, BN)) return ARMOR_ERR_CUDA;
+  static PerDeviceOnce attr;
+  if (ensure_dynamic_smem(attr, c->device, i8_few_kernel<BN, SP>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  p.n_tiles = (int)((p.N + BN - 1) / BN);
+  // pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight
+  int want = (int)(2 * (int64_t)c->n_sm / ((int64_t)p.m_tiles * p.n_tiles));
+  if (want > 8) want = 8;
+  if (want > p.k_tiles / 2) want = p.k_tiles / 2;
+  if (want < 1) want = 1;
+  p.per = (p.k_tiles + want - 1) / want;
+  const int pieces = (p.k_tiles + p.per - 1) / p.per;
+  return launch_few(c, i8_few_kernel<BN, SP>, dim3((unsigned)p.m_tiles, (unsigned)pieces, (unsigned)p.n_tiles), T::SMEM, s, mA, mB, mE, p);
+}
+
+template <bool SP>
+armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
+  KTimer kt(c, ARMOR_KC_GEMM, 2.0 * (double)p.M * (double)p.N * (double)K, s);      // (dense-equivalent)
+  p.status = c->status;
+  p.k_tiles = (int)((K + (SP ? 255 : 127)) / (SP ? 256 : 128));
+  p.m_tiles = (int)((p.M + 127) / 128);
+  if (p.N <= 256) {
+    if (p.N <= 16) return run_few<16, SP>(c, mA, mE, xq, ldx, K, p, s);
+    if (p.N <= 32) return run_few<32, SP>(c, mA, mE, xq, ldx, K, p, s);
+    if (p.N <= 64) return run_few<64, SP>(c, mA, mE, xq, ldx, K, p, s);
+    return run_few<128, SP>(c, mA, mE, xq, ldx, K, p, s);
+  }
+  using T = Many<SP>;
+  p.m_tiles = (int)((p.M + 255) / 256);
+  const int pairs = c->n_sm / 2;
+  // the width of a tile that costs least: rounds of the pairs times its tokens and what comes with every tile
+  int64_t least = 0;
+  for (int w = T::MAX_N; w >= 64; w -= 32) {
+    const int64_t tiles = (int64_t)p.m_tiles * ((p.N + w - 1) / w), cost = (tiles + pairs - 1) / pairs * (w + 64);
+    if (w == T::MAX_N || cost < least) { least = cost; p.tile_n = w; }
+  }
+  p.n_tiles = (int)((p.N + p.tile_n - 1) / p.tile_n);
+  CUtensorMap mB;
+  if (!make_map_i8(&mB, xq, p.N, K, ldx, p.tile_n / 2)) return ARMOR_ERR_CUDA;
+  static PerDeviceOnce attr;
+  if (ensure_dynamic_smem(attr, c->device, i8_many_kernel<SP>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
+  launch_dependent(i8_many_kernel<SP>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(MANY_THREADS), T::SMEM, LaunchStream(s, false, 2), mA, mB, mE, p);
+  c->launches++;
+  return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
+}
+
+I8P output(void* y, int32_t dtype, int64_t ldy, int64_t n, int64_t n_out, const float* xs, const float* ws, const float* bias, int ahead) {
+  I8P p{};
+  const int es = rows_dtype_bytes(dtype);
+  p.Y = y; p.ldy = ldy; p.out = dtype; p.xs = xs; p.ws = ws; p.bias = bias; p.M = n_out; p.N = n; p.ahead = ahead;
+  p.pairs = reinterpret_cast<uintptr_t>(y) % (2 * es) == 0 && ldy % 2 == 0;
+  return p;
+}
+
+// (rows up to whole tiles of 256: those beyond d_out hold positions too, 0 and 1, for an instruction that covers them)
+int64_t core_rows(int64_t d_out) { return (d_out + 255) / 256 * 256; }
+
+}  // namespace
+
+// y [n, n_out] = xq [n, n_in] wq [n_out, n_in]^T; ahead: the kernel before this one wrote xq and xs and nothing else that is read here,
+// and waits for the kernel before it ahead of letting this one in
+armor_status launch_linear_i8(armor_ctx* c, const int8_t* xq, int64_t ldx, const float* xs, const int8_t* wq, int64_t ldw, const float* ws,
+                              const float* bias, void* y, int32_t y_dtype, int64_t ldy, int64_t n, int64_t n_out, int64_t n_in, bool ahead,
+                              cudaStream_t s) {
+  CUtensorMap mA;
+  if (!make_map_i8(&mA, wq, n_out, n_in, ldw, BM)) return ARMOR_ERR_CUDA;
+  return product<false>(c, mA, mA, xq, ldx, n_in, output(y, y_dtype, ldy, n, n_out, xs, ws, bias, ahead ? 1 : 0), s);
+}
+
+// The core of a layer in 8 bits: values [d_out, d_in / 2], positions (packed_core_i8_e_bytes), scales [d_out]
+size_t packed_core_i8_e_bytes(int64_t d_out, int64_t d_in) { return (size_t)core_rows(d_out) * (size_t)((d_in + 255) / 256) * 32; }
+armor_status launch_pack_core_i8(armor_ctx* c, const float* S, const uint8_t* M, int8_t* V, void* E, float* scale, cudaStream_t s) {
+  const int64_t words = core_rows(c->d_out) * ((c->d_in + 255) / 256) * 8;
+  KTimer kt(c, ARMOR_KC_FORWARD, (double)c->wn * 4.875, s);
+  core_top_kernel<<<(unsigned)c->d_out, 256, 0, s>>>(S, M, c->T, c->d_in);
+  pack_core_i8_kernel<<<(unsigned)((words + 255) / 256), 256, 0, s>>>(S, M, c->T, V, static_cast<uint32_t*>(E), scale, c->d_out, c->d_in, c->status);
+  c->launches += 2;
+  return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
+}
+// z2 [n, d_out] = zq [n, d_in] core^T
+armor_status launch_core_i8(armor_ctx* c, const int8_t* zq, const float* zs, const int8_t* V, const void* E, const float* scale, void* z2,
+                            int32_t z2_dtype, int64_t n, bool ahead, cudaStream_t s) {
+  CUtensorMap mA, mE;
+  if (!make_map_i8(&mA, V, c->d_out, c->d_in / 2, c->d_in / 2, BM)) return ARMOR_ERR_CUDA;
+  if (!make_map_e(&mE, E, core_rows(c->d_out) / 128 * ((c->d_in + 255) / 256) * 256)) return ARMOR_ERR_CUDA;
+  return product<true>(c, mA, mE, zq, c->d_in, c->d_in, output(z2, z2_dtype, c->d_out, n, c->d_out, zs, scale, nullptr, ahead ? 1 : 0), s);
+}

@@ -1,0 +1,173 @@
+// Rows of bf16, fp16 or fp32 taken eight elements at a time, sums over a CTA, and the rounding of a row to int8: shared by
+// the kernels of the 8-bit products and of the norms.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "armor_internal.cuh"
+
+namespace rows {
+
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+// two 16-bit values in a register, the first in its low half
+__device__ __forceinline__ float2 unpack2(const __nv_bfloat16*, uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(const __half*, uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t pack2(const __nv_bfloat16*, float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(const __half*, float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Eight consecutive elements as they lie: a chunk of a row that waits in registers.
+template <typename T> struct Raw8 { uint4 w; };
+template <> struct Raw8<float> { float4 a, b; };
+
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw_load(const T* p) { return {*reinterpret_cast<const uint4*>(p)}; }
+__device__ __forceinline__ Raw8<float> raw_load(const float* p) {
+  return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + 4)};
+}
+template <typename T>
+__device__ __forceinline__ void raw_get(const Raw8<T>& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = unpack2(static_cast<const T*>(nullptr), w[i]);
+    v[2 * i] = f.x; v[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void raw_get(const Raw8<float>& r, float (&v)[8]) {
+  v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w; v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw_zero() { return {make_uint4(0u, 0u, 0u, 0u)}; }
+template <>
+__device__ __forceinline__ Raw8<float> raw_zero<float>() { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  const T* t = nullptr;
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack2(t, v[0], v[1]), pack2(t, v[2], v[3]), pack2(t, v[4], v[5]), pack2(t, v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// Elements e .. e + 7 of a row of n, zeros behind its end.  ALIGNED: rows start on 16-byte boundaries, so that only the last chunk of
+// a row whose length is no multiple of eight is taken element by element; else all are.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ Raw8<T> row_load(const T* row, int64_t e, int64_t n) {
+  if (ALIGNED && e + 8 <= n) return raw_load(row + e);
+  Raw8<T> r = raw_zero<T>();
+  T* const at = reinterpret_cast<T*>(&r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (e + i < n) at[i] = row[e + i];
+  return r;
+}
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void row_store(T* row, int64_t e, int64_t n, const float (&v)[8]) {
+  if (ALIGNED && e + 8 <= n) { store8(row + e, v); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (e + i < n) row[e + i] = from_f<T>(v[i]);
+}
+
+// ---------------------------------------------------------------- sums and maxima over a CTA of up to 32 warps
+// `buf` holds 32 values per use; a use may follow another on another buffer with no barrier of its own between.
+template <int N>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float (*buf)[32]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane < N) {
+    float mine = v[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) if (lane == k) mine = v[k];
+    buf[lane][warp] = mine;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float t = lane < warps ? buf[k][lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    v[k] = t;
+  }
+}
+__device__ __forceinline__ unsigned cta_max(unsigned v, float (*buf)[32]) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return v;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) buf[0][warp] = __uint_as_float(v);
+  __syncthreads();
+  return __reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(buf[0][lane]) : 0u);
+}
+
+// ---------------------------------------------------------------- a row as int8 with one scale
+// s = a / 127 with a the row's largest |x|, q = the integer next to 127 x / a, ties to even.  The quotient in fp32 is off by at most
+// 127 (2^-24 + 2^-24) < 1.6e-5 (127 / a and the product are rounded), so where it lies further than 4e-5 from a half its nearest integer
+// is right; nearer, 127 x and (k + 1/2) a are compared as 64-bit products, which hold them exactly (31 and 33 bits).  q is the exact one
+// for every input, so the order of a sum or another instruction never moves it.
+struct RowScale {
+  float pre;             // a power of two that brings the row into the middle of the exponent range; 0: the row's integers are zeros
+  float inv, top;        // 127 / (a pre), a pre
+  float s;               // the scale
+};
+// top_bits: the largest |x| as bits; at least those of infinity: the row holds a NaN or an infinity.  Such a row gets NaN as its
+// scale, so that what is made of it is NaN, and zeros; a row of zeros gets 0.
+__device__ __forceinline__ RowScale row_scale(unsigned top_bits) {
+  RowScale r;
+  const float a = __uint_as_float(top_bits);
+  if (top_bits >= 0x7f800000u) return {0.f, 0.f, 1.f, __uint_as_float(0x7fffffffu)};
+  if (top_bits == 0u) return {0.f, 0.f, 1.f, 0.f};
+  r.pre = a < 1e-18f ? 1.2676506002282294e30f : (a > 1e18f ? 7.8886090522101181e-31f : 1.f);    // 2^100, 2^-100
+  r.top = a * r.pre;
+  r.inv = __fdiv_rn(127.f, r.top);
+  r.s = __fdiv_rn(a, 127.f);
+  return r;
+}
+__device__ __forceinline__ int row_round(float x, const RowScale& r) {
+  if (r.pre == 0.f) return 0;
+  const float xs = x * r.pre, t = xs * r.inv, k = floorf(t);
+  if (fabsf(t - k - 0.5f) > 4e-5f) return __float2int_rn(t);
+  const double d = 127.0 * (double)xs - ((double)k + 0.5) * (double)r.top;
+  const int f = (int)k;
+  return d > 0.0 ? f + 1 : (d < 0.0 ? f : f + (f & 1));
+}
+__device__ __forceinline__ uint2 row_round8(const float (&v)[8], const RowScale& r) {
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    w[h] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[h] |= (uint32_t)(row_round(v[4 * h + i], r) & 255) << (8 * i);
+  }
+  return make_uint2(w[0], w[1]);
+}
+// the bits of max |v|: of floats without their sign, NaN above infinity above all others
+__device__ __forceinline__ unsigned abs_bits8(const float (&v)[8]) {
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+
+inline bool aligned16(const void* p, int64_t ld, int esize) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * esize % 16 == 0; }
+
+}  // namespace rows
