@@ -266,6 +266,54 @@ armor_status armor_pack_layer_i8(armor_ctx* ctx, const float* d_A, const float* 
 armor_status armor_apply_layer_i8(armor_ctx* ctx, const void* d_packed, const void* d_x, void* d_y, int64_t n_tokens,
                                   armor_stream_t stream);
 
+/* ---- norms between two blocks ------------------------------------------------------------------------------------
+ * What lies between a block's last linear layer (output y) and the first of the next block, for rows of d elements, with
+ * rms(v) = sqrt(mean(v^2) + eps):
+ *   u = y / rms(y) (.) w_post   (post != 0; else u = y)
+ *   h = residual_scale x + gate[row / rows_per_gate] (.) u       (no gate: ones; y NULL: h = residual_scale x)
+ *   n = h / rms(h) (.) w_pre    (pre != 0; else n = h)
+ * x and h are of stream_dtype, y and n of branch_dtype: both the same of F32, BF16, F16, or an F32 stream with a 16-bit branch.
+ * Weights and gate are fp32; w_post or w_pre NULL: ones.  gate [n_gates, ld_gate], with rows enough for n_rows.  Outputs: h, n and q
+ * with q_scale (n as armor_quantize_rows has it, from fp32), any of them NULL but not all; h may be x's and n may be y's own buffer
+ * with the same leading dimension.  n and q are those of h before its rounding.  d up to ARMOR_BLOCK_NORM_MAX_COLS, any leading
+ * dimensions and alignment (q as in armor_quantize_rows).  n_rows == 0 is a no-op.
+ * Backward: from h as it was stored (needed with pre), y (with post or dgate) and the gradients dh and dn of the two outputs (either may
+ * be NULL: zeros), any of dx, dy, dw_post [d], dw_pre [d], dgate [n_gates, d] (NULL: not wanted; the last three fp32, written, not
+ * added to; gates without rows get zeros).  Runs give the same bits.  dx may be dh's and dy may be dn's own buffer.  Sums over rows
+ * go through the context's workspace (WORKSPACE if it does not hold four rows of d fp32).
+ * Errors: INVALID_ARG (missing arrays, weights without their norm), SHAPE (d < 1, leading dimensions below d, too few gates),
+ * UNSUPPORTED (types), TOO_LARGE (d, or 2^31 rows). */
+#define ARMOR_BLOCK_NORM_MAX_COLS 16384
+typedef struct {
+  int64_t n_rows, d;
+  const void* x; int64_t ldx;
+  const void* y; int64_t ldy;
+  void* h; int64_t ldh;
+  void* n; int64_t ldn;
+  int8_t* q; int64_t ldq;
+  float* q_scale;
+  const float *w_post, *w_pre, *gate;
+  int64_t ld_gate, rows_per_gate, n_gates;
+  int32_t stream_dtype, branch_dtype, post, pre;
+  float residual_scale, eps;
+} armor_block_norm_args;
+typedef struct {
+  int64_t n_rows, d;
+  const void* h; int64_t ldh;
+  const void* y; int64_t ldy;
+  const void* dh; int64_t lddh;
+  const void* dn; int64_t lddn;
+  void* dx; int64_t lddx;
+  void* dy; int64_t lddy;
+  const float *w_post, *w_pre, *gate;
+  int64_t ld_gate, rows_per_gate, n_gates;
+  float *dw_post, *dw_pre, *dgate;
+  int32_t stream_dtype, branch_dtype, post, pre;
+  float residual_scale, eps;
+} armor_block_norm_grad_args;
+armor_status armor_block_norm(armor_ctx* ctx, const armor_block_norm_args* args, armor_stream_t stream);
+armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_grad_args* args, armor_stream_t stream);
+
 /* Copies up to n (at most 16) device status words to h_codes (host).
  *   word 0: Cholesky failures since the context was created; word 1: first failing block id + 1;
  *   word 2: bounded waits that gave up; word 3: last armor_status recorded by a kernel;

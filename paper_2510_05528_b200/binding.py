@@ -30,6 +30,7 @@ EXPORTS = ["armor_workspace_bytes", "armor_create", "armor_destroy", "armor_gram
            "armor_bcd_step", "armor_proxy_loss", "armor_apply", "armor_packed_core_bytes", "armor_pack_core", "armor_apply_packed",
            "armor_packed_layer_bytes", "armor_pack_layer", "armor_apply_layer",
            "armor_quantize_rows", "armor_linear_i8", "armor_packed_layer_i8_bytes", "armor_pack_layer_i8", "armor_apply_layer_i8",
+           "armor_block_norm", "armor_block_norm_backward",
            "armor_get_device_status",
            "armor_status_string", "armor_launch_count", "armor_gemm_timing_enable", "armor_gemm_timing",
            "armor_normalize_noalloc", "armor_block_product", "armor_block_product_dual", "armor_block_product_two_sided", "armor_selftest_wait_timeout", "armor_kernel_timing_enable", "armor_use_graphs", "armor_fuse_grams",
@@ -49,6 +50,25 @@ class armor_config(C.Structure):
                 ("phases", C.c_int32), ("ab_step", C.c_int32), ("mask_sweeps", C.c_int32), ("mask_groups", C.c_int32), ("ridge", C.c_float), ("adam_lr", C.c_float),
                 ("adam_beta1", C.c_float), ("adam_beta2", C.c_float), ("adam_eps", C.c_float), ("seed", C.c_uint64)]
 
+
+def _struct(name, *fields):
+    return type(name, (C.Structure,), {"_fields_": list(fields)})
+
+
+def _rows_of(*names):
+    return [f for n in names for f in ((n, C.c_void_p), ("ld" + n, C.c_int64))]
+
+
+_gate_sizes = [("ld_gate", C.c_int64), ("rows_per_gate", C.c_int64), ("n_gates", C.c_int64)]
+_norm_tail = [("stream_dtype", C.c_int32), ("branch_dtype", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32),
+              ("residual_scale", C.c_float), ("eps", C.c_float)]
+armor_block_norm_args = _struct(
+    "armor_block_norm_args", ("n_rows", C.c_int64), ("d", C.c_int64), *_rows_of("x", "y", "h", "n", "q"), ("q_scale", C.c_void_p),
+    ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("gate", C.c_void_p), *_gate_sizes, *_norm_tail)
+armor_block_norm_grad_args = _struct(
+    "armor_block_norm_grad_args", ("n_rows", C.c_int64), ("d", C.c_int64), *_rows_of("h", "y", "dh", "dn", "dx", "dy"),
+    ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("gate", C.c_void_p), *_gate_sizes,
+    ("dw_post", C.c_void_p), ("dw_pre", C.c_void_p), ("dgate", C.c_void_p), *_norm_tail)
 
 STATS_DTYPE = np.dtype([("loss_start", "<f8"), ("loss_A", "<f8"), ("loss_B", "<f8"), ("loss_S", "<f8"),
                         ("loss_mask", "<f8"), ("delta_L_mask", "<f8"), ("tau_B", "<f4"), ("tau_S", "<f4"),
@@ -85,6 +105,8 @@ def lib() -> C.CDLL:
         L.armor_packed_layer_i8_bytes.argtypes = [C.POINTER(armor_config), C.POINTER(C.c_size_t)]
         L.armor_pack_layer_i8.argtypes = [vp] + [vp] * 7 + [vp]
         L.armor_apply_layer_i8.argtypes = [vp, vp, vp, vp, i64, vp]
+        L.armor_block_norm.argtypes = [vp, C.POINTER(armor_block_norm_args), vp]
+        L.armor_block_norm_backward.argtypes = [vp, C.POINTER(armor_block_norm_grad_args), vp]
         L.armor_get_device_status.argtypes = [vp, C.POINTER(i32), i32]
         L.armor_status_string.argtypes = [C.c_int]
         L.armor_status_string.restype = C.c_char_p
@@ -325,6 +347,86 @@ def armor_apply_layer_i8(ctx, packed, x, y) -> None:
     code = lib().armor_apply_layer_i8(ctx, _ptr(packed, torch.uint8, "packed"), _ptr(x, None, "x"), _ptr(y, None, "y"), x.shape[0], _stream())
     if code:
         _check(code, "armor_apply_layer_i8")
+
+
+def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps):
+    """Fills what both directions of the norms share; returns the gate's rows."""
+    f = torch.float32
+    for w, name in ((w_post, "w_post"), (w_pre, "w_pre")):
+        if w is not None and w.numel() != d:
+            raise ValueError(f"{name} must have {d} elements")
+    a.n_rows, a.d = n_rows, d
+    a.w_post, a.w_pre = _ptr(w_post, f, "w_post"), _ptr(w_pre, f, "w_pre")
+    a.post, a.pre, a.residual_scale, a.eps = post, pre, residual_scale, eps
+    if gate is None:
+        return 0
+    if gate.dim() == 1:
+        gate = gate.unsqueeze(0)
+    a.gate, a.ld_gate = _row_ptr(gate, f, "gate", d)
+    n_gates = gate.shape[0]
+    if not rows_per_gate:
+        if n_gates < 1 or n_rows % n_gates:
+            raise ValueError(f"rows_per_gate must be given where {n_gates} gates do not divide {n_rows} rows")
+        rows_per_gate = max(1, n_rows // n_gates)
+    a.rows_per_gate, a.n_gates = rows_per_gate, n_gates
+    return n_gates
+
+
+def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0, w_post=None, w_pre=None, post=None, pre=True,
+                     residual_scale=1.0, eps=1e-6) -> None:
+    """h and n (and n as int8 q with q_scale) of the residual stream x and a block's output y (see armor.h).  post: None means with
+    w_post."""
+    a = armor_block_norm_args()
+    a.x, a.ldx = _row_ptr(x, x.dtype, "x")
+    rows, d = x.shape
+    a.stream_dtype = _row_dtype(x, "x")
+    branch = y if y is not None else n
+    bt = x.dtype if branch is None else branch.dtype
+    a.branch_dtype = a.stream_dtype if branch is None else _row_dtype(branch, "y")
+    for t, name in ((y, "y"), (h, "h"), (n, "n"), (q, "q"), (q_scale, "q_scale")):
+        if t is not None and t.shape[0] != rows:
+            raise ValueError(f"{name} must have the {rows} rows of x")
+    a.y, a.ldy = _row_ptr(y, bt, "y", d)
+    a.h, a.ldh = _row_ptr(h, x.dtype, "h", d)
+    a.n, a.ldn = _row_ptr(n, bt, "n", d)
+    a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
+    a.q_scale = _ptr(q_scale, torch.float32, "q_scale")
+    _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, int(w_post is not None if post is None else post), int(pre),
+                 residual_scale, eps)
+    code = lib().armor_block_norm(ctx, a, _stream())
+    if code:
+        _check(code, "armor_block_norm")
+
+
+def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, *, gate=None, rows_per_gate=0, w_post=None,
+                              w_pre=None, post=None, pre=True, residual_scale=1.0, eps=1e-6) -> None:
+    """The gradient of armor_block_norm (see armor.h)."""
+    f = torch.float32
+    a = armor_block_norm_grad_args()
+    stream = next((t for t in (h, dh, dx) if t is not None), None)
+    branch = next((t for t in (y, dn, dy) if t is not None), None)
+    if stream is None and branch is None:
+        raise ValueError("h, dh, dx, y, dn and dy are all missing")
+    ts, tb = (stream if stream is not None else branch), (branch if branch is not None else stream)
+    _row_ptr(ts, ts.dtype, "h")
+    rows, d = ts.shape
+    a.stream_dtype, a.branch_dtype = _row_dtype(ts, "h"), _row_dtype(tb, "y")
+    for name, t, dt in (("h", h, ts.dtype), ("y", y, tb.dtype), ("dh", dh, ts.dtype), ("dn", dn, tb.dtype), ("dx", dx, ts.dtype),
+                        ("dy", dy, tb.dtype)):
+        if t is not None and t.shape[0] != rows:
+            raise ValueError(f"{name} must have {rows} rows")
+        p, ld = _row_ptr(t, dt, name, d)
+        setattr(a, name, p)
+        setattr(a, "ld" + name, ld)
+    gates = _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, int(w_post is not None if post is None else post), int(pre),
+                         residual_scale, eps)
+    for name, t, n in (("dw_post", dw_post, d), ("dw_pre", dw_pre, d), ("dgate", dgate, gates * d)):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must have {n} elements")
+        setattr(a, name, _ptr(t, f, name))
+    code = lib().armor_block_norm_backward(ctx, a, _stream())
+    if code:
+        _check(code, "armor_block_norm_backward")
 
 
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
@@ -569,6 +671,42 @@ class ArmorContext:
         y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
         armor_apply_layer_i8(self.ctx, packed, x, y)
         return y
+
+    # -- norms between two blocks
+    def block_norm(self, x: torch.Tensor, y: torch.Tensor | None = None, **terms) -> tuple[torch.Tensor, torch.Tensor]:
+        """(h, n): the residual stream x plus a block's output y, normed, weighted and gated, and the normed stream that the next
+        block reads.  terms: gate [d] or [n_gates, d] with rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps."""
+        self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
+        h = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+        n = torch.empty(x.shape, dtype=x.dtype if y is None else y.dtype, device=self.device)
+        armor_block_norm(self.ctx, x, y, h, n, None, None, **terms)
+        return h, n
+
+    def block_norm_i8(self, x: torch.Tensor, y: torch.Tensor | None = None, **terms) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(h, q, scale): as block_norm, the normed stream as int8 rows for linear_i8."""
+        self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
+        h = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+        q = self.new_int8_rows(x.shape[0], x.shape[1])
+        scale = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
+        armor_block_norm(self.ctx, x, y, h, None, q, scale, **terms)
+        return h, q, scale
+
+    def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor, dh: torch.Tensor | None, dn: torch.Tensor | None,
+                            **terms) -> dict[str, torch.Tensor]:
+        """The gradients dx, dy and those of the weights and the gate that are given (fp32), from the h that block_norm returned, y and
+        the gradients of h and n."""
+        gate, w_post, w_pre = terms.get("gate"), terms.get("w_post"), terms.get("w_pre")
+        self._here(h, y, dh, dn, gate, w_post, w_pre)
+        f = dict(dtype=torch.float32, device=self.device)
+        out = {"dx": torch.empty(h.shape, dtype=h.dtype, device=self.device), "dy": torch.empty(y.shape, dtype=y.dtype, device=self.device)}
+        if w_pre is not None:
+            out["dw_pre"] = torch.empty(w_pre.shape, **f)
+        if w_post is not None:
+            out["dw_post"] = torch.empty(w_post.shape, **f)
+        if gate is not None:
+            out["dgate"] = torch.empty(gate.shape, **f)
+        armor_block_norm_backward(self.ctx, h, y, dh, dn, out["dx"], out["dy"], out.get("dw_post"), out.get("dw_pre"), out.get("dgate"), **terms)
+        return out
 
     def device_status(self) -> list[int]:
         torch.cuda.current_stream().synchronize()

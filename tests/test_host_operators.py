@@ -62,6 +62,58 @@ def test_packed_layer_i8_sizes(lib):
     assert lib.armor_apply_layer_i8(None, None, None, None, 4, None) == INVALID
 
 
+P = 0x10000
+NORM = {"n_rows": 6, "d": 64, "x": P, "ldx": 64, "y": P, "ldy": 64, "h": P, "ldh": 64, "n": P, "ldn": 64, "stream_dtype": BF16,
+        "branch_dtype": BF16, "pre": 1, "post": 1, "residual_scale": 1.0, "eps": 1e-6}
+GRAD = {"n_rows": 6, "d": 64, "h": P, "ldh": 64, "y": P, "ldy": 64, "dh": P, "lddh": 64, "dn": P, "lddn": 64, "dx": P, "lddx": 64, "dy": P,
+        "lddy": 64, "stream_dtype": BF16, "branch_dtype": BF16, "pre": 1, "post": 1, "residual_scale": 1.0, "eps": 1e-6}
+GATE = {"gate": P, "ld_gate": 64, "rows_per_gate": 3, "n_gates": 2}
+BOTH = [
+    (INVALID, {}), (INVALID, {"n_rows": -1}), (INVALID, {"eps": -1.0}), (INVALID, {"eps": float("nan")}), (SHAPE, {"d": 0}),
+    (TOO_LARGE, {"d": 16385}), (TOO_LARGE, {"n_rows": 2 ** 31}),
+    (UNSUPPORTED, {"stream_dtype": SPARSE}), (UNSUPPORTED, {"branch_dtype": I8}), (UNSUPPORTED, {"branch_dtype": F32}),
+    (UNSUPPORTED, {"stream_dtype": F16}), (SHAPE, {"ldy": 63}), (SHAPE, {"ldh": 63}),
+    (SHAPE, {**GATE, "n_gates": 1}), (SHAPE, {**GATE, "rows_per_gate": 0}), (SHAPE, {**GATE, "ld_gate": 63}), (SHAPE, {**GATE, "n_gates": 0}),
+    (INVALID, {"w_pre": P, "pre": 0}), (INVALID, {"w_post": P, "post": 0}), (INVALID, GATE),
+]
+
+
+@pytest.mark.parametrize("want,change", BOTH + [
+    (INVALID, {"y": None}), (INVALID, {"y": None, "post": 0, **GATE}), (SHAPE, {"ldx": 63}), (SHAPE, {"ldn": 63}),
+    (SHAPE, {"q": P, "q_scale": P, "ldq": 72}), (SHAPE, {"q": P + 8, "q_scale": P, "ldq": 64}), (SHAPE, {"q": P, "q_scale": P, "ldq": 48}),
+    (INVALID, {"q": P, "ldq": 64}),
+])
+def test_block_norm_refuses(lib, want, change):
+    assert lib.armor_block_norm(None, Bd.armor_block_norm_args(**{**NORM, **change}), None) == want
+    assert lib.armor_block_norm(None, None, None) == INVALID
+
+
+@pytest.mark.parametrize("want,change", BOTH + [
+    (SHAPE, {"lddh": 63}), (SHAPE, {"lddn": 63}), (SHAPE, {"lddx": 63}), (SHAPE, {"lddy": 63}),
+    (INVALID, {"dw_pre": P, "pre": 0}), (INVALID, {"dw_post": P, "post": 0}), (INVALID, {"dgate": P}),
+])
+def test_block_norm_backward_refuses(lib, want, change):
+    assert lib.armor_block_norm_backward(None, Bd.armor_block_norm_grad_args(**{**GRAD, **change}), None) == want
+    assert lib.armor_block_norm_backward(None, None, None) == INVALID
+
+
+def test_structs_are_laid_out_as_in_the_header(lib, tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    lines = []
+    for s in (Bd.armor_block_norm_args, Bd.armor_block_norm_grad_args):
+        lines += [f'printf("%zu\\n", offsetof({s.__name__}, {f}));' for f, _ in s._fields_] + [f'printf("%zu\\n", sizeof({s.__name__}));']
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "armor.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0;\n}\n")
+    subprocess.check_call(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "layout")])
+    got = [int(v) for v in subprocess.check_output([str(tmp_path / "layout")]).split()]
+    want = []
+    for s in (Bd.armor_block_norm_args, Bd.armor_block_norm_grad_args):
+        want += [getattr(s, f).offset for f, _ in s._fields_] + [C.sizeof(s)]
+    assert got == want
+
+
 def test_binding_refuses(lib):
     x = torch.zeros(4, 32)
     q, s = torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4)
@@ -73,3 +125,9 @@ def test_binding_refuses(lib):
         Bd.armor_linear_i8(None, x, None, q, s, None, x)
     with pytest.raises(ValueError, match="bf16"):
         Bd.armor_apply_layer_i8(None, q, x, x)
+    with pytest.raises(ValueError, match="CUDA"):
+        Bd.armor_block_norm(None, x, x, x, x, None, None)
+    with pytest.raises(ValueError, match="CUDA"):
+        Bd.armor_block_norm_backward(None, x, x, x, x, x, x, None, None, None)
+    with pytest.raises(ValueError, match="missing"):
+        Bd.armor_block_norm_backward(None, None, None, None, None, None, None, None, None, None)
