@@ -14,6 +14,7 @@
 // is left to chance; the CTAs' sums are added in order by a second kernel, in fp64.  A gate's rows may end inside a CTA's: the CTA
 // keeps two sums for the gates at its ends, and writes one that lies within its rows at once.
 #include "rows_io.cuh"
+#include "tc_common.cuh"
 
 namespace {
 
@@ -120,8 +121,186 @@ block_norm_kernel(const NormP p) {
   if (threadIdx.x == 0) p.q_scale[row] = r.s;
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// Many rows on 16-byte boundaries: persistent CTAs take consecutive rows through a ring of rows in shared memory, which a warp of its
+// own fills by bulk copies several rows ahead, and keep their share of the weights in registers.  (A CTA a row reads the three fp32
+// weights, 12 bytes an element, for every 8 bytes of a bf16 row.)  What bounds these kernels then is the issue of instructions,
+// with 16 warps an SM, hence the arithmetic in pairs, one barrier a row and the copies (100 cycles each) by another warp.
+constexpr int MAX_STAGES = 4;
+struct Ring {
+  int stages, stage_bytes;
+  uint32_t off[4], bytes[4];           // where an array's row lies in a stage and its length, 0: not there
+  int threads;                         // of the CTA, without the warp that copies
+};
+struct RingBars { uint64_t full[MAX_STAGES], empty[MAX_STAGES]; int abort_flag; };
+
+// full[s]: the bytes of a row; empty[s]: a warp each, when it has read the row
+__device__ __forceinline__ void ring_open(RingBars& b, const Ring& ring) {
+  if (threadIdx.x == 0) {
+    b.abort_flag = 0;
+    for (int k = 0; k < ring.stages; ++k) {
+      tc::mbar_init(tc::smem_u32(&b.full[k]), 1);
+      tc::mbar_init(tc::smem_u32(&b.empty[k]), ring.threads / 32);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+}
+// The copying warp (one lane): rows [r_lo, r_hi) of up to four arrays.  A wait that gives up raises the status word; it then waits, bounded,
+// for what it has in flight, and the others run on without further waits.
+struct RingRows { const char* at[4]; int64_t ld[4]; };      // (bytes)
+__device__ __forceinline__ void ring_copy(RingBars& b, const Ring& ring, uint8_t* mem, const RingRows& a, int64_t r_lo, int64_t r_hi, int32_t* status) {
+  const uint32_t full0 = tc::smem_u32(b.full), empty0 = tc::smem_u32(b.empty), mem0 = tc::smem_u32(mem);
+  int stage = 0;
+  uint32_t phase = 0;
+  int64_t row = r_lo;
+  bool ok = true;
+  for (; row < r_hi; ++row) {
+    if (!tc::mbar_wait(empty0 + 8 * stage, phase ^ 1, &b.abort_flag, status)) { ok = false; break; }
+    const uint32_t bar = full0 + 8 * stage, dst = mem0 + (uint32_t)(stage * ring.stage_bytes);
+    tc::mbar_expect_tx(bar, (uint32_t)ring.stage_bytes);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (ring.bytes[k]) tc::bulk_load(dst + ring.off[k], a.at[k] + row * a.ld[k], ring.bytes[k], bar);
+    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
+  }
+  if (!ok)
+    for (int back = 1; back <= ring.stages && back <= row - r_lo; ++back) {
+      int k = stage - back;
+      uint32_t ph = phase;
+      if (k < 0) { k += ring.stages; ph ^= 1; }
+      const long long t0 = clock64();
+      while (!tc::mbar_try(full0 + 8 * k, ph) && clock64() - t0 < 20000000ll) {}
+    }
+}
+
+// HAS_Y: there is a branch.  gate (.) w_post of a gate's row
+template <int CHUNKS, typename P, typename Each>
+__device__ __forceinline__ void gain_of(const P& p, int64_t at, F2 (&G)[CHUNKS][4], Each&& each) {
+  each([&](int c, uint32_t e) {
+    F2 g[4];
+    if (p.w_post) raw_get2(raw_load(p.w_post + e), G[c]);
+    if (p.gate) {
+      raw_get2(raw_load(p.gate + at * p.ldg + e), g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) G[c][i] = p.w_post ? f2_mul(G[c][i], g[i]) : g[i];
+    }
+  });
+}
+
+template <typename TS, typename TB, int CHUNKS, bool HAS_Y>
+__global__ void __launch_bounds__(544)
+block_norm_ring_kernel(const NormP p, const Ring ring, int32_t* status) {
+  grid_begin();
+  extern __shared__ __align__(16) uint8_t stage_mem[];
+  __shared__ __align__(8) RingBars bars;
+  __shared__ float red[3][2][32];
+  const int64_t r_lo = rows_lo(blockIdx.x, p.rows, gridDim.x), r_hi = rows_lo(blockIdx.x + 1, p.rows, gridDim.x);
+  ring_open(bars, ring);
+  const int nt = ring.threads;
+  if (threadIdx.x >= nt) {
+    if (threadIdx.x == nt) {
+      RingRows a{};
+      a.at[0] = static_cast<const char*>(p.x); a.ld[0] = p.ldx * (int64_t)sizeof(TS);
+      a.at[1] = static_cast<const char*>(p.y); a.ld[1] = p.ldy * (int64_t)sizeof(TB);
+      ring_copy(bars, ring, stage_mem, a, r_lo, r_hi, status);
+    }
+    return;
+  }
+  const uint32_t full0 = tc::smem_u32(bars.full), empty0 = tc::smem_u32(bars.empty);
+  const float inv_d = 1.f / (float)p.d;
+  const uint32_t e0 = threadIdx.x * 8, step = nt * 8, n_el = (uint32_t)p.d;
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const uint32_t e = e0 + c * step;
+      if (e < n_el) f(c, e);
+    }
+  };
+  F2 wpre[CHUNKS][4], G[CHUNKS][4], h[CHUNKS][4];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); }
+  if (p.w_pre) each([&](int c, uint32_t e) { raw_get2(raw_load(p.w_pre + e), wpre[c]); });
+  int64_t at = p.gate ? r_lo / p.per_gate : 0, until = p.gate ? (at + 1) * p.per_gate : p.rows;
+  if (HAS_Y) gain_of<CHUNKS>(p, at, G, each);
+  // sum y^2 of the row in a stage
+  auto square_y = [&](int stage) {
+    const TB* const y = reinterpret_cast<const TB*>(stage_mem + (size_t)stage * ring.stage_bytes + ring.off[1]);
+    F2 s = 0;
+    each([&](int, uint32_t e) {
+      F2 v[4];
+      raw_get2(raw_load(y + e), v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = f2_fma(v[i], v[i], s);
+    });
+    return f2_sum(s);
+  };
+  // One barrier a row: the sum over y of the row to come is formed beside that over h of the row at hand.
+  const bool post = HAS_Y && p.post;
+  const F2 a2 = f2(p.a);
+  int stage = 0;
+  uint32_t phase = 0;
+  float r1 = 1.f;
+  tc::mbar_wait(full0, 0, &bars.abort_flag, status);
+  if (post) {
+    float s[2] = {square_y(0), 0.f};
+    part_sums(s, red[2], nt);
+    r1 = rsqrtf(s[0] * inv_d + p.eps);
+  }
+  for (int64_t row = r_lo; row < r_hi; ++row) {
+    const uint8_t* const mem = stage_mem + (size_t)stage * ring.stage_bytes;
+    const TS* const x = reinterpret_cast<const TS*>(mem);
+    const TB* const y = reinterpret_cast<const TB*>(mem + ring.off[1]);
+    if (HAS_Y && row == until) { gain_of<CHUNKS>(p, ++at, G, each); until += p.per_gate; }
+    F2 hh = 0;
+    const F2 r12 = f2(r1);
+    each([&](int c, uint32_t e) {
+      F2 v[4], xv[4];
+      raw_get2(raw_load(x + e), xv);
+      if (HAS_Y) raw_get2(raw_load(y + e), v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[c][i] = f2_mul(a2, xv[i]);
+        if (HAS_Y) h[c][i] = f2_fma(f2_mul(v[i], G[c][i]), r12, h[c][i]);
+        hh = f2_fma(h[c][i], h[c][i], hh);
+      }
+    });
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) tc::mbar_arrive(empty0 + 8 * stage);          // the warp has read its part of the row
+    if (p.h) each([&](int c, uint32_t e) { store8(static_cast<TS*>(p.h) + row * p.ldh + e, h[c]); });
+    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
+    float s[2] = {f2_sum(hh), 0.f};
+    if (row + 1 < r_hi) {
+      tc::mbar_wait(full0 + 8 * stage, phase, &bars.abort_flag, status);
+      if (post) s[1] = square_y(stage);
+    }
+    part_sums(s, red[row & 1], nt);
+    if (post) r1 = rsqrtf(s[1] * inv_d + p.eps);
+    const F2 r2 = f2(p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 1.f);
+    each([&](int c, uint32_t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[c][i] = f2_mul(h[c][i], f2_mul(r2, wpre[c][i]));
+    });
+    if (p.n) each([&](int c, uint32_t e) { store8(static_cast<TB*>(p.n) + row * p.ldn + e, h[c]); });
+    if (p.q) {
+      unsigned top = 0;
+      float v[CHUNKS][8];
+      each([&](int c, uint32_t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 t = f2_get(h[c][i]); v[c][2 * i] = t.x; v[c][2 * i + 1] = t.y; }
+        top = max(top, abs_bits8(v[c]));
+      });
+      const RowScale r = row_scale(part_max(top, red[2], nt));
+      each([&](int c, uint32_t e) { *reinterpret_cast<uint2*>(p.q + row * p.ldq + e) = row_round8(v[c], r); });
+      if (threadIdx.x == 0) p.q_scale[row] = r.s;
+    }
+  }
+}
+
 struct GradP {
-  int64_t rows, d, ldh, ldy, lddh, lddn, lddx, lddy, ldg, per_gate, n_gates;
+  int64_t rows, d, ldh, ldy, lddh, lddn, lddx, lddy, ldg, per_gate, gates_used;
   const void *h, *y, *dh, *dn;
   void *dx, *dy;
   const float *w_post, *w_pre, *gate;
@@ -288,67 +467,317 @@ block_norm_grad_kernel(const GradP p) {
   if (p.dw_post) spill(s_post, p.part + ((int64_t)part_post(p) * p.ctas + blockIdx.x) * d);
 }
 
-// The CTAs' sums added up in order: blockIdx.y = 0, 1: the weights' gradients, from 2 on: the gates'.  32 columns x 8 lanes of CTAs.
-__global__ void __launch_bounds__(256)
+// The gradient through the same ring.  One barrier a row: sum f y, which needs dh', is taken apart,
+//   sum f y = sum (G y) dh + (sum (G y) g - mean(g hbar) / rms(h) sum (G y) h) / rms(h),   G = gate (.) w_post,
+// so that all six sums of a row are formed at once.  And one running sum serves both the gate and w_post: t = sum dh' ybar over the rows of a
+// gate gives dgate = w_post t, and gate t is what these rows add to dw_post.
+template <typename TS, typename TB, int CHUNKS, int THREADS, bool HAS_Y>
+__global__ void __launch_bounds__(THREADS + 32)
+block_norm_grad_ring_kernel(const GradP p, const Ring ring, int32_t* status) {
+  grid_begin();
+  extern __shared__ __align__(16) uint8_t stage_mem[];
+  __shared__ __align__(8) RingBars bars;
+  __shared__ float red[2][8][32];
+  const int64_t d = p.d;
+  const int64_t r_lo = rows_lo(blockIdx.x, p.rows, p.ctas), r_hi = rows_lo(blockIdx.x + 1, p.rows, p.ctas);
+  ring_open(bars, ring);
+  const int nt = ring.threads;
+  if (threadIdx.x >= nt) {
+    if (threadIdx.x == nt) {
+      RingRows a{};
+      a.at[0] = static_cast<const char*>(p.h); a.ld[0] = p.ldh * (int64_t)sizeof(TS);
+      a.at[1] = static_cast<const char*>(p.y); a.ld[1] = p.ldy * (int64_t)sizeof(TB);
+      a.at[2] = static_cast<const char*>(p.dh); a.ld[2] = p.lddh * (int64_t)sizeof(TS);
+      a.at[3] = static_cast<const char*>(p.dn); a.ld[3] = p.lddn * (int64_t)sizeof(TB);
+      ring_copy(bars, ring, stage_mem, a, r_lo, r_hi, status);
+    }
+    return;
+  }
+  const uint32_t full0 = tc::smem_u32(bars.full), empty0 = tc::smem_u32(bars.empty);
+  float* const s_post = reinterpret_cast<float*>(stage_mem + (size_t)ring.stages * ring.stage_bytes);    // dw_post so far
+  const float inv_d = 1.f / (float)d;
+  const uint32_t e0 = threadIdx.x * 8, step = nt * 8, n_el = (uint32_t)d;
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      const uint32_t e = e0 + c * step;
+      if (e < n_el) f(c, e);
+    }
+  };
+  // an array that is not given is read from a row of zeros behind the sums
+  uint8_t* const zeros = reinterpret_cast<uint8_t*>(s_post) + (HAS_Y && p.dw_post ? d * 4 : 0);
+  if (!p.h || !p.dh || !p.dn) each([&](int, uint32_t e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) reinterpret_cast<TS*>(zeros)[e + i] = from_f<TS>(0.f);     // (a thread reads what it has written; TB is no wider)
+    if (sizeof(TB) != sizeof(TS)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) reinterpret_cast<TB*>(zeros + d * sizeof(TS))[e + i] = from_f<TB>(0.f);
+    }
+  });
+  const uint8_t* const zeros_b = sizeof(TB) == sizeof(TS) ? zeros : zeros + d * sizeof(TS);
+  F2 wpre[CHUNKS][4], G[CHUNKS][4], a_pre[CHUNKS][4], a_t[CHUNKS][4];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); a_pre[c][i] = 0; a_t[c][i] = 0; }
+  if (p.w_pre) each([&](int c, uint32_t e) { raw_get2(raw_load(p.w_pre + e), wpre[c]); });
+  const int64_t g_first = p.gate ? r_lo / p.per_gate : 0;
+  int64_t at = g_first, until = p.gate ? (at + 1) * p.per_gate : p.rows;
+  if (HAS_Y) gain_of<CHUNKS>(p, at, G, each);
+  if (HAS_Y && p.dw_post) each([&](int, uint32_t e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s_post[e + i] = 0.f;
+  });
+  // the rows of a gate are through (or the CTA's share of them): its gradient or a sum for the CTA's first or its last gate, and dw_post
+  auto gate_done = [&](int64_t g) {
+    const int64_t g0 = g * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
+    float* const out = !p.dgate ? nullptr : (r_lo <= g0 && g1 <= r_hi ? p.dgate + g * d
+                                  : p.part + ((int64_t)(part_gate(p) + (g == g_first ? 0 : 1)) * p.ctas + blockIdx.x) * d);
+    each([&](int c, uint32_t e) {
+      F2 w[4], v[4];
+      if (out) {
+        if (p.w_post) raw_get2(raw_load(p.w_post + e), w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = p.w_post ? f2_mul(w[i], a_t[c][i]) : a_t[c][i];
+        store8(out + e, v);
+      }
+      if (p.dw_post) {
+        if (p.gate) raw_get2(raw_load(p.gate + g * p.ldg + e), w);
+        raw_get2(raw_load(static_cast<const float*>(s_post + e)), v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2_fma(p.gate ? w[i] : f2(1.f), a_t[c][i], v[i]);
+        store8(s_post + e, v);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a_t[c][i] = 0;
+    });
+  };
+  const F2 a2 = f2(p.a);
+  int stage = 0;
+  uint32_t phase = 0;
+  for (int64_t row = r_lo; row < r_hi; ++row) {
+    const uint8_t* const mem = stage_mem + (size_t)stage * ring.stage_bytes;
+    const TS* const h = reinterpret_cast<const TS*>(p.h ? mem + ring.off[0] : zeros);
+    const TB* const y = reinterpret_cast<const TB*>(mem + ring.off[1]);
+    const TS* const dh = reinterpret_cast<const TS*>(p.dh ? mem + ring.off[2] : zeros);
+    const TB* const dn = reinterpret_cast<const TB*>(p.dn ? mem + ring.off[3] : zeros_b);
+    if (HAS_Y && row == until) { gain_of<CHUNKS>(p, ++at, G, each); until += p.per_gate; }
+    tc::mbar_wait(full0 + 8 * stage, phase, &bars.abort_flag, status);
+    F2 q[6] = {0, 0, 0, 0, 0, 0};
+    each([&](int c, uint32_t e) {
+      F2 hv[4], gv[4], yv[4], dv[4];
+      raw_get2(raw_load(h + e), hv);
+      raw_get2(raw_load(dn + e), gv);
+      if (HAS_Y) {
+        raw_get2(raw_load(y + e), yv);
+        raw_get2(raw_load(dh + e), dv);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const F2 g = f2_mul(gv[i], wpre[c][i]);
+        q[0] = f2_fma(hv[i], hv[i], q[0]);
+        q[1] = f2_fma(g, hv[i], q[1]);
+        if (HAS_Y) {
+          const F2 u = f2_mul(yv[i], G[c][i]);
+          q[2] = f2_fma(yv[i], yv[i], q[2]);
+          q[3] = f2_fma(u, dv[i], q[3]);
+          q[4] = f2_fma(u, g, q[4]);
+          q[5] = f2_fma(u, hv[i], q[5]);
+        }
+      }
+    });
+    float s[8] = {f2_sum(q[0]), f2_sum(q[1]), f2_sum(q[2]), f2_sum(q[3]), f2_sum(q[4]), f2_sum(q[5]), 0.f, 0.f};
+    if (HAS_Y) part_sums(s, red[row & 1], nt);
+    else {
+      float two[2] = {s[0], s[1]};
+      part_sums(two, red[row & 1], nt);
+      s[0] = two[0]; s[1] = two[1];
+    }
+    const float r2 = p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 1.f, m2 = p.pre ? s[1] * inv_d * r2 * r2 : 0.f;
+    const float r1 = p.post ? rsqrtf(s[2] * inv_d + p.eps) : 1.f;
+    const float m1 = p.post ? (s[3] + r2 * (s[4] - m2 * s[5])) * inv_d * r1 * r1 : 0.f;
+    const F2 r22 = f2(r2), r12 = f2(r1), c2 = f2(-r2 * m2), c1 = f2(-r1 * m1);
+    each([&](int c, uint32_t e) {
+      F2 hv[4], nv[4], yv[4], dv[4], o[4];
+      raw_get2(raw_load(h + e), hv);
+      raw_get2(raw_load(dn + e), nv);
+      raw_get2(raw_load(dh + e), dv);
+      if (HAS_Y) raw_get2(raw_load(y + e), yv);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dv[i] = f2_fma(hv[i], c2, f2_fma(f2_mul(nv[i], wpre[c][i]), r22, dv[i]));           // dh'
+        o[i] = f2_mul(a2, dv[i]);
+        a_pre[c][i] = f2_fma(nv[i], f2_mul(hv[i], r22), a_pre[c][i]);
+        if (HAS_Y) a_t[c][i] = f2_fma(dv[i], f2_mul(yv[i], r12), a_t[c][i]);
+      }
+      if (p.dx) store8(static_cast<TS*>(p.dx) + row * p.lddx + e, o);
+      if (HAS_Y) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dv[i] = f2_fma(yv[i], c1, f2_mul(f2_mul(G[c][i], dv[i]), r12));
+      }
+      if (p.dy) store8(static_cast<TB*>(p.dy) + row * p.lddy + e, dv);
+    });
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) tc::mbar_arrive(empty0 + 8 * stage);          // the warp has read its part of the row
+    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
+    if (HAS_Y && (row + 1 == r_hi || row + 1 == until)) gate_done(at);
+  }
+  if (p.dw_pre) each([&](int c, uint32_t e) { store8(p.part + ((int64_t)part_pre(p) * p.ctas + blockIdx.x) * d + e, a_pre[c]); });
+  if (HAS_Y && p.dw_post) each([&](int, uint32_t e) {
+    F2 v[4];
+    raw_get2(raw_load(static_cast<const float*>(s_post + e)), v);
+    store8(p.part + ((int64_t)part_post(p) * p.ctas + blockIdx.x) * d + e, v);
+  });
+}
+
+// The CTAs' sums added up in order: blockIdx.y = 0, 1: the weights' gradients, from 2 on: the gates' that have rows of several CTAs, found
+// by the gate or, where gates are more than CTAs, by the border between two CTAs.  32 columns x 32 lanes of CTAs, a thread takes VEC columns.
+template <int VEC>
+__global__ void __launch_bounds__(1024 / VEC)
 block_norm_grad_sums_kernel(const GradP p) {
   grid_begin();
-  __shared__ double add[8][32];
-  const int64_t col = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int lane = threadIdx.x >> 5;
-  for (int64_t y = blockIdx.y; y < 2 + (p.dgate ? p.n_gates : 0); y += gridDim.y) {
-    int64_t b0 = 0, b1 = p.ctas;
-    float* out;
-    const float* part;
-    int64_t gate = -1;
-    if (y == 0) { out = p.dw_pre; part = p.part + (int64_t)part_pre(p) * p.ctas * p.d; }
-    else if (y == 1) { out = p.dw_post; part = p.part + (int64_t)part_post(p) * p.ctas * p.d; }
-    else {
-      gate = y - 2;
-      out = p.dgate + gate * p.d;
-      part = p.part + (int64_t)part_gate(p) * p.ctas * p.d;
-      const int64_t g0 = gate * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
-      if (g0 >= p.rows) b1 = 0;                             // no rows of its own
-      else {
-        b0 = rows_owner(g0, p.rows, p.ctas);
-        b1 = rows_owner(g1 - 1, p.rows, p.ctas) + 1;
-        if (b1 == b0 + 1) continue;                         // the CTA has written it
-      }
+  constexpr int CT = 32 / VEC;                              // threads side by side
+  __shared__ double add[32][33];
+  const int lane = threadIdx.x / CT, c0 = threadIdx.x % CT * VEC;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c0;
+  int64_t b0 = 0, b1 = p.ctas, second = p.ctas;
+  float* out;
+  const float* part;
+  const int y = blockIdx.y;
+  if (y == 0) { out = p.dw_pre; part = p.part + (int64_t)part_pre(p) * p.ctas * p.d; }
+  else if (y == 1) { out = p.dw_post; part = p.part + (int64_t)part_post(p) * p.ctas * p.d; }
+  else {
+    int64_t gate = y - 2;
+    if (p.gates_used > p.ctas) {
+      const int64_t first = rows_lo(y - 1, p.rows, p.ctas);
+      gate = first / p.per_gate;
+      if (first == gate * p.per_gate || rows_owner(gate * p.per_gate, p.rows, p.ctas) != y - 2) return;
     }
-    if (!out) continue;
-    double t = 0.0;
-    if (col < p.d)
-      for (int64_t b = b0 + lane; b < b1; b += 8) {
-        // a gate that is not the CTA's first lies in the CTA's second sum
-        const bool second = gate >= 0 && rows_lo(b, p.rows, p.ctas) / p.per_gate != gate;
-        t += (double)part[((second ? p.ctas : 0) + b) * p.d + col];
-      }
-    __syncthreads();
-    add[lane][threadIdx.x & 31] = t;
-    __syncthreads();
-    if (lane == 0 && col < p.d) {
+    out = p.dgate + gate * p.d;
+    part = p.part + (int64_t)part_gate(p) * p.ctas * p.d;
+    const int64_t g0 = gate * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
+    b0 = rows_owner(g0, p.rows, p.ctas);
+    b1 = rows_owner(g1 - 1, p.rows, p.ctas) + 1;
+    if (b1 == b0 + 1) return;                               // the CTA has written it
+    // a gate that is not its first CTA's first lies in that CTA's second sum; it is the others' first
+    if (rows_lo(b0, p.rows, p.ctas) / p.per_gate != gate) second = b0;
+  }
+  if (!out) return;
+  double t[VEC] = {};
+  if (col < p.d) {
+    const float* at = part + col;
+#pragma unroll 5
+    for (int64_t b = b0 + lane; b < b1; b += 32) {
+      const float* v = at + (b == second ? p.ctas + b : b) * p.d;
+      if (VEC == 4) {
+        const float4 f = *reinterpret_cast<const float4*>(v);
+        t[0] += f.x; t[1 % VEC] += f.y; t[2 % VEC] += f.z; t[3 % VEC] += f.w;
+      } else t[0] += *v;
+    }
+  }
 #pragma unroll
-      for (int k = 1; k < 8; ++k) t += add[k][threadIdx.x & 31];
-      out[col] = (float)t;
-    }
+  for (int i = 0; i < VEC; ++i) add[lane][c0 + i] = t[i];
+  __syncthreads();
+  // a warp adds a column at a time: the lanes' sums in a fixed tree
+  for (int c = threadIdx.x >> 5; c < 32; c += 32 / VEC) {
+    double u = add[threadIdx.x & 31][c];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+    const int64_t mine = (int64_t)blockIdx.x * 32 + c;
+    if ((threadIdx.x & 31) == 0 && mine < p.d) out[mine] = (float)u;
   }
 }
 
+// Ring and CTAs an SM for rows of d elements in arrays of these element sizes (0: not read), `kept` bytes of shared memory beside them
+// an element.  CHUNKS 1 up to `single` elements, 2 up to 8,192, CTAs of together 512 threads at least: the registers of an SM
+// hold about so many.  False: d is no multiple of eight, too long, or not even two rows fit.
+constexpr size_t RING_SMEM = 228 * 1024 - 4096;
+bool plan_ring(int64_t d, size_t e0, size_t e1, size_t e2, size_t e3, size_t kept, int64_t single, Ring& r, int& ctas, int& chunks, size_t& smem) {
+  if (d % 8 || d > 8192) return false;
+  chunks = d <= single ? 1 : 2;
+  const int threads = (int)(((d / 8 + chunks - 1) / chunks + 31) / 32 * 32);
+  const size_t es[4] = {e0, e1, e2, e3};
+  r.stage_bytes = 0;
+  r.threads = threads;
+  for (int k = 0; k < 4; ++k) {
+    r.off[k] = (uint32_t)r.stage_bytes;
+    r.bytes[k] = (uint32_t)(es[k] * (size_t)d);
+    r.stage_bytes += (int)r.bytes[k];
+  }
+  ctas = threads >= 512 ? 1 : (512 / threads < 8 ? 512 / threads : 8);
+  for (; ctas >= 1; --ctas) {
+    const size_t room = RING_SMEM / (size_t)ctas - 3072;
+    const size_t keep = kept * (size_t)d;
+    if (room < keep) continue;
+    int n = (int)((room - keep) / (size_t)r.stage_bytes);
+    if (n > MAX_STAGES) n = MAX_STAGES;
+    if (n >= 3 || (n == 2 && ctas == 1)) {
+      r.stages = n;
+      smem = (size_t)r.stages * r.stage_bytes + keep;
+      return true;
+    }
+  }
+  return false;
+}
+
 template <typename TS, typename TB, bool ALIGNED>
-void launch_norm(const NormP& p, int64_t rows, cudaStream_t s) {
+armor_status launch_norm(armor_ctx* c, const NormP& p, int64_t rows, cudaStream_t s) {
   const int64_t units = (p.d + 7) / 8;
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
+  Ring ring;
+  int ctas, chunks;
+  size_t smem;
+  if (ALIGNED && rows > 2 * c->n_sm && plan_ring(p.d, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 4096, ring, ctas, chunks, smem)) {
+    const int64_t grid = (int64_t)ctas * c->n_sm < rows ? (int64_t)ctas * c->n_sm : rows;
+    auto run = [&](auto kernel, PerDeviceOnce& attr) {
+      if (ensure_dynamic_smem(attr, c->device, kernel, RING_SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+      launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)ring.threads + 32), smem, s, p, ring, c->status);
+      return ARMOR_OK;
+    };
+    static PerDeviceOnce at1, at2, at3, at4;
+    if (chunks == 1) return p.y ? run(block_norm_ring_kernel<TS, TB, 1, true>, at1) : run(block_norm_ring_kernel<TS, TB, 1, false>, at2);
+    return p.y ? run(block_norm_ring_kernel<TS, TB, 2, true>, at3) : run(block_norm_ring_kernel<TS, TB, 2, false>, at4);
+  }
   const dim3 grid((unsigned)rows);
   if (units <= 128 || (rows <= 148 && units <= 1024)) launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 1>, grid, threads(1), 0, s, p);
   else if (units <= 512) launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 2>, grid, threads(2), 0, s, p);
   else launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 4>, grid, threads(4), 0, s, p);
+  return ARMOR_OK;
 }
 template <typename TS, typename TB, bool ALIGNED>
-armor_status launch_grad(armor_ctx* c, const GradP& p, cudaStream_t s) {
+armor_status launch_grad(armor_ctx* c, GradP p, cudaStream_t s) {
   const int64_t units = (p.d + 7) / 8;
   const int n_sums = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 1 : 0);
   const size_t smem = (size_t)n_sums * (size_t)units * 8 * sizeof(float);
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
-  if (units <= 1024) {
+  Ring ring;
+  int ctas = 2, chunks = 0;
+  size_t ring_smem = 0;
+  const size_t kept = (p.dw_post ? 4 : 0) + (p.h && p.dh && p.dn ? 0 : sizeof(TS) + (sizeof(TB) != sizeof(TS) ? sizeof(TB) : 0));
+  const bool use_ring = ALIGNED && plan_ring(p.d, p.h ? sizeof(TS) : 0, p.y ? sizeof(TB) : 0, p.dh ? sizeof(TS) : 0, p.dn ? sizeof(TB) : 0, kept, 5120, ring, ctas, chunks, ring_smem);
+  if (!use_ring) ctas = 2;
+  // CTAs as many as an SM runs, fewer where the workspace has no room for their sums
+  const int64_t parts = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 2 : 0);
+  int64_t n = (int64_t)ctas * c->n_sm;
+  if (n > p.rows) n = p.rows;
+  if (parts && n > ws_scratch_bytes(c) / (parts * p.d * 4)) n = ws_scratch_bytes(c) / (parts * p.d * 4);
+  if (n < 1) return ARMOR_ERR_WORKSPACE;
+  p.ctas = (int)n;
+  auto run_ring = [&](auto kernel, PerDeviceOnce& attr) {
+    if (ensure_dynamic_smem(attr, c->device, kernel, RING_SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+    launch_dependent(kernel, dim3((unsigned)p.ctas), dim3((unsigned)ring.threads + 32), ring_smem, s, p, ring, c->status);
+    return ARMOR_OK;
+  };
+  static PerDeviceOnce at[8];
+  armor_status st = ARMOR_OK;
+  if (use_ring) {
+    // (threads of a CTA by what the registers allow: 120, 96, 152 and 120 a thread)
+    if (p.d <= 4096) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 512, true>, at[0]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 512, false>, at[1]);
+    else if (p.d <= 5120) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 640, true>, at[2]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 640, false>, at[3]);
+    else if (p.d <= 6144) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 384, true>, at[4]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 384, false>, at[5]);
+    else st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 512, true>, at[6]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 512, false>, at[7]);
+    if (st != ARMOR_OK) return st;
+  } else if (units <= 1024) {
     static PerDeviceOnce attr;
     if (ensure_dynamic_smem(attr, c->device, block_norm_grad_kernel<TS, TB, ALIGNED, 1>, 98304) != ARMOR_OK) return ARMOR_ERR_CUDA;
     launch_dependent(block_norm_grad_kernel<TS, TB, ALIGNED, 1>, dim3((unsigned)p.ctas), threads(1), smem, s, p);
@@ -359,8 +788,10 @@ armor_status launch_grad(armor_ctx* c, const GradP& p, cudaStream_t s) {
   }
   c->launches++;
   if (n_sums) {
-    const int64_t sets = 2 + (p.dgate ? p.n_gates : 0);
-    launch_dependent(block_norm_grad_sums_kernel, dim3((unsigned)((p.d + 31) / 32), (unsigned)(sets < 64 ? sets : 64)), dim3(256), 0, s, p);
+    const int64_t sets = 2 + (p.dgate ? (p.gates_used > p.ctas ? p.ctas - 1 : p.gates_used) : 0);
+    const dim3 grid((unsigned)((p.d + 31) / 32), (unsigned)sets);
+    if (p.d % 4 == 0) launch_dependent(block_norm_grad_sums_kernel<4>, grid, dim3(256), 0, s, p);
+    else launch_dependent(block_norm_grad_sums_kernel<1>, grid, dim3(1024), 0, s, p);
     c->launches++;
   }
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
@@ -417,14 +848,13 @@ extern "C" armor_status armor_block_norm(armor_ctx* c, const armor_block_norm_ar
                   (!p.n || rows::aligned16(p.n, p.ldn, eb)) && (!p.gate || rows::aligned16(p.gate, p.ldg, 4)) && rows::aligned16(p.w_post, 0, 4) &&
                   rows::aligned16(p.w_pre, 0, 4);
   KTimer kt(c, ARMOR_KC_FORWARD, (double)p.rows * (double)p.d * (es + (p.y ? eb : 0) + (p.h ? es : 0) + (p.n ? eb : 0) + (p.q ? 1 : 0)), s);
-  by_types(g->stream_dtype, g->branch_dtype, [&](auto ts, auto tb) {
+  st = by_types(g->stream_dtype, g->branch_dtype, [&](auto ts, auto tb) {
     using TS = decltype(ts);
     using TB = decltype(tb);
-    if (al) launch_norm<TS, TB, true>(p, p.rows, s);
-    else launch_norm<TS, TB, false>(p, p.rows, s);
-    return ARMOR_OK;
+    return al ? launch_norm<TS, TB, true>(c, p, p.rows, s) : launch_norm<TS, TB, false>(c, p, p.rows, s);
   });
   c->launches++;
+  if (st != ARMOR_OK) return st;
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }
 
@@ -446,27 +876,23 @@ extern "C" armor_status armor_block_norm_backward(armor_ctx* c, const armor_bloc
   }
   if ((!g->dh && !g->dn) || (!g->dx && !g->dy && !g->dw_pre && !g->dw_post && !g->dgate)) return ARMOR_ERR_INVALID_ARG;
   if (!g->h && g->pre) return ARMOR_ERR_INVALID_ARG;
-  if (!g->y && (g->post || g->dgate)) return ARMOR_ERR_INVALID_ARG;
+  if (!g->y && (g->post || g->dgate)) return ARMOR_ERR_INVALID_ARG;   // (with a gate alone y is read where it is given)
   GradP p{};
   p.rows = g->n_rows; p.d = g->d; p.ldh = g->ldh; p.ldy = g->ldy; p.lddh = g->lddh; p.lddn = g->lddn; p.lddx = g->lddx; p.lddy = g->lddy;
-  p.ldg = g->ld_gate; p.per_gate = g->gate ? g->rows_per_gate : 1; p.n_gates = g->gate ? g->n_gates : 0;
-  p.h = g->pre ? g->h : nullptr; p.y = g->post || g->dgate ? g->y : nullptr; p.dh = g->dh; p.dn = g->dn; p.dx = g->dx; p.dy = g->dy;
+  p.ldg = g->ld_gate; p.per_gate = g->gate ? g->rows_per_gate : 1; p.gates_used = g->gate ? (p.rows - 1) / p.per_gate + 1 : 0;
+  p.h = g->pre ? g->h : nullptr; p.y = g->post || g->gate ? g->y : nullptr; p.dh = g->dh; p.dn = g->dn; p.dx = g->dx; p.dy = g->dy;
   p.w_post = g->w_post; p.w_pre = g->w_pre; p.gate = g->gate;
   p.dw_post = g->dw_post; p.dw_pre = g->dw_pre; p.dgate = g->dgate;
   p.part = c->T; p.a = g->residual_scale; p.eps = g->eps; p.post = g->post != 0; p.pre = g->pre != 0;
-  // Two CTAs an SM, fewer where the workspace has no room for their sums
-  const int64_t sums = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 2 : 0);
-  int64_t ctas = 2 * c->n_sm;
-  if (ctas > p.rows) ctas = p.rows;
-  if (sums && ctas > ws_scratch_bytes(c) / (sums * p.d * 4)) ctas = ws_scratch_bytes(c) / (sums * p.d * 4);
-  if (ctas < 1) return ARMOR_ERR_WORKSPACE;
-  p.ctas = (int)ctas;
   const int es = rows_dtype_bytes(g->stream_dtype), eb = rows_dtype_bytes(g->branch_dtype);
   const bool al = rows::aligned16(p.h, p.ldh, es) && rows::aligned16(p.y, p.ldy, eb) && rows::aligned16(p.dh, p.lddh, es) &&
                   rows::aligned16(p.dn, p.lddn, eb) && rows::aligned16(p.dx, p.lddx, es) && rows::aligned16(p.dy, p.lddy, eb) &&
-                  rows::aligned16(p.gate, p.ldg, 4) && rows::aligned16(p.w_post, 0, 4) && rows::aligned16(p.w_pre, 0, 4);
+                  rows::aligned16(p.gate, p.ldg, 4) && rows::aligned16(p.w_post, 0, 4) && rows::aligned16(p.w_pre, 0, 4) &&
+                  rows::aligned16(p.dgate, 0, 4);
   KTimer kt(c, ARMOR_KC_FORWARD, (double)p.rows * (double)p.d *
             ((p.h ? es : 0) + (p.y ? eb : 0) + (p.dh ? es : 0) + (p.dn ? eb : 0) + (p.dx ? es : 0) + (p.dy ? eb : 0)), s);
+  if (p.dgate && p.gates_used < g->n_gates)                 // gates without rows
+    ARMOR_CUDA_OK(cudaMemsetAsync(p.dgate + p.gates_used * p.d, 0, (size_t)(g->n_gates - p.gates_used) * (size_t)p.d * 4, s));
   return by_types(g->stream_dtype, g->branch_dtype, [&](auto ts, auto tb) {
     using TS = decltype(ts);
     using TB = decltype(tb);

@@ -63,6 +63,45 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// ---------------------------------------------------------------- pairs of floats: one instruction for two
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float2 f2_get(F2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float f2_sum(F2 v) { const float2 f = f2_get(v); return f.x + f.y; }
+template <typename T>
+__device__ __forceinline__ void raw_get2(const Raw8<T>& r, F2 (&v)[4]) {
+  float f[8];
+  raw_get(r, f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const F2 (&v)[4]) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 t = f2_get(v[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
+  store8(p, f);
+}
+
 // Elements e .. e + 7 of a row of n, zeros behind its end.  ALIGNED: rows start on 16-byte boundaries, so that only the last chunk of
 // a row whose length is no multiple of eight is taken element by element; else all are.
 template <bool ALIGNED, typename T>
@@ -108,6 +147,44 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float (*buf)[32]) {
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     v[k] = t;
   }
+}
+// Sums of N (2 or 8) values at once over the first `threads` threads of a CTA, which meet at barrier 1: the lanes of a warp halve the values
+// between them before they add (8: 9 shuffles where one value at a time takes 40), 32 / N neighbouring lanes end with a value each.  Between a
+// use of a buffer and the next one of the same lies the barrier of one on another buffer.
+template <int N>
+__device__ __forceinline__ void part_sums(float (&v)[N], float (*buf)[32], int threads) {
+  constexpr int LANES = 32 / N;                             // that hold one value
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
+#pragma unroll
+  for (int half = N / 2, o = 16; half > 0; half >>= 1, o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int k = 0; k < half; ++k) {
+      const float give = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
+      v[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  float t = v[0];
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  if (warps > 1) {
+    if (lane % LANES == 0) buf[lane / LANES][warp] = t;
+    asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+    t = 0.f;
+    for (int w = lane % LANES; w < warps; w += LANES) t += buf[lane / LANES][w];
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * LANES);
+}
+__device__ __forceinline__ unsigned part_max(unsigned v, float (*buf)[32], int threads) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
+  v = __reduce_max_sync(0xffffffffu, v);
+  if (warps == 1) return v;
+  if (lane == 0) buf[0][warp] = __uint_as_float(v);
+  asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+  return __reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(buf[0][lane]) : 0u);
 }
 __device__ __forceinline__ unsigned cta_max(unsigned v, float (*buf)[32]) {
   v = __reduce_max_sync(0xffffffffu, v);

@@ -77,6 +77,13 @@ __device__ __forceinline__ void tma_load_mn(uint32_t dst, const CUtensorMap* map
   }
 }
 
+// bytes (a multiple of 16) from global to shared memory, both on 16-byte boundaries
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 // x - trunc_tf32(x)
 __device__ __forceinline__ float4 low4(const float4 v) {
   return make_float4(v.x - __uint_as_float(__float_as_uint(v.x) & 0xffffe000u), v.y - __uint_as_float(__float_as_uint(v.y) & 0xffffe000u),

@@ -73,7 +73,9 @@ def terms(t, **kw):
     return dict(gate=t["gate"], rows_per_gate=t["rows_per_gate"], w_post=t["w_post"], w_pre=t["w_pre"], **kw)
 
 
-WIDTHS = [(1, 1), (3, 7), (5, 8), (2, 64), (37, 129), (300, 1024), (7, 1030), (160, 4096), (1, 4096), (33, 5121), (200, 8192), (5, 16384), (150, 10001)]
+WIDTHS = [(1, 1), (3, 7), (5, 8), (2, 64), (37, 129), (300, 1024), (7, 1030), (160, 4096), (1, 4096), (33, 5121), (200, 8192), (5, 16384), (150, 10001),
+          # rows through the ring in shared memory, at the edges of its threads and of their share of a row
+          (700, 8), (700, 264), (400, 2056), (330, 4104), (320, 5128), (310, 6152), (300, 8184)]
 
 
 # ---------------------------------------------------------------------------------------------- forward
