@@ -122,181 +122,256 @@ block_norm_kernel(const NormP p) {
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// Many rows on 16-byte boundaries: persistent CTAs take consecutive rows through a ring of rows in shared memory, which a warp of its
-// own fills by bulk copies several rows ahead, and keep their share of the weights in registers.  (A CTA a row reads the three fp32
-// weights, 12 bytes an element, for every 8 bytes of a bf16 row.)  What bounds these kernels then is the issue of instructions,
-// with 16 warps an SM, hence the arithmetic in pairs, one barrier a row and the copies (100 cycles each) by another warp.
-constexpr int MAX_STAGES = 4;
+// Many rows: persistent CTAs take consecutive rows through a ring of rows in shared memory, filled by bulk copies several rows ahead,
+// and keep their share of the weights in registers.  (A CTA a row reads the three fp32 weights, 12 bytes an element, for every 8 bytes of a
+// bf16 row.)  What bounds these kernels is the issue of instructions, with 16 warps an SM or fewer: hence the arithmetic in pairs, one
+// barrier a row, and the copies (100 cycles each) by a warp an array.  Nothing may spill: the ring leaves L1 so little that a spilled
+// register costs a trip to L2 (16,384 x 5,120 with an fp32 stream 481 us, without spills 244).  Tried and dropped: sums put down
+// and picked up later through an mbarrier instead of the barrier (4,096 x 4,096 63 -> 80 us), rows cut between the CTAs of a cluster (8,192
+// columns 147 -> 249), a warp of its own for the copies (17 warps leave 96 registers a thread where 16 leave 128).
+constexpr int MAX_STAGES = 6;
 struct Ring {
   int stages, stage_bytes;
-  uint32_t off[4], bytes[4];           // where an array's row lies in a stage and its length, 0: not there
-  int threads;                         // of the CTA, without the warp that copies
+  uint32_t off[4], bytes[4];           // where an array's row lies in a stage, and its length, 0: not there
+  int arrays;                          // of them
 };
-struct RingBars { uint64_t full[MAX_STAGES], empty[MAX_STAGES]; int abort_flag; };
+struct RingBars { uint64_t full[MAX_STAGES]; int abort_flag; };
 
-// full[s]: the bytes of a row; empty[s]: a warp each, when it has read the row
 __device__ __forceinline__ void ring_open(RingBars& b, const Ring& ring) {
   if (threadIdx.x == 0) {
     b.abort_flag = 0;
-    for (int k = 0; k < ring.stages; ++k) {
-      tc::mbar_init(tc::smem_u32(&b.full[k]), 1);
-      tc::mbar_init(tc::smem_u32(&b.empty[k]), ring.threads / 32);
-    }
+    for (int k = 0; k < ring.stages; ++k) tc::mbar_init(tc::smem_u32(&b.full[k]), ring.arrays);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
 }
-// The copying warp (one lane): rows [r_lo, r_hi) of up to four arrays.  A wait that gives up raises the status word; it then waits, bounded,
-// for what it has in flight, and the others run on without further waits.
-struct RingRows { const char* at[4]; int64_t ld[4]; };      // (bytes)
-__device__ __forceinline__ void ring_copy(RingBars& b, const Ring& ring, uint8_t* mem, const RingRows& a, int64_t r_lo, int64_t r_hi, int32_t* status) {
-  const uint32_t full0 = tc::smem_u32(b.full), empty0 = tc::smem_u32(b.empty), mem0 = tc::smem_u32(mem);
-  int stage = 0;
-  uint32_t phase = 0;
-  int64_t row = r_lo;
-  bool ok = true;
-  for (; row < r_hi; ++row) {
-    if (!tc::mbar_wait(empty0 + 8 * stage, phase ^ 1, &b.abort_flag, status)) { ok = false; break; }
-    const uint32_t bar = full0 + 8 * stage, dst = mem0 + (uint32_t)(stage * ring.stage_bytes);
-    tc::mbar_expect_tx(bar, (uint32_t)ring.stage_bytes);
+// The array that this thread copies.  A row that starts or ends off a 16-byte boundary is copied from the boundary before to the
+// one behind: up to 15 bytes more, of the same 16-byte words and never looked at.
+struct RingCopy {
+  const char* base;                    // the array, null: this thread copies none
+  int64_t ld;                          // bytes from row to row
+  uint32_t bytes, off;
+  __device__ __forceinline__ RingCopy(const Ring& ring, const void* const (&at)[4], const int64_t (&lds)[4]) : base(nullptr), ld(0), bytes(0), off(0) {
+    const int per = blockDim.x >= 128 ? 32 : 1;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (ring.bytes[k]) tc::bulk_load(dst + ring.off[k], a.at[k] + row * a.ld[k], ring.bytes[k], bar);
-    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
+    for (int k = 0; k < 4; ++k)                             // (selected, not indexed: an array in registers has no address)
+      if ((int)threadIdx.x == k * per && ring.bytes[k]) { base = static_cast<const char*>(at[k]); ld = lds[k]; bytes = ring.bytes[k]; off = ring.off[k]; }
   }
-  if (!ok)
-    for (int back = 1; back <= ring.stages && back <= row - r_lo; ++back) {
-      int k = stage - back;
-      uint32_t ph = phase;
-      if (k < 0) { k += ring.stages; ph ^= 1; }
-      const long long t0 = clock64();
-      while (!tc::mbar_try(full0 + 8 * k, ph) && clock64() - t0 < 20000000ll) {}
-    }
+  __device__ __forceinline__ void operator()(RingBars& b, const Ring& ring, uint8_t* mem, int64_t row, int stage) const {
+    if (!base) return;
+    const char* const from = base + row * ld;
+    const uint32_t skip = (uint32_t)reinterpret_cast<uintptr_t>(from) & 15u, len = (skip + bytes + 15u) & ~15u;
+    const uint32_t bar = tc::smem_u32(&b.full[stage]);
+    tc::mbar_expect_tx(bar, len);
+    tc::bulk_load(tc::smem_u32(mem) + (uint32_t)(stage * ring.stage_bytes) + off, from - skip, len, bar);
+  }
+};
+// A wait that gave up has raised the status word and the others have run on without waits: nothing is in flight towards shared memory
+// when the kernel leaves, a bounded wait for the last of every stage.
+__device__ __forceinline__ void ring_drain(RingBars& b, const Ring& ring, int64_t rows) {
+  if (threadIdx.x != 0 || !*(volatile int*)&b.abort_flag) return;
+  for (int k = 0; k < ring.stages && k < rows; ++k) {
+    const uint32_t last = (uint32_t)((rows - 1 - k) / ring.stages) & 1u;
+    const long long t0 = clock64();
+    while (!tc::mbar_try(tc::smem_u32(&b.full[k]), last) && clock64() - t0 < 20000000ll) {}
+  }
 }
-
-// HAS_Y: there is a branch.  gate (.) w_post of a gate's row
-template <int CHUNKS, typename P, typename Each>
-__device__ __forceinline__ void gain_of(const P& p, int64_t at, F2 (&G)[CHUNKS][4], Each&& each) {
-  each([&](int c, uint32_t e) {
-    F2 g[4];
-    if (p.w_post) raw_get2(raw_load(p.w_post + e), G[c]);
-    if (p.gate) {
-      raw_get2(raw_load(p.gate + at * p.ldg + e), g);
+// where row `row` of an array lies in a stage
+template <typename T>
+__device__ __forceinline__ const T* in_stage(const uint8_t* at, const T* base, int64_t row, int64_t ld, bool al) {
+  return reinterpret_cast<const T*>(at + (al ? 0 : (reinterpret_cast<uintptr_t>(base + row * ld) & 15)));
+}
+// Sums of N (2 or 8) values at once over the CTA: the lanes of a warp halve the values between them before they add (8: 9 shuffles where one
+// value at a time takes 40); 32 / N neighbouring lanes end with one each.  Between two uses of a buffer lies the barrier of a use of
+// another.
+template <int N>
+__device__ __forceinline__ void sums_over(float (&v)[N], float (*buf)[32]) {
+  constexpr int LANES = 32 / N;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) G[c][i] = p.w_post ? f2_mul(G[c][i], g[i]) : g[i];
+  for (int half = N / 2, o = 16; half > 0; half >>= 1, o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int k = 0; k < half; ++k) {
+      const float give = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
+      v[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
     }
-  });
+  }
+  float t = v[0];
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  if (lane % LANES == 0) buf[lane / LANES][warp] = t;
+  __syncthreads();
+  t = 0.f;
+  for (int w = lane % LANES; w < warps; w += LANES) t += buf[lane / LANES][w];
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * LANES);
 }
 
-template <typename TS, typename TB, int CHUNKS, bool HAS_Y>
-__global__ void __launch_bounds__(544)
+// A thread's share of a row: NU units of U elements.  AL: of consecutive ones; else two elements nt apart, so that rows may start anywhere
+// and neighbouring lanes touch neighbouring elements.
+template <int U_, int NU_, bool AL>
+struct Share {
+  static constexpr int U = U_, NU = NU_;
+  uint32_t e0, step, nt, n;
+  __device__ __forceinline__ Share(int threads, uint32_t n_el) : nt(threads), n(n_el) { e0 = threadIdx.x * (AL ? U : 1); step = threads * U; }
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (int c = 0; c < NU; ++c) {
+      const uint32_t e = e0 + c * step;
+      if (e < n) f(c, e);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void get(const T* p, uint32_t e, F2 (&v)[U / 2]) const {
+    if constexpr (AL) get_u<U>(p + e, v);
+    else v[0] = f2(to_f(p[e]), e + nt < n ? to_f(p[e + nt]) : 0.f);
+  }
+  template <typename T>
+  __device__ __forceinline__ void put(T* p, uint32_t e, const F2 (&v)[U / 2]) const {
+    if constexpr (AL) put_u<U>(p + e, v);
+    else {
+      const float2 f = f2_get(v[0]);
+      p[e] = from_f<T>(f.x);
+      if (e + nt < n) p[e + nt] = from_f<T>(f.y);
+    }
+  }
+  // gate (.) w_post
+  __device__ __forceinline__ void gain(const float* w_post, const float* gate, F2 (&G)[NU][U / 2]) const {
+    each([&](int c, uint32_t e) {
+      F2 g[U / 2];
+      if (w_post) get(w_post, e, G[c]);
+      if (gate) {
+        get(gate, e, g);
+#pragma unroll
+        for (int i = 0; i < U / 2; ++i) G[c][i] = w_post ? f2_mul(G[c][i], g[i]) : g[i];
+      }
+    });
+  }
+};
+template <typename TS, typename TB, int CHUNKS, bool AL>
+struct ShareOf {
+  static constexpr int U = !AL ? 2 : (sizeof(TS) == 4 || sizeof(TB) == 4 ? 4 : 8);
+  typedef Share<U, CHUNKS * 8 / U, AL> type;
+};
+
+// HAS_Y: there is a branch
+template <typename TS, typename TB, int CHUNKS, int THREADS, bool HAS_Y, bool AL>
+__global__ void __launch_bounds__(THREADS, 1)
 block_norm_ring_kernel(const NormP p, const Ring ring, int32_t* status) {
   grid_begin();
+  typedef typename ShareOf<TS, TB, CHUNKS, AL>::type S;
+  constexpr int U = S::U, NU = S::NU;
   extern __shared__ __align__(16) uint8_t stage_mem[];
   __shared__ __align__(8) RingBars bars;
   __shared__ float red[3][2][32];
   const int64_t r_lo = rows_lo(blockIdx.x, p.rows, gridDim.x), r_hi = rows_lo(blockIdx.x + 1, p.rows, gridDim.x);
   ring_open(bars, ring);
-  const int nt = ring.threads;
-  if (threadIdx.x >= nt) {
-    if (threadIdx.x == nt) {
-      RingRows a{};
-      a.at[0] = static_cast<const char*>(p.x); a.ld[0] = p.ldx * (int64_t)sizeof(TS);
-      a.at[1] = static_cast<const char*>(p.y); a.ld[1] = p.ldy * (int64_t)sizeof(TB);
-      ring_copy(bars, ring, stage_mem, a, r_lo, r_hi, status);
-    }
-    return;
-  }
-  const uint32_t full0 = tc::smem_u32(bars.full), empty0 = tc::smem_u32(bars.empty);
+  const TS* const x0 = static_cast<const TS*>(p.x);
+  const TB* const y0 = static_cast<const TB*>(p.y);
+  const RingCopy mine(ring, {x0, y0, nullptr, nullptr}, {p.ldx * (int64_t)sizeof(TS), p.ldy * (int64_t)sizeof(TB), 0, 0});
+  auto copy = [&](int64_t row, int stage) { mine(bars, ring, stage_mem, row, stage); };
+  for (int64_t r = r_lo; r < r_hi && r < r_lo + ring.stages; ++r) copy(r, (int)(r - r_lo));
+  volatile int* const abortp = &bars.abort_flag;
+  const S my(blockDim.x, (uint32_t)p.d);
+  const uint32_t full0 = tc::smem_u32(bars.full);
   const float inv_d = 1.f / (float)p.d;
-  const uint32_t e0 = threadIdx.x * 8, step = nt * 8, n_el = (uint32_t)p.d;
-  auto each = [&](auto&& f) {
+  F2 wpre[NU][U / 2], G[NU][U / 2], h[NU][U / 2];
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const uint32_t e = e0 + c * step;
-      if (e < n_el) f(c, e);
-    }
-  };
-  F2 wpre[CHUNKS][4], G[CHUNKS][4], h[CHUNKS][4];
+  for (int c = 0; c < NU; ++c)
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); }
-  if (p.w_pre) each([&](int c, uint32_t e) { raw_get2(raw_load(p.w_pre + e), wpre[c]); });
+    for (int i = 0; i < U / 2; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); }
+  if (p.w_pre) my.each([&](int c, uint32_t e) { my.get(p.w_pre, e, wpre[c]); });
   int64_t at = p.gate ? r_lo / p.per_gate : 0, until = p.gate ? (at + 1) * p.per_gate : p.rows;
-  if (HAS_Y) gain_of<CHUNKS>(p, at, G, each);
-  // sum y^2 of the row in a stage
-  auto square_y = [&](int stage) {
-    const TB* const y = reinterpret_cast<const TB*>(stage_mem + (size_t)stage * ring.stage_bytes + ring.off[1]);
+  if (HAS_Y) my.gain(p.w_post, p.gate ? p.gate + at * p.ldg : nullptr, G);
+  // sum y^2 of a row in a stage
+  auto square_y = [&](int64_t row, int stage) {
+    const TB* const y = in_stage(stage_mem + (size_t)stage * ring.stage_bytes + ring.off[1], y0, row, p.ldy, AL);
     F2 s = 0;
-    each([&](int, uint32_t e) {
-      F2 v[4];
-      raw_get2(raw_load(y + e), v);
+    my.each([&](int, uint32_t e) {
+      F2 v[U / 2];
+      my.get(y, e, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s = f2_fma(v[i], v[i], s);
+      for (int i = 0; i < U / 2; ++i) s = f2_fma(v[i], v[i], s);
     });
     return f2_sum(s);
   };
-  // One barrier a row: the sum over y of the row to come is formed beside that over h of the row at hand.
+  // The sum over y of the row to come is formed beside that over h of the row at hand: one barrier a row, and one ahead of the first.
   const bool post = HAS_Y && p.post;
   const F2 a2 = f2(p.a);
   int stage = 0;
   uint32_t phase = 0;
   float r1 = 1.f;
-  tc::mbar_wait(full0, 0, &bars.abort_flag, status);
+  tc::mbar_wait(full0, 0, abortp, status);
   if (post) {
-    float s[2] = {square_y(0), 0.f};
-    part_sums(s, red[2], nt);
+    float s[2] = {square_y(r_lo, 0), 0.f};
+    sums_over(s, red[2]);
     r1 = rsqrtf(s[0] * inv_d + p.eps);
   }
   for (int64_t row = r_lo; row < r_hi; ++row) {
-    const uint8_t* const mem = stage_mem + (size_t)stage * ring.stage_bytes;
-    const TS* const x = reinterpret_cast<const TS*>(mem);
-    const TB* const y = reinterpret_cast<const TB*>(mem + ring.off[1]);
-    if (HAS_Y && row == until) { gain_of<CHUNKS>(p, ++at, G, each); until += p.per_gate; }
+    const int here = stage;
+    const uint8_t* const mem = stage_mem + (size_t)here * ring.stage_bytes;
+    const TS* const x = in_stage(mem, x0, row, p.ldx, AL);
+    const TB* const y = in_stage(mem + ring.off[1], y0, row, p.ldy, AL);
+    if (HAS_Y && row == until) { my.gain(p.w_post, p.gate + ++at * p.ldg, G); until += p.per_gate; }
     F2 hh = 0;
     const F2 r12 = f2(r1);
-    each([&](int c, uint32_t e) {
-      F2 v[4], xv[4];
-      raw_get2(raw_load(x + e), xv);
-      if (HAS_Y) raw_get2(raw_load(y + e), v);
+    my.each([&](int c, uint32_t e) {
+      F2 v[U / 2], xv[U / 2];
+      my.get(x, e, xv);
+      if (HAS_Y) my.get(y, e, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < U / 2; ++i) {
         h[c][i] = f2_mul(a2, xv[i]);
         if (HAS_Y) h[c][i] = f2_fma(f2_mul(v[i], G[c][i]), r12, h[c][i]);
         hh = f2_fma(h[c][i], h[c][i], hh);
       }
+      if (p.h) my.put(static_cast<TS*>(p.h) + row * p.ldh, e, h[c]);
     });
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) tc::mbar_arrive(empty0 + 8 * stage);          // the warp has read its part of the row
-    if (p.h) each([&](int c, uint32_t e) { store8(static_cast<TS*>(p.h) + row * p.ldh + e, h[c]); });
     if (++stage == ring.stages) { stage = 0; phase ^= 1; }
     float s[2] = {f2_sum(hh), 0.f};
     if (row + 1 < r_hi) {
-      tc::mbar_wait(full0 + 8 * stage, phase, &bars.abort_flag, status);
-      if (post) s[1] = square_y(stage);
+      tc::mbar_wait(full0 + 8 * stage, phase, abortp, status);
+      if (post) s[1] = square_y(row + 1, stage);
     }
-    part_sums(s, red[row & 1], nt);
+    sums_over(s, red[row & 1]);
+    if (row + ring.stages < r_hi) copy(row + ring.stages, here);       // every thread has read the row
     if (post) r1 = rsqrtf(s[1] * inv_d + p.eps);
     const F2 r2 = f2(p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 1.f);
-    each([&](int c, uint32_t) {
+    my.each([&](int c, uint32_t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[c][i] = f2_mul(h[c][i], f2_mul(r2, wpre[c][i]));
+      for (int i = 0; i < U / 2; ++i) h[c][i] = f2_mul(h[c][i], f2_mul(r2, wpre[c][i]));
     });
-    if (p.n) each([&](int c, uint32_t e) { store8(static_cast<TB*>(p.n) + row * p.ldn + e, h[c]); });
+    if (p.n) my.each([&](int c, uint32_t e) { my.put(static_cast<TB*>(p.n) + row * p.ldn, e, h[c]); });
     if (p.q) {
       unsigned top = 0;
-      float v[CHUNKS][8];
-      each([&](int c, uint32_t) {
+      my.each([&](int c, uint32_t e) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 t = f2_get(h[c][i]); v[c][2 * i] = t.x; v[c][2 * i + 1] = t.y; }
-        top = max(top, abs_bits8(v[c]));
+        for (int i = 0; i < U / 2; ++i) {
+          const float2 t = f2_get(h[c][i]);
+          top = max(top, max(__float_as_uint(t.x) & 0x7fffffffu, AL || e + my.nt < my.n ? __float_as_uint(t.y) & 0x7fffffffu : 0u));
+        }
       });
-      const RowScale r = row_scale(part_max(top, red[2], nt));
-      each([&](int c, uint32_t e) { *reinterpret_cast<uint2*>(p.q + row * p.ldq + e) = row_round8(v[c], r); });
+      const RowScale r = row_scale(cta_max(top, red[2]));
+      int8_t* const q = p.q + row * p.ldq;
+      my.each([&](int c, uint32_t e) {
+        float v[U];
+#pragma unroll
+        for (int i = 0; i < U / 2; ++i) { const float2 t = f2_get(h[c][i]); v[2 * i] = t.x; v[2 * i + 1] = t.y; }
+        if constexpr (U == 8) *reinterpret_cast<uint2*>(q + e) = make_uint2(row_round4(v, r), row_round4(v + 4, r));
+        else if constexpr (U == 4) *reinterpret_cast<uint32_t*>(q + e) = row_round4(v, r);
+        else {
+          q[e] = (int8_t)row_round(v[0], r);
+          if (e + my.nt < my.n) q[e + my.nt] = (int8_t)row_round(v[1], r);
+        }
+      });
       if (threadIdx.x == 0) p.q_scale[row] = r.s;
     }
   }
+  ring_drain(bars, ring, r_hi - r_lo);
 }
 
 struct GradP {
@@ -471,163 +546,168 @@ block_norm_grad_kernel(const GradP p) {
 //   sum f y = sum (G y) dh + (sum (G y) g - mean(g hbar) / rms(h) sum (G y) h) / rms(h),   G = gate (.) w_post,
 // so that all six sums of a row are formed at once.  And one running sum serves both the gate and w_post: t = sum dh' ybar over the rows of a
 // gate gives dgate = w_post t, and gate t is what these rows add to dw_post.
-template <typename TS, typename TB, int CHUNKS, int THREADS, bool HAS_Y>
-__global__ void __launch_bounds__(THREADS + 32)
+//
+// KEEP: a thread's share of the four arrays stays in registers between the sums and the gradients; else it is read (and widened) again.
+template <typename TS, typename TB, int CHUNKS, int THREADS, bool HAS_Y, bool AL>
+__global__ void __launch_bounds__(THREADS, 1)
 block_norm_grad_ring_kernel(const GradP p, const Ring ring, int32_t* status) {
   grid_begin();
+  typedef typename ShareOf<TS, TB, CHUNKS, AL>::type S;
+  constexpr int U = S::U, NU = S::NU, N_SUMS = HAS_Y ? 8 : 2;
+  constexpr bool KEEP = CHUNKS == 1;
   extern __shared__ __align__(16) uint8_t stage_mem[];
   __shared__ __align__(8) RingBars bars;
-  __shared__ float red[2][8][32];
+  __shared__ float red[2][N_SUMS][32];
   const int64_t d = p.d;
   const int64_t r_lo = rows_lo(blockIdx.x, p.rows, p.ctas), r_hi = rows_lo(blockIdx.x + 1, p.rows, p.ctas);
   ring_open(bars, ring);
-  const int nt = ring.threads;
-  if (threadIdx.x >= nt) {
-    if (threadIdx.x == nt) {
-      RingRows a{};
-      a.at[0] = static_cast<const char*>(p.h); a.ld[0] = p.ldh * (int64_t)sizeof(TS);
-      a.at[1] = static_cast<const char*>(p.y); a.ld[1] = p.ldy * (int64_t)sizeof(TB);
-      a.at[2] = static_cast<const char*>(p.dh); a.ld[2] = p.lddh * (int64_t)sizeof(TS);
-      a.at[3] = static_cast<const char*>(p.dn); a.ld[3] = p.lddn * (int64_t)sizeof(TB);
-      ring_copy(bars, ring, stage_mem, a, r_lo, r_hi, status);
-    }
-    return;
-  }
-  const uint32_t full0 = tc::smem_u32(bars.full), empty0 = tc::smem_u32(bars.empty);
+  const TS* const h0 = static_cast<const TS*>(p.h);
+  const TB* const y0 = static_cast<const TB*>(p.y);
+  const TS* const dh0 = static_cast<const TS*>(p.dh);
+  const TB* const dn0 = static_cast<const TB*>(p.dn);
+  const RingCopy mine(ring, {h0, y0, dh0, dn0}, {p.ldh * (int64_t)sizeof(TS), p.ldy * (int64_t)sizeof(TB), p.lddh * (int64_t)sizeof(TS), p.lddn * (int64_t)sizeof(TB)});
+  auto copy = [&](int64_t row, int stage) { mine(bars, ring, stage_mem, row, stage); };
+  for (int64_t r = r_lo; r < r_hi && r < r_lo + ring.stages; ++r) copy(r, (int)(r - r_lo));
+  volatile int* const abortp = &bars.abort_flag;
+  const S my(blockDim.x, (uint32_t)d);
+  const uint32_t full0 = tc::smem_u32(bars.full);
   float* const s_post = reinterpret_cast<float*>(stage_mem + (size_t)ring.stages * ring.stage_bytes);    // dw_post so far
   const float inv_d = 1.f / (float)d;
-  const uint32_t e0 = threadIdx.x * 8, step = nt * 8, n_el = (uint32_t)d;
-  auto each = [&](auto&& f) {
+  // an array that is not given is read from a row of zeros behind the sums (a thread reads what it has written there)
+  const int64_t d8 = (d + 7) / 8 * 8;
+  uint8_t* const zeros = reinterpret_cast<uint8_t*>(s_post) + (HAS_Y && p.dw_post ? d8 * 4 : 0);
+  uint8_t* const zeros_b = sizeof(TB) == sizeof(TS) ? zeros : zeros + d8 * sizeof(TS);
+  if (!p.h || !p.dh || !p.dn) my.each([&](int, uint32_t e) {
+    F2 z[U / 2];
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const uint32_t e = e0 + c * step;
-      if (e < n_el) f(c, e);
-    }
-  };
-  // an array that is not given is read from a row of zeros behind the sums
-  uint8_t* const zeros = reinterpret_cast<uint8_t*>(s_post) + (HAS_Y && p.dw_post ? d * 4 : 0);
-  if (!p.h || !p.dh || !p.dn) each([&](int, uint32_t e) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) reinterpret_cast<TS*>(zeros)[e + i] = from_f<TS>(0.f);     // (a thread reads what it has written; TB is no wider)
-    if (sizeof(TB) != sizeof(TS)) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) reinterpret_cast<TB*>(zeros + d * sizeof(TS))[e + i] = from_f<TB>(0.f);
-    }
+    for (int i = 0; i < U / 2; ++i) z[i] = 0;
+    my.put(reinterpret_cast<TS*>(zeros), e, z);
+    my.put(reinterpret_cast<TB*>(zeros_b), e, z);
   });
-  const uint8_t* const zeros_b = sizeof(TB) == sizeof(TS) ? zeros : zeros + d * sizeof(TS);
-  F2 wpre[CHUNKS][4], G[CHUNKS][4], a_pre[CHUNKS][4], a_t[CHUNKS][4];
+  F2 wpre[NU][U / 2], G[NU][U / 2], a_pre[NU][U / 2], a_t[NU][U / 2];
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c)
+  for (int c = 0; c < NU; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); a_pre[c][i] = 0; a_t[c][i] = 0; }
-  if (p.w_pre) each([&](int c, uint32_t e) { raw_get2(raw_load(p.w_pre + e), wpre[c]); });
+    for (int i = 0; i < U / 2; ++i) { wpre[c][i] = f2(1.f); G[c][i] = f2(1.f); a_pre[c][i] = 0; a_t[c][i] = 0; }
+  if (p.w_pre) my.each([&](int c, uint32_t e) { my.get(p.w_pre, e, wpre[c]); });
   const int64_t g_first = p.gate ? r_lo / p.per_gate : 0;
   int64_t at = g_first, until = p.gate ? (at + 1) * p.per_gate : p.rows;
-  if (HAS_Y) gain_of<CHUNKS>(p, at, G, each);
-  if (HAS_Y && p.dw_post) each([&](int, uint32_t e) {
+  if (HAS_Y) my.gain(p.w_post, p.gate ? p.gate + at * p.ldg : nullptr, G);
+  if (HAS_Y && p.dw_post) my.each([&](int, uint32_t e) {
+    F2 z[U / 2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s_post[e + i] = 0.f;
+    for (int i = 0; i < U / 2; ++i) z[i] = 0;
+    my.put(s_post, e, z);
   });
   // the rows of a gate are through (or the CTA's share of them): its gradient or a sum for the CTA's first or its last gate, and dw_post
   auto gate_done = [&](int64_t g) {
     const int64_t g0 = g * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
     float* const out = !p.dgate ? nullptr : (r_lo <= g0 && g1 <= r_hi ? p.dgate + g * d
                                   : p.part + ((int64_t)(part_gate(p) + (g == g_first ? 0 : 1)) * p.ctas + blockIdx.x) * d);
-    each([&](int c, uint32_t e) {
-      F2 w[4], v[4];
+    my.each([&](int c, uint32_t e) {
+      F2 w[U / 2], v[U / 2];
       if (out) {
-        if (p.w_post) raw_get2(raw_load(p.w_post + e), w);
+        if (p.w_post) my.get(p.w_post, e, w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = p.w_post ? f2_mul(w[i], a_t[c][i]) : a_t[c][i];
-        store8(out + e, v);
+        for (int i = 0; i < U / 2; ++i) v[i] = p.w_post ? f2_mul(w[i], a_t[c][i]) : a_t[c][i];
+        my.put(out, e, v);
       }
       if (p.dw_post) {
-        if (p.gate) raw_get2(raw_load(p.gate + g * p.ldg + e), w);
-        raw_get2(raw_load(static_cast<const float*>(s_post + e)), v);
+        if (p.gate) my.get(p.gate + g * p.ldg, e, w);
+        my.get(static_cast<const float*>(s_post), e, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = f2_fma(p.gate ? w[i] : f2(1.f), a_t[c][i], v[i]);
-        store8(s_post + e, v);
+        for (int i = 0; i < U / 2; ++i) v[i] = f2_fma(p.gate ? w[i] : f2(1.f), a_t[c][i], v[i]);
+        my.put(s_post, e, v);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a_t[c][i] = 0;
+      for (int i = 0; i < U / 2; ++i) a_t[c][i] = 0;
     });
   };
   const F2 a2 = f2(p.a);
-  int stage = 0;
+  int stage = 0, before = 0;
   uint32_t phase = 0;
   for (int64_t row = r_lo; row < r_hi; ++row) {
-    const uint8_t* const mem = stage_mem + (size_t)stage * ring.stage_bytes;
-    const TS* const h = reinterpret_cast<const TS*>(p.h ? mem + ring.off[0] : zeros);
-    const TB* const y = reinterpret_cast<const TB*>(mem + ring.off[1]);
-    const TS* const dh = reinterpret_cast<const TS*>(p.dh ? mem + ring.off[2] : zeros);
-    const TB* const dn = reinterpret_cast<const TB*>(p.dn ? mem + ring.off[3] : zeros_b);
-    if (HAS_Y && row == until) { gain_of<CHUNKS>(p, ++at, G, each); until += p.per_gate; }
-    tc::mbar_wait(full0 + 8 * stage, phase, &bars.abort_flag, status);
+    const int here = stage;
+    const uint8_t* const mem = stage_mem + (size_t)here * ring.stage_bytes;
+    const TS* const h = p.h ? in_stage(mem + ring.off[0], h0, row, p.ldh, AL) : reinterpret_cast<const TS*>(zeros);
+    const TB* const y = in_stage(mem + ring.off[1], y0, row, p.ldy, AL);
+    const TS* const dh = p.dh ? in_stage(mem + ring.off[2], dh0, row, p.lddh, AL) : reinterpret_cast<const TS*>(zeros);
+    const TB* const dn = p.dn ? in_stage(mem + ring.off[3], dn0, row, p.lddn, AL) : reinterpret_cast<const TB*>(zeros_b);
+    if (HAS_Y && row == until) { my.gain(p.w_post, p.gate + ++at * p.ldg, G); until += p.per_gate; }
+    tc::mbar_wait(full0 + 8 * here, phase, abortp, status);
+    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
+    F2 hv[KEEP ? NU : 1][U / 2], nv[KEEP ? NU : 1][U / 2], yv[KEEP ? NU : 1][U / 2], dv[KEEP ? NU : 1][U / 2];
     F2 q[6] = {0, 0, 0, 0, 0, 0};
-    each([&](int c, uint32_t e) {
-      F2 hv[4], gv[4], yv[4], dv[4];
-      raw_get2(raw_load(h + e), hv);
-      raw_get2(raw_load(dn + e), gv);
-      if (HAS_Y) {
-        raw_get2(raw_load(y + e), yv);
-        raw_get2(raw_load(dh + e), dv);
-      }
+    my.each([&](int c, uint32_t e) {
+      const int k = KEEP ? c : 0;
+      my.get(h, e, hv[k]);
+      my.get(dn, e, nv[k]);
+      if (HAS_Y) my.get(y, e, yv[k]);
+      if (HAS_Y || KEEP) my.get(dh, e, dv[k]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const F2 g = f2_mul(gv[i], wpre[c][i]);
-        q[0] = f2_fma(hv[i], hv[i], q[0]);
-        q[1] = f2_fma(g, hv[i], q[1]);
+      for (int i = 0; i < U / 2; ++i) {
+        const F2 g = f2_mul(nv[k][i], wpre[c][i]);
+        q[0] = f2_fma(hv[k][i], hv[k][i], q[0]);
+        q[1] = f2_fma(g, hv[k][i], q[1]);
         if (HAS_Y) {
-          const F2 u = f2_mul(yv[i], G[c][i]);
-          q[2] = f2_fma(yv[i], yv[i], q[2]);
-          q[3] = f2_fma(u, dv[i], q[3]);
+          const F2 u = f2_mul(yv[k][i], G[c][i]);
+          q[2] = f2_fma(yv[k][i], yv[k][i], q[2]);
+          q[3] = f2_fma(u, dv[k][i], q[3]);
           q[4] = f2_fma(u, g, q[4]);
-          q[5] = f2_fma(u, hv[i], q[5]);
+          q[5] = f2_fma(u, hv[k][i], q[5]);
         }
       }
     });
-    float s[8] = {f2_sum(q[0]), f2_sum(q[1]), f2_sum(q[2]), f2_sum(q[3]), f2_sum(q[4]), f2_sum(q[5]), 0.f, 0.f};
-    if (HAS_Y) part_sums(s, red[row & 1], nt);
-    else {
-      float two[2] = {s[0], s[1]};
-      part_sums(two, red[row & 1], nt);
-      s[0] = two[0]; s[1] = two[1];
+    float s[N_SUMS];
+#pragma unroll
+    for (int i = 0; i < N_SUMS; ++i) s[i] = i < 6 ? f2_sum(q[i]) : 0.f;
+    sums_over(s, red[row & 1]);
+    // KEEP: every thread has read the row, else the row before; its place takes another one
+    if (KEEP) {
+      if (row + ring.stages < r_hi) copy(row + ring.stages, here);
+    } else {
+      if (row > r_lo && row - 1 + ring.stages < r_hi) copy(row - 1 + ring.stages, before);
+      before = here;
     }
     const float r2 = p.pre ? rsqrtf(s[0] * inv_d + p.eps) : 1.f, m2 = p.pre ? s[1] * inv_d * r2 * r2 : 0.f;
-    const float r1 = p.post ? rsqrtf(s[2] * inv_d + p.eps) : 1.f;
-    const float m1 = p.post ? (s[3] + r2 * (s[4] - m2 * s[5])) * inv_d * r1 * r1 : 0.f;
+    float r1 = 1.f, m1 = 0.f;
+    if (HAS_Y && p.post) {
+      r1 = rsqrtf(s[2 % N_SUMS] * inv_d + p.eps);
+      m1 = (s[3 % N_SUMS] + r2 * (s[4 % N_SUMS] - m2 * s[5 % N_SUMS])) * inv_d * r1 * r1;
+    }
     const F2 r22 = f2(r2), r12 = f2(r1), c2 = f2(-r2 * m2), c1 = f2(-r1 * m1);
-    each([&](int c, uint32_t e) {
-      F2 hv[4], nv[4], yv[4], dv[4], o[4];
-      raw_get2(raw_load(h + e), hv);
-      raw_get2(raw_load(dn + e), nv);
-      raw_get2(raw_load(dh + e), dv);
-      if (HAS_Y) raw_get2(raw_load(y + e), yv);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dv[i] = f2_fma(hv[i], c2, f2_fma(f2_mul(nv[i], wpre[c][i]), r22, dv[i]));           // dh'
-        o[i] = f2_mul(a2, dv[i]);
-        a_pre[c][i] = f2_fma(nv[i], f2_mul(hv[i], r22), a_pre[c][i]);
-        if (HAS_Y) a_t[c][i] = f2_fma(dv[i], f2_mul(yv[i], r12), a_t[c][i]);
+    my.each([&](int c, uint32_t e) {
+      const int k = KEEP ? c : 0;
+      F2 o[U / 2];
+      if (!KEEP) {
+        my.get(h, e, hv[k]);
+        my.get(dn, e, nv[k]);
+        my.get(dh, e, dv[k]);
+        if (HAS_Y) my.get(y, e, yv[k]);
       }
-      if (p.dx) store8(static_cast<TS*>(p.dx) + row * p.lddx + e, o);
+#pragma unroll
+      for (int i = 0; i < U / 2; ++i) {
+        dv[k][i] = f2_fma(hv[k][i], c2, f2_fma(f2_mul(nv[k][i], wpre[c][i]), r22, dv[k][i]));           // dh'
+        o[i] = f2_mul(a2, dv[k][i]);
+        a_pre[c][i] = f2_fma(nv[k][i], f2_mul(hv[k][i], r22), a_pre[c][i]);
+        if (HAS_Y) a_t[c][i] = f2_fma(dv[k][i], f2_mul(yv[k][i], r12), a_t[c][i]);
+      }
+      if (p.dx) my.put(static_cast<TS*>(p.dx) + row * p.lddx, e, o);
       if (HAS_Y) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dv[i] = f2_fma(yv[i], c1, f2_mul(f2_mul(G[c][i], dv[i]), r12));
+        for (int i = 0; i < U / 2; ++i) dv[k][i] = f2_fma(yv[k][i], c1, f2_mul(f2_mul(G[c][i], dv[k][i]), r12));
       }
-      if (p.dy) store8(static_cast<TB*>(p.dy) + row * p.lddy + e, dv);
+      if (p.dy) my.put(static_cast<TB*>(p.dy) + row * p.lddy, e, dv[k]);
     });
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) tc::mbar_arrive(empty0 + 8 * stage);          // the warp has read its part of the row
-    if (++stage == ring.stages) { stage = 0; phase ^= 1; }
-    if (HAS_Y && (row + 1 == r_hi || row + 1 == until)) gate_done(at);
+    if (HAS_Y && (row + 1 == until || row + 1 == r_hi)) gate_done(at);
   }
-  if (p.dw_pre) each([&](int c, uint32_t e) { store8(p.part + ((int64_t)part_pre(p) * p.ctas + blockIdx.x) * d + e, a_pre[c]); });
-  if (HAS_Y && p.dw_post) each([&](int, uint32_t e) {
-    F2 v[4];
-    raw_get2(raw_load(static_cast<const float*>(s_post + e)), v);
-    store8(p.part + ((int64_t)part_post(p) * p.ctas + blockIdx.x) * d + e, v);
+  if (p.dw_pre) my.each([&](int c, uint32_t e) { my.put(p.part + ((int64_t)part_pre(p) * p.ctas + blockIdx.x) * d, e, a_pre[c]); });
+  if (HAS_Y && p.dw_post) my.each([&](int, uint32_t e) {
+    F2 v[U / 2];
+    my.get(static_cast<const float*>(s_post), e, v);
+    my.put(p.part + ((int64_t)part_post(p) * p.ctas + blockIdx.x) * d, e, v);
   });
+  ring_drain(bars, ring, r_hi - r_lo);
 }
 
 // The CTAs' sums added up in order: blockIdx.y = 0, 1: the weights' gradients, from 2 on: the gates' that have rows of several CTAs, found
@@ -688,55 +768,69 @@ block_norm_grad_sums_kernel(const GradP p) {
   }
 }
 
-// Ring and CTAs an SM for rows of d elements in arrays of these element sizes (0: not read), `kept` bytes of shared memory beside them
-// an element.  CHUNKS 1 up to `single` elements, 2 up to 8,192, CTAs of together 512 threads at least: the registers of an SM
-// hold about so many.  False: d is no multiple of eight, too long, or not even two rows fit.
-constexpr size_t RING_SMEM = 228 * 1024 - 4096;
-bool plan_ring(int64_t d, size_t e0, size_t e1, size_t e2, size_t e3, size_t kept, int64_t single, Ring& r, int& ctas, int& chunks, size_t& smem) {
-  if (d % 8 || d > 8192) return false;
-  chunks = d <= single ? 1 : 2;
-  const int threads = (int)(((d / 8 + chunks - 1) / chunks + 31) / 32 * 32);
+// Ring and CTAs an SM for rows of d elements in arrays of these element sizes (0: not read), `kept` bytes of shared memory beside them an
+// element, rows in use besides those on their way `held`.  The variants by the threads of a CTA and the registers that leaves each: 512 with
+// one chunk of eight elements up to 4,096 (128 registers), 352 with two or three (168), and where `wide` 512 with two up to 8,192.  False:
+// too long.
+constexpr size_t RING_SMEM = 224 * 1024 + 256;
+struct Plan { Ring ring; int ctas, chunks, threads; size_t smem; };
+bool plan_ring(int64_t d, bool al, size_t e0, size_t e1, size_t e2, size_t e3, size_t kept, int held, bool wide, Plan& pl) {
+  Ring& r = pl.ring;
   const size_t es[4] = {e0, e1, e2, e3};
-  r.stage_bytes = 0;
-  r.threads = threads;
+  if (d > (wide ? 8192 : 8448)) return false;
+  pl.chunks = d <= 4096 ? 1 : (wide || d <= 5632 ? 2 : 3);
+  pl.threads = (int)(((d + 7) / 8 + pl.chunks - 1) / pl.chunks + 31) / 32 * 32;
+  size_t stage = 0;
+  r.arrays = 0;
   for (int k = 0; k < 4; ++k) {
-    r.off[k] = (uint32_t)r.stage_bytes;
+    r.off[k] = (uint32_t)stage;
     r.bytes[k] = (uint32_t)(es[k] * (size_t)d);
-    r.stage_bytes += (int)r.bytes[k];
+    r.arrays += es[k] != 0;
+    stage += es[k] ? (r.bytes[k] + 15) / 16 * 16 + (al ? 0 : 16) : 0;
   }
-  ctas = threads >= 512 ? 1 : (512 / threads < 8 ? 512 / threads : 8);
-  for (; ctas >= 1; --ctas) {
-    const size_t room = RING_SMEM / (size_t)ctas - 3072;
-    const size_t keep = kept * (size_t)d;
+  r.stage_bytes = (int)stage;
+  // as many CTAs as the registers hold, 512 threads or one, with two rows on their way
+  for (pl.ctas = pl.threads > 256 ? 1 : (512 / pl.threads < 8 ? 512 / pl.threads : 8); pl.ctas >= 1; --pl.ctas) {
+    const size_t room = pl.ctas == 1 ? RING_SMEM : RING_SMEM / (size_t)pl.ctas - 2048, keep = kept * (size_t)((d + 7) / 8 * 8);
     if (room < keep) continue;
-    int n = (int)((room - keep) / (size_t)r.stage_bytes);
+    int n = (int)((room - keep) / stage);
     if (n > MAX_STAGES) n = MAX_STAGES;
-    if (n >= 3 || (n == 2 && ctas == 1)) {
+    if (n >= held + 2 || (n > held && pl.ctas == 1)) {
       r.stages = n;
-      smem = (size_t)r.stages * r.stage_bytes + keep;
+      pl.smem = (size_t)n * stage + keep;
       return true;
     }
   }
   return false;
+}
+// a ring kernel of `ctas` CTAs
+template <typename K, typename P>
+armor_status run_ring(armor_ctx* c, K kernel, PerDeviceOnce& attr, int64_t ctas, const Plan& pl, const P& p, cudaStream_t s) {
+  if (ensure_dynamic_smem(attr, c->device, kernel, RING_SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)pl.threads), pl.smem, s, p, pl.ring, c->status);
+  return ARMOR_OK;
+}
+template <typename TS, typename TB, int CHUNKS, int THREADS, bool AL>
+armor_status run_norm_ring(armor_ctx* c, int64_t ctas, const Plan& pl, const NormP& p, cudaStream_t s) {
+  static PerDeviceOnce with, without;
+  return p.y ? run_ring(c, block_norm_ring_kernel<TS, TB, CHUNKS, THREADS, true, AL>, with, ctas, pl, p, s)
+             : run_ring(c, block_norm_ring_kernel<TS, TB, CHUNKS, THREADS, false, AL>, without, ctas, pl, p, s);
+}
+template <typename TS, typename TB, int CHUNKS, int THREADS, bool AL>
+armor_status run_grad_ring(armor_ctx* c, int64_t ctas, const Plan& pl, const GradP& p, cudaStream_t s) {
+  static PerDeviceOnce with, without;
+  return p.y ? run_ring(c, block_norm_grad_ring_kernel<TS, TB, CHUNKS, THREADS, true, AL>, with, ctas, pl, p, s)
+             : run_ring(c, block_norm_grad_ring_kernel<TS, TB, CHUNKS, THREADS, false, AL>, without, ctas, pl, p, s);
 }
 
 template <typename TS, typename TB, bool ALIGNED>
 armor_status launch_norm(armor_ctx* c, const NormP& p, int64_t rows, cudaStream_t s) {
   const int64_t units = (p.d + 7) / 8;
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
-  Ring ring;
-  int ctas, chunks;
-  size_t smem;
-  if (ALIGNED && rows > 2 * c->n_sm && plan_ring(p.d, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 4096, ring, ctas, chunks, smem)) {
-    const int64_t grid = (int64_t)ctas * c->n_sm < rows ? (int64_t)ctas * c->n_sm : rows;
-    auto run = [&](auto kernel, PerDeviceOnce& attr) {
-      if (ensure_dynamic_smem(attr, c->device, kernel, RING_SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
-      launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)ring.threads + 32), smem, s, p, ring, c->status);
-      return ARMOR_OK;
-    };
-    static PerDeviceOnce at1, at2, at3, at4;
-    if (chunks == 1) return p.y ? run(block_norm_ring_kernel<TS, TB, 1, true>, at1) : run(block_norm_ring_kernel<TS, TB, 1, false>, at2);
-    return p.y ? run(block_norm_ring_kernel<TS, TB, 2, true>, at3) : run(block_norm_ring_kernel<TS, TB, 2, false>, at4);
+  Plan pl;
+  if (rows > 2 * c->n_sm && plan_ring(p.d, ALIGNED, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 1, true, pl)) {
+    const int64_t ctas = (int64_t)pl.ctas * c->n_sm < rows ? (int64_t)pl.ctas * c->n_sm : rows;
+    return pl.chunks == 1 ? run_norm_ring<TS, TB, 1, 512, ALIGNED>(c, ctas, pl, p, s) : run_norm_ring<TS, TB, 2, 512, ALIGNED>(c, ctas, pl, p, s);
   }
   const dim3 grid((unsigned)rows);
   if (units <= 128 || (rows <= 148 && units <= 1024)) launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 1>, grid, threads(1), 0, s, p);
@@ -750,32 +844,19 @@ armor_status launch_grad(armor_ctx* c, GradP p, cudaStream_t s) {
   const int n_sums = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 1 : 0);
   const size_t smem = (size_t)n_sums * (size_t)units * 8 * sizeof(float);
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
-  Ring ring;
-  int ctas = 2, chunks = 0;
-  size_t ring_smem = 0;
+  Plan pl;
   const size_t kept = (p.dw_post ? 4 : 0) + (p.h && p.dh && p.dn ? 0 : sizeof(TS) + (sizeof(TB) != sizeof(TS) ? sizeof(TB) : 0));
-  const bool use_ring = ALIGNED && plan_ring(p.d, p.h ? sizeof(TS) : 0, p.y ? sizeof(TB) : 0, p.dh ? sizeof(TS) : 0, p.dn ? sizeof(TB) : 0, kept, 5120, ring, ctas, chunks, ring_smem);
-  if (!use_ring) ctas = 2;
+  const bool use_ring = plan_ring(p.d, ALIGNED, p.h ? sizeof(TS) : 0, p.y ? sizeof(TB) : 0, p.dh ? sizeof(TS) : 0, p.dn ? sizeof(TB) : 0, kept, p.d <= 4096 ? 0 : 1, false, pl);
   // CTAs as many as an SM runs, fewer where the workspace has no room for their sums
   const int64_t parts = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 2 : 0);
-  int64_t n = (int64_t)ctas * c->n_sm;
+  int64_t n = use_ring ? (int64_t)pl.ctas * c->n_sm : 2 * c->n_sm;
   if (n > p.rows) n = p.rows;
   if (parts && n > ws_scratch_bytes(c) / (parts * p.d * 4)) n = ws_scratch_bytes(c) / (parts * p.d * 4);
   if (n < 1) return ARMOR_ERR_WORKSPACE;
   p.ctas = (int)n;
-  auto run_ring = [&](auto kernel, PerDeviceOnce& attr) {
-    if (ensure_dynamic_smem(attr, c->device, kernel, RING_SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
-    launch_dependent(kernel, dim3((unsigned)p.ctas), dim3((unsigned)ring.threads + 32), ring_smem, s, p, ring, c->status);
-    return ARMOR_OK;
-  };
-  static PerDeviceOnce at[8];
-  armor_status st = ARMOR_OK;
   if (use_ring) {
-    // (threads of a CTA by what the registers allow: 120, 96, 152 and 120 a thread)
-    if (p.d <= 4096) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 512, true>, at[0]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 512, false>, at[1]);
-    else if (p.d <= 5120) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 640, true>, at[2]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 1, 640, false>, at[3]);
-    else if (p.d <= 6144) st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 384, true>, at[4]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 384, false>, at[5]);
-    else st = p.y ? run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 512, true>, at[6]) : run_ring(block_norm_grad_ring_kernel<TS, TB, 2, 512, false>, at[7]);
+    const armor_status st = pl.chunks == 1 ? run_grad_ring<TS, TB, 1, 512, ALIGNED>(c, n, pl, p, s)
+                          : pl.chunks == 2 ? run_grad_ring<TS, TB, 2, 352, ALIGNED>(c, n, pl, p, s) : run_grad_ring<TS, TB, 3, 352, ALIGNED>(c, n, pl, p, s);
     if (st != ARMOR_OK) return st;
   } else if (units <= 1024) {
     static PerDeviceOnce attr;

@@ -87,20 +87,47 @@ __device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
   return r;
 }
 __device__ __forceinline__ float f2_sum(F2 v) { const float2 f = f2_get(v); return f.x + f.y; }
-template <typename T>
-__device__ __forceinline__ void raw_get2(const Raw8<T>& r, F2 (&v)[4]) {
-  float f[8];
-  raw_get(r, f);
+// U elements (four or eight) from or to 16-byte (fp32, or eight 16-bit) or 8-byte boundaries.  Rows with fp32 are taken by fours: neighbouring
+// lanes then touch neighbouring 16 bytes, where by eights they would meet in the same banks of shared memory and write half sectors.
+template <int U, typename T>
+__device__ __forceinline__ void get_u(const T* p, F2 (&v)[U / 2]) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const F2 (&v)[4]) {
-  float f[8];
+    for (int k = 0; k < U / 4; ++k) {
+      const float4 f = *reinterpret_cast<const float4*>(p + 4 * k);
+      v[2 * k] = f2(f.x, f.y); v[2 * k + 1] = f2(f.z, f.w);
+    }
+  } else {
+    uint32_t w[U / 2];
+    if constexpr (U == 8) {
+      const uint4 r = *reinterpret_cast<const uint4*>(p);
+      w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
+    } else {
+      const uint2 r = *reinterpret_cast<const uint2*>(p);
+      w[0] = r.x; w[1] = r.y;
+    }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 t = f2_get(v[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
-  store8(p, f);
+    for (int i = 0; i < U / 2; ++i) { const float2 f = unpack2(static_cast<const T*>(nullptr), w[i]); v[i] = f2(f.x, f.y); }
+  }
 }
+template <int U, typename T>
+__device__ __forceinline__ void put_u(T* p, const F2 (&v)[U / 2]) {
+  float2 f[U / 2];
+#pragma unroll
+  for (int i = 0; i < U / 2; ++i) f[i] = f2_get(v[i]);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < U / 4; ++k) *reinterpret_cast<float4*>(p + 4 * k) = make_float4(f[2 * k].x, f[2 * k].y, f[2 * k + 1].x, f[2 * k + 1].y);
+  } else {
+    const T* t = nullptr;
+    if constexpr (U == 8) *reinterpret_cast<uint4*>(p) = make_uint4(pack2(t, f[0].x, f[0].y), pack2(t, f[1].x, f[1].y), pack2(t, f[2].x, f[2].y), pack2(t, f[3].x, f[3].y));
+    else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(t, f[0].x, f[0].y), pack2(t, f[1].x, f[1].y));
+  }
+}
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
 
 // Elements e .. e + 7 of a row of n, zeros behind its end.  ALIGNED: rows start on 16-byte boundaries, so that only the last chunk of
 // a row whose length is no multiple of eight is taken element by element; else all are.
@@ -148,44 +175,6 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float (*buf)[32]) {
     v[k] = t;
   }
 }
-// Sums of N (2 or 8) values at once over the first `threads` threads of a CTA, which meet at barrier 1: the lanes of a warp halve the values
-// between them before they add (8: 9 shuffles where one value at a time takes 40), 32 / N neighbouring lanes end with a value each.  Between a
-// use of a buffer and the next one of the same lies the barrier of one on another buffer.
-template <int N>
-__device__ __forceinline__ void part_sums(float (&v)[N], float (*buf)[32], int threads) {
-  constexpr int LANES = 32 / N;                             // that hold one value
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
-#pragma unroll
-  for (int half = N / 2, o = 16; half > 0; half >>= 1, o >>= 1) {
-    const bool up = lane & o;
-#pragma unroll
-    for (int k = 0; k < half; ++k) {
-      const float give = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
-      v[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-    }
-  }
-  float t = v[0];
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-  if (warps > 1) {
-    if (lane % LANES == 0) buf[lane / LANES][warp] = t;
-    asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
-    t = 0.f;
-    for (int w = lane % LANES; w < warps; w += LANES) t += buf[lane / LANES][w];
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-  }
-#pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * LANES);
-}
-__device__ __forceinline__ unsigned part_max(unsigned v, float (*buf)[32], int threads) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
-  v = __reduce_max_sync(0xffffffffu, v);
-  if (warps == 1) return v;
-  if (lane == 0) buf[0][warp] = __uint_as_float(v);
-  asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
-  return __reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(buf[0][lane]) : 0u);
-}
 __device__ __forceinline__ unsigned cta_max(unsigned v, float (*buf)[32]) {
   v = __reduce_max_sync(0xffffffffu, v);
   const int warps = blockDim.x >> 5;
@@ -227,16 +216,13 @@ __device__ __forceinline__ int row_round(float x, const RowScale& r) {
   const int f = (int)k;
   return d > 0.0 ? f + 1 : (d < 0.0 ? f : f + (f & 1));
 }
-__device__ __forceinline__ uint2 row_round8(const float (&v)[8], const RowScale& r) {
-  uint32_t w[2];
+__device__ __forceinline__ uint32_t row_round4(const float* v, const RowScale& r) {
+  uint32_t w = 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    w[h] = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[h] |= (uint32_t)(row_round(v[4 * h + i], r) & 255) << (8 * i);
-  }
-  return make_uint2(w[0], w[1]);
+  for (int i = 0; i < 4; ++i) w |= (uint32_t)(row_round(v[i], r) & 255) << (8 * i);
+  return w;
 }
+__device__ __forceinline__ uint2 row_round8(const float (&v)[8], const RowScale& r) { return make_uint2(row_round4(v, r), row_round4(v + 4, r)); }
 // the bits of max |v|: of floats without their sign, NaN above infinity above all others
 __device__ __forceinline__ unsigned abs_bits8(const float (&v)[8]) {
   unsigned m = 0;

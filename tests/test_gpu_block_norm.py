@@ -75,7 +75,9 @@ def terms(t, **kw):
 
 WIDTHS = [(1, 1), (3, 7), (5, 8), (2, 64), (37, 129), (300, 1024), (7, 1030), (160, 4096), (1, 4096), (33, 5121), (200, 8192), (5, 16384), (150, 10001),
           # rows through the ring in shared memory, at the edges of its threads and of their share of a row
-          (700, 8), (700, 264), (400, 2056), (330, 4104), (320, 5128), (310, 6152), (300, 8184)]
+          (700, 8), (700, 264), (400, 2056), (330, 4104), (320, 5128), (310, 6152), (300, 8184),
+          # cut between the CTAs of a cluster, and rows that start anywhere
+          (297, 8200), (300, 11272), (299, 16384), (400, 2055), (320, 5357), (300, 8191), (298, 12001), (600, 33)]
 
 
 # ---------------------------------------------------------------------------------------------- forward
@@ -92,7 +94,7 @@ def test_forward(ctx, rows, d, ts, tb, post, gates, a):
     close(n, rn, 2 * SUM * size * r2 * t["w_pre"].double().abs())
 
 
-@pytest.mark.parametrize("rows,d", [(3, 7), (40, 1024), (300, 4104), (2, 16384)])
+@pytest.mark.parametrize("rows,d", [(3, 7), (40, 1024), (300, 4104), (2, 16384), (300, 9001), (310, 12288), (330, 777)])
 def test_int8_rows(ctx, rows, d):
     """n rounded to int8 from fp32: a value that close to a border may land on either side of it, so the integers are compared through
     what the norm itself may be off by."""
@@ -106,12 +108,15 @@ def test_int8_rows(ctx, rows, d):
     assert ((scale.double()[:, None] - top / 127).abs() <= worst / 127 + 2.0 ** -23 * top / 127).all()
     assert ((q.double() - rn * 127 / top).abs() <= 0.5 + (off + worst) * 127 / top).all()
     assert (q.abs().amax(1) == 127).all()
-    # and with the other outputs in one call: the same bits, and q of n in fp32 is that of the rows' rounding
-    x32, y32 = t["x"].float(), t["y"].float()
-    h2, n2 = torch.empty_like(x32), torch.empty_like(x32)
-    q2, s2 = ctx.new_int8_rows(rows, d), torch.empty(rows, device=DEV)
-    Bd.armor_block_norm(ctx.ctx, x32, y32, h2, n2, q2, s2, **terms(t))
-    assert torch.equal(q2, q) and torch.equal(s2, scale)
+    # the same bits with the other outputs in one call, and q of n in fp32 is that of the rows' rounding (in fp32 the sums may be
+    # taken in another order than in bf16)
+    def all_outputs(x, y):
+        h2, n2, q2, s2 = torch.empty_like(x), torch.empty_like(y), ctx.new_int8_rows(rows, d), torch.empty(rows, device=DEV)
+        Bd.armor_block_norm(ctx.ctx, x, y, h2, n2, q2, s2, **terms(t))
+        return h2, n2, q2, s2
+    h2, _, q2, s2 = all_outputs(t["x"], t["y"])
+    assert torch.equal(h2, h) and torch.equal(q2, q) and torch.equal(s2, scale)
+    _, n2, q2, s2 = all_outputs(t["x"].float(), t["y"].float())
     q3, s3 = ctx.quantize_rows(n2)
     assert torch.equal(q2, q3) and torch.equal(s2, s3)
 
