@@ -274,6 +274,11 @@ def _row_ptr(t: torch.Tensor | None, dtype, name: str, cols: int | None = None) 
     """(address, leading dimension) of rows [n, cols] with unit column stride; (None, 0) of None."""
     if t is None:
         return None, 0
+    if t.dtype is dtype and t.is_cuda and t.dim() == 2 and t.is_contiguous():      # (the common case first: a call takes microseconds)
+        c = t.size(1)
+        if cols is None or c == cols:
+            ld = t.stride(0)                         # (of a single row it may be anything)
+            return t.data_ptr(), ld if ld > c else c
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor (this library has no CPU path)")
     if t.dtype is not dtype:
@@ -352,23 +357,32 @@ def armor_apply_layer_i8(ctx, packed, x, y) -> None:
 def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps):
     """Fills what both directions of the norms share; returns the gate's rows."""
     f = torch.float32
-    for w, name in ((w_post, "w_post"), (w_pre, "w_pre")):
-        if w is not None and w.numel() != d:
-            raise ValueError(f"{name} must have {d} elements")
-    a.n_rows, a.d = n_rows, d
-    a.w_post, a.w_pre = _ptr(w_post, f, "w_post"), _ptr(w_pre, f, "w_pre")
-    a.post, a.pre, a.residual_scale, a.eps = post, pre, residual_scale, eps
+    a.n_rows = n_rows
+    a.d = d
+    if w_pre is not None:
+        if w_pre.numel() != d:
+            raise ValueError(f"w_pre must have {d} elements")
+        a.w_pre = _ptr(w_pre, f, "w_pre")
+    if w_post is not None:
+        if w_post.numel() != d:
+            raise ValueError(f"w_post must have {d} elements")
+        a.w_post = _ptr(w_post, f, "w_post")
+    a.post = w_post is not None if post is None else post
+    a.pre = pre
+    a.residual_scale = residual_scale
+    a.eps = eps
     if gate is None:
         return 0
     if gate.dim() == 1:
         gate = gate.unsqueeze(0)
     a.gate, a.ld_gate = _row_ptr(gate, f, "gate", d)
-    n_gates = gate.shape[0]
+    n_gates = gate.size(0)
     if not rows_per_gate:
         if n_gates < 1 or n_rows % n_gates:
             raise ValueError(f"rows_per_gate must be given where {n_gates} gates do not divide {n_rows} rows")
         rows_per_gate = max(1, n_rows // n_gates)
-    a.rows_per_gate, a.n_gates = rows_per_gate, n_gates
+    a.rows_per_gate = rows_per_gate
+    a.n_gates = n_gates
     return n_gates
 
 
@@ -377,22 +391,29 @@ def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0,
     """h and n (and n as int8 q with q_scale) of the residual stream x and a block's output y (see armor.h).  post: None means with
     w_post."""
     a = armor_block_norm_args()
-    a.x, a.ldx = _row_ptr(x, x.dtype, "x")
+    dt = x.dtype
+    a.x, a.ldx = _row_ptr(x, dt, "x")
     rows, d = x.shape
     a.stream_dtype = _row_dtype(x, "x")
     branch = y if y is not None else n
-    bt = x.dtype if branch is None else branch.dtype
-    a.branch_dtype = a.stream_dtype if branch is None else _row_dtype(branch, "y")
+    if branch is None:
+        bt, a.branch_dtype = dt, a.stream_dtype
+    else:
+        bt, a.branch_dtype = branch.dtype, _row_dtype(branch, "y")
     for t, name in ((y, "y"), (h, "h"), (n, "n"), (q, "q"), (q_scale, "q_scale")):
-        if t is not None and t.shape[0] != rows:
+        if t is not None and t.size(0) != rows:
             raise ValueError(f"{name} must have the {rows} rows of x")
-    a.y, a.ldy = _row_ptr(y, bt, "y", d)
-    a.h, a.ldh = _row_ptr(h, x.dtype, "h", d)
-    a.n, a.ldn = _row_ptr(n, bt, "n", d)
-    a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
-    a.q_scale = _ptr(q_scale, torch.float32, "q_scale")
-    _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, int(w_post is not None if post is None else post), int(pre),
-                 residual_scale, eps)
+    if y is not None:
+        a.y, a.ldy = _row_ptr(y, bt, "y", d)
+    if h is not None:
+        a.h, a.ldh = _row_ptr(h, dt, "h", d)
+    if n is not None:
+        a.n, a.ldn = _row_ptr(n, bt, "n", d)
+    if q is not None:
+        a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
+    if q_scale is not None:
+        a.q_scale = _ptr(q_scale, torch.float32, "q_scale")
+    _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
     code = lib().armor_block_norm(ctx, a, _stream())
     if code:
         _check(code, "armor_block_norm")
@@ -403,27 +424,41 @@ def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate,
     """The gradient of armor_block_norm (see armor.h)."""
     f = torch.float32
     a = armor_block_norm_grad_args()
-    stream = next((t for t in (h, dh, dx) if t is not None), None)
-    branch = next((t for t in (y, dn, dy) if t is not None), None)
+    stream = h if h is not None else (dh if dh is not None else dx)
+    branch = y if y is not None else (dn if dn is not None else dy)
     if stream is None and branch is None:
         raise ValueError("h, dh, dx, y, dn and dy are all missing")
-    ts, tb = (stream if stream is not None else branch), (branch if branch is not None else stream)
-    _row_ptr(ts, ts.dtype, "h")
-    rows, d = ts.shape
-    a.stream_dtype, a.branch_dtype = _row_dtype(ts, "h"), _row_dtype(tb, "y")
-    for name, t, dt in (("h", h, ts.dtype), ("y", y, tb.dtype), ("dh", dh, ts.dtype), ("dn", dn, tb.dtype), ("dx", dx, ts.dtype),
-                        ("dy", dy, tb.dtype)):
-        if t is not None and t.shape[0] != rows:
+    one = stream if stream is not None else branch
+    ts, tb = one.dtype, (branch if branch is not None else stream).dtype
+    _row_ptr(one, ts, "h")
+    rows, d = one.shape
+    a.stream_dtype = _row_dtype(one, "h")
+    a.branch_dtype = a.stream_dtype if tb is ts else _row_dtype(branch, "y")
+    for t, name in ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn"), (dx, "dx"), (dy, "dy")):
+        if t is not None and t.size(0) != rows:
             raise ValueError(f"{name} must have {rows} rows")
-        p, ld = _row_ptr(t, dt, name, d)
-        setattr(a, name, p)
-        setattr(a, "ld" + name, ld)
-    gates = _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, int(w_post is not None if post is None else post), int(pre),
-                         residual_scale, eps)
-    for name, t, n in (("dw_post", dw_post, d), ("dw_pre", dw_pre, d), ("dgate", dgate, gates * d)):
-        if t is not None and t.numel() != n:
-            raise ValueError(f"{name} must have {n} elements")
-        setattr(a, name, _ptr(t, f, name))
+    if h is not None:
+        a.h, a.ldh = _row_ptr(h, ts, "h", d)
+    if y is not None:
+        a.y, a.ldy = _row_ptr(y, tb, "y", d)
+    if dh is not None:
+        a.dh, a.lddh = _row_ptr(dh, ts, "dh", d)
+    if dn is not None:
+        a.dn, a.lddn = _row_ptr(dn, tb, "dn", d)
+    if dx is not None:
+        a.dx, a.lddx = _row_ptr(dx, ts, "dx", d)
+    if dy is not None:
+        a.dy, a.lddy = _row_ptr(dy, tb, "dy", d)
+    gates = _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+    if (dw_post is not None and dw_post.numel() != d) or (dw_pre is not None and dw_pre.numel() != d) or \
+            (dgate is not None and dgate.numel() != gates * d):
+        raise ValueError(f"dw_post and dw_pre must have {d} elements, dgate {gates} x {d}")
+    if dw_post is not None:
+        a.dw_post = _ptr(dw_post, f, "dw_post")
+    if dw_pre is not None:
+        a.dw_pre = _ptr(dw_pre, f, "dw_pre")
+    if dgate is not None:
+        a.dgate = _ptr(dgate, f, "dgate")
     code = lib().armor_block_norm_backward(ctx, a, _stream())
     if code:
         _check(code, "armor_block_norm_backward")
@@ -518,6 +553,11 @@ def armor_gemm_timing(ctx) -> tuple[int, float, float]:
 
 
 # ---------------------------------------------------------------- convenience wrapper
+def _empty_rows(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of t's shape, type and device."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 @dataclass
 class LayerState:
     Wbar: torch.Tensor
@@ -538,6 +578,7 @@ class ArmorContext:
             raise ValueError("ArmorContext needs a CUDA device")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.cfg = make_config(d_out, d_in, d_block, **kw)
         self.d_out, self.d_in, self.d_block = d_out, d_in, d_block
         nbytes = armor_workspace_bytes(self.cfg)
@@ -629,10 +670,11 @@ class ArmorContext:
     # -- 8-bit products
     def _here(self, *tensors) -> None:
         """The context's device is the current one and holds every tensor given: the calls enqueue on its current stream."""
+        here = self._index
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != here:
                 raise ValueError(f"the context is on {self.device}, a tensor on {t.device}")
-        if torch._C._cuda_getDevice() != self.device.index:
+        if torch._C._cuda_getDevice() != here:
             raise ValueError(f"{self.device} must be the current device")
 
     def new_int8_rows(self, n: int, cols: int) -> torch.Tensor:
@@ -677,15 +719,15 @@ class ArmorContext:
         """(h, n): the residual stream x plus a block's output y, normed, weighted and gated, and the normed stream that the next
         block reads.  terms: gate [d] or [n_gates, d] with rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps."""
         self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
-        h = torch.empty(x.shape, dtype=x.dtype, device=self.device)
-        n = torch.empty(x.shape, dtype=x.dtype if y is None else y.dtype, device=self.device)
+        h = _empty_rows(x)
+        n = _empty_rows(x if y is None else y)
         armor_block_norm(self.ctx, x, y, h, n, None, None, **terms)
         return h, n
 
     def block_norm_i8(self, x: torch.Tensor, y: torch.Tensor | None = None, **terms) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """(h, q, scale): as block_norm, the normed stream as int8 rows for linear_i8."""
         self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
-        h = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+        h = _empty_rows(x)
         q = self.new_int8_rows(x.shape[0], x.shape[1])
         scale = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
         armor_block_norm(self.ctx, x, y, h, None, q, scale, **terms)
@@ -697,14 +739,13 @@ class ArmorContext:
         the gradients of h and n."""
         gate, w_post, w_pre = terms.get("gate"), terms.get("w_post"), terms.get("w_pre")
         self._here(h, y, dh, dn, gate, w_post, w_pre)
-        f = dict(dtype=torch.float32, device=self.device)
-        out = {"dx": torch.empty(h.shape, dtype=h.dtype, device=self.device), "dy": torch.empty(y.shape, dtype=y.dtype, device=self.device)}
+        out = {"dx": _empty_rows(h), "dy": _empty_rows(y)}
         if w_pre is not None:
-            out["dw_pre"] = torch.empty(w_pre.shape, **f)
+            out["dw_pre"] = torch.empty_like(w_pre)
         if w_post is not None:
-            out["dw_post"] = torch.empty(w_post.shape, **f)
+            out["dw_post"] = torch.empty_like(w_post)
         if gate is not None:
-            out["dgate"] = torch.empty(gate.shape, **f)
+            out["dgate"] = _empty_rows(gate)
         armor_block_norm_backward(self.ctx, h, y, dh, dn, out["dx"], out["dy"], out.get("dw_post"), out.get("dw_pre"), out.get("dgate"), **terms)
         return out
 
