@@ -243,12 +243,12 @@ armor_status armor_quantize_rows(armor_ctx* ctx, const void* d_x, int32_t x_dtyp
 
 /* A linear layer in 8 bits: y[t][m] = x_scale[t] w_scale[m] sum_k xq[t][k] wq[m][k] (+ bias[m]), the sum exact in int32.
  *   x_dtype I8: d_x holds xq [n_tokens, n_in] (leading dimension ldx) and d_x_scale [n_tokens] its scales;
- *   x_dtype F32, BF16, F16: x is rounded by armor_quantize_rows into the context's workspace first (d_x_scale NULL).
+ *   x_dtype F32, BF16, F16: x is rounded as armor_quantize_rows has it, in the context's workspace (d_x_scale NULL).
  * wq [n_out, n_in] with leading dimension ldw, w_scale [n_out], bias [n_out] fp32 or NULL; y [n_tokens, n_out] with leading dimension
  * ldy in y_dtype (F32, BF16, F16), rounded once from fp32.  wq (and xq where given) are 16-byte aligned with leading dimensions that are
  * multiples of 16; any n_out, n_in and n_tokens; columns behind n_in are not read.  y must not overlap x.  Errors: INVALID_ARG,
  * SHAPE (sizes below one, leading dimensions, alignment), UNSUPPORTED (types), TOO_LARGE (n_in above 131,071, where a sum
- * of products of -128 would leave int32; n_out or n_tokens above 2^30), WORKSPACE (not even one token fits the workspace). */
+ * of products of -128 would leave int32; n_out or n_tokens above 2^30), WORKSPACE (x needs it and not even one of its tokens fits). */
 armor_status armor_linear_i8(armor_ctx* ctx, const void* d_x, int32_t x_dtype, int64_t ldx, const float* d_x_scale, const int8_t* d_wq,
                              int64_t ldw, const float* d_w_scale, const float* d_bias, void* d_y, int32_t y_dtype, int64_t ldy,
                              int64_t n_tokens, int64_t n_out, int64_t n_in, armor_stream_t stream);

@@ -1008,6 +1008,10 @@ armor_status armor_linear_i8(armor_ctx* c, const void* d_x, int32_t x_dtype, int
                                              n_tokens, n_out, n_in, false, s);
     return st == ARMOR_OK ? finish_call(c) : st;
   }
+  {
+    const armor_status st = launch_linear_i8_raw(c, d_x, x_dtype, ldx, d_wq, ldw, d_w_scale, d_bias, d_y, y_dtype, ldy, n_tokens, n_out, n_in, s);
+    if (st != ARMOR_ERR_UNSUPPORTED) return st == ARMOR_OK ? finish_call(c) : st;
+  }
   // the tokens' int8 rows, then their scales, in the workspace; more tokens than it holds in chunks
   const int64_t ldq = (n_in + 15) / 16 * 16;
   int64_t chunk = (ws_scratch_bytes(c) - 256) / (ldq + 4);
@@ -1081,8 +1085,11 @@ armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void
     float* const zs = reinterpret_cast<float*>(zq + up(n_tokens * d_in));
     float* const z2 = reinterpret_cast<float*>(reinterpret_cast<char*>(zs) + up(4 * n_tokens));
     armor_status st = launch_fwd_small(c, d_x, 0, buf + l.b, z1, n_tokens, d_in, s, true);
-    if (st == ARMOR_OK) st = launch_quantize_rows(c, z1, ARMOR_DTYPE_F32, d_in, n_tokens, d_in, zq, d_in, zs, s);
-    if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_F32, n_tokens, true, s);
+    if (st == ARMOR_OK) st = launch_core_i8_raw(c, z1, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_F32, n_tokens, true, s);
+    if (st == ARMOR_ERR_UNSUPPORTED) {
+      st = launch_quantize_rows(c, z1, ARMOR_DTYPE_F32, d_in, n_tokens, d_in, zq, d_in, zs, s);
+      if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_F32, n_tokens, true, s);
+    }
     if (st == ARMOR_OK) st = launch_fwd_small(c, z2, 1, buf + l.a, d_y, n_tokens, d_out, s);
     return st == ARMOR_OK ? finish_call(c) : st;
   }

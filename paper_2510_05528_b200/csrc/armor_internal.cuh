@@ -531,6 +531,11 @@ armor_status launch_quantize_rows(armor_ctx* c, const void* x, int32_t dtype, in
 armor_status launch_linear_i8(armor_ctx* c, const int8_t* xq, int64_t ldx, const float* xs, const int8_t* wq, int64_t ldw, const float* ws,
                               const float* bias, void* y, int32_t y_dtype, int64_t ldy, int64_t n, int64_t n_out, int64_t n_in, bool ahead,
                               cudaStream_t s);
+// one token or two, rounded by the product itself; UNSUPPORTED where the rows have to be rounded first
+armor_status launch_linear_i8_raw(armor_ctx* c, const void* x, int32_t x_dtype, int64_t ldx, const int8_t* wq, int64_t ldw, const float* ws,
+                                  const float* bias, void* y, int32_t y_dtype, int64_t ldy, int64_t n, int64_t n_out, int64_t n_in, cudaStream_t s);
+armor_status launch_core_i8_raw(armor_ctx* c, const float* z1, const int8_t* V, const void* E, const float* scale, void* z2, int32_t z2_dtype, int64_t n,
+                                bool ahead, cudaStream_t s);
 size_t packed_core_i8_e_bytes(int64_t d_out, int64_t d_in);
 armor_status launch_pack_core_i8(armor_ctx* c, const float* S, const uint8_t* M, int8_t* V, void* E, float* scale, cudaStream_t s);
 armor_status launch_core_i8(armor_ctx* c, const int8_t* zq, const float* zs, const int8_t* V, const void* E, const float* scale, void* z2,

@@ -32,6 +32,8 @@ struct I8P {
   int64_t M, N;                                     // rows of W, tokens
   int m_tiles, n_tiles, k_tiles, tile_n;
   int per;                                          // few tokens: k tiles a CTA
+  const void* x; int64_t ldx, K;                    // few tokens: the rows of x, where the kernel rounds them itself, and their length
+  int x_aligned;
   int ahead;                                        // few tokens: W may be fetched before the wait for the kernel before
   int32_t* status;
 };
@@ -106,16 +108,22 @@ __device__ __forceinline__ void store_two(const I8P& p, int64_t tok, int64_t row
 // Few tokens: reading W is the cost.  A CTA takes a row tile, BN tokens and a piece of the contraction; the pieces of a tile are
 // a cluster, which adds its int32 sums through distributed shared memory (exact in any order): each CTA has a share of the rows and
 // writes their outputs.  W is fetched before the wait for the kernel that rounds the tokens.
-template <int BN, bool SP>
+//
+// X other than int8_t: one token or two, rounded here rather than by a kernel before (which takes longer than the product): every CTA
+// finds the largest |x| of the whole row, rounds its piece's part of it and lays it down as the tiles that a TMA load would have brought.
+template <int BN, bool SP, typename X>
 struct Few {
+  static constexpr bool RAW = sizeof(X) > 1;
   static constexpr int B_BYTES = BN * 128 * (SP ? 2 : 1);
-  static constexpr int STAGE = A_BYTES + B_BYTES + (SP ? E_BYTES : 0);
+  static constexpr int STAGE = A_BYTES + (RAW ? 0 : B_BYTES) + (SP ? E_BYTES : 0);
+  static constexpr int TILES = RAW ? 32 * 1024 : 0;                           // all tiles of x of a piece
   static constexpr int SUMS = BN * BM * 4;                                    // a CTA's sums, in the place of the stages
-  static constexpr int FIT = 110 * 1024 / STAGE;                              // two CTAs share an SM
+  static constexpr int FIT = (110 * 1024 - TILES) / STAGE;                    // two CTAs share an SM
   static constexpr int STAGES = FIT * STAGE >= SUMS ? FIT : (SUMS + STAGE - 1) / STAGE;
   static constexpr int NEED = BN + (SP ? 8 * STAGES : 0);
   static constexpr uint32_t COLS = NEED <= 32 ? 32 : (NEED <= 64 ? 64 : (NEED <= 128 ? 128 : 256));
-  static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024;
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE + TILES + 1024;
+  static constexpr int MAX_PER = RAW ? TILES / B_BYTES : 1 << 30;
 };
 constexpr int FEW_THREADS = 192;
 // the same place in shared memory of another piece's CTA
@@ -125,19 +133,53 @@ __device__ __forceinline__ uint32_t in_piece(uint32_t addr, uint32_t piece) {
   return r;
 }
 
-template <int BN, bool SP>
+// The rows of x rounded by threads 64 .. 191: their scales to scale[], the piece's part, k from `from` to `to`, to tiles of BN rows x 128 k
+template <int BN, typename X>
+__device__ __forceinline__ void round_rows(const I8P& p, uint32_t tiles, float* scale, unsigned (&red)[4], int64_t from, int64_t to) {
+  const int id = threadIdx.x - 64, warp = id >> 5, lane = id & 31;
+  for (int t = 0; t < (int)p.N; ++t) {
+    const X* const x = static_cast<const X*>(p.x) + t * p.ldx;
+    auto load = [&](int64_t e) { return p.x_aligned ? rows::row_load<true>(x, e, p.K) : rows::row_load<false>(x, e, p.K); };
+    unsigned top = 0;
+#pragma unroll 4
+    for (int64_t e = id * 8; e < p.K; e += 128 * 8) {
+      float v[8];
+      rows::raw_get(load(e), v);
+      top = max(top, rows::abs_bits8(v));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) red[warp] = top;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    const rows::RowScale r = rows::row_scale(max(max(red[0], red[1]), max(red[2], red[3])));
+    asm volatile("bar.sync 1, 128;" ::: "memory");          // (red is read before the next row writes it)
+    if (id == 0) scale[t] = r.s;
+    for (int64_t e = from + id * 8; e < to; e += 128 * 8) {
+      float v[8];
+      rows::raw_get(load(e), v);
+      const uint2 q = rows::row_round8(v, r);
+      const uint32_t k = (uint32_t)(e - from), b = k & 127u;
+      const uint32_t at = tiles + (k >> 7) * (BN * 128) + (uint32_t)t * 128 + ((((b >> 4) ^ ((uint32_t)t & 7u))) << 4) + (b & 8u);
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(q.x), "r"(q.y) : "memory");
+    }
+  }
+}
+
+template <int BN, bool SP, typename X>
 __global__ void __launch_bounds__(FEW_THREADS, 2)
 i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
               const __grid_constant__ CUtensorMap mapE, const I8P p) {
-  using T = Few<BN, SP>;
+  using T = Few<BN, SP, X>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  __shared__ __align__(8) uint64_t bars[2 * T::STAGES + 1];
+  __shared__ __align__(8) uint64_t bars[2 * T::STAGES + 2];
+  __shared__ float own_scale[T::RAW ? BN : 1];
+  __shared__ unsigned own_top[4];
   __shared__ uint32_t tmem_base_holder;
   __shared__ int abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[T::STAGES]), tfull = smem_u32(&bars[2 * T::STAGES]);
+  const uint32_t rounded = tfull + 8, tiles = smem_u32(smem) + T::STAGES * T::STAGE;
   const int mt = blockIdx.x, piece = blockIdx.y, pieces = gridDim.y;
   const int k0 = piece * p.per, k1 = min(p.k_tiles, k0 + p.per);
   const int64_t tok0 = (int64_t)blockIdx.z * BN;
@@ -146,6 +188,7 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
     abort_flag = 0;
     for (int s = 0; s < T::STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     mbar_init(tfull, 1);
+    mbar_init(rounded, 128);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -169,9 +212,10 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
         const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE), fb = full0 + 8 * stage;
         mbar_expect_tx(fb, T::STAGE);
         tma_load_2d(dst, &mapA, kt * 128, mt * BM, fb);
-        if (SP) tma_load_2d(dst + A_BYTES + T::B_BYTES, &mapE, 0, (mt * p.k_tiles + kt) * 256, fb);
+        if (SP) tma_load_2d(dst + T::STAGE - E_BYTES, &mapE, 0, (mt * p.k_tiles + kt) * 256, fb);
       };
       auto load_x = [&](int kt, int stage) {
+        if (T::RAW) return;
         const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE) + A_BYTES, fb = full0 + 8 * stage;
         tma_load_2d(dst, &mapB, kt * (SP ? 256 : 128), (int)tok0, fb);
         if (SP) tma_load_2d(dst + BN * 128, &mapB, kt * 256 + 128, (int)tok0, fb);
@@ -203,15 +247,15 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
     if (lane == 0) {
       const uint32_t idesc = idesc_i8(BM, BN, SP);
       int stage = 0; uint32_t phase = 0;
-      bool ok = true;
-      for (int kt = k0; kt < k1; ++kt) {
+      bool ok = !T::RAW || mbar_wait(rounded, 0, abortp, p.status);
+      for (int kt = k0; kt < k1 && ok; ++kt) {
         if (!mbar_wait(full0 + 8 * stage, phase, abortp, p.status)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t sa = smem_u32(smem + (size_t)stage * T::STAGE), sb = sa + A_BYTES;
+        const uint32_t sa = smem_u32(smem + (size_t)stage * T::STAGE), sb = T::RAW ? tiles + (uint32_t)((kt - k0) * T::B_BYTES) : sa + A_BYTES;
         const uint32_t meta = tmem_base + BN + (uint32_t)(8 * stage);
         if (SP) {
-          copy_e<1>(meta, desc_e(sb + T::B_BYTES));
-          copy_e<1>(meta + 4, desc_e(sb + T::B_BYTES + 2048));
+          copy_e<1>(meta, desc_e(sa + T::STAGE - E_BYTES));
+          copy_e<1>(meta + 4, desc_e(sa + T::STAGE - E_BYTES + 2048));
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -223,6 +267,13 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
       if (ok) umma_commit(tfull);
     }
   } else {
+    if constexpr (T::RAW) {
+      if (ahead) grid_dependency_wait();
+      const int64_t width = SP ? 256 : 128, to = k1 * width;
+      round_rows<BN, X>(p, tiles, own_scale, own_top, k0 * width, to < p.K ? to : p.K);
+      fence_proxy_async();
+      mbar_arrive(rounded);
+    }
     // the CTA's sums to shared memory, [token][row]: all stages have been read when they are complete
     if (mbar_wait_warp(tfull, 0, abortp, p.status)) {
       tc_fence_after();
@@ -260,7 +311,7 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
       const int64_t row = (int64_t)mt * BM + 2 * r2, tok = tok0 + t;
       if (row >= p.M) continue;
       const bool two = row + 1 < p.M;
-      const float xs = p.xs[tok];
+      const float xs = T::RAW ? own_scale[t] : p.xs[tok];
       float va = (float)a * (xs * p.ws[row]), vb = two ? (float)b * (xs * p.ws[row + 1]) : 0.f;
       if (p.bias) { va += p.bias[row]; if (two) vb += p.bias[row + 1]; }
       store_two(p, tok, row, va, vb);
@@ -558,35 +609,48 @@ armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStre
   return ARMOR_OK;
 }
 
-template <int BN, bool SP>
-armor_status run_few(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
-  using T = Few<BN, SP>;
-  CUtensorMap mB;
-  if (!make_map_i8(&mB, xq, p.N, K, ldx, BN)) return ARMOR_ERR_CUDA;
-  static PerDeviceOnce attr;
-  if (ensure_dynamic_smem(attr, c->device, i8_few_kernel<BN, SP>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
-  p.n_tiles = (int)((p.N + BN - 1) / BN);
-  // pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight
+// pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight
+int few_pieces(const armor_ctx* c, const I8P& p, int& per) {
   int want = (int)(2 * (int64_t)c->n_sm / ((int64_t)p.m_tiles * p.n_tiles));
   if (want > 8) want = 8;
   if (want > p.k_tiles / 2) want = p.k_tiles / 2;
   if (want < 1) want = 1;
-  p.per = (p.k_tiles + want - 1) / want;
-  const int pieces = (p.k_tiles + p.per - 1) / p.per;
-  return launch_few(c, i8_few_kernel<BN, SP>, dim3((unsigned)p.m_tiles, (unsigned)pieces, (unsigned)p.n_tiles), T::SMEM, s, mA, mB, mE, p);
+  per = (p.k_tiles + want - 1) / want;
+  return (p.k_tiles + per - 1) / per;
+}
+template <int BN, bool SP, typename X>
+armor_status run_few(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
+  using T = Few<BN, SP, X>;
+  CUtensorMap mB = mA;
+  if (!T::RAW && !make_map_i8(&mB, xq, p.N, K, ldx, BN)) return ARMOR_ERR_CUDA;
+  static PerDeviceOnce attr;
+  if (ensure_dynamic_smem(attr, c->device, i8_few_kernel<BN, SP, X>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  p.n_tiles = (int)((p.N + BN - 1) / BN);
+  const int pieces = few_pieces(c, p, p.per);
+  if (T::RAW && p.per > T::MAX_PER) return ARMOR_ERR_UNSUPPORTED;             // (fits_raw has looked)
+  return launch_few(c, i8_few_kernel<BN, SP, X>, dim3((unsigned)p.m_tiles, (unsigned)pieces, (unsigned)p.n_tiles), T::SMEM, s, mA, mB, mE, p);
 }
 
 template <bool SP>
-armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
+armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s,
+                     int32_t x_dtype = ARMOR_DTYPE_I8) {
   KTimer kt(c, ARMOR_KC_GEMM, 2.0 * (double)p.M * (double)p.N * (double)K, s);      // (dense-equivalent)
   p.status = c->status;
   p.k_tiles = (int)((K + (SP ? 255 : 127)) / (SP ? 256 : 128));
   p.m_tiles = (int)((p.M + 127) / 128);
+  if (p.x) {                                                // the kernel rounds x itself (rounds_itself)
+    if (x_dtype == ARMOR_DTYPE_F32) return run_few<16, SP, float>(c, mA, mE, nullptr, 0, K, p, s);
+    if constexpr (!SP) {
+      if (x_dtype == ARMOR_DTYPE_BF16) return run_few<16, SP, __nv_bfloat16>(c, mA, mE, nullptr, 0, K, p, s);
+      if (x_dtype == ARMOR_DTYPE_F16) return run_few<16, SP, __half>(c, mA, mE, nullptr, 0, K, p, s);
+    }
+    return ARMOR_ERR_UNSUPPORTED;
+  }
   if (p.N <= 256) {
-    if (p.N <= 16) return run_few<16, SP>(c, mA, mE, xq, ldx, K, p, s);
-    if (p.N <= 32) return run_few<32, SP>(c, mA, mE, xq, ldx, K, p, s);
-    if (p.N <= 64) return run_few<64, SP>(c, mA, mE, xq, ldx, K, p, s);
-    return run_few<128, SP>(c, mA, mE, xq, ldx, K, p, s);
+    if (p.N <= 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    if (p.N <= 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    if (p.N <= 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    return run_few<128, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
   }
   using T = Many<SP>;
   p.m_tiles = (int)((p.M + 255) / 256);
@@ -616,6 +680,12 @@ I8P output(void* y, int32_t dtype, int64_t ldy, int64_t n, int64_t n_out, const 
   return p;
 }
 
+I8P with_rows(I8P p, const void* x, int32_t dtype, int64_t ldx, int64_t K) {
+  p.x = x; p.ldx = ldx; p.K = K;
+  p.x_aligned = rows::aligned16(x, p.N > 1 ? ldx : 8, rows_dtype_bytes(dtype));
+  return p;
+}
+
 // (rows up to whole tiles of 256: those beyond d_out hold positions too, 0 and 1, for an instruction that covers them)
 int64_t core_rows(int64_t d_out) { return (d_out + 255) / 256 * 256; }
 
@@ -629,6 +699,35 @@ armor_status launch_linear_i8(armor_ctx* c, const int8_t* xq, int64_t ldx, const
   CUtensorMap mA;
   if (!make_map_i8(&mA, wq, n_out, n_in, ldw, BM)) return ARMOR_ERR_CUDA;
   return product<false>(c, mA, mA, xq, ldx, n_in, output(y, y_dtype, ldy, n, n_out, xs, ws, bias, ahead ? 1 : 0), s);
+}
+
+// Whether n rows of x of K elements are rounded by the product's own CTAs: each reads all of x, up to 32 KiB, and the part of a piece fits.
+static bool rounds_itself(const armor_ctx* c, bool sparse, int64_t n, int64_t n_out, int64_t K, int32_t dtype) {
+  if (n > 2 || n * K * rows_dtype_bytes(dtype) > 32768) return false;
+  I8P p{};
+  p.k_tiles = (int)((K + (sparse ? 255 : 127)) / (sparse ? 256 : 128));
+  p.m_tiles = (int)((n_out + 127) / 128);
+  p.n_tiles = 1;
+  int per = 0;
+  few_pieces(c, p, per);
+  return per <= (sparse ? Few<16, true, float>::MAX_PER : Few<16, false, float>::MAX_PER);
+}
+// The same from rows of x that are not rounded yet; UNSUPPORTED where they have to be rounded first.
+armor_status launch_linear_i8_raw(armor_ctx* c, const void* x, int32_t x_dtype, int64_t ldx, const int8_t* wq, int64_t ldw, const float* ws,
+                                  const float* bias, void* y, int32_t y_dtype, int64_t ldy, int64_t n, int64_t n_out, int64_t n_in, cudaStream_t s) {
+  if (!rounds_itself(c, false, n, n_out, n_in, x_dtype)) return ARMOR_ERR_UNSUPPORTED;
+  CUtensorMap mA;
+  if (!make_map_i8(&mA, wq, n_out, n_in, ldw, BM)) return ARMOR_ERR_CUDA;
+  return product<false>(c, mA, mA, nullptr, 0, n_in, with_rows(output(y, y_dtype, ldy, n, n_out, nullptr, ws, bias, 0), x, x_dtype, ldx, n_in), s, x_dtype);
+}
+armor_status launch_core_i8_raw(armor_ctx* c, const float* z1, const int8_t* V, const void* E, const float* scale, void* z2, int32_t z2_dtype, int64_t n,
+                                bool ahead, cudaStream_t s) {
+  if (!rounds_itself(c, true, n, c->d_out, c->d_in, ARMOR_DTYPE_F32)) return ARMOR_ERR_UNSUPPORTED;
+  CUtensorMap mA, mE;
+  if (!make_map_i8(&mA, V, c->d_out, c->d_in / 2, c->d_in / 2, BM)) return ARMOR_ERR_CUDA;
+  if (!make_map_e(&mE, E, core_rows(c->d_out) / 128 * ((c->d_in + 255) / 256) * 256)) return ARMOR_ERR_CUDA;
+  return product<true>(c, mA, mE, nullptr, 0, c->d_in, with_rows(output(z2, z2_dtype, c->d_out, n, c->d_out, nullptr, scale, nullptr, ahead ? 1 : 0), z1, ARMOR_DTYPE_F32,
+                       c->d_in, c->d_in), s, ARMOR_DTYPE_F32);
 }
 
 // The core of a layer in 8 bits: values [d_out, d_in / 2], positions (packed_core_i8_e_bytes), scales [d_out]

@@ -170,6 +170,25 @@ def test_linear_layer(ctx, n, n_out, n_in, bias, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("n", [1, 2, 3])
+@pytest.mark.parametrize("n_out,n_in,off", [(1, 1, 0), (300, 7, 0), (129, 129, 1), (1024, 4096, 0), (2048, 1000, 3), (256, 8192, 0), (20000, 4096, 0), (640, 12289, 0)])
+def test_one_token_or_two(ctx, n, n_out, n_in, off, dtype):
+    """These are rounded by the product itself, except for the widest rows and pieces; rows that start anywhere."""
+    g = gen(n * 3 + n_out + n_in)
+    x = (torch.randn(n, n_in + 5, generator=g, device=DEV) * 3).to(dtype)[:, off:off + n_in]
+    wq, ws = int8_rows(n_out, n_in, g), torch.exp2(torch.randint(-9, -5, (n_out,), generator=g, device=DEV).float())
+    y = ctx.linear_i8(x, wq, ws, out_dtype=F32)
+    xq, xs = quantized(x)
+    want = whole(xq, wq) * xs.double()[:, None] * ws.double()
+    assert ((y.double() - want).abs() <= 3 * 2.0 ** -24 * want.abs()).all()
+    if n == 2:
+        x = x.clone()
+        x[1, n_in // 2] = float("nan")
+        z = ctx.linear_i8(x, wq, ws, out_dtype=F32)
+        assert torch.isnan(z[1]).all() and torch.equal(z[0], y[0])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("n", [3, 90, 300])
 @pytest.mark.parametrize("n_out,ldy,off", [(130, 136, 0), (131, 140, 1), (129, 133, 2)])
 def test_output_rows_of_a_wider_array(ctx, n, n_out, ldy, off, dtype):
@@ -207,7 +226,7 @@ def test_tokens_in_chunks_of_the_workspace():
     one = torch.ones(1, device=DEV)
     with pytest.raises(Bd.ArmorError, match="workspace"):
         tiny = Bd.ArmorContext(4, 4, 4, device=DEV, h_mode=Bd.H_DIAG, precision=Bd.PREC_SIMT)
-        tiny.linear_i8(torch.ones(1, 4096, device=DEV), big.new_int8_rows(1, 4096), one)
+        tiny.linear_i8(torch.ones(3, 4096, device=DEV), big.new_int8_rows(1, 4096), one)
 
 
 def test_no_tokens(ctx):
@@ -248,7 +267,7 @@ SHAPES = [(256, 256, 128), (128, 384, 128), (384, 128, 128), (512, 768, 256), (2
 
 
 @pytest.mark.parametrize("d_out,d_in,db", SHAPES)
-@pytest.mark.parametrize("n", [1, 16, 17, 40, 64, 100, 128, 129, 200, 257, 600])
+@pytest.mark.parametrize("n", [1, 2, 3, 16, 17, 40, 64, 100, 128, 129, 200, 257, 600])
 def test_core_and_positions_are_exact(d_out, d_in, db, n):
     """Whole numbers throughout: the product with the 2:4 core is an integer, rounded to bf16 on its way to A and not again."""
     c = Bd.ArmorContext(d_out, d_in, db, device=DEV)
