@@ -1078,8 +1078,12 @@ armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void
   const float* const core_scale = reinterpret_cast<const float*>(buf + l.scale);
   char* const scratch = reinterpret_cast<char*>(c->T);
   auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
-  if (n_tokens <= ARMOR_SMALL_TOKENS) {
-    // z1 and z2 in fp32 (z2 is rounded to bf16 by the product with A): 5 d_in n + 4 d_out n bytes, n at most d_in and d_out
+  // The few-token wrapper kernels and a kernel that rounds the fp32 z1, four launches, against a memset and four persistent kernels, 22 us
+  // whatever their tokens.  By the wrapper products' size: 4096 x 4096, 768 tokens 34.6 and 35.5 us, 1,024 46.3 and 42.1; 14336 x 4096, 300 40.1
+  // and 41.1, 400 48.8 and 43.3; 8192 x 8192 in blocks of 256, 130 33.6 and 37.4, 200 40.9 and 38.9; 1024 x 1024, 300 12.6 and 22.7.
+  const bool few = n_tokens <= ARMOR_SMALL_TOKENS || (n_tokens * (d_in + d_out) * c->db <= 800000000 && n_tokens * (5 * d_in + 4 * d_out) <= 39 * c->wn);
+  if (few) {
+    // z1 and z2 in fp32 (z2 is rounded to bf16 by the product with A): 5 d_in n + 4 d_out n of the workspace's 40 d_in d_out bytes
     float* const z1 = reinterpret_cast<float*>(scratch);
     int8_t* const zq = reinterpret_cast<int8_t*>(scratch + up(4 * n_tokens * d_in));
     float* const zs = reinterpret_cast<float*>(zq + up(n_tokens * d_in));

@@ -294,27 +294,46 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
   if (pieces > 1) cluster_sync_all(); else __syncthreads();
   if (!*abortp) {
     grid_dependency_wait();                                 // (every thread that reads the tokens' scales)
-    // row pairs [u0, u1) of every token
-    const int u0 = 64 * piece / pieces, u1 = 64 * (piece + 1) / pieces, w = u1 - u0;
+    // Row pairs [u0, u1) of every token.  A lane keeps to a row pair and takes four tokens at a time, so that the loads from the other
+    // pieces are under way together.
+    const int u0 = 64 * piece / pieces, w = 64 * (piece + 1) / pieces - u0;
     const int nv = (int)(p.N - tok0 < BN ? p.N - tok0 : BN);
+    const int wide = w <= 8 ? 8 : (w <= 16 ? 16 : 32), abreast = 32 / wide * (FEW_THREADS / 32);      // tokens side by side
     const uint32_t base = smem_u32(smem);
-    for (int u = threadIdx.x; u < nv * w; u += FEW_THREADS) {
-      const int t = u / w, r2 = u0 + u - t * w;
-      int32_t a = 0, b = 0;
-      const uint32_t at = base + (uint32_t)(t * BM + 2 * r2) * 4;
-      for (int k = 0; k < pieces; ++k) {
-        int32_t x, y;
-        const uint32_t from = pieces > 1 ? in_piece(at, (uint32_t)k) : at;
-        asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(from) : "memory");
-        a += x; b += y;
-      }
-      const int64_t row = (int64_t)mt * BM + 2 * r2, tok = tok0 + t;
-      if (row >= p.M) continue;
+    for (int u = lane % wide; u < w; u += 32) {
+      const int r2 = u0 + u;
+      const int64_t row = (int64_t)mt * BM + 2 * r2;
+      if (row >= p.M) break;
       const bool two = row + 1 < p.M;
-      const float xs = T::RAW ? own_scale[t] : p.xs[tok];
-      float va = (float)a * (xs * p.ws[row]), vb = two ? (float)b * (xs * p.ws[row + 1]) : 0.f;
-      if (p.bias) { va += p.bias[row]; if (two) vb += p.bias[row + 1]; }
-      store_two(p, tok, row, va, vb);
+      const float wa = p.ws[row], wb = two ? p.ws[row + 1] : 0.f;
+      const float ba = p.bias ? p.bias[row] : 0.f, bb = p.bias && two ? p.bias[row + 1] : 0.f;
+      for (int t0 = warp * (32 / wide) + lane / wide; t0 < nv; t0 += 4 * abreast) {
+        int32_t a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
+        uint32_t at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = base + (uint32_t)(min(t0 + i * abreast, nv - 1) * BM + 2 * r2) * 4;
+        auto add = [&](int k) {                             // (no branch around a load: its wait would stand inside)
+          int32_t x[4], y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t from = pieces > 1 ? in_piece(at[i], (uint32_t)k) : at[i];
+            asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(x[i]), "=r"(y[i]) : "r"(from) : "memory");
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { a[i] += x[i]; b[i] += y[i]; }
+        };
+        int k = 0;
+        for (; k + 2 <= pieces; k += 2) { add(k); add(k + 1); }
+        if (k < pieces) add(k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + i * abreast;
+          if (t < nv) {
+            const float xs = T::RAW ? own_scale[t] : p.xs[tok0 + t];
+            store_two(p, tok0 + t, row, fmaf((float)a[i], xs * wa, ba), fmaf((float)b[i], xs * wb, bb));
+          }
+        }
+      }
     }
   }
   __syncwarp();
@@ -326,9 +345,48 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
 }
 
 // ---------------------------------------------------------------------------------------------------------
+// The way out of 32 tokens of a warp's 32 rows: sums from tensor memory (lanes are rows), scaled, and neighbouring lanes swap one value of
+// every pair of tokens, so that a lane stores two neighbouring rows of one token.  slot: 32 floats of the warp's own.
+template <typename T>
+__device__ __forceinline__ void put_two(T* at, float a, float b) { *reinterpret_cast<uint32_t*>(at) = rows::pack2(static_cast<const T*>(nullptr), a, b); }
+__device__ __forceinline__ void put_two(float* at, float a, float b) { *reinterpret_cast<float2*>(at) = make_float2(a, b); }
+template <typename T>
+__device__ __forceinline__ void way_out(const I8P& p, uint32_t taddr, int64_t row, int64_t tok0, float ws, float bias, float* slot, int lane) {
+  __syncwarp();
+  slot[lane] = tok0 + lane < p.N ? p.xs[tok0 + lane] : 0.f;
+  __syncwarp();
+  uint32_t r[32];
+  tmem_ld32(taddr, r);
+  const bool odd = lane & 1;
+  const int64_t even = row & ~int64_t(1);
+  const bool pair = p.pairs && even + 1 < p.M, full = tok0 + 32 <= p.N;
+  T* at = static_cast<T*>(p.Y) + (tok0 + odd) * p.ldy + even;
+  const int64_t step = 2 * p.ldy;
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(slot + i);
+    const float v[4] = {fmaf((float)(int32_t)r[i], x.x * ws, bias), fmaf((float)(int32_t)r[i + 1], x.y * ws, bias),
+                        fmaf((float)(int32_t)r[i + 2], x.z * ws, bias), fmaf((float)(int32_t)r[i + 3], x.w * ws, bias)};
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      const float got = __shfl_xor_sync(0xffffffffu, odd ? v[k] : v[k + 1], 1);
+      const float a = odd ? got : v[k], b = odd ? v[k + 1] : got;
+      if (full || tok0 + i + k + odd < p.N) {
+        if (pair) put_two(at, a, b);
+        else {
+          if (even < p.M) at[0] = rows::from_f<T>(a);
+          if (even + 1 < p.M) at[1] = rows::from_f<T>(b);
+        }
+      }
+      at += step;
+    }
+  }
+}
+
 // Many tokens: pairs of CTAs (cta_group::2), a tile of 256 rows of W by up to 256 tokens (sparse: 224), persistent, the next tile's
 // products beside the last one's way out (two accumulators).  Each CTA holds 128 rows of W (and their positions, in its tensor
-// memory) and half of the tile's tokens.
+// memory) and half of the tile's tokens.  (Two row tiles to a stage's tokens, with one accumulator each, lose what the second accumulator hides:
+// 28672 x 8192, 4,096 tokens dense 600 -> 688 us, sparse 452 -> 499.)
 //   full[s]   (even CTA): armed for the bytes of both CTAs, whose loads complete on it
 //   empty[s], tfull[2] (both CTAs): tcgen05.commit to the pair
 //   tempty[2] (even CTA): an arrival of every epilogue warp of either CTA
@@ -340,10 +398,11 @@ struct Many {
   static constexpr int STAGE = E_AT + (SP ? E_BYTES : 0);
   static constexpr int STAGES = 220 * 1024 / STAGE;
   static constexpr uint32_t META = 2 * MAX_N;
+  static constexpr int EPI = 8;                                               // epilogue warps, half of the tokens each four
+  static constexpr int THREADS = 64 + 32 * EPI;
   static constexpr size_t SMEM = (size_t)STAGES * STAGE + 1024;
   static_assert(!SP || META + 8 * STAGES <= 512, "tensor memory");
 };
-constexpr int MANY_THREADS = 192;
 constexpr uint32_t MANY_COLS = 512;
 
 constexpr int GROUP_M = 8;                          // row tiles that run side by side: see sparse_tcgen05.cu
@@ -356,7 +415,7 @@ __device__ __forceinline__ void tile_to_mn(int tile, int m_tiles, int n_tiles, i
 }
 
 template <bool SP>
-__global__ void __launch_bounds__(MANY_THREADS, 1)
+__global__ void __launch_bounds__(Many<SP>::THREADS, 1)
 i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const __grid_constant__ CUtensorMap mapE, const I8P p) {
   using T = Many<SP>;
@@ -364,6 +423,7 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ __align__(8) uint64_t bars[2 * STAGES + 4];
+  __shared__ __align__(16) float slots[T::EPI][32];
   __shared__ uint32_t tmem_base_holder;
   __shared__ int abort_flag;
 
@@ -378,7 +438,7 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(tfull0 + 8 * s, 1); mbar_init(tempty0 + 8 * s, 8); }
+    for (int s = 0; s < 2; ++s) { mbar_init(tfull0 + 8 * s, 1); mbar_init(tempty0 + 8 * s, 2 * T::EPI); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -406,7 +466,7 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
         const int row0 = mt * 256 + (int)rank * 128, tok0 = nt * p.tile_n + (int)rank * half_n;
         for (int kt = 0; kt < p.k_tiles; ++kt) {
           if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abortp, p.status)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * (A_BYTES + half_n * 128 * (SP ? 2 : 1) + (SP ? E_BYTES : 0)));
+          if (rank == 0) mbar_expect_tx(full0 + 8 * stage, 2 * (A_BYTES + (SP ? E_BYTES : 0) + half_n * 128 * (SP ? 2 : 1)));
           const uint32_t fb = map_to_cta(full0 + 8 * stage, 0);
           const uint32_t dst = smem_u32(smem + (size_t)stage * T::STAGE);
           tma_load_2d_pair(dst, &mapA, kt * 128, row0, fb);
@@ -462,7 +522,7 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     }
   } else {
     // ------------------------------------------------------------ epilogue warps (both CTAs)
-    const int q = warp & 3;
+    const int q = warp & 3, half = (warp - 2) >> 2;          // lane quarter; odd or even chunks of 32 tokens
     int local = 0;
     bool ok = true;
     for (int tile = pair; tile < n_tiles_total && ok; tile += n_pairs, ++local) {
@@ -473,23 +533,14 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
       const float ws = row < p.M ? p.ws[row] : 0.f, bias = p.bias && row < p.M ? p.bias[row] : 0.f;
       if (!mbar_wait_warp(tfull0 + 8 * as, (uint32_t)(local >> 1) & 1u, abortp, p.status)) { ok = false; break; }
       tc_fence_after();
-      const bool odd = lane & 1;
 #pragma unroll 1
-      for (int ch = 0; ch < p.tile_n / 32; ++ch) {
+      for (int ch = half; ch < p.tile_n / 32; ch += 2) {
         const int64_t tok0 = (int64_t)nt * p.tile_n + ch * 32;
         if (tok0 >= p.N) break;
-        const float xs = tok0 + lane < p.N ? p.xs[tok0 + lane] : 0.f;
-        uint32_t r[32];
-        tmem_ld32(tmem_base + (uint32_t)(as * T::MAX_N + ch * 32) + ((uint32_t)(q * 32) << 16), r);
-        // neighbouring lanes swap one value of every pair of tokens: a lane stores two rows of one token
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float v0 = fmaf((float)(int32_t)r[i], __shfl_sync(0xffffffffu, xs, i) * ws, bias);
-          const float v1 = fmaf((float)(int32_t)r[i + 1], __shfl_sync(0xffffffffu, xs, i + 1) * ws, bias);
-          const float got = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
-          const int64_t tok = tok0 + i + (odd ? 1 : 0);
-          if (tok < p.N) store_two(p, tok, row & ~int64_t(1), odd ? got : v0, odd ? v1 : got);
-        }
+        const uint32_t taddr = tmem_base + (uint32_t)(as * T::MAX_N + ch * 32) + ((uint32_t)(q * 32) << 16);
+        if (p.out == ARMOR_DTYPE_BF16) way_out<__nv_bfloat16>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
+        else if (p.out == ARMOR_DTYPE_F32) way_out<float>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
+        else way_out<__half>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
       }
       tc_fence_before();
       __syncwarp();
@@ -592,6 +643,7 @@ core_top_kernel(const float* __restrict__ S, const uint8_t* __restrict__ Mk, flo
   if (threadIdx.x == 0) top[row] = __uint_as_float(m);
 }
 
+constexpr int64_t JOIN = 1800;                      // what the way out of the pieces takes a token of the tile, in bytes of operands (128 tokens: 3.7 us)
 // a dependent launch whose CTAs along y are a cluster
 template <typename K>
 armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStream_t s, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mE,
@@ -646,28 +698,37 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
     }
     return ARMOR_ERR_UNSUPPORTED;
   }
-  if (p.N <= 256) {
-    if (p.N <= 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    if (p.N <= 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    if (p.N <= 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    return run_few<128, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-  }
+  // Pairs of CTAs, with the width of a tile that costs least: rounds of the pairs times what a stage brings in, or the few-token kernel with
+  // the contraction cut.  Either way an SM takes its operands at 60 GB/s, whatever the tile (4096 x 4096 to 14336 x 4096, 96 to 3,000
+  // tokens, to 10 %), so the bytes that an SM loads decide, and for the second what joining the pieces takes.  Pairs and pieces: 4096 x 4096, 96 tokens
+  // 16.9 and 13.3 us, 200 19.1 and 15.6, 300 20.3 and 22.7; 14336 x 4096, 64 17.5 and 14.4, 200 22.9 and 27.6; 512 x 8192, 512 30.2 and 21.0.
   using T = Many<SP>;
-  p.m_tiles = (int)((p.M + 255) / 256);
-  const int pairs = c->n_sm / 2;
-  // the width of a tile that costs least: rounds of the pairs times its tokens and what comes with every tile
+  constexpr int64_t W_BYTES = A_BYTES + (SP ? E_BYTES : 0);
+  const int pairs = c->n_sm / 2, rows256 = (int)((p.M + 255) / 256);
   int64_t least = 0;
   for (int w = T::MAX_N; w >= 64; w -= 32) {
-    const int64_t tiles = (int64_t)p.m_tiles * ((p.N + w - 1) / w), cost = (tiles + pairs - 1) / pairs * (w + 64);
+    const int64_t rounds = ((int64_t)rows256 * ((p.N + w - 1) / w) + pairs - 1) / pairs, cost = rounds * (W_BYTES + (SP ? 128 : 64) * w);
     if (w == T::MAX_N || cost < least) { least = cost; p.tile_n = w; }
   }
+  const int bn = p.N <= 16 ? 16 : (p.N <= 32 ? 32 : (p.N <= 64 ? 64 : 128));
+  p.n_tiles = (int)((p.N + bn - 1) / bn);
+  int per = 0;
+  const int64_t pieces = few_pieces(c, p, per);
+  const int64_t few = (pieces * p.m_tiles * p.n_tiles + c->n_sm - 1) / c->n_sm * per * (W_BYTES + (SP ? 256 : 128) * bn) + JOIN * bn;
+  if (p.N <= 32 || few < least * p.k_tiles) {
+    if (bn == 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    if (bn == 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    if (bn == 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+    return run_few<128, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+  }
+  p.m_tiles = rows256;
   p.n_tiles = (int)((p.N + p.tile_n - 1) / p.tile_n);
   CUtensorMap mB;
   if (!make_map_i8(&mB, xq, p.N, K, ldx, p.tile_n / 2)) return ARMOR_ERR_CUDA;
   static PerDeviceOnce attr;
   if (ensure_dynamic_smem(attr, c->device, i8_many_kernel<SP>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  launch_dependent(i8_many_kernel<SP>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(MANY_THREADS), T::SMEM, LaunchStream(s, false, 2), mA, mB, mE, p);
+  launch_dependent(i8_many_kernel<SP>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(T::THREADS), T::SMEM, LaunchStream(s, false, 2), mA, mB, mE, p);
   c->launches++;
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }

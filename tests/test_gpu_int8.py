@@ -267,7 +267,7 @@ SHAPES = [(256, 256, 128), (128, 384, 128), (384, 128, 128), (512, 768, 256), (2
 
 
 @pytest.mark.parametrize("d_out,d_in,db", SHAPES)
-@pytest.mark.parametrize("n", [1, 2, 3, 16, 17, 40, 64, 100, 128, 129, 200, 257, 600])
+@pytest.mark.parametrize("n", [1, 2, 3, 16, 17, 40, 64, 100, 128, 129, 200, 257, 600, 5000])
 def test_core_and_positions_are_exact(d_out, d_in, db, n):
     """Whole numbers throughout: the product with the 2:4 core is an integer, rounded to bf16 on its way to A and not again."""
     c = Bd.ArmorContext(d_out, d_in, db, device=DEV)
@@ -280,7 +280,7 @@ def test_core_and_positions_are_exact(d_out, d_in, db, n):
 
 
 @pytest.mark.parametrize("d_out,d_in,db", SHAPES)
-@pytest.mark.parametrize("n", [1, 37, 128, 300, 2100])
+@pytest.mark.parametrize("n", [1, 37, 128, 300, 2100, 7000])
 @pytest.mark.parametrize("denormalize", [False, True])
 def test_layer_against_64_bits(d_out, d_in, db, n, denormalize):
     """Bound, element by element: z1 is an fp32 sum, so where it is within 2^-16 of a step's border its integer may be the other one (counted
