@@ -643,7 +643,6 @@ core_top_kernel(const float* __restrict__ S, const uint8_t* __restrict__ Mk, flo
   if (threadIdx.x == 0) top[row] = __uint_as_float(m);
 }
 
-constexpr int64_t JOIN = 1800;                      // what the way out of the pieces takes a token of the tile, in bytes of operands (128 tokens: 3.7 us)
 // a dependent launch whose CTAs along y are a cluster
 template <typename K>
 armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStream_t s, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mE,
@@ -661,12 +660,14 @@ armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStre
   return ARMOR_OK;
 }
 
-// pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight
+// Pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight; one, two, four or eight where
+// there are several token tiles (4096 x 4096, 300 tokens: three pieces of 96 tiles 22.7 us, the pairs of CTAs 20.3).
 int few_pieces(const armor_ctx* c, const I8P& p, int& per) {
   int want = (int)(2 * (int64_t)c->n_sm / ((int64_t)p.m_tiles * p.n_tiles));
   if (want > 8) want = 8;
   if (want > p.k_tiles / 2) want = p.k_tiles / 2;
   if (want < 1) want = 1;
+  if (p.n_tiles > 1) want = want >= 8 ? 8 : (want >= 4 ? 4 : (want >= 2 ? 2 : 1));
   per = (p.k_tiles + want - 1) / want;
   return (p.k_tiles + per - 1) / per;
 }
@@ -698,10 +699,11 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
     }
     return ARMOR_ERR_UNSUPPORTED;
   }
-  // Pairs of CTAs, with the width of a tile that costs least: rounds of the pairs times what a stage brings in, or the few-token kernel with
-  // the contraction cut.  Either way an SM takes its operands at 60 GB/s, whatever the tile (4096 x 4096 to 14336 x 4096, 96 to 3,000
-  // tokens, to 10 %), so the bytes that an SM loads decide, and for the second what joining the pieces takes.  Pairs and pieces: 4096 x 4096, 96 tokens
-  // 16.9 and 13.3 us, 200 19.1 and 15.6, 300 20.3 and 22.7; 14336 x 4096, 64 17.5 and 14.4, 200 22.9 and 27.6; 512 x 8192, 512 30.2 and 21.0.
+  // Pairs of CTAs, with the width of a tile that costs least, or the few-token kernel with the contraction cut, by what they take beside what
+  // both do (nanoseconds): a pair's SM takes its stages at 60 bytes a ns, rounds of them; a CTA of the few-token kernel, two an
+  // SM, at 38, and joining its pieces 6 a token of the tile and piece.  Measured, pairs and pieces: 4096 x 4096, 128 tokens 17.3 and 15.7 us,
+  // 200 19.1 and 15.6; 14336 x 4096, 64 17.5 and 14.4, 200 22.9 and 27.6; 8192 x 8192, 128 27 and 18.3, 300 35 and 43; 512 x 8192, 512 30.2
+  // and 21.0.  Of the sizes tried it misses by 15 % at most (4096 x 14336, 512 tokens, pairs 49, pieces 42).
   using T = Many<SP>;
   constexpr int64_t W_BYTES = A_BYTES + (SP ? E_BYTES : 0);
   const int pairs = c->n_sm / 2, rows256 = (int)((p.M + 255) / 256);
@@ -714,8 +716,9 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
   p.n_tiles = (int)((p.N + bn - 1) / bn);
   int per = 0;
   const int64_t pieces = few_pieces(c, p, per);
-  const int64_t few = (pieces * p.m_tiles * p.n_tiles + c->n_sm - 1) / c->n_sm * per * (W_BYTES + (SP ? 256 : 128) * bn) + JOIN * bn;
-  if (p.N <= 32 || few < least * p.k_tiles) {
+  const int64_t waves = (pieces * p.m_tiles * p.n_tiles + 2 * c->n_sm - 1) / (2 * c->n_sm);
+  const int64_t few = waves * per * (W_BYTES + (SP ? 256 : 128) * bn) / 38 + (pieces - 1) * bn * 6, many = least * p.k_tiles / 60 + 1000;
+  if (p.N <= 32 || (p.N <= 512 && few < many)) {
     if (bn == 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
     if (bn == 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
     if (bn == 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
