@@ -386,28 +386,33 @@ def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, re
     return n_gates
 
 
-def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0, w_post=None, w_pre=None, post=None, pre=True,
-                     residual_scale=1.0, eps=1e-6) -> None:
-    """h and n (and n as int8 q with q_scale) of the residual stream x and a block's output y (see armor.h).  post: None means with
-    w_post."""
+def _block_norm(ctx, x, y, h, n, q, q_scale, made, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps) -> None:
+    # made: the outputs are this module's own, contiguous and of the right shape (a call takes microseconds, its checks as many)
     a = armor_block_norm_args()
     dt = x.dtype
+    code = ROW_DTYPES.get(dt)
+    a.stream_dtype = _row_dtype(x, "x") if code is None else code
     a.x, a.ldx = _row_ptr(x, dt, "x")
     rows, d = x.shape
-    a.stream_dtype = _row_dtype(x, "x")
-    branch = y if y is not None else n
-    if branch is None:
-        bt, a.branch_dtype = dt, a.stream_dtype
-    else:
-        bt, a.branch_dtype = branch.dtype, _row_dtype(branch, "y")
-    for t, name in ((y, "y"), (h, "h"), (n, "n"), (q, "q"), (q_scale, "q_scale")):
-        if t is not None and t.size(0) != rows:
-            raise ValueError(f"{name} must have the {rows} rows of x")
     if y is not None:
+        bt = y.dtype
         a.y, a.ldy = _row_ptr(y, bt, "y", d)
-    if h is not None:
+        if y.size(0) != rows:
+            raise ValueError(f"y must have the {rows} rows of x")
+    else:
+        bt = dt if n is None else n.dtype
+    a.branch_dtype = code if bt is dt else _row_dtype(n if y is None else y, "y")
+    if made:
+        a.h = h.data_ptr()
+        a.ldh = d
+        if n is not None:
+            a.n = n.data_ptr()
+            a.ldn = d
+    else:
+        for t, name in ((h, "h"), (n, "n"), (q, "q"), (q_scale, "q_scale")):
+            if t is not None and t.size(0) != rows:
+                raise ValueError(f"{name} must have the {rows} rows of x")
         a.h, a.ldh = _row_ptr(h, dt, "h", d)
-    if n is not None:
         a.n, a.ldn = _row_ptr(n, bt, "n", d)
     if q is not None:
         a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
@@ -419,9 +424,15 @@ def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0,
         _check(code, "armor_block_norm")
 
 
-def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, *, gate=None, rows_per_gate=0, w_post=None,
-                              w_pre=None, post=None, pre=True, residual_scale=1.0, eps=1e-6) -> None:
-    """The gradient of armor_block_norm (see armor.h)."""
+def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0, w_post=None, w_pre=None, post=None, pre=True,
+                     residual_scale=1.0, eps=1e-6) -> None:
+    """h and n (and n as int8 q with q_scale) of the residual stream x and a block's output y (see armor.h).  post: None means with
+    w_post."""
+    _block_norm(ctx, x, y, h, n, q, q_scale, False, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+
+
+def _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made, gate, rows_per_gate, w_post, w_pre, post, pre,
+                         residual_scale, eps) -> None:
     f = torch.float32
     a = armor_block_norm_grad_args()
     stream = h if h is not None else (dh if dh is not None else dx)
@@ -430,13 +441,11 @@ def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate,
         raise ValueError("h, dh, dx, y, dn and dy are all missing")
     one = stream if stream is not None else branch
     ts, tb = one.dtype, (branch if branch is not None else stream).dtype
-    _row_ptr(one, ts, "h")
+    if one.dim() != 2:
+        raise ValueError("h, y and their gradients must be [rows, cols]")
     rows, d = one.shape
     a.stream_dtype = _row_dtype(one, "h")
     a.branch_dtype = a.stream_dtype if tb is ts else _row_dtype(branch, "y")
-    for t, name in ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn"), (dx, "dx"), (dy, "dy")):
-        if t is not None and t.size(0) != rows:
-            raise ValueError(f"{name} must have {rows} rows")
     if h is not None:
         a.h, a.ldh = _row_ptr(h, ts, "h", d)
     if y is not None:
@@ -445,23 +454,38 @@ def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate,
         a.dh, a.lddh = _row_ptr(dh, ts, "dh", d)
     if dn is not None:
         a.dn, a.lddn = _row_ptr(dn, tb, "dn", d)
-    if dx is not None:
-        a.dx, a.lddx = _row_ptr(dx, ts, "dx", d)
-    if dy is not None:
-        a.dy, a.lddy = _row_ptr(dy, tb, "dy", d)
+    for t, name in ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn")) if made else ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn"), (dx, "dx"), (dy, "dy")):
+        if t is not None and t.size(0) != rows:
+            raise ValueError(f"{name} must have {rows} rows")
     gates = _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
-    if (dw_post is not None and dw_post.numel() != d) or (dw_pre is not None and dw_pre.numel() != d) or \
-            (dgate is not None and dgate.numel() != gates * d):
-        raise ValueError(f"dw_post and dw_pre must have {d} elements, dgate {gates} x {d}")
-    if dw_post is not None:
-        a.dw_post = _ptr(dw_post, f, "dw_post")
-    if dw_pre is not None:
-        a.dw_pre = _ptr(dw_pre, f, "dw_pre")
-    if dgate is not None:
-        a.dgate = _ptr(dgate, f, "dgate")
+    if made:
+        a.dx = dx.data_ptr()
+        a.dy = dy.data_ptr()
+        a.lddx = a.lddy = d
+        if dw_post is not None:
+            a.dw_post = dw_post.data_ptr()
+        if dw_pre is not None:
+            a.dw_pre = dw_pre.data_ptr()
+        if dgate is not None:
+            a.dgate = dgate.data_ptr()
+    else:
+        a.dx, a.lddx = _row_ptr(dx, ts, "dx", d)
+        a.dy, a.lddy = _row_ptr(dy, tb, "dy", d)
+        for name, t, n in (("dw_post", dw_post, d), ("dw_pre", dw_pre, d), ("dgate", dgate, gates * d)):
+            if t is not None:
+                if t.numel() != n:
+                    raise ValueError(f"{name} must have {n} elements")
+                setattr(a, name, _ptr(t, f, name))
     code = lib().armor_block_norm_backward(ctx, a, _stream())
     if code:
         _check(code, "armor_block_norm_backward")
+
+
+def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, *, gate=None, rows_per_gate=0, w_post=None,
+                              w_pre=None, post=None, pre=True, residual_scale=1.0, eps=1e-6) -> None:
+    """The gradient of armor_block_norm (see armor.h)."""
+    _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, False, gate, rows_per_gate, w_post, w_pre, post, pre,
+                         residual_scale, eps)
 
 
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
@@ -715,38 +739,46 @@ class ArmorContext:
         return y
 
     # -- norms between two blocks
-    def block_norm(self, x: torch.Tensor, y: torch.Tensor | None = None, **terms) -> tuple[torch.Tensor, torch.Tensor]:
+    def block_norm(self, x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None, rows_per_gate: int = 0,
+                   w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, post: bool | None = None, pre: bool = True,
+                   residual_scale: float = 1.0, eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor]:
         """(h, n): the residual stream x plus a block's output y, normed, weighted and gated, and the normed stream that the next
-        block reads.  terms: gate [d] or [n_gates, d] with rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps."""
-        self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
+        block reads.  gate: [d], or [n_gates, d] with rows_per_gate; post: a norm of y, None: with w_post."""
+        self._here(x, y, gate, w_post, w_pre)
         h = _empty_rows(x)
         n = _empty_rows(x if y is None else y)
-        armor_block_norm(self.ctx, x, y, h, n, None, None, **terms)
+        _block_norm(self.ctx, x, y, h, n, None, None, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
         return h, n
 
-    def block_norm_i8(self, x: torch.Tensor, y: torch.Tensor | None = None, **terms) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    def block_norm_i8(self, x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None, rows_per_gate: int = 0,
+                      w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, post: bool | None = None, pre: bool = True,
+                      residual_scale: float = 1.0, eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """(h, q, scale): as block_norm, the normed stream as int8 rows for linear_i8."""
-        self._here(x, y, terms.get("gate"), terms.get("w_post"), terms.get("w_pre"))
+        self._here(x, y, gate, w_post, w_pre)
         h = _empty_rows(x)
         q = self.new_int8_rows(x.shape[0], x.shape[1])
         scale = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
-        armor_block_norm(self.ctx, x, y, h, None, q, scale, **terms)
+        _block_norm(self.ctx, x, y, h, None, q, scale, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
         return h, q, scale
 
-    def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor, dh: torch.Tensor | None, dn: torch.Tensor | None,
-                            **terms) -> dict[str, torch.Tensor]:
+    def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor, dh: torch.Tensor | None, dn: torch.Tensor | None, *,
+                            gate: torch.Tensor | None = None, rows_per_gate: int = 0, w_post: torch.Tensor | None = None,
+                            w_pre: torch.Tensor | None = None, post: bool | None = None, pre: bool = True, residual_scale: float = 1.0,
+                            eps: float = 1e-6) -> dict[str, torch.Tensor]:
         """The gradients dx, dy and those of the weights and the gate that are given (fp32), from the h that block_norm returned, y and
         the gradients of h and n."""
-        gate, w_post, w_pre = terms.get("gate"), terms.get("w_post"), terms.get("w_pre")
         self._here(h, y, dh, dn, gate, w_post, w_pre)
-        out = {"dx": _empty_rows(h), "dy": _empty_rows(y)}
+        dx, dy = _empty_rows(h), _empty_rows(y)
+        out = {"dx": dx, "dy": dy}
+        dw_pre = dw_post = dgate = None
         if w_pre is not None:
-            out["dw_pre"] = torch.empty_like(w_pre)
+            out["dw_pre"] = dw_pre = torch.empty_like(w_pre)
         if w_post is not None:
-            out["dw_post"] = torch.empty_like(w_post)
+            out["dw_post"] = dw_post = torch.empty_like(w_post)
         if gate is not None:
-            out["dgate"] = _empty_rows(gate)
-        armor_block_norm_backward(self.ctx, h, y, dh, dn, out["dx"], out["dy"], out.get("dw_post"), out.get("dw_pre"), out.get("dgate"), **terms)
+            out["dgate"] = dgate = _empty_rows(gate)
+        _block_norm_backward(self.ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, True, gate, rows_per_gate, w_post, w_pre, post, pre,
+                             residual_scale, eps)
         return out
 
     def device_status(self) -> list[int]:

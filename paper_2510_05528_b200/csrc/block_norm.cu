@@ -790,7 +790,8 @@ bool plan_ring(int64_t d, bool al, size_t e0, size_t e1, size_t e2, size_t e3, s
   }
   r.stage_bytes = (int)stage;
   // as many CTAs as the registers hold, 512 threads or one, with two rows on their way
-  for (pl.ctas = pl.threads > 256 ? 1 : (512 / pl.threads < 8 ? 512 / pl.threads : 8); pl.ctas >= 1; --pl.ctas) {
+  const int most = wide ? 16 : 8;                           // (of the gradient's every CTA leaves sums behind)
+  for (pl.ctas = pl.threads > 256 ? 1 : (512 / pl.threads < most ? 512 / pl.threads : most); pl.ctas >= 1; --pl.ctas) {
     const size_t room = pl.ctas == 1 ? RING_SMEM : RING_SMEM / (size_t)pl.ctas - 2048, keep = kept * (size_t)((d + 7) / 8 * 8);
     if (room < keep) continue;
     int n = (int)((room - keep) / stage);
