@@ -295,6 +295,36 @@ def _row_ptr(t: torch.Tensor | None, dtype, name: str, cols: int | None = None) 
     return t.data_ptr(), ld
 
 
+def _rows_at(t: torch.Tensor, dtype, cols: int | None, name: str, here: int) -> tuple[int | None, int, int]:
+    """(address, leading dimension, rows) of [rows, cols] on device `here`.  The common case in as few steps as there are: a small call
+    takes ten microseconds, most of them its checks."""
+    if t.dtype is dtype and t.get_device() == here and t.is_contiguous():
+        shape = t.shape
+        if len(shape) == 2 and (cols is None or shape[1] == cols):
+            n, c = shape
+            return t.data_ptr(), (c if n > 1 else max(c, t.stride(0))), n
+    if t.is_cuda and t.get_device() != here:
+        raise ValueError(f"{name} must be on cuda:{here}, the context's device, not on {t.device}")
+    p, ld = _row_ptr(t, dtype, name, cols)
+    return p, ld, t.shape[0]
+
+
+def _cuda_index(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.get_device()
+
+
+def _vector_at(t: torch.Tensor, n: int, name: str, here: int) -> int:
+    """The address of n contiguous floats on device `here`."""
+    if t.dtype is torch.float32 and t.get_device() == here and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    if t.is_cuda and t.get_device() != here:
+        raise ValueError(f"{name} must be on cuda:{here}, the context's device, not on {t.device}")
+    _ptr(t, torch.float32, name)
+    raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+
+
 def _row_dtype(t: torch.Tensor, name: str) -> int:
     code = ROW_DTYPES.get(t.dtype)
     if code is None:
@@ -354,19 +384,14 @@ def armor_apply_layer_i8(ctx, packed, x, y) -> None:
         _check(code, "armor_apply_layer_i8")
 
 
-def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps):
+def _norm_params(a, d, n_rows, here, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps):
     """Fills what both directions of the norms share; returns the gate's rows."""
-    f = torch.float32
     a.n_rows = n_rows
     a.d = d
     if w_pre is not None:
-        if w_pre.numel() != d:
-            raise ValueError(f"w_pre must have {d} elements")
-        a.w_pre = _ptr(w_pre, f, "w_pre")
+        a.w_pre = _vector_at(w_pre, d, "w_pre", here)
     if w_post is not None:
-        if w_post.numel() != d:
-            raise ValueError(f"w_post must have {d} elements")
-        a.w_post = _ptr(w_post, f, "w_post")
+        a.w_post = _vector_at(w_post, d, "w_post", here)
     a.post = w_post is not None if post is None else post
     a.pre = pre
     a.residual_scale = residual_scale
@@ -375,8 +400,7 @@ def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, re
         return 0
     if gate.dim() == 1:
         gate = gate.unsqueeze(0)
-    a.gate, a.ld_gate = _row_ptr(gate, f, "gate", d)
-    n_gates = gate.size(0)
+    a.gate, a.ld_gate, n_gates = _rows_at(gate, torch.float32, d, "gate", here)
     if not rows_per_gate:
         if n_gates < 1 or n_rows % n_gates:
             raise ValueError(f"rows_per_gate must be given where {n_gates} gates do not divide {n_rows} rows")
@@ -386,21 +410,21 @@ def _norm_params(a, d, n_rows, gate, rows_per_gate, w_post, w_pre, post, pre, re
     return n_gates
 
 
-def _block_norm(ctx, x, y, h, n, q, q_scale, made, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps) -> None:
-    # made: the outputs are this module's own, contiguous and of the right shape (a call takes microseconds, its checks as many)
+def _block_norm(ctx, here, x, y, h, n, q, q_scale, made, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps) -> None:
+    # made: the outputs are this module's own, contiguous and of the right shape
     a = armor_block_norm_args()
     dt = x.dtype
-    code = ROW_DTYPES.get(dt)
-    a.stream_dtype = _row_dtype(x, "x") if code is None else code
-    a.x, a.ldx = _row_ptr(x, dt, "x")
-    rows, d = x.shape
+    a.stream_dtype = code = _row_dtype(x, "x")
+    a.x, a.ldx, rows = _rows_at(x, dt, None, "x", here)
+    d = x.size(1)
+    bt = dt
     if y is not None:
         bt = y.dtype
-        a.y, a.ldy = _row_ptr(y, bt, "y", d)
-        if y.size(0) != rows:
+        a.y, a.ldy, n_y = _rows_at(y, bt, d, "y", here)
+        if n_y != rows:
             raise ValueError(f"y must have the {rows} rows of x")
-    else:
-        bt = dt if n is None else n.dtype
+    elif n is not None:
+        bt = n.dtype
     a.branch_dtype = code if bt is dt else _row_dtype(n if y is None else y, "y")
     if made:
         a.h = h.data_ptr()
@@ -418,7 +442,7 @@ def _block_norm(ctx, x, y, h, n, q, q_scale, made, gate, rows_per_gate, w_post, 
         a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
     if q_scale is not None:
         a.q_scale = _ptr(q_scale, torch.float32, "q_scale")
-    _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+    _norm_params(a, d, rows, here, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
     code = lib().armor_block_norm(ctx, a, _stream())
     if code:
         _check(code, "armor_block_norm")
@@ -428,17 +452,14 @@ def armor_block_norm(ctx, x, y, h, n, q, q_scale, *, gate=None, rows_per_gate=0,
                      residual_scale=1.0, eps=1e-6) -> None:
     """h and n (and n as int8 q with q_scale) of the residual stream x and a block's output y (see armor.h).  post: None means with
     w_post."""
-    _block_norm(ctx, x, y, h, n, q, q_scale, False, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+    _block_norm(ctx, _cuda_index(x, "x"), x, y, h, n, q, q_scale, False, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
 
 
-def _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made, gate, rows_per_gate, w_post, w_pre, post, pre,
+def _block_norm_backward(ctx, here, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made, gate, rows_per_gate, w_post, w_pre, post, pre,
                          residual_scale, eps) -> None:
-    f = torch.float32
     a = armor_block_norm_grad_args()
     stream = h if h is not None else (dh if dh is not None else dx)
     branch = y if y is not None else (dn if dn is not None else dy)
-    if stream is None and branch is None:
-        raise ValueError("h, dh, dx, y, dn and dy are all missing")
     one = stream if stream is not None else branch
     ts, tb = one.dtype, (branch if branch is not None else stream).dtype
     if one.dim() != 2:
@@ -446,18 +467,18 @@ def _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made
     rows, d = one.shape
     a.stream_dtype = _row_dtype(one, "h")
     a.branch_dtype = a.stream_dtype if tb is ts else _row_dtype(branch, "y")
+    n_h = n_y = n_dh = n_dn = rows
     if h is not None:
-        a.h, a.ldh = _row_ptr(h, ts, "h", d)
+        a.h, a.ldh, n_h = _rows_at(h, ts, d, "h", here)
     if y is not None:
-        a.y, a.ldy = _row_ptr(y, tb, "y", d)
+        a.y, a.ldy, n_y = _rows_at(y, tb, d, "y", here)
     if dh is not None:
-        a.dh, a.lddh = _row_ptr(dh, ts, "dh", d)
+        a.dh, a.lddh, n_dh = _rows_at(dh, ts, d, "dh", here)
     if dn is not None:
-        a.dn, a.lddn = _row_ptr(dn, tb, "dn", d)
-    for t, name in ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn")) if made else ((h, "h"), (y, "y"), (dh, "dh"), (dn, "dn"), (dx, "dx"), (dy, "dy")):
-        if t is not None and t.size(0) != rows:
-            raise ValueError(f"{name} must have {rows} rows")
-    gates = _norm_params(a, d, rows, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+        a.dn, a.lddn, n_dn = _rows_at(dn, tb, d, "dn", here)
+    if not n_h == n_y == n_dh == n_dn == rows:
+        raise ValueError("h, y, dh and dn must have as many rows")
+    gates = _norm_params(a, d, rows, here, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
     if made:
         a.dx = dx.data_ptr()
         a.dy = dy.data_ptr()
@@ -469,13 +490,14 @@ def _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made
         if dgate is not None:
             a.dgate = dgate.data_ptr()
     else:
+        for t, name in ((dx, "dx"), (dy, "dy")):
+            if t is not None and t.size(0) != rows:
+                raise ValueError(f"{name} must have {rows} rows")
         a.dx, a.lddx = _row_ptr(dx, ts, "dx", d)
         a.dy, a.lddy = _row_ptr(dy, tb, "dy", d)
         for name, t, n in (("dw_post", dw_post, d), ("dw_pre", dw_pre, d), ("dgate", dgate, gates * d)):
             if t is not None:
-                if t.numel() != n:
-                    raise ValueError(f"{name} must have {n} elements")
-                setattr(a, name, _ptr(t, f, name))
+                setattr(a, name, _vector_at(t, n, name, here))
     code = lib().armor_block_norm_backward(ctx, a, _stream())
     if code:
         _check(code, "armor_block_norm_backward")
@@ -484,8 +506,11 @@ def _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, made
 def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, *, gate=None, rows_per_gate=0, w_post=None,
                               w_pre=None, post=None, pre=True, residual_scale=1.0, eps=1e-6) -> None:
     """The gradient of armor_block_norm (see armor.h)."""
-    _block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, False, gate, rows_per_gate, w_post, w_pre, post, pre,
-                         residual_scale, eps)
+    one = next((t for t in (h, dh, dx, y, dn, dy) if t is not None), None)
+    if one is None:
+        raise ValueError("h, dh, dx, y, dn and dy are all missing")
+    _block_norm_backward(ctx, _cuda_index(one, "h, y and their gradients"), h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, False, gate, rows_per_gate, w_post, w_pre, post,
+                         pre, residual_scale, eps)
 
 
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
@@ -603,6 +628,7 @@ class ArmorContext:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
+        self._packed_i8_bytes = None
         self.cfg = make_config(d_out, d_in, d_block, **kw)
         self.d_out, self.d_in, self.d_block = d_out, d_in, d_block
         nbytes = armor_workspace_bytes(self.cfg)
@@ -701,6 +727,19 @@ class ArmorContext:
         if torch._C._cuda_getDevice() != here:
             raise ValueError(f"{self.device} must be the current device")
 
+    def _current(self) -> int:
+        """The index of the context's device, which has to be the current one."""
+        here = self._index
+        if torch._C._cuda_getDevice() != here:
+            raise ValueError(f"{self.device} must be the current device")
+        return here
+
+    @property
+    def _packed_i8(self) -> int:
+        if self._packed_i8_bytes is None:
+            self._packed_i8_bytes = armor_packed_layer_i8_bytes(self.cfg)
+        return self._packed_i8_bytes
+
     def new_int8_rows(self, n: int, cols: int) -> torch.Tensor:
         """[n, cols] int8 whose rows start on 16-byte boundaries."""
         return torch.empty(n, (cols + 15) // 16 * 16, dtype=torch.int8, device=self.device)[:, :cols]
@@ -717,25 +756,44 @@ class ArmorContext:
                   x_scale: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
         """y = x W^T (+ bias) in 8 bits with W = w_scale wq as quantize_rows gives it.  x: fp32, bf16 or fp16 (rounded to int8 here), or
         int8 with its x_scale; out_dtype: x's by default, bf16 for int8."""
-        self._here(x, wq, w_scale, bias, x_scale)
+        here = self._current()
+        dt = x.dtype
+        code = DTYPE_I8 if dt is torch.int8 else _row_dtype(x, "x")
+        xp, ldx, n = _rows_at(x, dt, None, "x", here)
+        n_in = x.size(1)
+        wp, ldw, n_out = _rows_at(wq, torch.int8, n_in, "wq", here)
         if out_dtype is None:
-            out_dtype = torch.bfloat16 if x.dtype is torch.int8 else x.dtype
-        y = torch.empty(x.shape[0], wq.shape[0], dtype=out_dtype, device=self.device)
-        armor_linear_i8(self.ctx, x, x_scale, wq, w_scale, bias, y)
+            out_dtype = torch.bfloat16 if code == DTYPE_I8 else dt
+        y = torch.empty(n, n_out, dtype=out_dtype, device=self.device)
+        code = lib().armor_linear_i8(self.ctx, xp, code, ldx, None if x_scale is None else _vector_at(x_scale, n, "x_scale", here), wp, ldw,
+                                     _vector_at(w_scale, n_out, "w_scale", here), None if bias is None else _vector_at(bias, n_out, "bias", here),
+                                     y.data_ptr(), _row_dtype(y, "y"), n_out, n, n_out, n_in, _stream())
+        if code:
+            _check(code, "armor_linear_i8")
         return y
 
     def pack_layer_i8(self, st: LayerState, denormalize: bool = False) -> torch.Tensor:
         """Core in 8 bits (a scale for each row) and bf16 wrappers, packed for apply_layer_i8."""
         self._here(st.A, st.B, st.S, st.M)
-        packed = torch.empty(armor_packed_layer_i8_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+        packed = torch.empty(self._packed_i8, dtype=torch.uint8, device=self.device)
         r1, r2 = (st.r1, st.r2) if denormalize else (None, None)
         armor_pack_layer_i8(self.ctx, st.A, st.B, st.S, st.M, r1, r2, packed)
         return packed
 
     def apply_layer_i8(self, packed: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
-        self._here(packed, x)
-        y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
-        armor_apply_layer_i8(self.ctx, packed, x, y)
+        here = self._current()
+        bf16 = torch.bfloat16
+        if x.dtype is not bf16:
+            raise ValueError("the packed layer takes bf16 x and y")
+        xp, ld, n = _rows_at(x, bf16, self.d_in, "x", here)
+        if ld != self.d_in and n > 1:
+            raise ValueError("x must be contiguous")
+        if packed.dtype is not torch.uint8 or packed.get_device() != here or packed.numel() < self._packed_i8 or not packed.is_contiguous():
+            raise ValueError(f"packed must be what pack_layer_i8 made for this shape: {self._packed_i8} bytes on {self.device}")
+        y = torch.empty(n, self.d_out, dtype=bf16, device=self.device)
+        code = lib().armor_apply_layer_i8(self.ctx, packed.data_ptr(), xp, y.data_ptr(), n, _stream())
+        if code:
+            _check(code, "armor_apply_layer_i8")
         return y
 
     # -- norms between two blocks
@@ -744,21 +802,21 @@ class ArmorContext:
                    residual_scale: float = 1.0, eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor]:
         """(h, n): the residual stream x plus a block's output y, normed, weighted and gated, and the normed stream that the next
         block reads.  gate: [d], or [n_gates, d] with rows_per_gate; post: a norm of y, None: with w_post."""
-        self._here(x, y, gate, w_post, w_pre)
+        here = self._current()
         h = _empty_rows(x)
         n = _empty_rows(x if y is None else y)
-        _block_norm(self.ctx, x, y, h, n, None, None, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+        _block_norm(self.ctx, here, x, y, h, n, None, None, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
         return h, n
 
     def block_norm_i8(self, x: torch.Tensor, y: torch.Tensor | None = None, *, gate: torch.Tensor | None = None, rows_per_gate: int = 0,
                       w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, post: bool | None = None, pre: bool = True,
                       residual_scale: float = 1.0, eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """(h, q, scale): as block_norm, the normed stream as int8 rows for linear_i8."""
-        self._here(x, y, gate, w_post, w_pre)
+        here = self._current()
         h = _empty_rows(x)
         q = self.new_int8_rows(x.shape[0], x.shape[1])
         scale = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
-        _block_norm(self.ctx, x, y, h, None, q, scale, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
+        _block_norm(self.ctx, here, x, y, h, None, q, scale, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
         return h, q, scale
 
     def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor, dh: torch.Tensor | None, dn: torch.Tensor | None, *,
@@ -767,7 +825,7 @@ class ArmorContext:
                             eps: float = 1e-6) -> dict[str, torch.Tensor]:
         """The gradients dx, dy and those of the weights and the gate that are given (fp32), from the h that block_norm returned, y and
         the gradients of h and n."""
-        self._here(h, y, dh, dn, gate, w_post, w_pre)
+        here = self._current()
         dx, dy = _empty_rows(h), _empty_rows(y)
         out = {"dx": dx, "dy": dy}
         dw_pre = dw_post = dgate = None
@@ -777,7 +835,7 @@ class ArmorContext:
             out["dw_post"] = dw_post = torch.empty_like(w_post)
         if gate is not None:
             out["dgate"] = dgate = _empty_rows(gate)
-        _block_norm_backward(self.ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, True, gate, rows_per_gate, w_post, w_pre, post, pre,
+        _block_norm_backward(self.ctx, here, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, True, gate, rows_per_gate, w_post, w_pre, post, pre,
                              residual_scale, eps)
         return out
 
