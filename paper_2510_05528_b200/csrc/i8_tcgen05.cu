@@ -118,11 +118,11 @@ struct Few {
   static constexpr int STAGE = A_BYTES + (RAW ? 0 : B_BYTES) + (SP ? E_BYTES : 0);
   static constexpr int TILES = RAW ? 32 * 1024 : 0;                           // all tiles of x of a piece
   static constexpr int SUMS = BN * BM * 4;                                    // a CTA's sums, in the place of the stages
-  static constexpr int FIT = (110 * 1024 - TILES) / STAGE;                    // two CTAs share an SM
-  static constexpr int STAGES = FIT * STAGE >= SUMS ? FIT : (SUMS + STAGE - 1) / STAGE;
+  static constexpr int STAGES = (110 * 1024 - TILES) / STAGE;                 // two CTAs share an SM
   static constexpr int NEED = BN + (SP ? 8 * STAGES : 0);
   static constexpr uint32_t COLS = NEED <= 32 ? 32 : (NEED <= 64 ? 64 : (NEED <= 128 ? 128 : 256));
-  static constexpr size_t SMEM = (size_t)STAGES * STAGE + TILES + 1024;
+  static constexpr size_t SMEM = (size_t)(STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS) + TILES + 1024;
+  static_assert(STAGES >= 2 && SMEM <= 111 * 1024 && (!RAW || STAGES * STAGE >= SUMS), "");
   static constexpr int MAX_PER = RAW ? TILES / B_BYTES : 1 << 30;
 };
 constexpr int FEW_THREADS = 192;
@@ -660,28 +660,37 @@ armor_status launch_few(armor_ctx* c, K kernel, dim3 grid, size_t smem, cudaStre
   return ARMOR_OK;
 }
 
-// Pieces of the contraction: two CTAs an SM while a piece keeps two stages, at most a cluster of eight; one, two, four or eight where
-// there are several token tiles (4096 x 4096, 300 tokens: three pieces of 96 tiles 22.7 us, the pairs of CTAs 20.3).
-int few_pieces(const armor_ctx* c, const I8P& p, int& per) {
-  int want = (int)(2 * (int64_t)c->n_sm / ((int64_t)p.m_tiles * p.n_tiles));
-  if (want > 8) want = 8;
-  if (want > p.k_tiles / 2) want = p.k_tiles / 2;
-  if (want < 1) want = 1;
-  if (p.n_tiles > 1) want = want >= 8 ? 8 : (want >= 4 ? 4 : (want >= 2 ? 2 : 1));
-  per = (p.k_tiles + want - 1) / want;
-  return (p.k_tiles + per - 1) / per;
+// What the few-token kernel takes with tiles of w tokens, in nanoseconds, and the pieces of the contraction with which it takes least: a CTA, two
+// an SM, takes its stages at 38 bytes a ns, and 6 ns to add a token of a piece.  Clusters have to find room all at once (28672 x 8192, 320
+// tokens, five rounds of three pieces 142 us, pairs of CTAs 94), and the machine holds fewer CTAs in clusters: of 296 what `held` says (the
+// occupancy calculator's figures), and some clusters less while the kernel before still rounds many tokens (4096 x 14336, 32 tiles, pieces
+// eight and seven: 17 tokens 12.1 and 13.3 us, 24 18.3 and 13.8, 37 19.1 to 21.1 and 14.6).
+struct FewPlan { int w, n_tiles, pieces, per; int64_t cost; };
+FewPlan few_plan(const armor_ctx* c, const I8P& p, bool sparse, int w) {
+  constexpr int held[9] = {0, 296, 296, 279, 284, 280, 270, 259, 264};
+  FewPlan best{w, (int)((p.N + w - 1) / w), 0, 0, 0};
+  const int64_t stage = A_BYTES + (sparse ? E_BYTES + 256 * w : 128 * w), tiles = (int64_t)p.m_tiles * best.n_tiles;
+  const int64_t taken = p.N * p.k_tiles * (sparse ? 256 : 128) > 1 << 18 ? 20 : 0;
+  for (int want = 1; want <= 8 && (want == 1 || 2 * want <= p.k_tiles); ++want) {
+    const int per = (p.k_tiles + want - 1) / want, pieces = (p.k_tiles + per - 1) / per;
+    if (pieces > 1 && tiles * pieces > (int64_t)held[pieces] * c->n_sm / 148 - taken) continue;
+    const int64_t waves = (tiles * pieces + 2 * c->n_sm - 1) / (2 * c->n_sm), cost = waves * per * stage / 38 + (pieces - 1) * w * 6;
+    if (best.pieces == 0 || cost < best.cost) { best.pieces = pieces; best.per = per; best.cost = cost; }
+  }
+  return best;
 }
 template <int BN, bool SP, typename X>
-armor_status run_few(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, cudaStream_t s) {
+armor_status run_few(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE, const int8_t* xq, int64_t ldx, int64_t K, I8P p, const FewPlan& plan,
+                     cudaStream_t s) {
   using T = Few<BN, SP, X>;
   CUtensorMap mB = mA;
   if (!T::RAW && !make_map_i8(&mB, xq, p.N, K, ldx, BN)) return ARMOR_ERR_CUDA;
   static PerDeviceOnce attr;
   if (ensure_dynamic_smem(attr, c->device, i8_few_kernel<BN, SP, X>, T::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
-  p.n_tiles = (int)((p.N + BN - 1) / BN);
-  const int pieces = few_pieces(c, p, p.per);
-  if (T::RAW && p.per > T::MAX_PER) return ARMOR_ERR_UNSUPPORTED;             // (fits_raw has looked)
-  return launch_few(c, i8_few_kernel<BN, SP, X>, dim3((unsigned)p.m_tiles, (unsigned)pieces, (unsigned)p.n_tiles), T::SMEM, s, mA, mB, mE, p);
+  p.n_tiles = plan.n_tiles;
+  p.per = plan.per;
+  if (plan.w != BN || (T::RAW && p.per > T::MAX_PER)) return ARMOR_ERR_UNSUPPORTED;              // (rounds_itself has looked)
+  return launch_few(c, i8_few_kernel<BN, SP, X>, dim3((unsigned)p.m_tiles, (unsigned)plan.pieces, (unsigned)p.n_tiles), T::SMEM, s, mA, mB, mE, p);
 }
 
 template <bool SP>
@@ -691,19 +700,21 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
   p.status = c->status;
   p.k_tiles = (int)((K + (SP ? 255 : 127)) / (SP ? 256 : 128));
   p.m_tiles = (int)((p.M + 127) / 128);
+  FewPlan few = few_plan(c, p, SP, 16);
   if (p.x) {                                                // the kernel rounds x itself (rounds_itself)
-    if (x_dtype == ARMOR_DTYPE_F32) return run_few<16, SP, float>(c, mA, mE, nullptr, 0, K, p, s);
+    if (x_dtype == ARMOR_DTYPE_F32) return run_few<16, SP, float>(c, mA, mE, nullptr, 0, K, p, few, s);
     if constexpr (!SP) {
-      if (x_dtype == ARMOR_DTYPE_BF16) return run_few<16, SP, __nv_bfloat16>(c, mA, mE, nullptr, 0, K, p, s);
-      if (x_dtype == ARMOR_DTYPE_F16) return run_few<16, SP, __half>(c, mA, mE, nullptr, 0, K, p, s);
+      if (x_dtype == ARMOR_DTYPE_BF16) return run_few<16, SP, __nv_bfloat16>(c, mA, mE, nullptr, 0, K, p, few, s);
+      if (x_dtype == ARMOR_DTYPE_F16) return run_few<16, SP, __half>(c, mA, mE, nullptr, 0, K, p, few, s);
     }
     return ARMOR_ERR_UNSUPPORTED;
   }
-  // Pairs of CTAs, with the width of a tile that costs least, or the few-token kernel with the contraction cut, by what they take beside what
-  // both do (nanoseconds): a pair's SM takes its stages at 60 bytes a ns, rounds of them; a CTA of the few-token kernel, two an
-  // SM, at 38, and joining its pieces 6 a token of the tile and piece.  Measured, pairs and pieces: 4096 x 4096, 128 tokens 17.3 and 15.7 us,
-  // 200 19.1 and 15.6; 14336 x 4096, 64 17.5 and 14.4, 200 22.9 and 27.6; 8192 x 8192, 128 27 and 18.3, 300 35 and 43; 512 x 8192, 512 30.2
-  // and 21.0.  Of the sizes tried it misses by 15 % at most (4096 x 14336, 512 tokens, pairs 49, pieces 42).
+  // Pairs of CTAs, or the few-token kernel with the contraction cut, each with the width of tile that costs least, by what they take
+  // beside what both do (nanoseconds): a pair's SM takes its stages at 60 bytes a ns, rounds of them; the other as few_plan has it.  Measured, pairs
+  // and pieces: 4096 x 4096, 128 tokens 17.3 and 13.0 us; 8192 x 8192, 192 32.6 and 27.6; 4096 x 14336, 320 47.4 and 31.9; 512 x 8192, 512 30.2 and
+  // 19.2; 256 x 14336, 1,024 49 and 26.5; 14336 x 4096, 200 22.9 and 27.6; 8192 x 8192, 300 35 and 43.  Beyond 512 tokens the estimate of the
+  // pieces is short (1024 x 1024, 1,024 tokens 11.5 us for 10.5): they have to win by a quarter.  Widths of the pieces: 1024 x 1024, 64
+  // tokens, one tile of 64 8.0 us, four of 16 6.4; 14336 x 4096, 96 tokens, a tile of 128 19.1, of 96 16.6.
   using T = Many<SP>;
   constexpr int64_t W_BYTES = A_BYTES + (SP ? E_BYTES : 0);
   const int pairs = c->n_sm / 2, rows256 = (int)((p.M + 255) / 256);
@@ -712,17 +723,22 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
     const int64_t rounds = ((int64_t)rows256 * ((p.N + w - 1) / w) + pairs - 1) / pairs, cost = rounds * (W_BYTES + (SP ? 128 : 64) * w);
     if (w == T::MAX_N || cost < least) { least = cost; p.tile_n = w; }
   }
-  const int bn = p.N <= 16 ? 16 : (p.N <= 32 ? 32 : (p.N <= 64 ? 64 : 128));
-  p.n_tiles = (int)((p.N + bn - 1) / bn);
-  int per = 0;
-  const int64_t pieces = few_pieces(c, p, per);
-  const int64_t waves = (pieces * p.m_tiles * p.n_tiles + 2 * c->n_sm - 1) / (2 * c->n_sm);
-  const int64_t few = waves * per * (W_BYTES + (SP ? 256 : 128) * bn) / 38 + (pieces - 1) * bn * 6, many = least * p.k_tiles / 60 + 1000;
-  if (p.N <= 32 || (p.N <= 512 && few < many)) {
-    if (bn == 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    if (bn == 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    if (bn == 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
-    return run_few<128, SP, int8_t>(c, mA, mE, xq, ldx, K, p, s);
+  for (const int w : {32, 64, 96, 128, 160, 192}) {
+    if (w - 32 >= p.N || w > (SP ? 128 : 192)) break;       // (wider ones with positions and twice the tokens leave a CTA no second stage)
+    const FewPlan plan = few_plan(c, p, SP, w);
+    if (plan.cost < few.cost) few = plan;
+  }
+  const int64_t many = least * p.k_tiles / 60 + 1000;
+  if (p.N <= 32 || (p.N <= 512 && few.cost < many) || (p.N <= 1024 && 4 * few.cost < 3 * many)) {
+    if (few.w == 16) return run_few<16, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+    if (few.w == 32) return run_few<32, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+    if (few.w == 64) return run_few<64, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+    if (few.w == 96) return run_few<96, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+    if constexpr (!SP) {
+      if (few.w == 160) return run_few<160, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+      if (few.w == 192) return run_few<192, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
+    }
+    return run_few<128, SP, int8_t>(c, mA, mE, xq, ldx, K, p, few, s);
   }
   p.m_tiles = rows256;
   p.n_tiles = (int)((p.N + p.tile_n - 1) / p.tile_n);
@@ -771,9 +787,8 @@ static bool rounds_itself(const armor_ctx* c, bool sparse, int64_t n, int64_t n_
   I8P p{};
   p.k_tiles = (int)((K + (sparse ? 255 : 127)) / (sparse ? 256 : 128));
   p.m_tiles = (int)((n_out + 127) / 128);
-  p.n_tiles = 1;
-  int per = 0;
-  few_pieces(c, p, per);
+  p.N = n;
+  const int per = few_plan(c, p, sparse, 16).per;
   return per <= (sparse ? Few<16, true, float>::MAX_PER : Few<16, false, float>::MAX_PER);
 }
 // The same from rows of x that are not rounded yet; UNSUPPORTED where they have to be rounded first.
