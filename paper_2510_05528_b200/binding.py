@@ -481,7 +481,8 @@ def _block_norm_backward(ctx, here, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate
     gates = _norm_params(a, d, rows, here, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
     if made:
         a.dx = dx.data_ptr()
-        a.dy = dy.data_ptr()
+        if dy is not None:
+            a.dy = dy.data_ptr()
         a.lddx = a.lddy = d
         if dw_post is not None:
             a.dw_post = dw_post.data_ptr()
@@ -819,15 +820,17 @@ class ArmorContext:
         _block_norm(self.ctx, here, x, y, h, None, q, scale, True, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
         return h, q, scale
 
-    def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor, dh: torch.Tensor | None, dn: torch.Tensor | None, *,
+    def block_norm_backward(self, h: torch.Tensor, y: torch.Tensor | None, dh: torch.Tensor | None, dn: torch.Tensor | None, *,
                             gate: torch.Tensor | None = None, rows_per_gate: int = 0, w_post: torch.Tensor | None = None,
                             w_pre: torch.Tensor | None = None, post: bool | None = None, pre: bool = True, residual_scale: float = 1.0,
                             eps: float = 1e-6) -> dict[str, torch.Tensor]:
-        """The gradients dx, dy and those of the weights and the gate that are given (fp32), from the h that block_norm returned, y and
-        the gradients of h and n."""
+        """The gradients dx, dy (where there is a y) and those of the weights and the gate that are given (fp32), from the h that
+        block_norm returned, y and the gradients of h and n."""
         here = self._current()
-        dx, dy = _empty_rows(h), _empty_rows(y)
-        out = {"dx": dx, "dy": dy}
+        out = {"dx": _empty_rows(h)}
+        dx, dy = out["dx"], None
+        if y is not None:
+            out["dy"] = dy = _empty_rows(y)
         dw_pre = dw_post = dgate = None
         if w_pre is not None:
             out["dw_pre"] = dw_pre = torch.empty_like(w_pre)

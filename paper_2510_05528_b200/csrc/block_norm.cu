@@ -432,6 +432,10 @@ block_norm_grad_kernel(const GradP p) {
       for (int k = 0; k < 2; ++k) {
         const float4 t = at[(2 * c + k) * blockDim.x];
         const float v[4] = {t.x, t.y, t.z, t.w};
+        if (ALIGNED && d % 4 == 0) {
+          if (e + 4 * k < d) *reinterpret_cast<float4*>(out + e + 4 * k) = t;
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (e + 4 * k + i < d) out[e + 4 * k + i] = v[i];

@@ -402,3 +402,14 @@ def test_refused_calls(ctx):
     with pytest.raises(Bd.ArmorError, match="size"):
         ctx.block_norm(wide, wide)
     assert ctx.device_status()[:4] == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("rows,d", [(3, 77), (400, 1032), (320, 9000)])
+def test_gradient_without_a_branch(ctx, rows, d):
+    """h = residual_scale x, n = h / rms(h) w_pre: dx and dw_pre, and no dy."""
+    t = inputs(rows, d, BF16, BF16, post=False, gates=0)
+    h, _ = ctx.block_norm(t["x"], w_pre=t["w_pre"], residual_scale=0.5)
+    got = ctx.block_norm_backward(h, None, t["dh"], t["dn"], w_pre=t["w_pre"], residual_scale=0.5)
+    assert sorted(got) == ["dw_pre", "dx"]
+    want, sizes = backward64(t, h, post=False, a=0.5)
+    check_backward(got, want, sizes)
