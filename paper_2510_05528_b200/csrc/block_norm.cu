@@ -742,6 +742,7 @@ block_norm_grad_sums_kernel(const GradP p) {
   __shared__ double add[32][33];
   const int lane = threadIdx.x / CT, c0 = threadIdx.x % CT * VEC;
   const int64_t col = (int64_t)blockIdx.x * 32 + c0;
+  __shared__ int64_t own[4];                                // the gate and the CTAs with its rows (64-bit divisions: by one thread)
   int64_t b0 = 0, b1 = p.ctas, second = p.ctas;
   float* out;
   const float* part;
@@ -749,20 +750,25 @@ block_norm_grad_sums_kernel(const GradP p) {
   if (y == 0) { out = p.dw_pre; part = p.part + (int64_t)part_pre(p) * p.ctas * p.d; }
   else if (y == 1) { out = p.dw_post; part = p.part + (int64_t)part_post(p) * p.ctas * p.d; }
   else {
-    int64_t gate = y - 2;
-    if (p.gates_used > p.ctas) {
-      const int64_t first = rows_lo(y - 1, p.rows, p.ctas);
-      gate = first / p.per_gate;
-      if (first == gate * p.per_gate || rows_owner(gate * p.per_gate, p.rows, p.ctas) != y - 2) return;
+    if (threadIdx.x == 0) {
+      int64_t gate = y - 2, first = p.ctas;
+      bool none = false;
+      if (p.gates_used > p.ctas) {
+        const int64_t row = rows_lo(y - 1, p.rows, p.ctas);
+        gate = row / p.per_gate;
+        none = row == gate * p.per_gate || rows_owner(gate * p.per_gate, p.rows, p.ctas) != y - 2;
+      }
+      const int64_t g0 = gate * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
+      const int64_t lo = rows_owner(g0, p.rows, p.ctas), hi = rows_owner(g1 - 1, p.rows, p.ctas) + 1;
+      // a gate that is not its first CTA's first lies in that CTA's second sum; it is the others' first
+      if (rows_lo(lo, p.rows, p.ctas) / p.per_gate != gate) first = lo;
+      own[0] = gate; own[1] = lo; own[2] = none ? lo + 1 : hi; own[3] = first;
     }
-    out = p.dgate + gate * p.d;
-    part = p.part + (int64_t)part_gate(p) * p.ctas * p.d;
-    const int64_t g0 = gate * p.per_gate, g1 = g0 + p.per_gate < p.rows ? g0 + p.per_gate : p.rows;
-    b0 = rows_owner(g0, p.rows, p.ctas);
-    b1 = rows_owner(g1 - 1, p.rows, p.ctas) + 1;
+    __syncthreads();
+    b0 = own[1]; b1 = own[2]; second = own[3];
     if (b1 == b0 + 1) return;                               // the CTA has written it
-    // a gate that is not its first CTA's first lies in that CTA's second sum; it is the others' first
-    if (rows_lo(b0, p.rows, p.ctas) / p.per_gate != gate) second = b0;
+    out = p.dgate + own[0] * p.d;
+    part = p.part + (int64_t)part_gate(p) * p.ctas * p.d;
   }
   if (!out) return;
   double t[VEC] = {};
@@ -792,15 +798,15 @@ block_norm_grad_sums_kernel(const GradP p) {
 
 // Ring and CTAs an SM for rows of d elements in arrays of these element sizes (0: not read), `kept` bytes of shared memory beside them an
 // element, rows in use besides those on their way `held`.  The variants by the threads of a CTA and the registers that leaves each: 512 with
-// one chunk of eight elements up to 4,096 (128 registers), 352 with two or three (168), and where `wide` 512 with two up to 8,192.  False:
+// one chunk of eight elements up to 4,096 (128 registers), 352 with two or three up to 8,448 (168), and where `wide` 512 with up to four.  False:
 // too long.
 constexpr size_t RING_SMEM = 224 * 1024 + 256;
 struct Plan { Ring ring; int ctas, chunks, threads; size_t smem; };
 bool plan_ring(int64_t d, bool al, size_t e0, size_t e1, size_t e2, size_t e3, size_t kept, int held, bool wide, Plan& pl) {
   Ring& r = pl.ring;
   const size_t es[4] = {e0, e1, e2, e3};
-  if (d > (wide ? 8192 : 8448)) return false;
-  pl.chunks = d <= 4096 ? 1 : (wide || d <= 5632 ? 2 : 3);
+  if (!wide && d > 8448) return false;
+  pl.chunks = wide ? (int)((d + 4095) / 4096) : (d <= 4096 ? 1 : (d <= 5632 ? 2 : 3));
   pl.threads = (int)(((d + 7) / 8 + pl.chunks - 1) / pl.chunks + 31) / 32 * 32;
   size_t stage = 0;
   r.arrays = 0;
@@ -851,9 +857,16 @@ armor_status launch_norm(armor_ctx* c, const NormP& p, int64_t rows, cudaStream_
   const int64_t units = (p.d + 7) / 8;
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
   Plan pl;
-  if (rows > 2 * c->n_sm && plan_ring(p.d, ALIGNED, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 1, true, pl)) {
+  // The ring, or a CTA a row with the row in registers where there are few rows: 400 x 9,216 bf16 10.0 and 8.1 us, 2,000 x 14,336 49 and 60; rows
+  // that start anywhere, 2,000 x 9,001 62 and 107, 3,068 x 10,332 with an fp32 stream 110 and 242.
+  if (rows > (ALIGNED && p.d > 8192 ? 4 : 2) * c->n_sm && plan_ring(p.d, ALIGNED, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 1, true, pl)) {
     const int64_t ctas = (int64_t)pl.ctas * c->n_sm < rows ? (int64_t)pl.ctas * c->n_sm : rows;
-    return pl.chunks == 1 ? run_norm_ring<TS, TB, 1, 512, ALIGNED>(c, ctas, pl, p, s) : run_norm_ring<TS, TB, 2, 512, ALIGNED>(c, ctas, pl, p, s);
+    switch (pl.chunks) {
+      case 1: return run_norm_ring<TS, TB, 1, 512, ALIGNED>(c, ctas, pl, p, s);
+      case 2: return run_norm_ring<TS, TB, 2, 512, ALIGNED>(c, ctas, pl, p, s);
+      case 3: return run_norm_ring<TS, TB, 3, 512, ALIGNED>(c, ctas, pl, p, s);
+      default: return run_norm_ring<TS, TB, 4, 512, ALIGNED>(c, ctas, pl, p, s);
+    }
   }
   const dim3 grid((unsigned)rows);
   if (units <= 128 || (rows <= 148 && units <= 1024)) launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 1>, grid, threads(1), 0, s, p);
