@@ -142,21 +142,17 @@ __device__ __forceinline__ void round_rows(const I8P& p, uint32_t tiles, float* 
     auto load = [&](int64_t e) { return p.x_aligned ? rows::row_load<true>(x, e, p.K) : rows::row_load<false>(x, e, p.K); };
     unsigned top = 0;
 #pragma unroll 4
-    for (int64_t e = id * 8; e < p.K; e += 128 * 8) {
-      float v[8];
-      rows::raw_get(load(e), v);
-      top = max(top, rows::abs_bits8(v));
-    }
+    for (int64_t e = id * 8; e < p.K; e += 128 * 8) top = max(top, rows::raw_top(load(e)));
     top = __reduce_max_sync(0xffffffffu, top);
     if (lane == 0) red[warp] = top;
     asm volatile("bar.sync 1, 128;" ::: "memory");
-    const rows::RowScale r = rows::row_scale(max(max(red[0], red[1]), max(red[2], red[3])));
+    const rows::RowScale r = rows::row_scale<sizeof(X) == 2>(max(max(red[0], red[1]), max(red[2], red[3])));
     asm volatile("bar.sync 1, 128;" ::: "memory");          // (red is read before the next row writes it)
     if (id == 0) scale[t] = r.s;
     for (int64_t e = from + id * 8; e < to; e += 128 * 8) {
       float v[8];
       rows::raw_get(load(e), v);
-      const uint2 q = rows::row_round8(v, r);
+      const uint2 q = rows::row_round8<sizeof(X) == 2>(v, r);
       const uint32_t k = (uint32_t)(e - from), b = k & 127u;
       const uint32_t at = tiles + (k >> 7) * (BN * 128) + (uint32_t)t * 128 + ((((b >> 4) ^ ((uint32_t)t & 7u))) << 4) + (b & 8u);
       asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(q.x), "r"(q.y) : "memory");

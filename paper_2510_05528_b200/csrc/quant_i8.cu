@@ -24,19 +24,15 @@ quantize_rows_kernel(const T* x, int64_t ldx, int64_t cols, int8_t* __restrict__
     raw[c] = e < cols ? row_load<ALIGNED>(xr, e, cols) : raw_zero<T>();
   }
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
-    float v[8];
-    raw_get(raw[c], v);
-    top = max(top, abs_bits8(v));
-  }
-  const RowScale r = row_scale(cta_max(top, red));
+  for (int c = 0; c < CHUNKS; ++c) top = max(top, raw_top(raw[c]));
+  const RowScale r = row_scale<sizeof(T) == 2>(cta_max(top, red));
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int64_t e = ((int64_t)c * blockDim.x + threadIdx.x) * 8;
     if (e < cols) {
       float v[8];
       raw_get(raw[c], v);
-      *reinterpret_cast<uint2*>(q + row * ldq + e) = row_round8(v, r);     // (a row of q has room for the eight: ldq is a multiple of 16)
+      *reinterpret_cast<uint2*>(q + row * ldq + e) = row_round8<sizeof(T) == 2>(v, r);     // (a row of q has room for the eight: ldq is a multiple of 16)
     }
   }
   if (threadIdx.x == 0) scale[row] = r.s;
@@ -51,16 +47,12 @@ quantize_long_rows_kernel(const T* x, int64_t ldx, int64_t cols, int8_t* __restr
   const int64_t row = blockIdx.x;
   const T* const xr = x + row * ldx;
   unsigned top = 0;
+  for (int64_t e = threadIdx.x * 8; e < cols; e += 8 * blockDim.x) top = max(top, raw_top(row_load<ALIGNED>(xr, e, cols)));
+  const RowScale r = row_scale<sizeof(T) == 2>(cta_max(top, red));
   for (int64_t e = threadIdx.x * 8; e < cols; e += 8 * blockDim.x) {
     float v[8];
     raw_get(row_load<ALIGNED>(xr, e, cols), v);
-    top = max(top, abs_bits8(v));
-  }
-  const RowScale r = row_scale(cta_max(top, red));
-  for (int64_t e = threadIdx.x * 8; e < cols; e += 8 * blockDim.x) {
-    float v[8];
-    raw_get(row_load<ALIGNED>(xr, e, cols), v);
-    *reinterpret_cast<uint2*>(q + row * ldq + e) = row_round8(v, r);
+    *reinterpret_cast<uint2*>(q + row * ldq + e) = row_round8<sizeof(T) == 2>(v, r);
   }
   if (threadIdx.x == 0) scale[row] = r.s;
 }

@@ -195,10 +195,17 @@ struct RowScale {
   float pre;             // a power of two that brings the row into the middle of the exponent range; 0: the row's integers are zeros
   float inv, top;        // 127 / (a pre), a pre
   float s;               // the scale
-  float edge;            // distance from an integer beyond which an element is looked at closely; -1: all are (pre is not 1)
+  float edge;            // distance from an integer beyond which an element is looked at closely; -1: all are (pre is not 1); 2: none is
 };
 // top_bits: the largest |x| as bits; at least those of infinity: the row holds a NaN or an infinity.  Such a row gets NaN as its
 // scale, so that what is made of it is NaN, and zeros; a row of zeros gets 0.
+//
+// SHORT: a row of bf16 or fp16, whose significands are whole numbers X, A below 2^11.  With s the difference of the exponents, 127 x / a is off from a
+// half by |254 X - (2k + 1) A 2^s| / (2 A 2^s), so it is a half or further from it than 1 / (2 A 2^s), which is 16 times the error of x
+// times an inverse that is a rounding off (127 X / (A 2^s) x 2^-23).  A half needs 127 to divide (2k + 1) A: unless it divides A, only x = a / 2 is
+// one, 63.5 steps, which an inverse rounded up brings to the even 64.  So nothing is looked at closely (of bf16 rows one element in
+// a thousand is half of the largest, and the whole warp waits for its comparison: 4,096 x 8,192 bf16 33.0 us, so 25.5).
+template <bool SHORT = false>
 __device__ __forceinline__ RowScale row_scale(unsigned top_bits) {
   RowScale r;
   const float a = __uint_as_float(top_bits);
@@ -209,6 +216,10 @@ __device__ __forceinline__ RowScale row_scale(unsigned top_bits) {
   r.inv = __fdiv_rn(127.f, r.top);
   r.s = __fdiv_rn(a, 127.f);
   r.edge = r.pre == 1.f ? 0.49998f : -1.f;
+  if (SHORT && r.pre == 1.f && ((top_bits & 0x7fffffu) | 0x800000u) % 127u != 0u) {
+    r.inv = __fdiv_ru(127.f, r.top);
+    r.edge = 2.f;
+  }
   return r;
 }
 static __device__ __noinline__ int row_round(float x, float pre, float inv, float top) {
@@ -220,31 +231,69 @@ static __device__ __noinline__ int row_round(float x, float pre, float inv, floa
   return d > 0.0 ? f + 1 : (d < 0.0 ? f : f + (f & 1));
 }
 __device__ __forceinline__ int row_round(float x, const RowScale& r) { return row_round(x, r.pre, r.inv, r.top); }
-__device__ __forceinline__ uint32_t row_round4(const float* v, const RowScale& r) {
-  constexpr float M = 12582912.f;                           // 1.5 x 2^23: its neighbours are whole numbers
-  uint32_t b[4];
+// N elements (four or eight), two at a time.  SHORT: row_scale's.
+template <int N, bool SHORT>
+__device__ __forceinline__ void row_round_n(const float* v, const RowScale& r, uint32_t (&w)[N / 4]) {
+  const F2 M = f2(12582912.f), inv = f2(r.inv), minus = f2(-1.f);            // 1.5 x 2^23: its neighbours are whole numbers
+  float2 b[N / 2];
   float far = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float sum = fmaf(v[i], r.inv, M), k = sum - M;
-    far = fmaxf(far, fabsf(fmaf(v[i], r.inv, -k)));
-    b[i] = __float_as_uint(sum);
+  for (int i = 0; i < N / 2; ++i) {
+    const F2 x = f2(v[2 * i], v[2 * i + 1]), sum = f2_fma(x, inv, M);
+    b[i] = f2_get(sum);
+    if (SHORT && r.edge > 1.f) continue;
+    const float2 off = f2_get(f2_fma(x, inv, f2_fma(sum, minus, M)));        // (M - sum is exact)
+    far = fmaxf(far, fmaxf(fabsf(off.x), fabsf(off.y)));
   }
-  uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-  if (far > r.edge) {
-    w = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)(row_round(v[i], r) & 255) << (8 * i);
+  for (int k = 0; k < N / 4; ++k)
+    w[k] = __byte_perm(__byte_perm(__float_as_uint(b[2 * k].x), __float_as_uint(b[2 * k].y), 0x0040),
+                       __byte_perm(__float_as_uint(b[2 * k + 1].x), __float_as_uint(b[2 * k + 1].y), 0x0040), 0x5410);
+  if (far > r.edge) {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) {
+      w[k] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[k] |= (uint32_t)(row_round(v[4 * k + i], r) & 255) << (8 * i);
+    }
   }
-  return w;
 }
-__device__ __forceinline__ uint2 row_round8(const float (&v)[8], const RowScale& r) { return make_uint2(row_round4(v, r), row_round4(v + 4, r)); }
+__device__ __forceinline__ uint32_t row_round4(const float* v, const RowScale& r) {
+  uint32_t w[1];
+  row_round_n<4, false>(v, r, w);
+  return w[0];
+}
+template <bool SHORT = false>
+__device__ __forceinline__ uint2 row_round8(const float (&v)[8], const RowScale& r) {
+  uint32_t w[2];
+  row_round_n<8, SHORT>(v, r, w);
+  return make_uint2(w[0], w[1]);
+}
 // the bits of max |v|: of floats without their sign, NaN above infinity above all others
 __device__ __forceinline__ unsigned abs_bits8(const float (&v)[8]) {
   unsigned m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
   return m;
+}
+
+// The same of a chunk as it lies.  16-bit values without their signs stand in the order of their bits, NaN above infinity: two at a time.
+template <typename T>
+__device__ __forceinline__ unsigned raw_top(const Raw8<T>& r) {
+  auto most = [](uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+  };
+  constexpr uint32_t ABS = 0x7fff7fffu;
+  const uint32_t m = most(most(r.w.x & ABS, r.w.y & ABS), most(r.w.z & ABS, r.w.w & ABS));
+  const float2 f = unpack2(static_cast<const T*>(nullptr), max(m & 0xffffu, m >> 16));
+  return __float_as_uint(f.x);
+}
+__device__ __forceinline__ unsigned raw_top(const Raw8<float>& r) {
+  float v[8];
+  raw_get(r, v);
+  return abs_bits8(v);
 }
 
 inline bool aligned16(const void* p, int64_t ld, int esize) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * esize % 16 == 0; }

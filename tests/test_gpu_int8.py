@@ -81,6 +81,28 @@ def test_ties_and_their_neighbours(ctx):
     assert q.min() == -127 and q.max() == 127
 
 
+@pytest.mark.parametrize("dtype,bits", [(BF16, 7), (F16, 10)])
+def test_every_quotient_of_16_bit_rows(ctx, dtype, bits):
+    """Every significand as a row's largest, against every number of ten binades below it, of either sign."""
+    m = 2 ** bits
+    a = torch.arange(m, 2 * m, device=DEV, dtype=torch.float64)
+    below = torch.cat([a * 2.0 ** -s for s in range(10)])
+    x = torch.where(below[None] <= a[:, None], below[None], 0.0)
+    x = torch.cat([x, -x], 1).to(dtype)
+    assert torch.equal(x.double().abs().amax(1), a)
+    q, s = ctx.quantize_rows(x)
+    rq, rs = quantized(x)
+    assert torch.equal(q, rq) and torch.equal(s, rs)
+    # the rows one by one through a product of ones, whose sums they are
+    wq = torch.ones(1, 256, dtype=torch.int8, device=DEV)
+    for r in range(0, m, 7):
+        cols = x[r:r + 1, r * 8 % (x.shape[1] - 256):][:, :255]
+        row = torch.cat([x[r:r + 1, r:r + 1], cols], 1).contiguous()
+        y = ctx.linear_i8(row, wq, torch.ones(1, device=DEV), out_dtype=F32)
+        rq, rs = quantized(row)
+        assert torch.equal(y, rq.float().sum(1, keepdim=True) * rs)
+
+
 def test_rows_of_extreme_values(ctx):
     inf, nan = float("inf"), float("nan")
     tiny, big = 2.0 ** -149, 3.4e38
