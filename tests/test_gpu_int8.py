@@ -154,6 +154,16 @@ def test_sums_are_exact(ctx, n, n_out, n_in):
     assert torch.equal(y, want.float())
 
 
+@pytest.mark.parametrize("n", [40, 90, 120, 129, 150, 190, 320, 380, 700, 1024])
+@pytest.mark.parametrize("n_out,n_in", [(8192, 2048), (14300, 1000), (4096, 5000), (256, 8200)])
+def test_sums_of_every_width_of_tile(ctx, n, n_out, n_in):
+    g = gen(n + n_out)
+    xq, wq = int8_rows(n, n_in, g), int8_rows(n_out, n_in, g, -128)
+    one = torch.ones(max(n, n_out), device=DEV)
+    y = ctx.linear_i8(xq, wq, one[:n_out], x_scale=one[:n], out_dtype=F32)
+    assert torch.equal(y, whole(xq, wq).float())
+
+
 def test_sums_of_the_largest_products(ctx):
     """-128 x -128 over the longest contraction, and sums beyond 2^24: exact in int32, rounded once to fp32."""
     n_in = 131071
@@ -299,6 +309,12 @@ def test_core_and_positions_are_exact(d_out, d_in, db, n):
     y = c.apply_layer_i8(c.pack_layer_i8(st), x.to(BF16))
     assert torch.equal(y, (x.double() @ st.S.double().t()).to(BF16))
     assert c.device_status()[:5] == [0, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("n", [40, 90, 120, 250, 500, 1000])
+@pytest.mark.parametrize("d_out,d_in", [(8192, 1024), (4096, 2048), (14336, 512)])
+def test_core_of_many_rows_is_exact(d_out, d_in, n):
+    test_core_and_positions_are_exact(d_out, d_in, 128, n)
 
 
 @pytest.mark.parametrize("d_out,d_in,db", SHAPES)
