@@ -252,6 +252,7 @@ struct Share {
     });
   }
 };
+// (AL: rows on 16-byte boundaries of whole units.  A unit that ends behind its row would take what lies there into the sums and write it.)
 template <typename TS, typename TB, int CHUNKS, bool AL>
 struct ShareOf {
   static constexpr int U = !AL ? 2 : (sizeof(TS) == 4 || sizeof(TB) == 4 ? 4 : 8);
@@ -852,21 +853,38 @@ armor_status run_grad_ring(armor_ctx* c, int64_t ctas, const Plan& pl, const Gra
              : run_ring(c, block_norm_grad_ring_kernel<TS, TB, CHUNKS, THREADS, false, AL>, without, ctas, pl, p, s);
 }
 
+// Rows that the ring's aligned variant takes: no unit of theirs reaches behind their end.  Others on 16-byte boundaries (1,001 columns of
+// rows 1,008 apart) go to the variant for rows that start anywhere.
+template <typename TS, typename TB>
+bool whole_units(int64_t d) { return d % ShareOf<TS, TB, 1, true>::U == 0; }
+
+template <typename TS, typename TB, bool AL>
+armor_status launch_norm_ring(armor_ctx* c, int64_t ctas, const Plan& pl, const NormP& p, cudaStream_t s) {
+  switch (pl.chunks) {
+    case 1: return run_norm_ring<TS, TB, 1, 512, AL>(c, ctas, pl, p, s);
+    case 2: return run_norm_ring<TS, TB, 2, 512, AL>(c, ctas, pl, p, s);
+    case 3: return run_norm_ring<TS, TB, 3, 512, AL>(c, ctas, pl, p, s);
+    default: return run_norm_ring<TS, TB, 4, 512, AL>(c, ctas, pl, p, s);
+  }
+}
+template <typename TS, typename TB, bool AL>
+armor_status launch_grad_ring(armor_ctx* c, int64_t ctas, const Plan& pl, const GradP& p, cudaStream_t s) {
+  if (pl.chunks == 1) return run_grad_ring<TS, TB, 1, 512, AL>(c, ctas, pl, p, s);
+  return pl.chunks == 2 ? run_grad_ring<TS, TB, 2, 352, AL>(c, ctas, pl, p, s) : run_grad_ring<TS, TB, 3, 352, AL>(c, ctas, pl, p, s);
+}
+
 template <typename TS, typename TB, bool ALIGNED>
 armor_status launch_norm(armor_ctx* c, const NormP& p, int64_t rows, cudaStream_t s) {
   const int64_t units = (p.d + 7) / 8;
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
+  const bool al = ALIGNED && whole_units<TS, TB>(p.d);
   Plan pl;
   // The ring, or a CTA a row with the row in registers where there are few rows: 400 x 9,216 bf16 10.0 and 8.1 us, 2,000 x 14,336 49 and 60; rows
   // that start anywhere, 2,000 x 9,001 62 and 107, 3,068 x 10,332 with an fp32 stream 110 and 242.
-  if (rows > (ALIGNED && p.d > 8192 ? 4 : 2) * c->n_sm && plan_ring(p.d, ALIGNED, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 1, true, pl)) {
+  if (rows > (ALIGNED && p.d > 8192 ? 4 : 2) * c->n_sm && plan_ring(p.d, al, sizeof(TS), p.y ? sizeof(TB) : 0, 0, 0, 0, 1, true, pl)) {
     const int64_t ctas = (int64_t)pl.ctas * c->n_sm < rows ? (int64_t)pl.ctas * c->n_sm : rows;
-    switch (pl.chunks) {
-      case 1: return run_norm_ring<TS, TB, 1, 512, ALIGNED>(c, ctas, pl, p, s);
-      case 2: return run_norm_ring<TS, TB, 2, 512, ALIGNED>(c, ctas, pl, p, s);
-      case 3: return run_norm_ring<TS, TB, 3, 512, ALIGNED>(c, ctas, pl, p, s);
-      default: return run_norm_ring<TS, TB, 4, 512, ALIGNED>(c, ctas, pl, p, s);
-    }
+    if constexpr (ALIGNED) if (al) return launch_norm_ring<TS, TB, true>(c, ctas, pl, p, s);
+    return launch_norm_ring<TS, TB, false>(c, ctas, pl, p, s);
   }
   const dim3 grid((unsigned)rows);
   if (units <= 128 || (rows <= 148 && units <= 1024)) launch_dependent(block_norm_kernel<TS, TB, ALIGNED, 1>, grid, threads(1), 0, s, p);
@@ -879,9 +897,10 @@ armor_status launch_grad(armor_ctx* c, GradP p, cudaStream_t s) {
   const int64_t units = (p.d + 7) / 8;
   const int n_sums = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 1 : 0);
   auto threads = [&](int chunks) { return dim3((unsigned)(((units + chunks - 1) / chunks + 31) / 32 * 32)); };
+  const bool al = ALIGNED && whole_units<TS, TB>(p.d);
   Plan pl;
   const size_t kept = (p.dw_post ? 4 : 0) + (p.h && p.dh && p.dn ? 0 : sizeof(TS) + (sizeof(TB) != sizeof(TS) ? sizeof(TB) : 0));
-  const bool use_ring = plan_ring(p.d, ALIGNED, p.h ? sizeof(TS) : 0, p.y ? sizeof(TB) : 0, p.dh ? sizeof(TS) : 0, p.dn ? sizeof(TB) : 0, kept, p.d <= 4096 ? 0 : 1, false, pl);
+  const bool use_ring = plan_ring(p.d, al, p.h ? sizeof(TS) : 0, p.y ? sizeof(TB) : 0, p.dh ? sizeof(TS) : 0, p.dn ? sizeof(TB) : 0, kept, p.d <= 4096 ? 0 : 1, false, pl);
   // CTAs as many as an SM runs, fewer where the workspace has no room for their sums
   const int64_t parts = (p.dw_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.dgate ? 2 : 0);
   int64_t n = use_ring ? (int64_t)pl.ctas * c->n_sm : 2 * c->n_sm;
@@ -890,8 +909,9 @@ armor_status launch_grad(armor_ctx* c, GradP p, cudaStream_t s) {
   if (n < 1) return ARMOR_ERR_WORKSPACE;
   p.ctas = (int)n;
   if (use_ring) {
-    const armor_status st = pl.chunks == 1 ? run_grad_ring<TS, TB, 1, 512, ALIGNED>(c, n, pl, p, s)
-                          : pl.chunks == 2 ? run_grad_ring<TS, TB, 2, 352, ALIGNED>(c, n, pl, p, s) : run_grad_ring<TS, TB, 3, 352, ALIGNED>(c, n, pl, p, s);
+    armor_status st;
+    if constexpr (ALIGNED) st = al ? launch_grad_ring<TS, TB, true>(c, n, pl, p, s) : launch_grad_ring<TS, TB, false>(c, n, pl, p, s);
+    else st = launch_grad_ring<TS, TB, false>(c, n, pl, p, s);
     if (st != ARMOR_OK) return st;
   } else if (units <= 1024) {
     static PerDeviceOnce attr;
