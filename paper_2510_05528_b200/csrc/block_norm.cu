@@ -570,6 +570,7 @@ block_norm_grad_kernel(const GradP p) {
 // so that all six sums of a row are formed at once.  And one running sum serves both the gate and w_post: t = sum dh' ybar over the rows of a
 // gate gives dgate = w_post t, and gate t is what these rows add to dw_post.
 //
+// HAS_Y: y is read.  Without it there is no norm of it and no gradient of the gate; a gate may still stand between dh' and dy.
 // KEEP: a thread's share of the four arrays stays in registers between the sums and the gradients; else it is read (and widened) again.
 template <typename TS, typename TB, int CHUNKS, int THREADS, bool HAS_Y, bool AL>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -615,7 +616,9 @@ block_norm_grad_ring_kernel(const GradP p, const Ring ring, int32_t* status) {
   if (p.w_pre) my.each([&](int c, uint32_t e) { my.get(p.w_pre, e, wpre[c]); });
   const int64_t g_first = p.gate ? r_lo / p.per_gate : 0;
   int64_t at = g_first, until = p.gate ? (at + 1) * p.per_gate : p.rows;
-  if (HAS_Y) my.gain(p.w_post, p.gate ? p.gate + at * p.ldg : nullptr, G);
+  // (dy = gate (.) dh' needs no y)
+  const bool gated = HAS_Y || (p.gate && p.dy);
+  if (gated) my.gain(p.w_post, p.gate ? p.gate + at * p.ldg : nullptr, G);
   if (HAS_Y && p.dw_post) my.each([&](int, uint32_t e) {
     F2 z[U / 2];
 #pragma unroll
@@ -656,7 +659,7 @@ block_norm_grad_ring_kernel(const GradP p, const Ring ring, int32_t* status) {
     const TB* const y = in_stage(mem + ring.off[1], y0, row, p.ldy, AL);
     const TS* const dh = p.dh ? in_stage(mem + ring.off[2], dh0, row, p.lddh, AL) : reinterpret_cast<const TS*>(zeros);
     const TB* const dn = p.dn ? in_stage(mem + ring.off[3], dn0, row, p.lddn, AL) : reinterpret_cast<const TB*>(zeros_b);
-    if (HAS_Y && row == until) { my.gain(p.w_post, p.gate + ++at * p.ldg, G); until += p.per_gate; }
+    if (gated && row == until) { my.gain(p.w_post, p.gate + ++at * p.ldg, G); until += p.per_gate; }
     tc::mbar_wait(full0 + 8 * here, phase, abortp, status);
     if (++stage == ring.stages) { stage = 0; phase ^= 1; }
     F2 hv[KEEP ? NU : 1][U / 2], nv[KEEP ? NU : 1][U / 2], yv[KEEP ? NU : 1][U / 2], dv[KEEP ? NU : 1][U / 2];
@@ -719,6 +722,9 @@ block_norm_grad_ring_kernel(const GradP p, const Ring ring, int32_t* status) {
       if (HAS_Y) {
 #pragma unroll
         for (int i = 0; i < U / 2; ++i) dv[k][i] = f2_fma(yv[k][i], c1, f2_mul(f2_mul(G[c][i], dv[k][i]), r12));
+      } else {
+#pragma unroll
+        for (int i = 0; i < U / 2; ++i) dv[k][i] = f2_mul(G[c][i], dv[k][i]);
       }
       if (p.dy) my.put(static_cast<TB*>(p.dy) + row * p.lddy, e, dv[k]);
     });
