@@ -257,7 +257,7 @@ armor_status armor_linear_i8(armor_ctx* ctx, const void* d_x, int32_t x_dtype, i
  * armor_quantize_rows has it, over what the row keeps), 0.625 bytes for an entry of S where the bf16 core has 1.125; the wrappers are
  * bf16 as there.  armor_apply_layer_i8: bf16 x [n_tokens, d_in] -> bf16 y [n_tokens, d_out] (both 16-byte aligned):
  *   z1 = (r1 . x) B^T, rounded from fp32 to int8 with a scale for each token; z2 = z1 S^T on the sparse tensor cores, exact int32
- *   sums, scaled and rounded to bf16; y = r2 . (z2 A^T).
+ *   sums, scaled in fp32; y = r2 . (z2 A^T) with z2 as the sum of two bf16 numbers, 15 bits or more of it.
  * Same shapes and errors as armor_pack_layer and armor_apply_layer; a group of d_M with more than two kept positions raises
  * device status word 4 and contributes its first two. */
 armor_status armor_packed_layer_i8_bytes(const armor_config* cfg, size_t* out_bytes);

@@ -1079,11 +1079,11 @@ armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void
   char* const scratch = reinterpret_cast<char*>(c->T);
   auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
   // The few-token wrapper kernels and a kernel that rounds the fp32 z1, four launches, against a memset and four persistent kernels, 22 us
-  // whatever their tokens.  By the wrapper products' size: 4096 x 4096, 768 tokens 34.6 and 35.5 us, 1,024 46.3 and 42.1; 14336 x 4096, 300 40.1
-  // and 41.1, 400 48.8 and 43.3; 8192 x 8192 in blocks of 256, 130 33.6 and 37.4, 200 40.9 and 38.9; 1024 x 1024, 300 12.6 and 22.7.
+  // whatever their tokens.  By the wrapper products' size: 4096 x 4096, 768 tokens 37.3 and 40.3 us, 1,024 48.5 and 45.8; 14336 x 4096, 300 43.3
+  // and 45.9, 400 52.0 and 51.4; 8192 x 8192 in blocks of 256, 160 39.0 and 40.8, 200 43.4 and 41.9; 1024 x 1024, 300 14.1 and 22.8.
   const bool few = n_tokens <= ARMOR_SMALL_TOKENS || (n_tokens * (d_in + d_out) * c->db <= 800000000 && n_tokens * (5 * d_in + 4 * d_out) <= 39 * c->wn);
   if (few) {
-    // z1 and z2 in fp32 (z2 is rounded to bf16 by the product with A): 5 d_in n + 4 d_out n of the workspace's 40 d_in d_out bytes
+    // z1 and z2 in fp32 (the product with A takes z2 as two bf16 numbers): 5 d_in n + 4 d_out n of the workspace's 40 d_in d_out bytes
     float* const z1 = reinterpret_cast<float*>(scratch);
     int8_t* const zq = reinterpret_cast<int8_t*>(scratch + up(4 * n_tokens * d_in));
     float* const zs = reinterpret_cast<float*>(zq + up(n_tokens * d_in));
@@ -1094,12 +1094,13 @@ armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void
       st = launch_quantize_rows(c, z1, ARMOR_DTYPE_F32, d_in, n_tokens, d_in, zq, d_in, zs, s);
       if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_F32, n_tokens, true, s);
     }
-    if (st == ARMOR_OK) st = launch_fwd_small(c, z2, 1, buf + l.a, d_y, n_tokens, d_out, s);
+    if (st == ARMOR_OK) st = launch_fwd_small(c, z2, 1, buf + l.a, d_y, n_tokens, d_out, s, false, true);
     return st == ARMOR_OK ? finish_call(c) : st;
   }
-  // a chunk: int8 z1 [chunk, d_in], its maxima and scales, bf16 z2 [chunk, d_out], 24 of the workspace's 40 bytes an entry of S at most
-  const int64_t least = d_out < d_in ? d_out : d_in;
-  const int64_t chunk = 8 * least < n_tokens ? 8 * least : n_tokens;
+  // Chunks of even size: int8 z1 [chunk, d_in], its maxima and scales, z2 as two bf16 arrays [chunk, d_out], 35 of the workspace's 40 bytes an
+  // entry of S at most.  (z2 in one bf16 number adds an error as large as the rounding of y: 2.3e-3 of y's norm against 1.66e-3.  It takes
+  // less time: 28672 x 8192, 4,096 tokens 594 us, so 688, 470 MB more; 4096 x 4096, 4,096 tokens 88 and 101; one token 9.8 and 10.2.)
+  const int64_t most = 7 * (d_out < d_in ? d_out : d_in), chunks = (n_tokens + most - 1) / most, chunk = (n_tokens + chunks - 1) / chunks;
   int8_t* const zq = reinterpret_cast<int8_t*>(scratch);
   unsigned* const top = reinterpret_cast<unsigned*>(scratch + up(chunk * d_in));
   float* const zs = reinterpret_cast<float*>(reinterpret_cast<char*>(top) + up(4 * chunk));
@@ -1111,8 +1112,8 @@ armor_status armor_apply_layer_i8(armor_ctx* c, const void* d_packed, const void
     ARMOR_CUDA_OK(cudaMemsetAsync(top, 0, (size_t)n * 4, s));
     armor_status st = launch_fwd_block_top(c, xc, buf + l.b, top, n, d_in, s);
     if (st == ARMOR_OK) st = launch_fwd_block_i8(c, xc, buf + l.b, top, zq, zs, n, d_in, s);
-    if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, ARMOR_DTYPE_BF16, n, false, s);
-    if (st == ARMOR_OK) st = launch_fwd_block(c, z2, buf + l.a, yc, n, d_out, s);
+    if (st == ARMOR_OK) st = launch_core_i8(c, zq, zs, core, buf + l.e, core_scale, z2, OUT_TWO_BF16, n, false, s);
+    if (st == ARMOR_OK) st = launch_fwd_block_two(c, z2, buf + l.a, yc, n, d_out, s);
     if (st != ARMOR_OK) return st;
   }
   return finish_call(c);

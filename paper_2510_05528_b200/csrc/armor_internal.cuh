@@ -510,6 +510,8 @@ void launch_pack_blocks(armor_ctx* c, const float* P, const float* rowscale, con
                         cudaStream_t s);
 armor_status launch_fwd_block(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d,
                               cudaStream_t s);
+// X as two bf16 arrays, one behind the other, whose sum it is (OUT_TWO_BF16)
+armor_status launch_fwd_block_two(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d, cudaStream_t s);
 // The same product rounded to int8 rows with a scale each, in two passes: the rows' maxima (bits of |.|, added to what top holds), then
 // the values.  The product itself is in no memory.
 armor_status launch_fwd_block_top(armor_ctx* c, const void* X, const void* Q, unsigned* top, int64_t rows, int64_t d, cudaStream_t s);
@@ -519,13 +521,15 @@ armor_status launch_fwd_block_i8(armor_ctx* c, const void* X, const void* Q, con
 // run as latency-bound kernels whose contraction over d_in is split over the chip; the tiles of the persistent kernels fill it themselves.
 static const int64_t ARMOR_SMALL_TOKENS = 128;
 armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const void* Q, void* out, int64_t rows, int64_t d,
-                              cudaStream_t s, bool out_f32 = false);
+                              cudaStream_t s, bool out_f32 = false, bool two = false);
 armor_status launch_tc_sparse_small(armor_ctx* c, const void* Sc, const void* E, const void* z1_bf16, float* Zp, int64_t n,
                                     int* pieces, cudaStream_t s);
 
 // ---------------------------------------------------------------- 8-bit products (quant_i8.cu, i8_tcgen05.cu)
 // bytes of an element of an ARMOR_DTYPE_* that rows are given in; 0: none of them
 int rows_dtype_bytes(int32_t dtype);
+// a product's output as two bf16 arrays [n][ldy], the second behind the first, that hold 15 bits of it or more between them (split2)
+static const int32_t OUT_TWO_BF16 = 64;
 armor_status launch_quantize_rows(armor_ctx* c, const void* x, int32_t dtype, int64_t ldx, int64_t n, int64_t cols, int8_t* q,
                                   int64_t ldq, float* scale, cudaStream_t s);
 armor_status launch_linear_i8(armor_ctx* c, const int8_t* xq, int64_t ldx, const float* xs, const int8_t* wq, int64_t ldw, const float* ws,

@@ -74,7 +74,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int DB, int N, int OUT>
+// PARTS 2: X is the sum of two arrays, the second p.rows rows behind the first, both multiplied into the same sums.
+template <int DB, int N, int OUT, int PARTS>
 __global__ void __launch_bounds__(NTHREADS, 1)
 fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapC,
                  const FParams p) {
@@ -132,11 +133,12 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
           ++q_loads;
           cur = b;
         }
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int k = 0; k < PARTS * KT; ++k) {
+          const int kt = k % KT;
           if (!mbar_wait(empty0 + 8 * stage, phase ^ 1, abortp, p.status)) { ok = false; break; }
           const uint32_t fb = full0 + 8 * stage;
           mbar_expect_tx(fb, X_BYTES);
-          tma_load_2d(smem_u32(stage0 + (size_t)stage * X_BYTES), &mapX, b / (DB / N) * DB + kt * BKE, mt * BM, fb);
+          tma_load_2d(smem_u32(stage0 + (size_t)stage * X_BYTES), &mapX, b / (DB / N) * DB + kt * BKE, mt * BM + (k < KT ? 0 : (int)p.rows), fb);
           ++issued;
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
@@ -174,10 +176,10 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
         if (!mbar_wait(tempty0 + 8 * as, aphase ^ 1, abortp, p.status)) { ok = false; break; }
         tc_fence_after();
         const uint32_t tacc = tmem_base + (uint32_t)(as * N);
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int kt = 0; kt < PARTS * KT; ++kt) {
           if (!mbar_wait(full0 + 8 * stage, phase, abortp, p.status)) { ok = false; break; }
           tc_fence_after();
-          const uint64_t dx = dx0 + (uint64_t)(uint32_t)(stage * (X_BYTES >> 4)), dq = dq0 + (uint64_t)(uint32_t)(kt * (N * 128 >> 4));
+          const uint64_t dx = dx0 + (uint64_t)(uint32_t)(stage * (X_BYTES >> 4)), dq = dq0 + (uint64_t)(uint32_t)(kt % KT * (N * 128 >> 4));
 #pragma unroll
           for (int k = 0; k < BKE / 16; ++k) umma_bf16(tacc, dx + 2 * k, dq + 2 * k, idesc, (uint32_t)((kt > 0) | (k != 0)));
           umma_commit(empty0 + 8 * stage);
@@ -283,7 +285,8 @@ fwd_block_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant
 // consecutive k (16 bytes) of its rows as the operands of two instructions; the columns of the two n-tiles are dealt out so
 // that a lane ends with four neighbouring ones.
 // out32 non-null: the product is written there in fp32 instead.
-// SUM: the tokens come as `pieces` arrays of fp32 partial sums [rows][d], added in order and rounded to bf16 once.
+// SUM: the tokens come as `pieces` arrays of fp32 partial sums [rows][d], added in order and rounded to bf16 once; TWO: kept as two bf16
+// numbers each (split2), both multiplied.
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -291,12 +294,12 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int DB, bool SUM>
+template <int DB, bool SUM, bool TWO>
 __global__ void __launch_bounds__(256)
 fwd_small_kernel(const void* X, int pieces, const __nv_bfloat16* Q, __nv_bfloat16* __restrict__ out,
                  int rows, int64_t d, float* out32) {
   constexpr int LD = DB * 2 + 64;                     // bytes per staged token: eight lanes of a phase hit eight banks
-  __shared__ __align__(16) uint8_t tok[16 * LD];
+  __shared__ __align__(16) uint8_t tok[(TWO ? 2 : 1) * 16 * LD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t n0 = (int64_t)blockIdx.x * 128 + warp * 16;
   const int64_t kbase = (int64_t)blockIdx.x * 128 / DB * DB;   // first column of X of the block these columns belong to
@@ -315,7 +318,7 @@ fwd_small_kernel(const void* X, int pieces, const __nv_bfloat16* Q, __nv_bfloat1
 #pragma unroll
   for (int e = threadIdx.x; e < 16 * DB / 8; e += 256) {
     const int r = e / (DB / 8), c8 = e % (DB / 8);
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u), rest = v;
     if (r0 + r < rows) {
       const int64_t o = (int64_t)(r0 + r) * d + kbase + 8 * c8;
       if (SUM) {
@@ -328,19 +331,27 @@ fwd_small_kernel(const void* X, int pieces, const __nv_bfloat16* Q, __nv_bfloat1
           a.x += a2.x; a.y += a2.y; a.z += a2.z; a.w += a2.w;
           b.x += b2.x; b.y += b2.y; b.z += b2.z; b.w += b2.w;
         }
-        v = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+        if (TWO) {
+          rows::split2(a.x, a.y, v.x, rest.x); rows::split2(a.z, a.w, v.y, rest.y);
+          rows::split2(b.x, b.y, v.z, rest.z); rows::split2(b.z, b.w, v.w, rest.w);
+        } else {
+          v = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+        }
       } else {
         v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(X) + o);
       }
     }
     *reinterpret_cast<uint4*>(tok + r * LD + 16 * c8) = v;
+    if (TWO) *reinterpret_cast<uint4*>(tok + (16 + r) * LD + 16 * c8) = rest;
   }
   __syncthreads();
   float acc[2][4] = {};
 #pragma unroll
+  for (int part = 0; part < (TWO ? 2 : 1); ++part)
+#pragma unroll
   for (int ch = 0; ch < DB / 32; ++ch) {
-    const uint4 a0 = *reinterpret_cast<const uint4*>(tok + g * LD + ch * 64 + t * 16);
-    const uint4 a1 = *reinterpret_cast<const uint4*>(tok + (g + 8) * LD + ch * 64 + t * 16);
+    const uint4 a0 = *reinterpret_cast<const uint4*>(tok + (16 * part + g) * LD + ch * 64 + t * 16);
+    const uint4 a1 = *reinterpret_cast<const uint4*>(tok + (16 * part + g + 8) * LD + ch * 64 + t * 16);
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
       mma_bf16(acc[nt], a0.x, a1.x, a0.y, a1.y, w[nt][ch].x, w[nt][ch].y);
@@ -389,19 +400,19 @@ bool make_map_bf16(CUtensorMap* map, const void* base, int64_t rows, int64_t col
   return r == CUDA_SUCCESS;
 }
 
-template <int DB, int N, int OUT>
+template <int DB, int N, int OUT, int PARTS>
 armor_status launch_block(armor_ctx* c, const void* X, const void* Q, void* out, FParams p, int64_t rows, int64_t d, cudaStream_t s) {
   CUtensorMap mX, mQ, mC;
-  if (!make_map_bf16(&mX, X, rows, d, d, BM) || !make_map_bf16(&mQ, Q, d, DB, DB, N)) return ARMOR_ERR_CUDA;
+  if (!make_map_bf16(&mX, X, PARTS * rows, d, d, BM) || !make_map_bf16(&mQ, Q, d, DB, DB, N)) return ARMOR_ERR_CUDA;
   if (OUT != OUT_BF16) mC = mX;                      // (nothing is stored through it)
   else if (!make_map_bf16(&mC, out, rows, d, d, 32)) return ARMOR_ERR_CUDA;
   p.rows = rows; p.m_tiles = (int)((rows + BM - 1) / BM); p.n_groups = (int)(d / N);
   p.status = c->status;
   static PerDeviceOnce attr;
-  if (ensure_dynamic_smem(attr, c->device, fwd_block_kernel<DB, N, OUT>, Geo<DB, N>::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  if (ensure_dynamic_smem(attr, c->device, fwd_block_kernel<DB, N, OUT, PARTS>, Geo<DB, N>::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
   const int64_t tiles = (int64_t)p.m_tiles * p.n_groups;
-  KTimer kt(c, ARMOR_KC_FORWARD, (OUT == OUT_BF16 ? 4.0 : (OUT == OUT_TOP ? 2.0 : 3.0)) * (double)rows * (double)d, s);
-  launch_dependent(fwd_block_kernel<DB, N, OUT>, (unsigned)(tiles < c->n_sm ? tiles : c->n_sm), NTHREADS, Geo<DB, N>::SMEM, s, mX, mQ, mC, p);
+  KTimer kt(c, ARMOR_KC_FORWARD, (OUT == OUT_BF16 ? 2.0 + 2.0 * PARTS : (OUT == OUT_TOP ? 2.0 : 3.0)) * (double)rows * (double)d, s);
+  launch_dependent(fwd_block_kernel<DB, N, OUT, PARTS>, (unsigned)(tiles < c->n_sm ? tiles : c->n_sm), NTHREADS, Geo<DB, N>::SMEM, s, mX, mQ, mC, p);
   c->launches++;
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }
@@ -420,14 +431,14 @@ void launch_pack_blocks(armor_ctx* c, const float* P, const float* rowscale, con
   c->launches++;
 }
 
-template <int OUT>
+template <int OUT, int PARTS = 1>
 static armor_status block_product(armor_ctx* c, const void* X, const void* Q, void* out, const FParams& p, int64_t rows, int64_t d, cudaStream_t s) {
   if (!fwd_block_ok(c) || rows <= 0 || d % c->db) return ARMOR_ERR_UNSUPPORTED;
-  if (c->db == 128) return launch_block<128, 128, OUT>(c, X, Q, out, p, rows, d, s);
+  if (c->db == 128) return launch_block<128, 128, OUT, PARTS>(c, X, Q, out, p, rows, d, s);
   // a block of 256 in halves while an SM has no more than one: 4096 columns x 400 tokens 28.1 us a forward in halves, 30.4 whole;
   // x 640 31.8 and 30.9; x 1,000 34.3 and 31.9
-  return 2 * ((rows + BM - 1) / BM) * (d / 256) <= c->n_sm ? launch_block<256, 128, OUT>(c, X, Q, out, p, rows, d, s)
-                                                          : launch_block<256, 256, OUT>(c, X, Q, out, p, rows, d, s);
+  return 2 * ((rows + BM - 1) / BM) * (d / 256) <= c->n_sm ? launch_block<256, 128, OUT, PARTS>(c, X, Q, out, p, rows, d, s)
+                                                          : launch_block<256, 256, OUT, PARTS>(c, X, Q, out, p, rows, d, s);
 }
 
 // out[rows][d] (bf16) = X[rows][d] (bf16) times the block-diagonal matrix whose stacked blocks are Q[d][db] (bf16):
@@ -435,6 +446,9 @@ static armor_status block_product(armor_ctx* c, const void* X, const void* Q, vo
 armor_status launch_fwd_block(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d,
                               cudaStream_t s) {
   return block_product<OUT_BF16>(c, X, Q, out, FParams{}, rows, d, s);
+}
+armor_status launch_fwd_block_two(armor_ctx* c, const void* X, const void* Q, void* out, int64_t rows, int64_t d, cudaStream_t s) {
+  return block_product<OUT_BF16, 2>(c, X, Q, out, FParams{}, rows, d, s);
 }
 armor_status launch_fwd_block_top(armor_ctx* c, const void* X, const void* Q, unsigned* top, int64_t rows, int64_t d, cudaStream_t s) {
   FParams p{};
@@ -450,8 +464,9 @@ armor_status launch_fwd_block_i8(armor_ctx* c, const void* X, const void* Q, con
 
 // The same for few rows.  pieces == 0: X is bf16 [rows][d]; otherwise X holds that many fp32 arrays
 // [rows][d] whose sum, rounded to bf16, is the operand.  Either way a dependent launch.  out_f32 (pieces == 0): out is fp32.
+// two (pieces > 0): the sum is not rounded to one bf16 number but kept as two.
 armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const void* Q, void* out, int64_t rows, int64_t d,
-                              cudaStream_t s, bool out_f32) {
+                              cudaStream_t s, bool out_f32, bool two) {
   if (!fwd_block_ok(c) || rows <= 0 || d % 128) return ARMOR_ERR_UNSUPPORTED;
   KTimer kt(c, ARMOR_KC_FORWARD, 4.0 * (double)rows * (double)d, s);
   cudaLaunchConfig_t cfg{};
@@ -465,10 +480,12 @@ armor_status launch_fwd_small(armor_ctx* c, const void* X, int pieces, const voi
   float* o32 = out_f32 ? static_cast<float*>(out) : nullptr;   // (not with pieces)
   const int n = (int)rows;
   cudaError_t e;
-  if (c->db == 128) e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, true>, X, pieces, q, o, n, d, o32)
-                                   : cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, false>, X, 0, q, o, n, d, o32);
-  else e = pieces > 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, true>, X, pieces, q, o, n, d, o32)
-                      : cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, false>, X, 0, q, o, n, d, o32);
+  if (c->db == 128) e = pieces == 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, false, false>, X, 0, q, o, n, d, o32)
+                      : two ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, true, true>, X, pieces, q, o, n, d, o32)
+                            : cudaLaunchKernelEx(&cfg, fwd_small_kernel<128, true, false>, X, pieces, q, o, n, d, o32);
+  else e = pieces == 0 ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, false, false>, X, 0, q, o, n, d, o32)
+         : two ? cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, true, true>, X, pieces, q, o, n, d, o32)
+               : cudaLaunchKernelEx(&cfg, fwd_small_kernel<256, true, false>, X, pieces, q, o, n, d, o32);
   c->launches++;
   return e == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
 }

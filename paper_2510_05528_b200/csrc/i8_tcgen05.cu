@@ -26,7 +26,8 @@ constexpr int A_BYTES = BM * 128;                   // a stage of W
 constexpr int E_BYTES = 128 * 32;                   // positions of a sparse stage
 
 struct I8P {
-  void* Y; int64_t ldy; int out;                    // ARMOR_DTYPE_* of Y
+  void* Y; int64_t ldy; int out;                    // ARMOR_DTYPE_* of Y, or OUT_TWO_BF16
+  int64_t second;                                   // elements from the first array of the two to the second
   int pairs;                                        // two neighbouring rows of W may be stored at once
   const float *xs, *ws, *bias;
   int64_t M, N;                                     // rows of W, tokens
@@ -84,6 +85,13 @@ __device__ __forceinline__ void copy_e(uint32_t taddr, uint64_t sdesc) {
   else asm volatile("tcgen05.cp.cta_group::2.128x128b [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
 
+// two neighbouring elements, on a 4-byte boundary, of Y and of the array behind it
+__device__ __forceinline__ void put_split(__nv_bfloat16* at, int64_t second, float a, float b) {
+  uint32_t hi, lo;
+  rows::split2(a, b, hi, lo);
+  *reinterpret_cast<uint32_t*>(at) = hi;
+  *reinterpret_cast<uint32_t*>(at + second) = lo;
+}
 __device__ __forceinline__ void store_one(const I8P& p, int64_t tok, int64_t row, float v) {
   const int64_t o = tok * p.ldy + row;
   if (p.out == ARMOR_DTYPE_F32) static_cast<float*>(p.Y)[o] = v;
@@ -91,10 +99,12 @@ __device__ __forceinline__ void store_one(const I8P& p, int64_t tok, int64_t row
   else static_cast<__half*>(p.Y)[o] = __float2half_rn(v);
 }
 // rows row, row + 1 (row even) of one token
+template <bool SP>
 __device__ __forceinline__ void store_two(const I8P& p, int64_t tok, int64_t row, float a, float b) {
   if (p.pairs && row + 1 < p.M) {
     const int64_t o = tok * p.ldy + row;
-    if (p.out == ARMOR_DTYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(p.Y) + o) = make_float2(a, b);
+    if (SP && p.out == OUT_TWO_BF16) put_split(static_cast<__nv_bfloat16*>(p.Y) + o, p.second, a, b);
+    else if (p.out == ARMOR_DTYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(p.Y) + o) = make_float2(a, b);
     else if (p.out == ARMOR_DTYPE_BF16)
       *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.Y) + o) = rows::pack2(static_cast<const __nv_bfloat16*>(nullptr), a, b);
     else *reinterpret_cast<uint32_t*>(static_cast<__half*>(p.Y) + o) = rows::pack2(static_cast<const __half*>(nullptr), a, b);
@@ -326,7 +336,7 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
           const int t = t0 + i * abreast;
           if (t < nv) {
             const float xs = T::RAW ? own_scale[t] : p.xs[tok0 + t];
-            store_two(p, tok0 + t, row, fmaf((float)a[i], xs * wa, ba), fmaf((float)b[i], xs * wb, bb));
+            store_two<SP>(p, tok0 + t, row, fmaf((float)a[i], xs * wa, ba), fmaf((float)b[i], xs * wb, bb));
           }
         }
       }
@@ -346,7 +356,8 @@ i8_few_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ 
 template <typename T>
 __device__ __forceinline__ void put_two(T* at, float a, float b) { *reinterpret_cast<uint32_t*>(at) = rows::pack2(static_cast<const T*>(nullptr), a, b); }
 __device__ __forceinline__ void put_two(float* at, float a, float b) { *reinterpret_cast<float2*>(at) = make_float2(a, b); }
-template <typename T>
+// TWO: OUT_TWO_BF16 (M, ldy and Y's address even: those of a core).
+template <typename T, bool TWO = false>
 __device__ __forceinline__ void way_out(const I8P& p, uint32_t taddr, int64_t row, int64_t tok0, float ws, float bias, float* slot, int lane) {
   __syncwarp();
   slot[lane] = tok0 + lane < p.N ? p.xs[tok0 + lane] : 0.f;
@@ -368,7 +379,8 @@ __device__ __forceinline__ void way_out(const I8P& p, uint32_t taddr, int64_t ro
       const float got = __shfl_xor_sync(0xffffffffu, odd ? v[k] : v[k + 1], 1);
       const float a = odd ? got : v[k], b = odd ? v[k + 1] : got;
       if (full || tok0 + i + k + odd < p.N) {
-        if (pair) put_two(at, a, b);
+        if constexpr (TWO) { if (pair) put_split(at, p.second, a, b); }
+        else if (pair) put_two(at, a, b);
         else {
           if (even < p.M) at[0] = rows::from_f<T>(a);
           if (even + 1 < p.M) at[1] = rows::from_f<T>(b);
@@ -535,6 +547,7 @@ i8_many_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
         if (tok0 >= p.N) break;
         const uint32_t taddr = tmem_base + (uint32_t)(as * T::MAX_N + ch * 32) + ((uint32_t)(q * 32) << 16);
         if (p.out == ARMOR_DTYPE_BF16) way_out<__nv_bfloat16>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
+        else if (SP && p.out == OUT_TWO_BF16) way_out<__nv_bfloat16, true>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
         else if (p.out == ARMOR_DTYPE_F32) way_out<float>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
         else way_out<__half>(p, taddr, row, tok0, ws, bias, slots[warp - 2], lane);
       }
@@ -750,8 +763,8 @@ armor_status product(armor_ctx* c, const CUtensorMap& mA, const CUtensorMap& mE,
 
 I8P output(void* y, int32_t dtype, int64_t ldy, int64_t n, int64_t n_out, const float* xs, const float* ws, const float* bias, int ahead) {
   I8P p{};
-  const int es = rows_dtype_bytes(dtype);
-  p.Y = y; p.ldy = ldy; p.out = dtype; p.xs = xs; p.ws = ws; p.bias = bias; p.M = n_out; p.N = n; p.ahead = ahead;
+  const int es = dtype == OUT_TWO_BF16 ? 2 : rows_dtype_bytes(dtype);
+  p.Y = y; p.ldy = ldy; p.out = dtype; p.second = n * ldy; p.xs = xs; p.ws = ws; p.bias = bias; p.M = n_out; p.N = n; p.ahead = ahead;
   p.pairs = reinterpret_cast<uintptr_t>(y) % (2 * es) == 0 && ldy % 2 == 0;
   return p;
 }

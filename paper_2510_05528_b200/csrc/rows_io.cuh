@@ -27,6 +27,17 @@ __device__ __forceinline__ uint32_t pack2(const __half*, float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// Two floats as two bf16 numbers each: the nearest one, and what is missing rounded towards zero, 15 bits or more together.  (The rest stays
+// below a half step of the first number where it was, so that the sum of the two rounds to bf16 as the float does.)  A first number
+// that is not finite stands alone.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat16* t = nullptr;
+  hi = pack2(t, a, b);
+  const float2 h = unpack2(t, hi);
+  const float ra = fabsf(h.x) < __int_as_float(0x7f800000) ? a - h.x : 0.f, rb = fabsf(h.y) < __int_as_float(0x7f800000) ? b - h.y : 0.f;
+  lo = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
+}
+
 // Eight consecutive elements as they lie: a chunk of a row that waits in registers.
 template <typename T> struct Raw8 { uint4 w; };
 template <> struct Raw8<float> { float4 a, b; };
