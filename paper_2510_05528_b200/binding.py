@@ -270,10 +270,8 @@ def armor_apply_layer(ctx, packed, x, y) -> None:
         _check(code, "armor_apply_layer")
 
 
-def _row_ptr(t: torch.Tensor | None, dtype, name: str, cols: int | None = None) -> tuple[int | None, int]:
-    """(address, leading dimension) of rows [n, cols] with unit column stride; (None, 0) of None."""
-    if t is None:
-        return None, 0
+def _row_ptr(t: torch.Tensor, dtype, name: str, cols: int | None = None) -> tuple[int, int]:
+    """(address, leading dimension) of rows [n, cols] with unit column stride."""
     if t.dtype is dtype and t.is_cuda and t.dim() == 2 and t.is_contiguous():      # (the common case first: a call takes microseconds)
         c = t.size(1)
         if cols is None or c == cols:
@@ -295,7 +293,7 @@ def _row_ptr(t: torch.Tensor | None, dtype, name: str, cols: int | None = None) 
     return t.data_ptr(), ld
 
 
-def _rows_at(t: torch.Tensor, dtype, cols: int | None, name: str, here: int) -> tuple[int | None, int, int]:
+def _rows_at(t: torch.Tensor, dtype, cols: int | None, name: str, here: int) -> tuple[int, int, int]:
     """(address, leading dimension, rows) of [rows, cols] on device `here`.  The common case in as few steps as there are: a small call
     takes ten microseconds, most of them its checks."""
     if t.dtype is dtype and t.get_device() == here and t.is_contiguous():
@@ -304,15 +302,19 @@ def _rows_at(t: torch.Tensor, dtype, cols: int | None, name: str, here: int) -> 
             n, c = shape
             return t.data_ptr(), (c if n > 1 else max(c, t.stride(0))), n
     if t.is_cuda and t.get_device() != here:
-        raise ValueError(f"{name} must be on cuda:{here}, the context's device, not on {t.device}")
+        raise ValueError(f"{name} must be on cuda:{here}, the call's device, not on {t.device}")
     p, ld = _row_ptr(t, dtype, name, cols)
     return p, ld, t.shape[0]
 
 
 def _cuda_index(t: torch.Tensor, name: str) -> int:
+    """The device of a call, which enqueues on that device's current stream."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    return t.get_device()
+    here = t.get_device()
+    if torch._C._cuda_getDevice() != here:
+        raise ValueError(f"{t.device}, which holds {name}, must be the current device")
+    return here
 
 
 def _vector_at(t: torch.Tensor, n: int, name: str, here: int) -> int:
@@ -320,7 +322,7 @@ def _vector_at(t: torch.Tensor, n: int, name: str, here: int) -> int:
     if t.dtype is torch.float32 and t.get_device() == here and t.numel() == n and t.is_contiguous():
         return t.data_ptr()
     if t.is_cuda and t.get_device() != here:
-        raise ValueError(f"{name} must be on cuda:{here}, the context's device, not on {t.device}")
+        raise ValueError(f"{name} must be on cuda:{here}, the call's device, not on {t.device}")
     _ptr(t, torch.float32, name)
     raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
 
@@ -335,29 +337,29 @@ def _row_dtype(t: torch.Tensor, name: str) -> int:
 def armor_quantize_rows(ctx, x, q, scale) -> None:
     """q [n, c] int8 (rows on 16-byte boundaries) and scale [n] fp32 of x [n, c] (see armor.h)."""
     code = _row_dtype(x, "x")
-    xp, ldx = _row_ptr(x, x.dtype, "x")
-    n, c = x.shape
-    qp, ldq = _row_ptr(q, torch.int8, "q", c)
-    if q.shape[0] != n or scale.numel() != n:
-        raise ValueError(f"q and scale must have the {n} rows of x")
-    _check(lib().armor_quantize_rows(ctx, xp, code, ldx, n, c, qp, ldq, _ptr(scale, torch.float32, "scale"), _stream()),
+    here = _cuda_index(x, "x")
+    xp, ldx, n = _rows_at(x, x.dtype, None, "x", here)
+    c = x.size(1)
+    qp, ldq, n_q = _rows_at(q, torch.int8, c, "q", here)
+    if n_q != n:
+        raise ValueError(f"q must have the {n} rows of x")
+    _check(lib().armor_quantize_rows(ctx, xp, code, ldx, n, c, qp, ldq, _vector_at(scale, n, "scale", here), _stream()),
            "armor_quantize_rows")
 
 
 def armor_linear_i8(ctx, x, x_scale, wq, w_scale, bias, y) -> None:
     """y [n, n_out] = x [n, n_in] wq^T with the scales of both (see armor.h); x_scale None: x is rounded on the way."""
-    f = torch.float32
     code = DTYPE_I8 if x.dtype is torch.int8 else _row_dtype(x, "x")
-    xp, ldx = _row_ptr(x, x.dtype, "x")
-    n, n_in = x.shape
-    wp, ldw = _row_ptr(wq, torch.int8, "wq", n_in)
-    n_out = wq.shape[0]
-    yp, ldy = _row_ptr(y, y.dtype, "y", n_out)
-    if y.shape[0] != n or w_scale.numel() != n_out or (bias is not None and bias.numel() != n_out) or \
-            (x_scale is not None and x_scale.numel() != n):
-        raise ValueError(f"y and x_scale must have the {n} rows of x, w_scale and bias the {n_out} of wq")
-    code = lib().armor_linear_i8(ctx, xp, code, ldx, _ptr(x_scale, f, "x_scale"), wp, ldw, _ptr(w_scale, f, "w_scale"),
-                                 _ptr(bias, f, "bias"), yp, _row_dtype(y, "y"), ldy, n, n_out, n_in, _stream())
+    here = _cuda_index(x, "x")
+    xp, ldx, n = _rows_at(x, x.dtype, None, "x", here)
+    n_in = x.size(1)
+    wp, ldw, n_out = _rows_at(wq, torch.int8, n_in, "wq", here)
+    yp, ldy, n_y = _rows_at(y, y.dtype, n_out, "y", here)
+    if n_y != n:
+        raise ValueError(f"y must have the {n} rows of x")
+    code = lib().armor_linear_i8(ctx, xp, code, ldx, None if x_scale is None else _vector_at(x_scale, n, "x_scale", here), wp, ldw,
+                                 _vector_at(w_scale, n_out, "w_scale", here), None if bias is None else _vector_at(bias, n_out, "bias", here),
+                                 yp, _row_dtype(y, "y"), ldy, n, n_out, n_in, _stream())
     if code:
         _check(code, "armor_linear_i8")
 
@@ -379,6 +381,12 @@ def armor_apply_layer_i8(ctx, packed, x, y) -> None:
     bf16 = torch.bfloat16
     if x.dtype is not bf16 or y.dtype is not bf16:
         raise ValueError("the packed layer takes bf16 x and y")
+    here = _cuda_index(x, "x")
+    for t, name in ((packed, "packed"), (y, "y")):
+        if t.is_cuda and t.get_device() != here:
+            raise ValueError(f"{name} must be on cuda:{here}, as x is, not on {t.device}")
+    if x.dim() != 2 or y.dim() != 2 or y.size(0) != x.size(0):
+        raise ValueError(f"x and y must be [tokens, d_in] and [tokens, d_out], got {list(x.shape)} and {list(y.shape)}")
     code = lib().armor_apply_layer_i8(ctx, _ptr(packed, torch.uint8, "packed"), _ptr(x, None, "x"), _ptr(y, None, "y"), x.shape[0], _stream())
     if code:
         _check(code, "armor_apply_layer_i8")
@@ -432,16 +440,20 @@ def _block_norm(ctx, here, x, y, h, n, q, q_scale, made, gate, rows_per_gate, w_
         if n is not None:
             a.n = n.data_ptr()
             a.ldn = d
+        if q is not None:
+            a.q, a.ldq, _ = _rows_at(q, torch.int8, d, "q", here)
     else:
-        for t, name in ((h, "h"), (n, "n"), (q, "q"), (q_scale, "q_scale")):
-            if t is not None and t.size(0) != rows:
-                raise ValueError(f"{name} must have the {rows} rows of x")
-        a.h, a.ldh = _row_ptr(h, dt, "h", d)
-        a.n, a.ldn = _row_ptr(n, bt, "n", d)
-    if q is not None:
-        a.q, a.ldq = _row_ptr(q, torch.int8, "q", d)
+        n_h = n_n = n_q = rows
+        if h is not None:
+            a.h, a.ldh, n_h = _rows_at(h, dt, d, "h", here)
+        if n is not None:
+            a.n, a.ldn, n_n = _rows_at(n, bt, d, "n", here)
+        if q is not None:
+            a.q, a.ldq, n_q = _rows_at(q, torch.int8, d, "q", here)
+        if not n_h == n_n == n_q == rows:
+            raise ValueError(f"h, n and q must have the {rows} rows of x")
     if q_scale is not None:
-        a.q_scale = _ptr(q_scale, torch.float32, "q_scale")
+        a.q_scale = _vector_at(q_scale, rows, "q_scale", here)
     _norm_params(a, d, rows, here, gate, rows_per_gate, w_post, w_pre, post, pre, residual_scale, eps)
     code = lib().armor_block_norm(ctx, a, _stream())
     if code:
@@ -491,11 +503,13 @@ def _block_norm_backward(ctx, here, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate
         if dgate is not None:
             a.dgate = dgate.data_ptr()
     else:
-        for t, name in ((dx, "dx"), (dy, "dy")):
-            if t is not None and t.size(0) != rows:
-                raise ValueError(f"{name} must have {rows} rows")
-        a.dx, a.lddx = _row_ptr(dx, ts, "dx", d)
-        a.dy, a.lddy = _row_ptr(dy, tb, "dy", d)
+        n_dx = n_dy = rows
+        if dx is not None:
+            a.dx, a.lddx, n_dx = _rows_at(dx, ts, d, "dx", here)
+        if dy is not None:
+            a.dy, a.lddy, n_dy = _rows_at(dy, tb, d, "dy", here)
+        if not n_dx == n_dy == rows:
+            raise ValueError(f"dx and dy must have {rows} rows")
         for name, t, n in (("dw_post", dw_post, d), ("dw_pre", dw_pre, d), ("dgate", dgate, gates * d)):
             if t is not None:
                 setattr(a, name, _vector_at(t, n, name, here))
@@ -775,9 +789,9 @@ class ArmorContext:
 
     def pack_layer_i8(self, st: LayerState, denormalize: bool = False) -> torch.Tensor:
         """Core in 8 bits (a scale for each row) and bf16 wrappers, packed for apply_layer_i8."""
-        self._here(st.A, st.B, st.S, st.M)
-        packed = torch.empty(self._packed_i8, dtype=torch.uint8, device=self.device)
         r1, r2 = (st.r1, st.r2) if denormalize else (None, None)
+        self._here(st.A, st.B, st.S, st.M, r1, r2)
+        packed = torch.empty(self._packed_i8, dtype=torch.uint8, device=self.device)
         armor_pack_layer_i8(self.ctx, st.A, st.B, st.S, st.M, r1, r2, packed)
         return packed
 
