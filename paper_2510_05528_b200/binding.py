@@ -643,7 +643,7 @@ class ArmorContext:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
-        self._packed_i8_bytes = None
+        self._sizes = {}
         self.cfg = make_config(d_out, d_in, d_block, **kw)
         self.d_out, self.d_in, self.d_block = d_out, d_in, d_block
         nbytes = armor_workspace_bytes(self.cfg)
@@ -715,6 +715,7 @@ class ArmorContext:
         return packed
 
     def apply_packed(self, st: LayerState, packed: torch.Tensor, x: torch.Tensor, denormalize: bool = False) -> torch.Tensor:
+        self._packed(packed, armor_packed_core_bytes, "pack_core")
         y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
         r1, r2 = (st.r1, st.r2) if denormalize else (None, None)
         armor_apply_packed(self.ctx, st.A, st.B, packed, r1, r2, x, y)
@@ -728,6 +729,7 @@ class ArmorContext:
         return packed
 
     def apply_layer(self, packed: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
+        self._packed(packed, armor_packed_layer_bytes, "pack_layer")
         y = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=self.device)
         armor_apply_layer(self.ctx, packed, x, y)
         return y
@@ -749,11 +751,16 @@ class ArmorContext:
             raise ValueError(f"{self.device} must be the current device")
         return here
 
-    @property
-    def _packed_i8(self) -> int:
-        if self._packed_i8_bytes is None:
-            self._packed_i8_bytes = armor_packed_layer_i8_bytes(self.cfg)
-        return self._packed_i8_bytes
+    def _packed(self, packed: torch.Tensor, size, made_by: str, exact: bool = False) -> None:
+        """`packed` holds what `made_by` packs: the kinds differ in size alone, and a larger one's forward reads behind a smaller one's end."""
+        want = self._size(size)
+        if packed.dtype is not torch.uint8 or packed.numel() < want or (exact and packed.numel() != want):
+            raise ValueError(f"packed must be what {made_by} made for this shape: {want} bytes, got {packed.numel()} elements of {packed.dtype}")
+
+    def _size(self, size) -> int:
+        if size not in self._sizes:
+            self._sizes[size] = size(self.cfg)
+        return self._sizes[size]
 
     def new_int8_rows(self, n: int, cols: int) -> torch.Tensor:
         """[n, cols] int8 whose rows start on 16-byte boundaries."""
@@ -791,7 +798,7 @@ class ArmorContext:
         """Core in 8 bits (a scale for each row) and bf16 wrappers, packed for apply_layer_i8."""
         r1, r2 = (st.r1, st.r2) if denormalize else (None, None)
         self._here(st.A, st.B, st.S, st.M, r1, r2)
-        packed = torch.empty(self._packed_i8, dtype=torch.uint8, device=self.device)
+        packed = torch.empty(self._size(armor_packed_layer_i8_bytes), dtype=torch.uint8, device=self.device)
         armor_pack_layer_i8(self.ctx, st.A, st.B, st.S, st.M, r1, r2, packed)
         return packed
 
@@ -803,8 +810,9 @@ class ArmorContext:
         xp, ld, n = _rows_at(x, bf16, self.d_in, "x", here)
         if ld != self.d_in and n > 1:
             raise ValueError("x must be contiguous")
-        if packed.dtype is not torch.uint8 or packed.get_device() != here or packed.numel() < self._packed_i8 or not packed.is_contiguous():
-            raise ValueError(f"packed must be what pack_layer_i8 made for this shape: {self._packed_i8} bytes on {self.device}")
+        self._packed(packed, armor_packed_layer_i8_bytes, "pack_layer_i8", exact=True)
+        if packed.get_device() != here or not packed.is_contiguous():
+            raise ValueError(f"packed must be contiguous and on {self.device}")
         y = torch.empty(n, self.d_out, dtype=bf16, device=self.device)
         code = lib().armor_apply_layer_i8(self.ctx, packed.data_ptr(), xp, y.data_ptr(), n, _stream())
         if code:

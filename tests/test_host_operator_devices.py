@@ -105,3 +105,20 @@ def test_arrays_of_too_few_elements(name):
                 continue                                   # (others would have to follow)
             with pytest.raises(ValueError):
                 call(**{**arrays, k: v})
+
+
+def test_what_another_call_packed():
+    """A core, a layer and a layer in 8 bits are bytes alike: each forward refuses what is too small for it, and the 8-bit one whatever is
+    not its own."""
+    ctx = object.__new__(Bd.ArmorContext)
+    ctx.cfg, ctx.d_out, ctx.d_in, ctx._index, ctx._sizes, ctx.device = Bd.make_config(512, 768, 128), 512, 768, 0, {}, torch.device("meta")
+    core, layer, layer8 = (torch.empty(f(ctx.cfg), dtype=U8) for f in (Bd.armor_packed_core_bytes, Bd.armor_packed_layer_bytes, Bd.armor_packed_layer_i8_bytes))
+    x = Array(3, 768)
+    for call, mine, wrong in ((lambda p: ctx.apply_packed(None, p, x), "pack_core", [core[:-1], core.view(torch.int8)]),
+                              (lambda p: ctx.apply_layer(p, x), "pack_layer", [core, layer8, layer[1:], layer.float()]),
+                              (lambda p: ctx.apply_layer_i8(p, x), "pack_layer_i8", [core, layer, layer8[1:], layer8.view(torch.int8)])):
+        for p in wrong:
+            with pytest.raises(ValueError, match=f"what {mine} made"):
+                call(p)
+    with pytest.raises(ValueError, match="on meta"):       # (of the right size, and in host memory)
+        ctx.apply_layer_i8(layer8, x)
