@@ -98,3 +98,21 @@ def test_one_array_padded_and_arrays_left_out(ctx, d):
     Bd.armor_block_norm_backward(ctx.ctx, p["x"], None, None, p["dn"], dx, None, None, None, None, w_pre=p["w_pre"])
     assert torch.equal(dx, ctx.block_norm_backward(t["x"], None, torch.zeros_like(t["x"]), t["dn"], w_pre=t["w_pre"])["dx"])
     assert (behind(xb, dx) == KEPT).all()
+
+
+@pytest.mark.parametrize("ts,tb", PAIRS)
+@pytest.mark.parametrize("rows,d", [(700, 1), (701, 2), (2000, 3), (20000, 5)])
+def test_rows_shorter_than_a_vector(ctx, rows, d, ts, tb):
+    """Many rows of a few elements, one behind the other: most start and end inside a vector that holds neighbours too."""
+    t = inputs(rows, d, ts, tb, post=True, gates=2)
+    h, q, scale = ctx.block_norm_i8(t["x"], t["y"], **terms(t))
+    n = ctx.block_norm(t["x"], t["y"], **terms(t))[1]
+    rh, rn, size = forward64(t, post=True)
+    close(h, rh, SUM * size)
+    off = 2 * SUM * size / (rh.square().mean(1, keepdim=True) + 1e-6).sqrt() * t["w_pre"].double().abs()
+    close(n, rn, off)
+    top, worst = rn.abs().amax(1, keepdim=True), off.amax(1, keepdim=True)
+    assert ((q.double() - rn * 127 / top).abs() <= 0.5 + (off + worst) * 127 / top).all()
+    got = ctx.block_norm_backward(t["x"], t["y"], t["dh"], t["dn"], **terms(t))
+    want, sizes = backward64(t, t["x"], post=True)
+    check_backward(got, want, sizes)
