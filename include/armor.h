@@ -279,7 +279,8 @@ armor_status armor_apply_layer_i8(armor_ctx* ctx, const void* d_packed, const vo
  * dimensions and alignment (q as in armor_quantize_rows).  n_rows == 0 is a no-op.
  * Backward: from h as it was stored (needed with pre), y (with post or dgate) and the gradients dh and dn of the two outputs (either may
  * be NULL: zeros), any of dx, dy, dw_post [d], dw_pre [d], dgate [n_gates, d] (NULL: not wanted; the last three fp32, written, not
- * added to; gates without rows get zeros).  Runs give the same bits.  dx may be dh's and dy may be dn's own buffer.  Sums over rows
+ * added to; gates without rows get zeros).  Runs give the same bits.  The sums over rows are
+ * fp32 over a CTA's rows, one behind the other, and fp64 over the CTAs.  dx may be dh's and dy may be dn's own buffer.  Sums over rows
  * go through the context's workspace (WORKSPACE if it does not hold four rows of d fp32).
  * Errors: INVALID_ARG (missing arrays, weights without their norm), SHAPE (d < 1, leading dimensions below d, too few gates),
  * UNSUPPORTED (types), TOO_LARGE (d, or 2^31 rows). */

@@ -10,9 +10,10 @@
 //   dh' = dh + (g - hbar mean(g hbar)) / rms(h)      dx = a dh'      e = gate (.) dh'      f = e (.) w_post
 //   dy = (f - ybar mean(f ybar)) / rms(y)   (or e)
 //   dw_pre = sum_t dn hbar      dw_post = sum_t e ybar      dgate = sum over the row's rows of dh' u
-// The sums over rows: a CTA takes consecutive rows and adds into shared memory, where an element of the row has one owner, so no order
-// is left to chance; the CTAs' sums are added in order by a second kernel, in fp64.  A gate's rows may end inside a CTA's: the CTA
-// keeps two sums for the gates at its ends, and writes one that lies within its rows at once.
+// The sums over rows: a CTA takes consecutive rows and adds in fp32, an element of the row by one owner, so no order is left to chance: in registers
+// where rows go through the ring (the share of w_post, once a gate, in shared memory), in shared memory beyond its widths.  A second kernel
+// adds the CTAs' sums in order, in fp64.  A gate's rows may end inside a CTA's: the CTA keeps two sums for the gates at its ends, and writes one
+// that lies within its rows at once.
 #include "rows_io.cuh"
 #include "tc_common.cuh"
 

@@ -1,8 +1,8 @@
 // Products of int8 rows with a scale each on the tensor cores (tcgen05.mma kind::i8, int32 sums in tensor memory):
 //   Y[t][m] = xs[t] ws[m] sum_k Xq[t][k] Wq[m][k] (+ b[m])
 // with W dense, or the 2:4 core of a factorised layer given as its kept values (int8, two of every four along k) and their
-// positions (tcgen05.mma.sp).  The sums are exact: |q| <= 128, so 131,071 products fit an int32.  The one rounding is that of the sum to
-// fp32 on its way out, a further one where Y is bf16 or fp16.
+// positions (tcgen05.mma.sp).  The sums are exact: |q| <= 128, so 131,071 products fit an int32.  On their way out fp32 rounds the sum, the
+// product of the scales, and the multiplication of the two with the bias added; a further rounding where Y is bf16 or fp16.
 //
 // W is the A operand, lanes of an accumulator are its rows and columns are tokens, from one token to many.  One instruction
 // multiplies 32 k (dense; 32 bytes of each operand) or 64 (sparse; 32 bytes of kept values, 64 of tokens).  A stage is 128 bytes of W's
