@@ -315,6 +315,62 @@ typedef struct {
 armor_status armor_block_norm(armor_ctx* ctx, const armor_block_norm_args* args, armor_stream_t stream);
 armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_grad_args* args, armor_stream_t stream);
 
+/* ---- a paged cache of keys and values, and the attention over it --------------------------------------------------
+ * What a served model's block has between its q / k / v product and its output product.  The cache: n_pages pages of page_size slots (any
+ * number) for kv_heads heads of head_dim (64 or 128); a slot of a head holds a row of keys and one of values as int8 with an fp32 scale
+ * each, as armor_quantize_rows has them.  k and v are 16-byte aligned and share their strides, in elements, multiples of 16 for the
+ * values; any order of pages, heads and slots.
+ * A batch of n_seqs sequences (device, int32): rows starts[b] .. starts[b + 1] - 1 of the packed arrays (n_b of them; starts rise) stand for the
+ * last n_b of the lengths[b] positions of sequence b: its row i has position p = lengths[b] - n_b + i, which lies in slot p % page_size
+ * of page pages[b * ld_pages + p / page_size].  Positions below zero are padding.  Rows from starts[n_seqs] on belong to no sequence and
+ * are left as they are.  Nothing of a batch is read on the host: a captured call follows what the arrays hold when it is replayed.
+ * A page out of [0, n_pages), a position behind the table's max_pages and a sequence whose rows are out of range are counted in device
+ * status word 11 and neither read nor written.  n_rows (of the packed arrays) 0 or n_seqs 0: a no-op. */
+typedef struct {
+  int8_t *k, *v;
+  float *k_scale, *v_scale;
+  int64_t n_pages, page_size, kv_heads, head_dim;
+  int64_t page_stride, head_stride, slot_stride;
+  int64_t scale_page_stride, scale_head_stride, scale_slot_stride;
+} armor_kv_cache;
+typedef struct {
+  int64_t n_seqs, max_pages, ld_pages;
+  const int32_t *pages, *lengths, *starts;
+} armor_kv_batch;
+/* Packed rows [n_rows][kv_heads][head_dim] of keys and values (dtype F32, BF16, F16), strides in elements, any alignment of
+ * their rows.  armor_kv_write rounds them into the cache; two rows of one call must not have the same place (pages that sequences share are
+ * complete, or each is written by one).  armor_kv_read writes what the cache holds, rounded once from fp32 (rows of padding, and
+ * those refused: zeros).  Errors: INVALID_ARG (missing arrays, negative counts), SHAPE (sizes, strides, alignment), UNSUPPORTED (dtype, head_dim),
+ * TOO_LARGE (2^31 pages, slots, rows). */
+typedef struct {
+  const void *k, *v;                       /* written to by armor_kv_read */
+  int64_t n_rows;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t dtype;
+} armor_kv_rows;
+armor_status armor_kv_write(armor_ctx* ctx, const armor_kv_cache* cache, const armor_kv_batch* batch, const armor_kv_rows* rows,
+                            armor_stream_t stream);
+armor_status armor_kv_read(armor_ctx* ctx, const armor_kv_cache* cache, const armor_kv_batch* batch, const armor_kv_rows* rows,
+                           armor_stream_t stream);
+/* o[i][h] = sum_j w_j V_j / sum_j w_j, w_j = exp(scale q[i][h] . K_j), K and V as the cache holds them for head h / (heads / kv_heads), over
+ * the positions j <= p of row i's own position p, with window > 0 only j > p - window; a row with none (padding): zeros.  The new rows'
+ * own keys and values are in the cache already (armor_kv_write).  q and o [n_rows][heads][head_dim], BF16 or F16, strides in elements, any alignment;
+ * o must not overlap q.  Weights are rounded to fp16 on their way to the tensor cores, q's values, keys and values are exact; sums are fp32.
+ * max_chunk: how many rows a sequence is expected to have at most (0: not known); a hint for the choice of the kernel, never of the
+ * result's meaning.  Runs give the same bits.  Uses the context's workspace.  Errors as above; SHAPE also where kv_heads does not divide
+ * heads, INVALID_ARG for a negative or infinite scale, window or max_chunk. */
+typedef struct {
+  const void* q;
+  void* o;
+  int64_t n_rows, heads;
+  int64_t q_row_stride, q_head_stride, o_row_stride, o_head_stride;
+  int64_t window, max_chunk;
+  float scale;
+  int32_t dtype;
+} armor_kv_attend_args;
+armor_status armor_kv_attend(armor_ctx* ctx, const armor_kv_cache* cache, const armor_kv_batch* batch, const armor_kv_attend_args* args,
+                             armor_stream_t stream);
+
 /* Copies up to n (at most 16) device status words to h_codes (host).
  *   word 0: Cholesky failures since the context was created; word 1: first failing block id + 1;
  *   word 2: bounded waits that gave up; word 3: last armor_status recorded by a kernel;
@@ -328,6 +384,7 @@ armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_gr
  *   word 10 (ARMOR_PREC_FP16X3): entries of H that, after the scaling by its diagonal, lie beyond the fp16 range and
  *     were clamped (cumulative).  A positive semidefinite H has none; a non-zero count means the products with H
  *     were not those of the H that was passed.
+ *   word 11: pages and sequences that armor_kv_write, armor_kv_read and armor_kv_attend refused (counted once or more each; cumulative).
  * The caller must have synchronised the stream the context's work ran on.  (This call itself copies
  * synchronously.) */
 armor_status armor_get_device_status(armor_ctx* ctx, int32_t* h_codes, int32_t n);

@@ -30,7 +30,7 @@ EXPORTS = ["armor_workspace_bytes", "armor_create", "armor_destroy", "armor_gram
            "armor_bcd_step", "armor_proxy_loss", "armor_apply", "armor_packed_core_bytes", "armor_pack_core", "armor_apply_packed",
            "armor_packed_layer_bytes", "armor_pack_layer", "armor_apply_layer",
            "armor_quantize_rows", "armor_linear_i8", "armor_packed_layer_i8_bytes", "armor_pack_layer_i8", "armor_apply_layer_i8",
-           "armor_block_norm", "armor_block_norm_backward",
+           "armor_block_norm", "armor_block_norm_backward", "armor_kv_write", "armor_kv_read", "armor_kv_attend",
            "armor_get_device_status",
            "armor_status_string", "armor_launch_count", "armor_gemm_timing_enable", "armor_gemm_timing",
            "armor_normalize_noalloc", "armor_block_product", "armor_block_product_dual", "armor_block_product_two_sided", "armor_selftest_wait_timeout", "armor_kernel_timing_enable", "armor_use_graphs", "armor_fuse_grams",
@@ -70,6 +70,19 @@ armor_block_norm_grad_args = _struct(
     ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("gate", C.c_void_p), *_gate_sizes,
     ("dw_post", C.c_void_p), ("dw_pre", C.c_void_p), ("dgate", C.c_void_p), *_norm_tail)
 
+armor_kv_cache = _struct(
+    "armor_kv_cache", *[(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")],
+    *[(n, C.c_int64) for n in ("n_pages", "page_size", "kv_heads", "head_dim", "page_stride", "head_stride", "slot_stride",
+                               "scale_page_stride", "scale_head_stride", "scale_slot_stride")])
+armor_kv_batch = _struct("armor_kv_batch", ("n_seqs", C.c_int64), ("max_pages", C.c_int64), ("ld_pages", C.c_int64),
+                         ("pages", C.c_void_p), ("lengths", C.c_void_p), ("starts", C.c_void_p))
+armor_kv_rows = _struct("armor_kv_rows", ("k", C.c_void_p), ("v", C.c_void_p), ("n_rows", C.c_int64),
+                        *[(n, C.c_int64) for n in ("k_row_stride", "k_head_stride", "v_row_stride", "v_head_stride")], ("dtype", C.c_int32))
+armor_kv_attend_args = _struct(
+    "armor_kv_attend_args", ("q", C.c_void_p), ("o", C.c_void_p),
+    *[(n, C.c_int64) for n in ("n_rows", "heads", "q_row_stride", "q_head_stride", "o_row_stride", "o_head_stride", "window", "max_chunk")],
+    ("scale", C.c_float), ("dtype", C.c_int32))
+
 STATS_DTYPE = np.dtype([("loss_start", "<f8"), ("loss_A", "<f8"), ("loss_B", "<f8"), ("loss_S", "<f8"),
                         ("loss_mask", "<f8"), ("delta_L_mask", "<f8"), ("tau_B", "<f4"), ("tau_S", "<f4"),
                         ("groups_changed", "<i4"), ("mask_accepted", "<i4"), ("chol_failed", "<i4"),
@@ -107,6 +120,8 @@ def lib() -> C.CDLL:
         L.armor_apply_layer_i8.argtypes = [vp, vp, vp, vp, i64, vp]
         L.armor_block_norm.argtypes = [vp, C.POINTER(armor_block_norm_args), vp]
         L.armor_block_norm_backward.argtypes = [vp, C.POINTER(armor_block_norm_grad_args), vp]
+        for f, g in (("write", armor_kv_rows), ("read", armor_kv_rows), ("attend", armor_kv_attend_args)):
+            getattr(L, "armor_kv_" + f).argtypes = [vp, C.POINTER(armor_kv_cache), C.POINTER(armor_kv_batch), C.POINTER(g), vp]
         L.armor_get_device_status.argtypes = [vp, C.POINTER(i32), i32]
         L.armor_status_string.argtypes = [C.c_int]
         L.armor_status_string.restype = C.c_char_p
@@ -528,6 +543,125 @@ def armor_block_norm_backward(ctx, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate,
                          pre, residual_scale, eps)
 
 
+class KvCache:
+    """A paged cache of int8 keys and values with an fp32 scale for each row: k and v [n_pages, kv_heads, page_size, head_dim], k_scale
+    and v_scale [n_pages, kv_heads, page_size], views in any order of the first three dimensions (k and v alike, k_scale and v_scale alike)
+    whose rows start on 16-byte boundaries.  It keeps the tensors and their layout; what they hold may change from call to call."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        for name, t, dtype, dims in (("k", k, torch.int8, 4), ("v", v, torch.int8, 4), ("k_scale", k_scale, torch.float32, 3),
+                                     ("v_scale", v_scale, torch.float32, 3)):
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor (this library has no CPU path)")
+            if t.device != k.device:
+                raise ValueError(f"{name} must be on {k.device}, as k is, not on {t.device}")
+            if t.dtype is not dtype or t.dim() != dims:
+                raise ValueError(f"{name} must be {dtype} with {dims} dimensions, got {t.dtype} {list(t.shape)}")
+            if t.shape != k.shape[:dims]:
+                raise ValueError(f"{name} must be {list(k.shape[:dims])}, got {list(t.shape)}")
+        if k.numel() == 0:
+            raise ValueError("the cache must hold a page")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("the rows of k and v must be contiguous")
+        steps, scale_steps = _steps(k), _steps(k_scale)
+        if steps != _steps(v) or scale_steps != _steps(v_scale):
+            raise ValueError("k and v, k_scale and v_scale must be laid out alike")
+        if min(steps) < k.size(3) or min(scale_steps) < 1:
+            raise ValueError("pages, heads and slots must not overlap")
+        if any(n % 16 for n in (*steps, k.data_ptr(), v.data_ptr())):
+            raise ValueError("rows of k and v must start on 16-byte boundaries")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.index = k.get_device()
+        self.n_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.args = armor_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), self.n_pages, self.page_size,
+                                   self.kv_heads, self.head_dim, *steps, *scale_steps)
+
+
+def _steps(t: torch.Tensor) -> list[int]:
+    """Strides of pages, heads and slots; of a dimension of one entry, whose stride says nothing, a row's."""
+    return [n if size > 1 else (t.size(3) if t.dim() == 4 else 1) for n, size in zip(t.stride()[:3], t.shape[:3])]
+
+
+class KvBatch:
+    """Sequences of a call on a cache (int32 tensors on its device): rows starts[b] .. starts[b + 1] - 1 of the packed arrays are the last
+    positions of sequence b, which has lengths[b] and its pages, in order, in pages[b].  It keeps the tensors; what they hold may
+    change from call to call, also under a captured one."""
+
+    def __init__(self, pages: torch.Tensor, lengths: torch.Tensor, starts: torch.Tensor):
+        for name, t, dims in (("pages", pages, 2), ("lengths", lengths, 1), ("starts", starts, 1)):
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor (this library has no CPU path)")
+            if t.device != pages.device:
+                raise ValueError(f"{name} must be on {pages.device}, as pages is, not on {t.device}")
+            if t.dtype is not torch.int32 or t.dim() != dims:
+                raise ValueError(f"{name} must be int32 with {dims} dimensions, got {t.dtype} {list(t.shape)}")
+        n, m = pages.shape
+        if lengths.numel() != n or starts.numel() != n + 1:
+            raise ValueError(f"{n} sequences have {n} lengths and {n + 1} starts, got {lengths.numel()} and {starts.numel()}")
+        if not lengths.is_contiguous() or not starts.is_contiguous() or (m > 1 and pages.stride(1) != 1) or (n > 1 and pages.stride(0) < m):
+            raise ValueError("lengths, starts and the rows of pages must be contiguous")
+        self.pages, self.lengths, self.starts = pages, lengths, starts
+        self.index = pages.get_device()
+        self.n_seqs = n
+        self.args = armor_kv_batch(n, m, pages.stride(0) if n > 1 else max(m, 1), pages.data_ptr(), lengths.data_ptr(), starts.data_ptr())
+
+
+def _heads_at(t: torch.Tensor, dtype, rows: int | None, heads: int | None, dim: int, name: str, here: int) -> tuple[int, int, int]:
+    """(address, stride of rows, stride of heads) of [rows, heads, dim] on device `here`."""
+    if t.get_device() != here:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor (this library has no CPU path)")
+        raise ValueError(f"{name} must be on cuda:{here}, the call's device, not on {t.device}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim or (rows is not None and shape[0] != rows) or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'heads' if heads is None else heads}, {dim}], got {list(shape)}")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), row if shape[0] > 1 else max(row, dim), head if shape[1] > 1 else max(head, dim)
+
+
+def _kv_rows(cache: KvCache, batch: KvBatch, k, v, here) -> armor_kv_rows:
+    if cache.index != here or batch.index != here:
+        raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, the call's device is cuda:{here}")
+    code = _row_dtype(k, "k")
+    kp, kr, kh = _heads_at(k, k.dtype, None, cache.kv_heads, cache.head_dim, "k", here)
+    vp, vr, vh = _heads_at(v, k.dtype, k.size(0), cache.kv_heads, cache.head_dim, "v", here)
+    return armor_kv_rows(kp, vp, k.size(0), kr, kh, vr, vh, code)
+
+
+def armor_kv_write(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
+    """The rows of k and v [rows, kv_heads, head_dim] rounded into the cache's pages (see armor.h)."""
+    code = lib().armor_kv_write(ctx, cache.args, batch.args, _kv_rows(cache, batch, k, v, _cuda_index(k, "k")), _stream())
+    if code:
+        _check(code, "armor_kv_write")
+
+
+def armor_kv_read(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
+    """The same rows of the cache, to k and v."""
+    code = lib().armor_kv_read(ctx, cache.args, batch.args, _kv_rows(cache, batch, k, v, _cuda_index(k, "k")), _stream())
+    if code:
+        _check(code, "armor_kv_read")
+
+
+def armor_kv_attend(ctx, cache: KvCache, batch: KvBatch, q, o, scale: float, window: int = 0, max_chunk: int = 0) -> None:
+    """o [rows, heads, head_dim] = attention of q over the cache (see armor.h)."""
+    here = _cuda_index(q, "q")
+    if cache.index != here or batch.index != here:
+        raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, q on cuda:{here}")
+    code = _row_dtype(q, "q")
+    dim = cache.head_dim
+    qp, qr, qh = _heads_at(q, q.dtype, None, None, dim, "q", here)
+    rows, heads, _ = q.shape
+    op, orow, oh = _heads_at(o, q.dtype, rows, heads, dim, "o", here)
+    code = lib().armor_kv_attend(ctx, cache.args, batch.args, armor_kv_attend_args(qp, op, rows, heads, qr, qh, orow, oh, window, max_chunk, scale, code),
+                                 _stream())
+    if code:
+        _check(code, "armor_kv_attend")
+
+
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
     buf = (C.c_int32 * n)()
     _check(lib().armor_get_device_status(ctx, buf, n), "armor_get_device_status")
@@ -862,6 +996,45 @@ class ArmorContext:
             out["dgate"] = dgate = _empty_rows(gate)
         _block_norm_backward(self.ctx, here, h, y, dh, dn, dx, dy, dw_post, dw_pre, dgate, True, gate, rows_per_gate, w_post, w_pre, post, pre,
                              residual_scale, eps)
+        return out
+
+    # -- a paged cache of keys and values, and the attention over it
+    def new_kv_cache(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int) -> KvCache:
+        """An empty cache of int8 keys and values."""
+        k, v = (torch.zeros(n_pages, kv_heads, page_size, head_dim, dtype=torch.int8, device=self.device) for _ in range(2))
+        return KvCache(k, v, *(torch.zeros(n_pages, kv_heads, page_size, dtype=torch.float32, device=self.device) for _ in range(2)))
+
+    def kv_write(self, cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Puts the new rows k and v [rows, kv_heads, head_dim] (fp32, bf16 or fp16) into the cache, rounded to int8 with a scale each."""
+        self._current()
+        armor_kv_write(self.ctx, cache, batch, k, v)
+
+    def kv_read(self, cache: KvCache, batch: KvBatch, rows: int, dtype: torch.dtype = torch.bfloat16, *,
+                out: tuple[torch.Tensor, torch.Tensor] | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+        """(k, v) [rows, kv_heads, head_dim] of the batch's positions as the cache holds them.  Rows behind the last sequence are left as
+        they are (in new tensors: not set)."""
+        here = self._current()
+        if out is None:
+            k, v = out = tuple(torch.empty(rows, cache.kv_heads, cache.head_dim, dtype=dtype, device=self.device) for _ in range(2))
+        else:
+            k, v = out
+            if k.size(0) != rows or k.dtype is not dtype:
+                raise ValueError(f"out must have {rows} rows of {dtype}, got {k.size(0)} of {k.dtype}")
+        if k.get_device() != here:
+            raise ValueError(f"out must be on {self.device}")
+        armor_kv_read(self.ctx, cache, batch, k, v)
+        return out
+
+    def kv_attend(self, cache: KvCache, batch: KvBatch, q: torch.Tensor, *, scale: float | None = None, window: int = 0, max_chunk: int = 0,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+        """Attention of q [rows, heads, head_dim] (bf16 or fp16) over the cache, each row over the positions of its sequence up to its own, the
+        last `window` of them if that is not 0; scale: head_dim ** -0.5.  The new rows' keys and values have been written.  Heads
+        share keys in groups of heads / kv_heads.  max_chunk: the most rows of a sequence, where the caller knows it (a hint).  Rows
+        behind the last sequence are left as they are (in a new tensor: not set)."""
+        self._current()
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        armor_kv_attend(self.ctx, cache, batch, q, out, cache.head_dim ** -0.5 if scale is None else scale, window, max_chunk)
         return out
 
     def device_status(self) -> list[int]:

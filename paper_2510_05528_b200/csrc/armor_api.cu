@@ -143,6 +143,7 @@ size_t carve(const armor_config& cfg, armor_ctx* c, char* base) {
   TAKE(tab_key, float*, (size_t)nbo * nbi * sizeof(float));
   TAKE(tab_g, unsigned long long*, (size_t)nbo * nbi * sizeof(unsigned long long));
   TAKE(status, int32_t*, ST_COUNT * sizeof(int32_t));
+  TAKE(kv_counters, int32_t*, ARMOR_KV_COUNTERS * sizeof(int32_t));
   TAKE(screen, int32_t*, 4 * sizeof(int32_t));
   TAKE(core_dense, int32_t*, sizeof(int32_t));
   TAKE(it_dev, int64_t*, sizeof(int64_t));
@@ -349,6 +350,7 @@ armor_status armor_create(armor_ctx** out, const armor_config* cfg, void* d_work
   c->ev_created = 0;
   carve(*cfg, c, c->ws);
   if (cudaMemset(c->status, 0, ST_COUNT * sizeof(int32_t)) != cudaSuccess) { delete c; return ARMOR_ERR_CUDA; }
+  if (cudaMemset(c->kv_counters, 0, ARMOR_KV_COUNTERS * sizeof(int32_t)) != cudaSuccess) { delete c; return ARMOR_ERR_CUDA; }
   if (cudaMemset(c->sc, 0, SC_COUNT * sizeof(double)) != cudaSuccess) { delete c; return ARMOR_ERR_CUDA; }
   *out = c;
   return ARMOR_OK;

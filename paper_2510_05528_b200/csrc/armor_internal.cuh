@@ -43,6 +43,7 @@ enum {
   ST_DEAD_CHANNELS = 8,  // zero diagonal entries of H in the last screened call (legal: the channel carries no weight)
   ST_POISON = 9,         // 1 while the last screened call had unusable inputs: its updates were all withheld
   ST_H_RANGE = 10,       // entries of the scaled H beyond the fp16 range (FP16X3; H not positive semidefinite): clamped
+  ST_KV_REFUSED = 11,    // pages of a cache's table out of range, sequences whose rows are (cumulative)
   ST_COUNT = 16
 };
 
@@ -59,6 +60,7 @@ struct SelRec {
   float old_val[8];
 };
 
+static const int ARMOR_KV_COUNTERS = 1024; // counters of the attention's cut units, one a CTA
 static const int ARMOR_GEMM_SLABS = 160;  // slabs of partial sums of cut tiles in the workspace
 static const int ARMOR_DOT_BLOCKS = 592;  // 4 x 148 partial sums per reduction
 
@@ -110,6 +112,7 @@ struct armor_ctx {
   float* tab_key;     // [nbo * nbi] winning race key of every block (single draw)
   unsigned long long* tab_g;   // its global group index
   int32_t* status;    // [ST_COUNT]
+  int32_t* kv_counters;  // [ARMOR_KV_COUNTERS] zero between calls
   int32_t* screen;    // [4] per-call counters of the input screening
   int32_t* core_dense;   // fp32 forward: 1 if the core is not 2:4, so that the dense product runs instead of the sparse one
   int64_t* it_dev;    // iteration index inside the running armor_bcd_step call (advanced by the first kernel of an iteration)

@@ -1,0 +1,538 @@
+// Attention of few rows a sequence (decoding) over a paged cache of int8 keys and values.
+//
+// A row is one query head of one new token; the rows of a key head's group share its keys.  With kq, vq the int8 rows and ks, vs their
+// scales, for a row of position p:
+//   t_j = (q . kq_j) ks_j scale log2 e + log2 vs_j     over j <= p (and j > p - window)
+//   w_j = 2^(t_j - m),  O = sum w_j vq_j,  l = sum w_j / vs_j,  o = O / l
+// m is a maximum of the t_j seen so far, so that w_j, the weight a value's bytes are taken with, is a factor of at most 2^LAZY and its rounding to
+// fp16 is one of 2^-12 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
+// a multiplication by a power of two; products and sums are fp32.  l is summed from the unrounded weights.  No row: zeros.
+//
+// Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time from memory straight to registers, in the
+// layout that mma.sync m16n8k16 wants of its M side, where a product over the dimensions may take them in any order: positions are the M side of
+// the scores, S^T = K Q^T, dimensions the M side of O^T = V^T P^T, rows of q the N side of both, eight at a time, so that for up to eight rows
+// nothing is computed twice and O takes dim / 4 registers.  (tcgen05 would multiply 128 rows for these eight.)  A byte becomes fp16 by a
+// permutation, 1024 + (byte + 128), and a subtraction.  Two warps of eight never meet before the end of a CTA's share.
+//
+// All positions of all (sequence, key head, tile of rows) units, 64 at a time, stand in one line that is cut into equal
+// shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
+// last, by a counter, adds them up in the order of the parts: no CTA waits for another and the bits do not depend on the run.
+#include "kv_cache.cuh"
+
+namespace {
+
+using namespace rows;
+using namespace kv;
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, STEP = 16 * WARPS;      // positions a step of a CTA
+constexpr int SEQS = 1024;                  // sequences a launch
+constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
+constexpr float LEAST = 7.888609e-31f;      // 2^-100: scales of values below count as this (their values are below 1e-28)
+
+template <int DIM, int NT>
+struct Few {
+  static constexpr int R = 8 * NT;          // rows of a tile
+  static constexpr int KW = DIM / 16;       // words of a key that a lane holds; steps of the scores' product
+  static constexpr int VB = DIM / 8;        // bytes of a value that a lane holds
+  static constexpr int PART = R * DIM + 2 * R;     // floats of a part: O, m, l
+  static constexpr int CTAS = NT == 1 ? 4 : 3;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// bytes of x (biased by 128) that `sel` picks, as fp16: 1024 + byte, exactly, less 1152
+__device__ __forceinline__ uint32_t bytes_half(uint32_t x, uint32_t sel) {
+  const uint32_t w = __byte_perm(x, 0x64646464u, sel);
+  const uint32_t off = 0x64806480u;         // 1152
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(off));
+  return r;
+}
+
+struct FewP {
+  KvAttend a;
+  int64_t limit;                            // rows of a sequence at most: those with more are left out
+  float* parts;                             // two of every CTA
+  int* counters;                            // one of every CTA, zero between calls
+  int min_steps;
+  int32_t* status;
+};
+
+struct Unit { int64_t per, steps; int tiles; };       // steps in all, of one unit; tiles of rows
+template <int R>
+__device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
+  Unit u{0, 0, 0};
+  const int64_t rows = (int64_t)s.n * p.a.group;
+  if (rows < 1 || rows > p.limit) return u;
+  u.tiles = (int)((rows + R - 1) / R);
+  const int64_t lo = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
+  u.steps = max((int64_t)1, ((int64_t)s.length + STEP - 1) / STEP - lo / STEP);
+  u.per = u.steps * u.tiles * p.a.c.heads;
+  return u;
+}
+
+// Sixteen positions of a warp on their way: keys lane / 4 and lane / 4 + 8, values 2 (lane % 4) + {0, 1, 8, 9}
+template <int DIM>
+struct Load {
+  uint32_t k[2][DIM / 16], v[4][DIM / 32];
+  float ks[2], vs[2];
+};
+// where the sixteen from position j on lie, if they share a page: the first one's row and scale
+struct Where { int64_t row, scale; int j; bool none; };
+
+template <typename T, int DIM, int NT>
+__global__ void __launch_bounds__(THREADS, Few<DIM, NT>::CTAS)
+kv_attend_few_kernel(const FewP p) {
+  grid_begin();
+  using F = Few<DIM, NT>;
+  constexpr int R = F::R;
+  __shared__ float sO[WARPS][R][DIM + 4];
+  __shared__ float sM[WARPS][R], sL[WARPS][R];
+  __shared__ int64_t scan[WARPS];
+  __shared__ int64_t at_base;
+  __shared__ int at_seq, last_one;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, part = lane & 3;
+  const Cache& c = p.a.c;
+  const Batch& b = p.a.b;
+
+  // ---- the line of all steps, this CTA's share of it and the sequence that it begins in
+  int64_t total, begin, end;
+  int n_ctas;
+  {
+    const int per = (b.n + THREADS - 1) / THREADS, s0 = min(b.n, (int)threadIdx.x * per), s1 = min(b.n, s0 + per);
+    int64_t mine = 0;
+    for (int i = s0; i < s1; ++i) {
+      bool bad;
+      const Seq s = sequence(b, i, bad);
+      if (bad && blockIdx.x == 0) report(p.status);
+      mine += units_of<R>(p, s).per;
+    }
+    int64_t up_to = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, up_to, o);
+      if (lane >= o) up_to += v;
+    }
+    if (lane == 31) scan[warp] = up_to;
+    __syncthreads();
+    total = 0;
+    int64_t before = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) before += scan[w];
+      total += scan[w];
+    }
+    n_ctas = (int)min((int64_t)gridDim.x, (total + p.min_steps - 1) / p.min_steps);
+    if ((int)blockIdx.x >= n_ctas) return;
+    begin = (int64_t)blockIdx.x * total / n_ctas;
+    end = (int64_t)(blockIdx.x + 1) * total / n_ctas;
+    int64_t base = before + up_to - mine;
+    if (base <= begin && begin < base + mine)
+      for (int i = s0; i < s1; ++i) {
+        bool bad;
+        const int64_t w = units_of<R>(p, sequence(b, i, bad)).per;
+        if (begin < base + w) { at_seq = i; at_base = base; break; }
+        base += w;
+      }
+    __syncthreads();
+  }
+  int seq = at_seq;
+  int64_t base = at_base;
+
+  while (begin < end) {
+    bool bad;
+    const Seq s = sequence(b, seq, bad);
+    const Unit un = units_of<R>(p, s);
+    if (begin >= base + un.per) { base += un.per; ++seq; continue; }
+    const int64_t unit = (begin - base) / un.steps, u0 = base + unit * un.steps;
+    const int first = (int)(begin - u0), count = (int)(min(end, u0 + un.steps) - begin);
+    const int head = (int)(unit / un.tiles), tile = (int)(unit - (int64_t)head * un.tiles);
+    const int rows = s.n * p.a.group - tile * R;        // of this tile, if fewer than R
+    const int64_t lo_all = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
+    const int step0 = (int)(lo_all / STEP) + first;
+
+    // ---- q: rows lane / 4 of each eight, four dimensions for each step of the product, in the order that keys come in
+    uint32_t q[NT][F::KW][2];
+    float factor;
+    {
+      const T* const t = nullptr;
+      float top = 0.f;
+      uint32_t raw[NT][F::KW][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int r = tile * R + n * 8 + quad;
+        const bool there = n * 8 + quad < rows;
+        const int i = there ? r / p.a.group : 0, g = there ? r - i * p.a.group : 0;
+        const T* const row = static_cast<const T*>(p.a.q) + (int64_t)(s.first + i) * p.a.q_row + (int64_t)(head * p.a.group + g) * p.a.q_head;
+#pragma unroll
+        for (int h = 0; h < DIM / 64; ++h) {
+          const int d = h * 64 + part * 16;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const Raw8<T> x = !there ? raw_zero<T>() : (p.a.aligned ? raw_load(row + d + 8 * e) : row_load<false>(row, d + 8 * e, DIM));
+            raw[n][h * 4 + 2 * e][0] = x.w.x; raw[n][h * 4 + 2 * e][1] = x.w.y;
+            raw[n][h * 4 + 2 * e + 1][0] = x.w.z; raw[n][h * 4 + 2 * e + 1][1] = x.w.w;
+          }
+        }
+      }
+      int shift = 0;
+      if (sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value) {
+        // bf16 in fp16: by the power of two that brings the largest finite |q| of the tile to [2^14, 2^15), so that what is lost is below 2^-39 of it
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int k = 0; k < F::KW; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 v = unpack2(t, raw[n][k][e]);
+              const float x = fabsf(v.x), y = fabsf(v.y);
+              if (x < __int_as_float(0x7f800000)) top = fmaxf(top, x);
+              if (y < __int_as_float(0x7f800000)) top = fmaxf(top, y);
+            }
+        top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+        shift = top > 0.f ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -120), 120) : 0;
+      }
+      const float up = __int_as_float((127 + shift) << 23);
+      factor = p.a.scale * __int_as_float((127 - shift) << 23);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < F::KW; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if (std::is_same<T, __half>::value) q[n][k][e] = raw[n][k][e];
+            else { const float2 v = unpack2(t, raw[n][k][e]); q[n][k][e] = half2_bits(v.x * up, v.y * up); }
+          }
+    }
+
+    // ---- the positions that rows 2 part and 2 part + 1 of each eight see: [low, high)
+    int low[NT][2], high[NT][2];
+    int inner_lo = 0, inner_hi = 0x7fffffff;            // what all of the tile's rows see
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = n * 8 + 2 * part + e;
+        low[n][e] = high[n][e] = 0;
+        if (r < rows) {
+          const int64_t at = (int64_t)s.length - s.n + (tile * R + r) / p.a.group;
+          high[n][e] = (int)max((int64_t)0, at + 1);
+          low[n][e] = p.a.window ? (int)max((int64_t)0, at + 1 - p.a.window) : 0;
+          inner_lo = max(inner_lo, low[n][e]);
+          inner_hi = min(inner_hi, high[n][e]);
+        }
+      }
+    inner_lo = __reduce_max_sync(0xffffffffu, inner_lo);
+    inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
+
+    const int last = max(s.length - 1, 0);
+    const bool shared = (c.page_size & 15u) == 0;          // sixteen positions share a page
+    // the place of position j, or any place in the cache for one that has none
+    auto at = [&](int j, Where& w) {
+      uint32_t page = 0, slot = 0;
+      w.none = !place(c, b, seq, (uint32_t)min(j, last), page, slot);
+      if (w.none) page = slot = 0;
+      w.row = page * c.page + head * c.head + slot * c.slot;
+      w.scale = page * c.spage + head * c.shead + slot * c.sslot;
+    };
+    auto find = [&](int j0, Where& w) {
+      if (shared) at(min(j0, last & ~15), w);
+      w.j = j0;
+    };
+    auto load_k = [&](Where& w, Load<DIM>& x) {
+      bool none = false;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = quad + 8 * e;
+        Where one{w.row + r * c.slot, w.scale + r * c.sslot, 0, false};
+        if (!shared) { at(w.j + r, one); none |= one.none; }
+#pragma unroll
+        for (int h = 0; h < DIM / 64; ++h) {
+          const uint4 v = *reinterpret_cast<const uint4*>(c.k + one.row + h * 64 + part * 16);
+          x.k[e][4 * h] = v.x; x.k[e][4 * h + 1] = v.y; x.k[e][4 * h + 2] = v.z; x.k[e][4 * h + 3] = v.w;
+        }
+        x.ks[e] = c.ks[one.scale];
+        x.vs[e] = c.vs[one.scale];
+      }
+      if (!shared) w.none = __any_sync(0xffffffffu, none);
+    };
+    auto load_v = [&](const Where& w, Load<DIM>& x) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 2 * part + (e & 1) + (e >> 1) * 8;
+        Where one{w.row + r * c.slot, 0, 0, false};
+        if (!shared) at(w.j + r, one);
+        const int8_t* const from = c.v + one.row + quad * F::VB;
+        if constexpr (DIM == 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(from);
+          x.v[e][0] = v.x; x.v[e][1] = v.y; x.v[e][2] = v.z; x.v[e][3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(from);
+          x.v[e][0] = v.x; x.v[e][1] = v.y;
+        }
+      }
+    };
+
+    float O[NT][DIM / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int d = 0; d < DIM / 16; ++d) O[n][d][0] = O[n][d][1] = O[n][d][2] = O[n][d][3] = 0.f;
+      m[n][0] = m[n][1] = -__int_as_float(0x7f800000);
+      l[n][0] = l[n][1] = 0.f;
+    }
+
+    Where w, next;                                        // of the sixteen whose values are next, and of those after them
+    Load<DIM> x;
+    find(step0 * STEP + warp * 16, w);
+    load_k(w, x);
+    load_v(w, x);
+    next = w;
+    if (count > 1) find((step0 + 1) * STEP + warp * 16, next);
+    for (int i = 0; i < count; ++i) {
+      const int j0 = w.j;
+      const bool bad_page = w.none;
+      if (bad_page && j0 < inner_hi && lane == 0) report(p.status);
+
+      // ---- scores
+      float t[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) t[n][0] = t[n][1] = t[n][2] = t[n][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < F::KW; ++k) {
+        const uint32_t a0 = x.k[0][k] ^ 0x80808080u, a1 = x.k[1][k] ^ 0x80808080u;
+        const uint32_t a[4] = {bytes_half(a0, 0x4140), bytes_half(a1, 0x4140), bytes_half(a0, 0x4342), bytes_half(a1, 0x4342)};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma(t[n], a, q[n][k][0], q[n][k][1]);
+      }
+      float ka[2], kb[2], kr[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float vs = x.vs[e] < LEAST ? LEAST : x.vs[e];
+        ka[e] = x.ks[e] * factor;
+        kb[e] = __log2f(vs);
+        kr[e] = __fdividef(1.f, vs);
+      }
+      if (i + 1 < count) load_k(next, x);                 // the next keys set out
+      const bool whole = !bad_page && j0 >= inner_lo && j0 + 16 <= inner_hi;
+      uint32_t P[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[n][e] = fmaf(t[n][e], ka[e >> 1], kb[e >> 1]);
+        float r[4] = {kr[0], kr[0], kr[1], kr[1]};
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + quad + 8 * (e >> 1);
+            if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) { t[n][e] = -__int_as_float(0x7f800000); r[e] = 0.f; }
+          }
+        }
+        // the sixteen's maxima, and m with them where it is passed by far
+        float top[2] = {fmaxf(t[n][0], t[n][2]), fmaxf(t[n][1], t[n][3])};
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
+          top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[n][0] + LAZY || top[1] > m[n][1] + LAZY)) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float to = fmaxf(m[n][e], top[e]);
+            f[e] = m[n][e] == to ? 1.f : exp2_fast(m[n][e] - to);       // (nothing yet: 2^-inf)
+            m[n][e] = to;
+            l[n][e] *= f[e];
+          }
+#pragma unroll
+          for (int d = 0; d < DIM / 16; ++d) { O[n][d][0] *= f[0]; O[n][d][1] *= f[1]; O[n][d][2] *= f[0]; O[n][d][3] *= f[1]; }
+        }
+        float wgt[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float mm = m[n][e & 1] == -__int_as_float(0x7f800000) ? 0.f : m[n][e & 1];
+          wgt[e] = exp2_fast(t[n][e] - mm);
+          l[n][e & 1] = fmaf(wgt[e], r[e], l[n][e & 1]);
+        }
+        P[n][0] = transpose8(half2_bits(wgt[0], wgt[1]));
+        P[n][1] = transpose8(half2_bits(wgt[2], wgt[3]));
+      }
+
+      // ---- O^T += V^T P^T: a lane's dimensions quad DIM / 8 + 2 d, + 1
+#pragma unroll
+      for (int h = 0; h < DIM / 32; ++h) {
+        uint32_t V[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) V[e] = x.v[e][h] ^ 0x80808080u;
+        const uint32_t a01 = __byte_perm(V[0], V[1], 0x5140), b01 = __byte_perm(V[0], V[1], 0x7362);
+        const uint32_t a23 = __byte_perm(V[2], V[3], 0x5140), b23 = __byte_perm(V[2], V[3], 0x7362);
+        const uint32_t lo[4] = {bytes_half(a01, 0x4140), bytes_half(a01, 0x4342), bytes_half(a23, 0x4140), bytes_half(a23, 0x4342)};
+        const uint32_t hi[4] = {bytes_half(b01, 0x4140), bytes_half(b01, 0x4342), bytes_half(b23, 0x4140), bytes_half(b23, 0x4342)};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma(O[n][2 * h], lo, P[n][0], P[n][1]);
+          mma(O[n][2 * h + 1], hi, P[n][0], P[n][1]);
+        }
+      }
+      if (i + 1 < count) {                                // and the next values
+        w = next;
+        load_v(w, x);
+        if (i + 2 < count) find((step0 + i + 2) * STEP + warp * 16, next);
+      }
+    }
+
+    // ---- the four warps' sums to one
+    __syncthreads();                                      // (what a previous unit left has been read)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], o);
+        const int r = n * 8 + 2 * part + e;
+        if (quad == 0) { sM[warp][r] = m[n][e]; sL[warp][r] = l[n][e]; }
+#pragma unroll
+        for (int d = 0; d < DIM / 16; ++d)
+          *reinterpret_cast<float2*>(&sO[warp][r][quad * F::VB + 2 * d]) = make_float2(O[n][d][e], O[n][d][e + 2]);
+      }
+    }
+    __syncthreads();
+    const bool cut = count < un.steps;
+    float* const parts = p.parts;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first == 0 ? 1 : 0);
+    auto put = [&](int r, int d, float4 o, float l) {     // four dimensions of a row of the output
+      const float inv = l == 0.f ? 0.f : 1.f / l;         // (a row that sees nothing: zeros)
+      const int rr = tile * R + r, i = rr / p.a.group, g = rr - i * p.a.group;
+      T* const to = static_cast<T*>(p.a.o) + (int64_t)(s.first + i) * p.a.o_row + (int64_t)(head * p.a.group + g) * p.a.o_head + d;
+      if (p.a.aligned) {
+        const T* const t = nullptr;
+        *reinterpret_cast<uint2*>(to) = make_uint2(pack2(t, o.x * inv, o.y * inv), pack2(t, o.z * inv, o.w * inv));
+      } else {
+        to[0] = from_f<T>(o.x * inv); to[1] = from_f<T>(o.y * inv); to[2] = from_f<T>(o.z * inv); to[3] = from_f<T>(o.w * inv);
+      }
+    };
+    auto weight = [](float m, float top) { return m == -__int_as_float(0x7f800000) ? 0.f : exp2_fast(m - top); };
+    for (int u = threadIdx.x; u < R * (DIM / 4); u += THREADS) {
+      const int r = u / (DIM / 4), d = u % (DIM / 4) * 4;
+      if (r >= rows) break;
+      float top = sM[0][r];
+#pragma unroll
+      for (int w2 = 1; w2 < WARPS; ++w2) top = fmaxf(top, sM[w2][r]);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float sum = 0.f;
+#pragma unroll
+      for (int w2 = 0; w2 < WARPS; ++w2) {
+        const float f = weight(sM[w2][r], top);
+        const float4 v = *reinterpret_cast<const float4*>(&sO[w2][r][d]);
+        sum = fmaf(f, sL[w2][r], sum);
+        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+      }
+      if (!cut) { put(r, d, o, sum); continue; }
+      float* const to = parts + slot * F::PART;
+      *reinterpret_cast<float4*>(to + r * DIM + d) = o;
+      if (d == 0) { to[R * DIM + r] = top; to[R * DIM + R + r] = sum; }
+    }
+    if (cut) {
+      // ---- the parts of the unit: those of the CTAs from the one that holds its first step to the one that holds its last
+      __threadfence();
+      __syncthreads();
+      const int64_t c0 = ((u0 + 1) * n_ctas - 1) / total, c1 = ((u0 + un.steps) * n_ctas - 1) / total;
+      if (threadIdx.x == 0) {
+        const int had = atomicAdd(&p.counters[c0], 1);
+        last_one = had == (int)(c1 - c0);
+        if (last_one) p.counters[c0] = 0;
+      }
+      __syncthreads();
+      if (last_one) {
+        __threadfence();
+        for (int u = threadIdx.x; u < R * (DIM / 4); u += THREADS) {
+          const int r = u / (DIM / 4), d = u % (DIM / 4) * 4;
+          if (r >= rows) break;
+          float top = -__int_as_float(0x7f800000);
+          for (int64_t k = c0; k <= c1; ++k) top = fmaxf(top, __ldcg(parts + (2 * k + (k == c0)) * F::PART + R * DIM + r));
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+          float sum = 0.f;
+#pragma unroll 4
+          for (int64_t k = c0; k <= c1; ++k) {
+            const float* const from = parts + (2 * k + (k == c0)) * F::PART;
+            const float f = weight(__ldcg(from + R * DIM + r), top);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(from + r * DIM + d));
+            sum = fmaf(f, __ldcg(from + R * DIM + R + r), sum);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+          }
+          put(r, d, o, sum);
+        }
+      }
+    }
+    begin += count;
+  }
+}
+
+}  // namespace
+
+namespace {
+
+template <typename T, int DIM, int NT>
+void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
+  using F = Few<DIM, NT>;
+  // two parts a CTA have to find room in the workspace (a single CTA leaves none)
+  int64_t n = (int64_t)c->n_sm * F::CTAS;
+  const int64_t room = ws_scratch_bytes(c) / (2 * F::PART * (int64_t)sizeof(float));
+  if (n > room) n = room;
+  if (n > ARMOR_KV_COUNTERS) n = ARMOR_KV_COUNTERS;
+  if (n < 1) n = 1;
+  const Batch all = p.a.b;
+  for (int b0 = 0; b0 < all.n; b0 += SEQS) {
+    p.a.b.n = all.n - b0 < SEQS ? all.n - b0 : SEQS;
+    p.a.b.lengths = all.lengths + b0;
+    p.a.b.starts = all.starts + b0;
+    p.a.b.pages = all.pages + b0 * all.ld;
+    launch_dependent(kv_attend_few_kernel<T, DIM, NT>, dim3((unsigned)n), dim3(THREADS), 0, s, p);
+    c->launches++;
+  }
+}
+template <typename T, int DIM>
+void launch_by_rows(armor_ctx* c, const FewP& p, int64_t rows, cudaStream_t s) {
+  if (rows <= 8) launch_typed<T, DIM, 1>(c, p, s);
+  else launch_typed<T, DIM, 2>(c, p, s);
+}
+
+}  // namespace
+
+armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s) {
+  FewP p;
+  p.a = a;
+  p.limit = limit;
+  p.status = c->status;
+  p.counters = c->kv_counters;
+  p.parts = c->T;
+  p.min_steps = 2;
+  const int64_t rows = (a.max_chunk ? a.max_chunk : (a.b.rows + a.b.n - 1) / a.b.n) * a.group;
+  KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
+  if (a.dtype == ARMOR_DTYPE_BF16) {
+    if (a.dim == 64) launch_by_rows<__nv_bfloat16, 64>(c, p, rows, s);
+    else launch_by_rows<__nv_bfloat16, 128>(c, p, rows, s);
+  } else {
+    if (a.dim == 64) launch_by_rows<__half, 64>(c, p, rows, s);
+    else launch_by_rows<__half, 128>(c, p, rows, s);
+  }
+  return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
+}

@@ -1,0 +1,100 @@
+// A paged cache of keys and values as int8 rows with a scale each, seen from a kernel: where a sequence's positions lie, and which rows of the
+// packed arrays are whose.  Nothing that a table or an offset holds is trusted: what it names outside of the arrays is neither read nor
+// written, and raises a status word.
+#pragma once
+#include "rows_io.cuh"
+
+namespace kv {
+
+struct Cache {
+  int8_t *k, *v;
+  float *ks, *vs;
+  int64_t page, head, slot;                 // strides of the values, in elements
+  int64_t spage, shead, sslot;              // strides of the scales
+  uint32_t n_pages, page_size;
+  uint32_t mul; int shift;                  // p / page_size = p mul >> shift for p < 2^31
+  int heads;
+};
+struct Batch {
+  const int32_t *pages, *lengths, *starts;
+  int64_t ld;
+  int n, max_pages;
+  int64_t rows;                             // rows of the packed arrays
+};
+
+// (the rounded-up reciprocal: with 2^(s-1) < d <= 2^s, m = ceil(2^(31+s) / d) is at most 2^32 - 1 for d > 1 and
+// exceeds 2^(31+s) / d by less than one, so that p m >> (31 + s) is p / d for all p < 2^31; d = 1: m = 2^31, s = 0)
+inline void divisor(uint32_t d, uint32_t& mul, int& shift) {
+  int s = 0;
+  while ((1ull << s) < d) ++s;
+  mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+  shift = 31 + s;
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t p, uint32_t mul, int shift) { return (uint32_t)(((uint64_t)p * mul) >> shift); }
+
+// what a sequence is made of: n new rows from row `first` on, the last n of `length` positions
+struct Seq { int first, n, length; };
+__device__ __forceinline__ Seq sequence(const Batch& b, int at, bool& bad) {
+  Seq s;
+  s.first = b.starts[at];
+  const int64_t n = (int64_t)b.starts[at + 1] - s.first;
+  s.length = max(b.lengths[at], 0);
+  bad = s.first < 0 || n < 0 || s.first + n > b.rows;
+  s.n = bad ? 0 : (int)n;
+  return s;
+}
+__device__ __forceinline__ void report(int32_t* status) {
+  atomicAdd(&status[ST_KV_REFUSED], 1);
+  status[ST_LAST_ERR] = ARMOR_ERR_INVALID_ARG;
+}
+
+// The sequence of row t, by a whole warp (t may differ between lanes): 32 offsets are compared at a time.  -1: behind the last one.
+__device__ __forceinline__ int sequence_of(const Batch& b, int64_t t) {
+  const int lane = threadIdx.x & 31;
+  int mine = -2;
+  for (;;) {
+    const unsigned open = __ballot_sync(0xffffffffu, mine == -2);
+    if (!open) return mine;
+    const int64_t row = __shfl_sync(0xffffffffu, t, __ffs(open) - 1);
+    // how many of starts[1 .. n] are at most `row`: the sequence that holds it
+    int lo = 0, hi = b.n;                   // the count lies in [lo, hi]
+    while (hi > lo) {
+      const int step = (hi - lo + 31) >> 5;
+      const int i = lo + (lane + 1) * step; // starts[i] is looked at: the count is at least i where it is at most `row`
+      const bool at_most = i <= hi && b.starts[i] <= row;
+      const int c = __popc(__ballot_sync(0xffffffffu, at_most));
+      lo += c * step;
+      if (step == 1) break;
+      hi = min(hi, lo + step - 1);
+    }
+    const int found = lo < b.n ? lo : -1;
+    const int64_t first = found < 0 ? 0 : b.starts[found], last = found < 0 ? 0 : b.starts[found + 1];
+    if (mine == -2 && (t == row || (found >= 0 && t >= first && t < last))) mine = found;
+  }
+}
+
+// Page and slot of position p of sequence `at`; false where the table has none
+__device__ __forceinline__ bool place(const Cache& c, const Batch& b, int at, uint32_t p, uint32_t& page, uint32_t& slot) {
+  const uint32_t i = quotient(p, c.mul, c.shift);
+  slot = p - i * c.page_size;
+  if (i >= (uint32_t)b.max_pages) return false;
+  page = (uint32_t)b.pages[(int64_t)at * b.ld + i];
+  return page < c.n_pages;
+}
+
+}  // namespace kv
+
+// kv_attend_few.cu, kv_attend_tcgen05.cu
+struct KvAttend {
+  kv::Cache c;
+  kv::Batch b;
+  const void* q; int64_t q_row, q_head;
+  void* o; int64_t o_row, o_head;
+  int group, dim;
+  int dtype;
+  int64_t window;                           // 0: none
+  int64_t max_chunk;                        // rows of a sequence expected; 0: not known
+  float scale;                              // of the scores, times log2 e
+  int aligned;                              // rows of q and o start on 16-byte boundaries
+};
+armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s);
