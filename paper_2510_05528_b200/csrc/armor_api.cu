@@ -144,6 +144,7 @@ size_t carve(const armor_config& cfg, armor_ctx* c, char* base) {
   TAKE(tab_g, unsigned long long*, (size_t)nbo * nbi * sizeof(unsigned long long));
   TAKE(status, int32_t*, ST_COUNT * sizeof(int32_t));
   TAKE(kv_counters, int32_t*, ARMOR_KV_COUNTERS * sizeof(int32_t));
+  TAKE(kv_cuts, int32_t*, ARMOR_KV_COUNTERS * 4 * sizeof(int32_t));
   TAKE(screen, int32_t*, 4 * sizeof(int32_t));
   TAKE(core_dense, int32_t*, sizeof(int32_t));
   TAKE(it_dev, int64_t*, sizeof(int64_t));

@@ -113,6 +113,7 @@ struct armor_ctx {
   unsigned long long* tab_g;   // its global group index
   int32_t* status;    // [ST_COUNT]
   int32_t* kv_counters;  // [ARMOR_KV_COUNTERS] zero between calls
+  int32_t* kv_cuts;      // [ARMOR_KV_COUNTERS][4] units of the attention that were cut, written and read within a call
   int32_t* screen;    // [4] per-call counters of the input screening
   int32_t* core_dense;   // fp32 forward: 1 if the core is not 2:4, so that the dense product runs instead of the sparse one
   int64_t* it_dev;    // iteration index inside the running armor_bcd_step call (advanced by the first kernel of an iteration)

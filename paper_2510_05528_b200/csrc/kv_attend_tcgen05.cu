@@ -1,0 +1,709 @@
+// Attention of chunks of new tokens over a paged cache of int8 keys and values, on the tensor cores (tcgen05).  The formulas are those of
+// kv_attend_few.cu: S = Q Kq^T in fp32, t = S ks factor + log2 vs, weights 2^(t - m) in fp16, O = W Vq, l = sum w / vs, o = O / l.
+//
+// A unit is a tile of 256 rows (a token and a head of the group each; the heads of a group share keys) of one sequence and key head against the
+// blocks of 128 positions that its rows see.  A CTA takes it as two halves of 128 rows, so that the tensor cores have the one half's
+// products while the other's weights are formed:
+//   warps 0-3, 4-7 : the rows of a half each, a thread a row: S from tensor memory, weights back in its place, O rescaled there when the maximum moves by
+//                    far (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16)
+//   warps 8-11     : keys and values from their pages through registers to fp16 in shared memory, two blocks of each, loaded a block ahead; the
+//                    three numbers of a position (ks factor, log2 vs, 1 / vs)
+//   warp 12        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
+// Tensor memory: S of either half (128 columns each; W in its first 64), O of either half.
+//
+// All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
+// workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
+// that no barrier is missed, and the status says that its output is worthless.
+#include "kv_cache.cuh"
+#include "tc_common.cuh"
+
+namespace {
+
+using namespace rows;
+using namespace kv;
+using namespace tc;
+
+constexpr int THREADS = 512, HALF = 128, ROWS = 2 * HALF, KEYS = 128;
+constexpr int SEQS = 1024;                  // sequences a launch
+constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
+constexpr float LEAST = 7.888609e-31f;
+constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
+
+template <int DIM>
+struct Tile {
+  static constexpr int CHUNK = 128 * 128;                       // 128 rows of 64 fp16
+  static constexpr int BYTES = DIM / 64 * CHUNK;                // 128 rows of q, keys or values
+  static constexpr int PART = ROWS * (DIM + 2);                 // floats of a part: O, m, l
+  // Q of both halves, two blocks of K, of V, two blocks of a position's three numbers
+  static constexpr int Q0 = 0, K0 = 2 * BYTES, V0 = 4 * BYTES, C0 = 6 * BYTES;
+  static constexpr int CONSTS = 3 * KEYS * 4;
+  static constexpr size_t SMEM = C0 + 2 * CONSTS + 1024;
+};
+
+struct Cut { int seq, head, tile, last; };  // a unit whose first part is this CTA's; last: the CTA of its last part (-1: none)
+
+struct TileP {
+  KvAttend a;
+  int64_t limit;                            // sequences of so many rows or fewer are left out
+  float* parts;                             // two of every CTA
+  Cut* cuts;                                // one of every CTA
+  int whole;                                // no room for parts: units are not cut
+  int32_t* status;
+};
+
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
+__device__ __forceinline__ uint32_t bytes_half(uint32_t x, uint32_t sel) {       // (kv_attend_few.cu)
+  const uint32_t w = __byte_perm(x, 0x64646464u, sel);
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));
+  return r;
+}
+__device__ __forceinline__ void put16(uint32_t at, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float4 get16(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// fp16 operands, fp32 sums; M = 128
+__device__ __forceinline__ uint32_t idesc_f16(int n, int b_mn) {
+  return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+__device__ __forceinline__ void umma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
+      : "memory");
+}
+// 32 columns of a warp's lanes; the caller waits
+__device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---------------------------------------------------------------- units
+// The blocks that a tile's rows see, from `block` on
+struct Blocks { int block, count; };
+__device__ __forceinline__ Blocks blocks_of(const KvAttend& a, const Seq& s, int tile) {
+  const int rows = s.n * a.group, r0 = tile * ROWS, r1 = min(rows, r0 + ROWS) - 1;
+  const int64_t at = (int64_t)s.length - s.n;
+  const int64_t hi = max((int64_t)0, at + r1 / a.group + 1);
+  const int64_t lo = a.window ? max((int64_t)0, at + r0 / a.group + 1 - a.window) : 0;
+  Blocks b;
+  b.block = (int)(lo / KEYS);
+  b.count = max(1, (int)((hi + KEYS - 1) / KEYS) - b.block);
+  return b;
+}
+__device__ __forceinline__ int tiles_of(const TileP& p, const Seq& s) {
+  const int64_t rows = (int64_t)s.n * p.a.group;
+  return rows > p.limit ? (int)((rows + ROWS - 1) / ROWS) : 0;
+}
+
+// A CTA's share as segments of units, in the same order for all warps
+struct Segments {
+  const TileP& p;
+  const int64_t* prefix;                    // [n + 1] blocks ahead of a sequence
+  int64_t left;                             // blocks of the share from this segment on
+  int seq, head, tile, tiles;
+  Seq s;
+  int first, count, total, block;           // of the segment: its first block in the unit, its blocks, the unit's, the position block of first
+  __device__ __forceinline__ Segments(const TileP& p_, const int64_t* prefix_) : p(p_), prefix(prefix_) {}
+  __device__ __forceinline__ void load() {
+    bool bad;
+    s = sequence(p.a.b, seq, bad);
+    tiles = tiles_of(p, s);
+  }
+  __device__ __forceinline__ void set(int off) {
+    const Blocks b = blocks_of(p.a, s, tile);
+    total = b.count;
+    first = off;
+    block = b.block + off;
+    count = p.whole ? b.count : (int)min(left, (int64_t)(b.count - off));
+  }
+  // by whole warps: the unit of block `begin` of the line, in sequence seq_
+  __device__ __forceinline__ void start(int64_t begin, int64_t end, int seq_) {
+    left = end - begin;
+    if (left <= 0) return;
+    seq = seq_;
+    load();
+    const int64_t a_head = (prefix[seq + 1] - prefix[seq]) / p.a.c.heads, off = begin - prefix[seq];
+    head = (int)(off / a_head);
+    int64_t rem = off - head * a_head;
+    const int lane = threadIdx.x & 31;
+    for (int t0 = 0;; t0 += 32) {
+      const int t = t0 + lane;
+      const int mine = t < tiles ? blocks_of(p.a, s, t).count : 0;
+      int64_t upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, upto > rem);
+      if (past || t0 + 32 >= tiles) {
+        const int l = past ? __ffs(past) - 1 : 0;
+        tile = t0 + l;
+        rem -= __shfl_sync(0xffffffffu, upto, l) - __shfl_sync(0xffffffffu, mine, l);
+        break;
+      }
+      rem -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    set((int)rem);
+    if (p.whole && first > 0) {             // the unit is that of the CTA where it begins
+      left -= total - first;
+      advance();
+    }
+  }
+  __device__ __forceinline__ void advance() {
+    if (left <= 0) return;
+    if (++tile == tiles) {
+      tile = 0;
+      if (++head == p.a.c.heads) {
+        head = 0;
+        do { ++seq; } while (seq < p.a.b.n && prefix[seq + 1] == prefix[seq]);
+        if (seq >= p.a.b.n) { left = 0; return; }
+        load();
+      }
+    }
+    set(0);
+  }
+  __device__ __forceinline__ bool more() const { return left > 0; }
+  __device__ __forceinline__ void next() { left -= count; advance(); }
+  __device__ __forceinline__ int rows() const { return s.n * p.a.group - tile * ROWS; }      // of the tile, if fewer than ROWS
+  __device__ __forceinline__ bool cut() const { return count < total; }
+};
+
+// one row of q as fp16 in shared memory, rows of 128 bytes, swizzled
+template <typename T, int DIM>
+__device__ __forceinline__ void put_row(uint32_t base, int row, const uint4 (&raw)[DIM / 8], float up) {
+  const T* const t = nullptr;
+#pragma unroll
+  for (int c = 0; c < DIM / 8; ++c) {
+    uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+    if (!std::is_same<T, __half>::value) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { const float2 v = unpack2(t, w[i]); w[i] = pack2(static_cast<const __half*>(nullptr), v.x * up, v.y * up); }
+    }
+    put16(base + (c >> 3) * Tile<DIM>::CHUNK + row * 128 + (((c & 7) ^ (row & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void put_out(const KvAttend& a, T* to, const float (&v)[32]) {
+  if (a.aligned) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float w[8] = {v[8 * c], v[8 * c + 1], v[8 * c + 2], v[8 * c + 3], v[8 * c + 4], v[8 * c + 5], v[8 * c + 6], v[8 * c + 7]};
+      store8(to + 8 * c, w);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) to[i] = from_f<T>(v[i]);
+  }
+}
+
+template <typename T, int DIM>
+__global__ void __launch_bounds__(THREADS, 1)
+kv_attend_tile_kernel(const TileP p) {
+  using L = Tile<DIM>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  __shared__ __align__(8) uint64_t bars[18];
+  __shared__ int64_t prefix[SEQS + 1];
+  __shared__ float tops[2][8], factors[2];
+  __shared__ uint32_t tmem_base_holder;
+  __shared__ int abort_flag, at_seq;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar0 = smem_u32(&bars[0]);
+  // (a pair each)
+  const uint32_t q_full = bar0, s_full = bar0 + 16, p_full = bar0 + 32, o_full = bar0 + 48, k_full = bar0 + 64, k_empty = bar0 + 80, v_full = bar0 + 96,
+                 v_empty = bar0 + 112, c_full = bar0 + 128;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full + 8 * i, HALF);
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, HALF);
+      mbar_init(o_full + 8 * i, 1);
+      mbar_init(k_full + 8 * i, 128);
+      mbar_init(k_empty + 8 * i, 1);
+      mbar_init(v_full + 8 * i, 128);
+      mbar_init(v_empty + 8 * i, 1);
+      mbar_init(c_full + 8 * i, 128);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_holder)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_begin();
+  const uint32_t tmem = tmem_base_holder;
+  volatile int* const abortp = &abort_flag;
+  const Cache& c = p.a.c;
+  const Batch& b = p.a.b;
+
+  // ---- the line of all blocks, this CTA's share of it and the sequence that it begins in
+  for (int i = warp; i < b.n; i += THREADS / 32) {
+    bool bad;
+    const Seq s = sequence(b, i, bad);
+    if (bad && blockIdx.x == 0 && lane == 0) report(p.status);
+    const int tiles = tiles_of(p, s);
+    int64_t sum = 0;
+    for (int t = lane; t < tiles; t += 32) sum += blocks_of(p.a, s, t).count;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) prefix[i + 1] = sum * c.heads;
+  }
+  if (threadIdx.x == 0) at_seq = 0;
+  __syncthreads();
+  if (warp == 0) {
+    const int per = (b.n + 31) / 32, i0 = min(b.n, lane * per), i1 = min(b.n, i0 + per);
+    int64_t sum = 0;
+    for (int i = i0; i < i1; ++i) sum += prefix[i + 1];
+    int64_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    int64_t run = upto - sum;
+    if (lane == 0) prefix[0] = 0;
+    for (int i = i0; i < i1; ++i) { run += prefix[i + 1]; prefix[i + 1] = run; }
+  }
+  __syncthreads();
+  const int64_t total = prefix[b.n];
+  const int n_ctas = (int)min((int64_t)gridDim.x, total);
+  const bool idle = (int)blockIdx.x >= n_ctas;
+  const int64_t begin = idle ? 0 : (int64_t)blockIdx.x * total / n_ctas, end = idle ? 0 : (int64_t)(blockIdx.x + 1) * total / n_ctas;
+  for (int i = threadIdx.x; i < b.n; i += THREADS)
+    if (prefix[i] <= begin && begin < prefix[i + 1]) at_seq = i;
+  if (threadIdx.x == 0) p.cuts[blockIdx.x].last = -1;
+  __syncthreads();
+  Segments at(p, prefix);
+  at.start(begin, end, at_seq);
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int half = warp >> 2, row = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + half * 128 + lanes, tO = tmem + 256 + half * 128 + lanes;
+    uint32_t seg = 0, blocks = 0, turn = 0, done = 0;                   // segments, blocks of the CTA, blocks and segments of this half
+    for (; at.more(); at.next(), ++seg) {
+      const int rows = at.rows() - half * HALF;                         // of this half
+      const bool there = row < rows;
+      const int r = there ? at.tile * ROWS + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
+      const int64_t out_row = (int64_t)(at.s.first + tok), out_head = (int64_t)(at.head * p.a.group + g);
+      // ---- q
+      {
+        uint4 raw[DIM / 8];
+        const T* const from = static_cast<const T*>(p.a.q) + out_row * p.a.q_row + out_head * p.a.q_head;
+#pragma unroll
+        for (int i = 0; i < DIM / 8; ++i)
+          raw[i] = !there ? make_uint4(0u, 0u, 0u, 0u) : (p.a.aligned ? raw_load(from + 8 * i).w : row_load<false>(from, 8 * i, DIM).w);
+        int shift = 0;
+        if (std::is_same<T, __nv_bfloat16>::value) {
+          // by the power of two that brings the largest finite |q| of the tile to [2^14, 2^15): what is lost is below 2^-39 of it
+          unsigned top = 0;
+#pragma unroll
+          for (int i = 0; i < DIM / 8; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t lo = w[k] & 0x7fffu, hi = (w[k] >> 16) & 0x7fffu;
+              if (lo < 0x7f80u) top = max(top, lo);
+              if (hi < 0x7f80u) top = max(top, hi);
+            }
+          }
+          top = __reduce_max_sync(0xffffffffu, top);
+          if (lane == 0) tops[seg & 1][warp] = __uint_as_float(top);
+          barrier(1, ROWS);
+          top = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(tops[seg & 1][i]));
+          shift = top ? min(max(14 - ((int)(top >> 7) - 127), -120), 120) : 0;
+        }
+        if (threadIdx.x == 0) factors[seg & 1] = p.a.scale * __int_as_float((127 - shift) << 23);
+        if (rows > 0) {
+          put_row<T, DIM>(smem + L::Q0 + half * L::BYTES, row, raw, __int_as_float((127 + shift) << 23));
+          fence_proxy_async();
+          mbar_arrive(q_full + 8 * half);
+        }
+      }
+      if (rows <= 0) { blocks += at.count; continue; }
+      // ---- the positions that the row sees: [low, high)
+      int low = 0, high = 0x7fffffff;                                   // (a row that does not exist: whatever costs nothing)
+      if (there) {
+        const int64_t pos = (int64_t)at.s.length - at.s.n + tok;
+        high = (int)max((int64_t)0, pos + 1);
+        low = p.a.window ? (int)max((int64_t)0, pos + 1 - p.a.window) : 0;
+      }
+      float m = minus_inf();
+      F2 l = f2(0.f);
+      for (int i = 0; i < at.count; ++i, ++blocks, ++turn) {
+        const int j0 = (at.block + i) * KEYS;
+        const uint32_t consts = smem + L::C0 + (blocks & 1) * L::CONSTS;
+        mbar_wait_warp(c_full + 8 * (blocks & 1), (blocks >> 1) & 1, abortp, p.status);
+        mbar_wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);
+        tc_fence_after();
+        uint32_t raw[128];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_get32(tS + 32 * k, raw + 32 * k);
+        tmem_wait_ld();
+        F2 t[64];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const float4 fa = get16(consts + 16 * k), fb = get16(consts + KEYS * 4 + 16 * k);
+          t[2 * k] = f2_fma(f2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), f2(fa.x, fa.y), f2(fb.x, fb.y));
+          t[2 * k + 1] = f2_fma(f2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), f2(fa.z, fa.w), f2(fb.z, fb.w));
+        }
+        const bool masked = __any_sync(0xffffffffu, j0 < low || j0 + KEYS > high);
+        if (masked) {
+#pragma unroll
+          for (int k = 0; k < 64; ++k) {
+            float2 v = f2_get(t[k]);
+            if (j0 + 2 * k < low || j0 + 2 * k >= high) v.x = minus_inf();
+            if (j0 + 2 * k + 1 < low || j0 + 2 * k + 1 >= high) v.y = minus_inf();
+            t[k] = f2(v.x, v.y);
+          }
+        }
+        float top = minus_inf();
+#pragma unroll
+        for (int k = 0; k < 64; ++k) { const float2 v = f2_get(t[k]); top = fmaxf(top, fmaxf(v.x, v.y)); }
+        if (__any_sync(0xffffffffu, top > m + LAZY)) {
+          // (S has come behind the product of the block before: O is at rest)
+          const float to = fmaxf(m, top), f = m == to ? 1.f : exp2_fast(m - to);
+          if (i > 0) {
+#pragma unroll 1
+            for (int k = 0; k < DIM / 32; ++k) {
+              uint32_t o[32];
+              tmem_get32(tO + 32 * k, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st32(tO + 32 * k, o);
+            }
+          }
+          l = f2_mul(l, f2(f));
+          m = to;
+        }
+        const F2 minus_m = f2(m == minus_inf() ? 0.f : -m);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[32];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float4 fr = get16(consts + 2 * KEYS * 4 + 16 * (16 * h + k));
+            const float2 x = f2_get(f2_add(t[32 * h + 2 * k], minus_m)), y = f2_get(f2_add(t[32 * h + 2 * k + 1], minus_m));
+            const float4 e = make_float4(exp2_fast(x.x), exp2_fast(x.y), exp2_fast(y.x), exp2_fast(y.y));
+            if (masked) {                                               // (what is not seen may be no number)
+              const int j = j0 + 64 * h + 4 * k;
+              if (j < low || j >= high) fr.x = 0.f;
+              if (j + 1 < low || j + 1 >= high) fr.y = 0.f;
+              if (j + 2 < low || j + 2 >= high) fr.z = 0.f;
+              if (j + 3 < low || j + 3 >= high) fr.w = 0.f;
+            }
+            l = f2_fma(f2(e.x, e.y), f2(fr.x, fr.y), l);
+            l = f2_fma(f2(e.z, e.w), f2(fr.z, fr.w), l);
+            w[2 * k] = pack2(static_cast<const __half*>(nullptr), e.x, e.y);
+            w[2 * k + 1] = pack2(static_cast<const __half*>(nullptr), e.z, e.w);
+          }
+          tmem_st32(tS + 32 * h, w);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(p_full + 8 * half);
+      }
+      // ---- O out
+      mbar_wait_warp(o_full + 8 * half, done & 1, abortp, p.status);
+      ++done;
+      tc_fence_after();
+      const float2 l2 = f2_get(l);
+      const float sum = l2.x + l2.y;
+      const bool cut = at.cut();
+      float* const part = p.parts + (2 * (int64_t)blockIdx.x + (at.first == 0 ? 1 : 0)) * L::PART;
+      const int pr = half * HALF + row;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;                   // (a row that sees nothing: zeros)
+#pragma unroll 1
+      for (int k = 0; k < DIM / 32; ++k) {
+        uint32_t o[32];
+        tmem_get32(tO + 32 * k, o);
+        tmem_wait_ld();
+        if (!there) continue;
+        if (cut) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint4*>(part + pr * DIM + 32 * k + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        } else {
+          float v[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * inv;
+          put_out(p.a, static_cast<T*>(p.a.o) + out_row * p.a.o_row + out_head * p.a.o_head + 32 * k, v);
+        }
+      }
+      if (cut && there) { part[ROWS * DIM + pr] = m; part[ROWS * (DIM + 1) + pr] = sum; }
+      if (cut && at.first == 0 && threadIdx.x == 0) {
+        // parts up to the CTA that holds the unit's last block
+        const int64_t u0 = begin + (end - begin - at.left);
+        p.cuts[blockIdx.x] = Cut{at.seq, at.head, at.tile, (int)(((u0 + at.total) * n_ctas - 1) / total)};
+      }
+    }
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    // A warp takes 32 positions of a block: a lane knows where one of them lies and forms its numbers; eight lanes load a row, four rows at a time
+    const int w = warp - 8, sub = lane & 7, quarter = lane >> 3;
+    constexpr int SUBS = DIM / 16;                                      // lanes of a row
+    constexpr int LOADS = SUBS;                                         // rows that a lane takes part in: 32 / (32 / SUBS)
+    struct Ahead { uint4 k[LOADS], v[LOADS]; float ks, vs; bool seen; };
+    const int lane_sub = lane % SUBS, lane_row = lane / SUBS;
+    (void)sub; (void)quarter;
+    Segments ld = at;                                                   // of the block that is loaded next
+    int ld_i = 0;
+    int64_t row_at = 0;
+    bool seen = false;
+    float ks = 0.f, vs = 0.f;
+    auto find = [&]() {
+      const int64_t j = (int64_t)(ld.block + ld_i) * KEYS + w * 32 + lane;
+      uint32_t page = 0, slot = 0;
+      seen = j < ld.s.length;
+      if (seen && !place(c, b, ld.seq, (uint32_t)j, page, slot)) { report(p.status); seen = false; }
+      if (!seen) page = slot = 0;
+      row_at = page * c.page + ld.head * c.head + slot * c.slot;
+      const int64_t sc = page * c.spage + ld.head * c.shead + slot * c.sslot;
+      ks = c.ks[sc];
+      vs = c.vs[sc];
+    };
+    uint4 kr[LOADS], vr[LOADS];
+    auto load = [&](const int8_t* from, uint4 (&to)[LOADS]) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int64_t r = __shfl_sync(0xffffffffu, row_at, i * (32 / SUBS) + lane_row);
+        to[i] = *reinterpret_cast<const uint4*>(from + r + lane_sub * 16);
+      }
+    };
+    // sixteen bytes of row i as fp16, two pieces of sixteen bytes (the second first in half of the lanes: eight lanes then meet in no bank)
+    auto store = [&](uint32_t base, const uint4 (&from)[LOADS]) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = w * 32 + i * (32 / SUBS) + lane_row;
+        const uint32_t a = from[i].x ^ 0x80808080u, d = from[i].y ^ 0x80808080u, e = from[i].z ^ 0x80808080u, f = from[i].w ^ 0x80808080u;
+        const uint4 lo = make_uint4(bytes_half(a, 0x4140), bytes_half(a, 0x4342), bytes_half(d, 0x4140), bytes_half(d, 0x4342));
+        const uint4 hi = make_uint4(bytes_half(e, 0x4140), bytes_half(e, 0x4342), bytes_half(f, 0x4140), bytes_half(f, 0x4342));
+        const uint32_t line = base + (lane_sub >> 2) * L::CHUNK + r * 128;
+        const uint32_t swap = (lane_sub >> 2) & 1, x = (lane_sub & 3) * 2, k = r & 7;
+        put16(line + (((x + swap) ^ k) << 4), swap ? hi : lo);
+        put16(line + (((x + 1 - swap) ^ k) << 4), swap ? lo : hi);
+      }
+    };
+    auto step = [&]() {                                                 // on to the next block; false behind the last one
+      if (++ld_i < ld.count) return true;
+      ld_i = 0;
+      ld.next();
+      return ld.more();
+    };
+    bool more = ld.more();
+    if (more) { find(); load(c.k, kr); load(c.v, vr); }
+    uint32_t blocks = 0, seg = 0;
+    for (; at.more(); at.next(), ++seg) {
+      for (int i = 0; i < at.count; ++i, ++blocks) {
+        const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
+        mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abortp, p.status);
+        store(smem + L::K0 + st * L::BYTES, kr);
+        fence_proxy_async();
+        mbar_arrive(k_full + 8 * st);
+        // (the block's numbers, before the next one's come)
+        const bool mine = seen;
+        const float my_ks = ks, my_vs = vs < LEAST ? LEAST : vs;
+        more = step();
+        if (more) { find(); load(c.k, kr); }
+        if (i == 0) mbar_wait_warp(q_full, seg & 1, abortp, p.status);     // (the factor)
+        mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abortp, p.status);
+        {
+          const uint32_t to = smem + L::C0 + st * L::CONSTS + (w * 32 + lane) * 4;
+          const float fa = mine ? my_ks * *(volatile float*)&factors[seg & 1] : 0.f, fb = mine ? __log2f(my_vs) : minus_inf(),
+                      fr = mine ? __fdividef(1.f, my_vs) : 0.f;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(fb) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 2 * KEYS * 4), "f"(fr) : "memory");
+          mbar_arrive(c_full + 8 * st);
+        }
+        store(smem + L::V0 + st * L::BYTES, vr);
+        fence_proxy_async();
+        mbar_arrive(v_full + 8 * st);
+        if (more) load(c.v, vr);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 12) {
+      const uint32_t leader = elect_lane();
+      const uint32_t qk = idesc_f16(KEYS, 0), pv = idesc_f16(DIM, 1);
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait_warp(bar, parity, abortp, p.status) && ok; };
+      auto scores = [&](int half, uint32_t st) {
+        if (!ok) return;
+        const uint64_t dq = smem_desc_sw128(smem + L::Q0 + half * L::BYTES, 16, 1024), dk = smem_desc_sw128(smem + L::K0 + st * L::BYTES, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < DIM / 16; ++k) {
+          const uint64_t o = (uint64_t)(((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4);
+          umma_ss(leader, tmem + half * 128, dq + o, dk + o, qk, k > 0);
+        }
+        umma_commit_w(leader, s_full + 8 * half);
+      };
+      auto values = [&](int half, uint32_t st, bool acc) {
+        if (!ok) return;
+        const uint64_t dv = smem_desc_sw128(smem + L::V0 + st * L::BYTES, L::CHUNK, 1024);
+#pragma unroll
+        for (int k = 0; k < KEYS / 16; ++k)
+          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
+      };
+      uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
+      for (; at.more(); at.next(), ++seg) {
+        const int halves = at.rows() > HALF ? 2 : 1;
+        wait(q_full, seg & 1);
+        if (halves == 2) wait(q_full + 8, seg1++ & 1);
+        wait(k_full + 8 * (n & 1), (n >> 1) & 1);
+        tc_fence_after();
+        scores(0, n & 1);
+        if (halves == 2) scores(1, n & 1);
+        if (ok) umma_commit_w(leader, k_empty + 8 * (n & 1));
+        for (int i = 0; i < at.count; ++i, ++n) {
+          const bool last = i + 1 == at.count;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h == halves) break;
+            wait(p_full + 8 * h, turn[h]++ & 1);
+            if (h == 0) wait(v_full + 8 * (n & 1), (n >> 1) & 1);
+            tc_fence_after();
+            values(h, n & 1, i > 0);
+            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * (n & 1));
+            if (ok && last) umma_commit_w(leader, o_full + 8 * h);
+            if (!last) {
+              const uint32_t nn = n + 1;
+              if (h == 0) { wait(k_full + 8 * (nn & 1), (nn >> 1) & 1); tc_fence_after(); }
+              scores(h, nn & 1);
+              if (ok && h + 1 == halves) umma_commit_w(leader, k_empty + 8 * (nn & 1));
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+// The parts of units that were cut: CTA x takes the unit whose first part is that of CTA x, JOIN_ROWS rows of it.
+template <typename T, int DIM>
+__global__ void __launch_bounds__(128)
+kv_join_kernel(const TileP p) {
+  grid_begin();
+  using L = Tile<DIM>;
+  const Cut cut = p.cuts[blockIdx.x];
+  if (cut.last < 0) return;
+  bool bad;
+  const Seq s = sequence(p.a.b, cut.seq, bad);
+  const int rows = s.n * p.a.group - cut.tile * ROWS, c0 = blockIdx.x;
+  constexpr int PER = DIM / 4;                                          // lanes of a row
+  const int end = min(rows, ((int)blockIdx.y + 1) * JOIN_ROWS);
+  for (int r = blockIdx.y * JOIN_ROWS + threadIdx.x / PER; r < end; r += 128 / PER) {
+    const int d = threadIdx.x % PER * 4;
+    auto part = [&](int k) { return p.parts + (2 * (int64_t)k + (k == c0)) * L::PART; };
+    float top = minus_inf();
+    for (int k = c0; k <= cut.last; ++k) top = fmaxf(top, part(k)[ROWS * DIM + r]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int k = c0; k <= cut.last; ++k) {
+      const float* const from = part(k);
+      const float m = from[ROWS * DIM + r], f = m == minus_inf() ? 0.f : exp2_fast(m - top);
+      const float4 v = *reinterpret_cast<const float4*>(from + r * DIM + d);
+      sum = fmaf(f, from[ROWS * (DIM + 1) + r], sum);
+      o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int rr = cut.tile * ROWS + r, tok = rr / p.a.group, g = rr - tok * p.a.group;
+    T* const to = static_cast<T*>(p.a.o) + (int64_t)(s.first + tok) * p.a.o_row + (int64_t)(cut.head * p.a.group + g) * p.a.o_head + d;
+    const T* const t = nullptr;
+    if (p.a.aligned) *reinterpret_cast<uint2*>(to) = make_uint2(pack2(t, o.x * inv, o.y * inv), pack2(t, o.z * inv, o.w * inv));
+    else { to[0] = from_f<T>(o.x * inv); to[1] = from_f<T>(o.y * inv); to[2] = from_f<T>(o.z * inv); to[3] = from_f<T>(o.w * inv); }
+  }
+}
+
+template <typename T, int DIM>
+armor_status launch_typed(armor_ctx* c, TileP p, cudaStream_t s) {
+  using L = Tile<DIM>;
+  static PerDeviceOnce once;
+  if (ensure_dynamic_smem(once, c->device, kv_attend_tile_kernel<T, DIM>, L::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  const unsigned n = (unsigned)c->n_sm;
+  const int64_t part_bytes = (int64_t)L::PART * 4, need = 2 * n * part_bytes;
+  p.whole = ws_scratch_bytes(c) < need;
+  p.parts = c->T;
+  p.cuts = reinterpret_cast<Cut*>(c->kv_cuts);
+  const Batch all = p.a.b;
+  for (int b0 = 0; b0 < all.n; b0 += SEQS) {
+    p.a.b.n = all.n - b0 < SEQS ? all.n - b0 : SEQS;
+    p.a.b.lengths = all.lengths + b0;
+    p.a.b.starts = all.starts + b0;
+    p.a.b.pages = all.pages + b0 * all.ld;
+    launch_dependent(kv_attend_tile_kernel<T, DIM>, dim3(n), dim3(THREADS), L::SMEM, s, p);
+    c->launches++;
+    if (!p.whole) {
+      launch_dependent(kv_join_kernel<T, DIM>, dim3(n, ROWS / JOIN_ROWS), dim3(128), 0, s, p);
+      c->launches++;
+    }
+  }
+  return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
+}
+
+}  // namespace
+
+armor_status launch_kv_attend_tile(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s) {
+  TileP p;
+  p.a = a;
+  p.limit = limit;
+  p.status = c->status;
+  KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
+  if (a.dtype == ARMOR_DTYPE_BF16) return a.dim == 64 ? launch_typed<__nv_bfloat16, 64>(c, p, s) : launch_typed<__nv_bfloat16, 128>(c, p, s);
+  return a.dim == 64 ? launch_typed<__half, 64>(c, p, s) : launch_typed<__half, 128>(c, p, s);
+}

@@ -252,6 +252,15 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   a.scale = g->scale * 1.4426950408889634f;
   a.aligned = aligned16(a.q, a.q_row, 2) && aligned16(a.o, a.o_row, 2) && a.q_head % 8 == 0 && a.o_head % 8 == 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if ((st = launch_kv_attend_few(c, a, MOST, s)) != ARMOR_OK) return st;
+  // Which kernels: the one for few rows a sequence reads keys and values once for every KV_FEW_ROWS of them, the other one once for 256.  Where
+  // the host cannot tell (lengths are on the device), both run, each on its sequences.
+  const int64_t chunk = g->max_chunk ? g->max_chunk : (a.b.n == 1 ? g->n_rows : 0), rows = chunk * a.group;
+  if (chunk ? rows <= KV_FEW_ROWS : g->n_rows <= batch->n_seqs && a.group <= KV_FEW_ROWS) st = launch_kv_attend_few(c, a, MOST, s);
+  else if (a.b.n == 1 || a.group > KV_FEW_ROWS) st = launch_kv_attend_tile(c, a, 0, s);
+  else {
+    st = launch_kv_attend_tile(c, a, KV_FEW_ROWS, s);
+    if (st == ARMOR_OK) st = launch_kv_attend_few(c, a, KV_FEW_ROWS, s);
+  }
+  if (st != ARMOR_OK) return st;
   return finish_call(c);
 }

@@ -97,4 +97,8 @@ struct KvAttend {
   float scale;                              // of the scores, times log2 e
   int aligned;                              // rows of q and o start on 16-byte boundaries
 };
+// sequences of up to `limit` rows (a token and a head of the group each)
 armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s);
+// sequences of more
+armor_status launch_kv_attend_tile(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s);
+constexpr int64_t KV_FEW_ROWS = 16;
