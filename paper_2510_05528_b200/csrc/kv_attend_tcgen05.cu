@@ -4,11 +4,14 @@
 // A unit is a tile of 256 rows (a token and a head of the group each; the heads of a group share keys) of one sequence and key head against the
 // blocks of 128 positions that its rows see.  A CTA takes it as two halves of 128 rows, so that the tensor cores have the one half's
 // products while the other's weights are formed:
-//   warps 0-3, 4-7 : the rows of a half each, a thread a row: S from tensor memory, weights back in its place, O rescaled there when the maximum moves by
-//                    far (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16)
+//   warps 0-3, 4-7 : the rows of a half each: S from tensor memory, weights back in its place, O rescaled there when the maximum moves by far
+//                    (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16).  A lane has 32 of
+//                    the block's columns in four rows, not a row (a lane a row reads all positions' numbers: 96 reads of 16 bytes a
+//                    warp, each of them 512 bytes into registers; blocks took 11,000 cycles)
 //   warps 8-11     : keys and values from their pages through registers to fp16 in shared memory, two blocks of each, loaded a block ahead; the
 //                    three numbers of a position (ks factor, log2 vs, 1 / vs)
 //   warp 12        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
+//   warp 13        : finds the units of the CTA's share, a few ahead of the others
 // Tensor memory: S of either half (128 columns each; W in its first 64), O of either half.
 //
 // All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
@@ -36,7 +39,7 @@ struct Tile {
   static constexpr int PART = ROWS * (DIM + 2);                 // floats of a part: O, m, l
   // Q of both halves, two blocks of K, of V, two blocks of a position's three numbers
   static constexpr int Q0 = 0, K0 = 2 * BYTES, V0 = 4 * BYTES, C0 = 6 * BYTES;
-  static constexpr int CONSTS = 3 * KEYS * 4;
+  static constexpr int CONSTS = 3 * KEYS * 4;                   // for two positions: factors, logarithms (16 bytes); behind those of all: inverses
   static constexpr size_t SMEM = C0 + 2 * CONSTS + 1024;
 };
 
@@ -71,12 +74,17 @@ __device__ __forceinline__ uint32_t bytes_half(uint32_t x, uint32_t sel) {      
 __device__ __forceinline__ void put16(uint32_t at, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+// (behind the wait for the numbers, which is volatile too)
 __device__ __forceinline__ float4 get16(uint32_t at) {
   float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
   return v;
 }
-__device__ __forceinline__ void barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ float2 get8(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at));
+  return v;
+}
 
 // fp16 operands, fp32 sums; M = 128
 __device__ __forceinline__ uint32_t idesc_f16(int n, int b_mn) {
@@ -100,17 +108,36 @@ __device__ __forceinline__ void umma_ts(uint32_t leader, uint32_t d, uint32_t a,
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(leader)
       : "memory");
 }
-// 32 columns of a warp's lanes; the caller waits
+// 32 columns of a warp's lanes, a lane a row; the caller waits
 __device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr));
+}
+// 16 rows of 64 columns, dealt out as the accumulators of an mma are: r[4 g ..]: columns 8 g + 2 (lane % 4), + 1 of row lane / 4, then of row lane / 4 + 8
+__device__ __forceinline__ void tmem_get_frag(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_put_frag(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// the same of pairs of 16-bit numbers: 32 columns of 32 bits, r[2 g ..]: column 4 g + lane % 4 of row lane / 4, then of row lane / 4 + 8
+__device__ __forceinline__ void tmem_put_pairs(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -133,15 +160,28 @@ __device__ __forceinline__ int tiles_of(const TileP& p, const Seq& s) {
   return rows > p.limit ? (int)((rows + ROWS - 1) / ROWS) : 0;
 }
 
-// A CTA's share as segments of units, in the same order for all warps
-struct Segments {
+// What a CTA does with a unit, or with a piece of one: count blocks of positions from `block` on (0: there is no more)
+struct __align__(16) Segment {
+  int count, block;
+  int rows;                                 // of the tile, if fewer than ROWS
+  int seq, head;
+  int first_row;                            // the tile's first row in its group: token r / group, head of the group r % group
+  int row0;                                 // the sequence's first row in the packed arrays
+  int n, length;                            // its new tokens, its positions
+  int part;                                 // the place of the part that is left; -1: the unit is done here
+  int pad[2];
+};
+constexpr int RING = 4;
+
+// The CTA's share of the line, walked by one warp
+struct Walk {
   const TileP& p;
   const int64_t* prefix;                    // [n + 1] blocks ahead of a sequence
   int64_t left;                             // blocks of the share from this segment on
   int seq, head, tile, tiles;
   Seq s;
   int first, count, total, block;           // of the segment: its first block in the unit, its blocks, the unit's, the position block of first
-  __device__ __forceinline__ Segments(const TileP& p_, const int64_t* prefix_) : p(p_), prefix(prefix_) {}
+  __device__ __forceinline__ Walk(const TileP& p_, const int64_t* prefix_) : p(p_), prefix(prefix_) {}
   __device__ __forceinline__ void load() {
     bool bad;
     s = sequence(p.a.b, seq, bad);
@@ -154,7 +194,6 @@ struct Segments {
     block = b.block + off;
     count = p.whole ? b.count : (int)min(left, (int64_t)(b.count - off));
   }
-  // by whole warps: the unit of block `begin` of the line, in sequence seq_
   __device__ __forceinline__ void start(int64_t begin, int64_t end, int seq_) {
     left = end - begin;
     if (left <= 0) return;
@@ -203,8 +242,6 @@ struct Segments {
   }
   __device__ __forceinline__ bool more() const { return left > 0; }
   __device__ __forceinline__ void next() { left -= count; advance(); }
-  __device__ __forceinline__ int rows() const { return s.n * p.a.group - tile * ROWS; }      // of the tile, if fewer than ROWS
-  __device__ __forceinline__ bool cut() const { return count < total; }
 };
 
 // one row of q as fp16 in shared memory, rows of 128 bytes, swizzled
@@ -242,9 +279,11 @@ kv_attend_tile_kernel(const TileP p) {
   using L = Tile<DIM>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) uint64_t bars[18];
+  __shared__ __align__(8) uint64_t bars[19 + 2 * RING];
+  __shared__ Segment ring[RING];
   __shared__ int64_t prefix[SEQS + 1];
-  __shared__ float tops[2][8], factors[2];
+  __shared__ unsigned tops[2][8];
+  __shared__ float factors[2];
   __shared__ uint32_t tmem_base_holder;
   __shared__ int abort_flag, at_seq;
 
@@ -252,7 +291,7 @@ kv_attend_tile_kernel(const TileP p) {
   const uint32_t bar0 = smem_u32(&bars[0]);
   // (a pair each)
   const uint32_t q_full = bar0, s_full = bar0 + 16, p_full = bar0 + 32, o_full = bar0 + 48, k_full = bar0 + 64, k_empty = bar0 + 80, v_full = bar0 + 96,
-                 v_empty = bar0 + 112, c_full = bar0 + 128;
+                 v_empty = bar0 + 112, c_full = bar0 + 128, t_full = bar0 + 144, r_full = bar0 + 152, r_empty = r_full + 8 * RING;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
@@ -265,6 +304,11 @@ kv_attend_tile_kernel(const TileP p) {
       mbar_init(v_full + 8 * i, 128);
       mbar_init(v_empty + 8 * i, 1);
       mbar_init(c_full + 8 * i, 128);
+    }
+    mbar_init(t_full, 8);
+    for (int i = 0; i < RING; ++i) {
+      mbar_init(r_full + 8 * i, 1);
+      mbar_init(r_empty + 8 * i, 13);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -316,22 +360,32 @@ kv_attend_tile_kernel(const TileP p) {
   const int64_t begin = idle ? 0 : (int64_t)blockIdx.x * total / n_ctas, end = idle ? 0 : (int64_t)(blockIdx.x + 1) * total / n_ctas;
   for (int i = threadIdx.x; i < b.n; i += THREADS)
     if (prefix[i] <= begin && begin < prefix[i + 1]) at_seq = i;
-  if (threadIdx.x == 0) p.cuts[blockIdx.x].last = -1;
+  if (warp == 13 && lane == 0) p.cuts[blockIdx.x].last = -1;
   __syncthreads();
-  Segments at(p, prefix);
-  at.start(begin, end, at_seq);
 
+  // the n-th segment of the share, by a whole warp; the ring has its place back
+  auto segment = [&](uint32_t n) {
+    const uint32_t i = n % RING;
+    Segment g;
+    if (!mbar_wait_warp(r_full + 8 * i, (n / RING) & 1, abortp, p.status)) g.count = 0;
+    else g = ring[i];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(r_empty + 8 * i);
+    return g;
+  };
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    const int half = warp >> 2, row = threadIdx.x & 127;
+    const int half = warp >> 2, row = threadIdx.x & 127, quad = lane >> 2, pair = lane & 3;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + half * 128 + lanes, tO = tmem + 256 + half * 128 + lanes;
     uint32_t seg = 0, blocks = 0, turn = 0, done = 0;                   // segments, blocks of the CTA, blocks and segments of this half
-    for (; at.more(); at.next(), ++seg) {
-      const int rows = at.rows() - half * HALF;                         // of this half
+    for (;; ++seg) {
+      const Segment at = segment(seg);
+      if (!at.count) break;
+      const int rows = at.rows - half * HALF;                           // of this half
       const bool there = row < rows;
-      const int r = there ? at.tile * ROWS + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
-      const int64_t out_row = (int64_t)(at.s.first + tok), out_head = (int64_t)(at.head * p.a.group + g);
+      const int r = there ? at.first_row + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
+      const int64_t out_row = (int64_t)(at.row0 + tok), out_head = (int64_t)(at.head * p.a.group + g);
       // ---- q
       {
         uint4 raw[DIM / 8];
@@ -354,11 +408,14 @@ kv_attend_tile_kernel(const TileP p) {
             }
           }
           top = __reduce_max_sync(0xffffffffu, top);
-          if (lane == 0) tops[seg & 1][warp] = __uint_as_float(top);
-          barrier(1, ROWS);
+          if (lane == 0) {
+            tops[seg & 1][warp] = top;
+            mbar_arrive(t_full);
+          }
+          mbar_wait_warp(t_full, seg & 1, abortp, p.status);
           top = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(tops[seg & 1][i]));
+          for (int i = 0; i < 8; ++i) top = max(top, *(volatile unsigned*)&tops[seg & 1][i]);
           shift = top ? min(max(14 - ((int)(top >> 7) - 127), -120), 120) : 0;
         }
         if (threadIdx.x == 0) factors[seg & 1] = p.a.scale * __int_as_float((127 - shift) << 23);
@@ -369,97 +426,143 @@ kv_attend_tile_kernel(const TileP p) {
         }
       }
       if (rows <= 0) { blocks += at.count; continue; }
-      // ---- the positions that the row sees: [low, high)
-      int low = 0, high = 0x7fffffff;                                   // (a row that does not exist: whatever costs nothing)
-      if (there) {
-        const int64_t pos = (int64_t)at.s.length - at.s.n + tok;
-        high = (int)max((int64_t)0, pos + 1);
-        low = p.a.window ? (int)max((int64_t)0, pos + 1 - p.a.window) : 0;
+      // ---- the positions that rows lane / 4 + {0, 8, 16, 24} of the warp's see: [low, high)
+      int low[4], high[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int rr = (warp & 3) * 32 + quad + 8 * k;
+        low[k] = 0;
+        high[k] = 0x7fffffff;                                           // (a row that does not exist: whatever costs nothing)
+        if (rr < rows) {
+          const int64_t pos = (int64_t)at.length - at.n + (at.first_row + half * HALF + rr) / p.a.group;
+          high[k] = (int)max((int64_t)0, pos + 1);
+          low[k] = p.a.window ? (int)max((int64_t)0, pos + 1 - p.a.window) : 0;
+        }
       }
-      float m = minus_inf();
-      F2 l = f2(0.f);
+      float m[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
+      F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
+      const int inner_lo = max(max(low[0], low[1]), max(low[2], low[3])), inner_hi = min(min(high[0], high[1]), min(high[2], high[3]));
       for (int i = 0; i < at.count; ++i, ++blocks, ++turn) {
         const int j0 = (at.block + i) * KEYS;
         const uint32_t consts = smem + L::C0 + (blocks & 1) * L::CONSTS;
         mbar_wait_warp(c_full + 8 * (blocks & 1), (blocks >> 1) & 1, abortp, p.status);
         mbar_wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);
         tc_fence_after();
-        uint32_t raw[128];
+        F2 t[4][16];
+        {
+          uint32_t raw[4][32];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_get32(tS + 32 * k, raw + 32 * k);
-        tmem_wait_ld();
-        F2 t[64];
+          for (int h = 0; h < 4; ++h) tmem_get_frag(tS + ((uint32_t)((h >> 1) * 16) << 16) + (h & 1) * 64, raw[h]);
+          tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const float4 fa = get16(consts + 16 * k), fb = get16(consts + KEYS * 4 + 16 * k);
-          t[2 * k] = f2_fma(f2(__uint_as_float(raw[4 * k]), __uint_as_float(raw[4 * k + 1])), f2(fa.x, fa.y), f2(fb.x, fb.y));
-          t[2 * k + 1] = f2_fma(f2(__uint_as_float(raw[4 * k + 2]), __uint_as_float(raw[4 * k + 3])), f2(fa.z, fa.w), f2(fb.z, fb.w));
+          for (int g = 0; g < 16; ++g) {
+            const float4 ab = get16(consts + 16 * (4 * g + pair));
+            const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t* const x = &raw[(k >> 1) * 2 + (g >> 3)][4 * (g & 7) + 2 * (k & 1)];
+              t[k][g] = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, fb);
+            }
+          }
         }
-        const bool masked = __any_sync(0xffffffffu, j0 < low || j0 + KEYS > high);
+        const bool masked = __any_sync(0xffffffffu, j0 < inner_lo || j0 + KEYS > inner_hi);
         if (masked) {
 #pragma unroll
-          for (int k = 0; k < 64; ++k) {
-            float2 v = f2_get(t[k]);
-            if (j0 + 2 * k < low || j0 + 2 * k >= high) v.x = minus_inf();
-            if (j0 + 2 * k + 1 < low || j0 + 2 * k + 1 >= high) v.y = minus_inf();
-            t[k] = f2(v.x, v.y);
-          }
-        }
-        float top = minus_inf();
+          for (int g = 0; g < 16; ++g)
 #pragma unroll
-        for (int k = 0; k < 64; ++k) { const float2 v = f2_get(t[k]); top = fmaxf(top, fmaxf(v.x, v.y)); }
-        if (__any_sync(0xffffffffu, top > m + LAZY)) {
-          // (S has come behind the product of the block before: O is at rest)
-          const float to = fmaxf(m, top), f = m == to ? 1.f : exp2_fast(m - to);
+            for (int k = 0; k < 4; ++k) {
+              const int j = j0 + 8 * g + 2 * pair;
+              float2 v = f2_get(t[k][g]);
+              if (j < low[k] || j >= high[k]) v.x = minus_inf();
+              if (j + 1 < low[k] || j + 1 >= high[k]) v.y = minus_inf();
+              t[k][g] = f2(v.x, v.y);
+            }
+        }
+        float top[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          top[k] = minus_inf();
+#pragma unroll
+          for (int g = 0; g < 16; ++g) { const float2 v = f2_get(t[k][g]); top[k] = fmaxf(top[k], fmaxf(v.x, v.y)); }
+          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
+          float f[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float to = fmaxf(m[k], top[k]);
+            f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
+            l[k] = f2_mul(l[k], f2(f[k]));
+            m[k] = to;
+          }
           if (i > 0) {
+            // (S has come behind the product of the block before: O is at rest)
 #pragma unroll 1
-            for (int k = 0; k < DIM / 32; ++k) {
+            for (int h = 0; h < DIM / 32; ++h) {
               uint32_t o[32];
-              tmem_get32(tO + 32 * k, o);
+              const float f0 = h & 1 ? f[2] : f[0], f1 = h & 1 ? f[3] : f[1];
+              const uint32_t where = tO + ((uint32_t)((h & 1) * 16) << 16) + (h >> 1) * 64;
+              tmem_get_frag(where, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st32(tO + 32 * k, o);
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (e & 2 ? f1 : f0));
+              tmem_put_frag(where, o);
             }
           }
-          l = f2_mul(l, f2(f));
-          m = to;
         }
-        const F2 minus_m = f2(m == minus_inf() ? 0.f : -m);
+        F2 minus_m[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
+        for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
+        // weights of 64 positions at a time; those of what is not seen, which may be no number, out of the sum
+        auto weights = [&](auto some_hidden) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float4 fr = get16(consts + 2 * KEYS * 4 + 16 * (16 * h + k));
-            const float2 x = f2_get(f2_add(t[32 * h + 2 * k], minus_m)), y = f2_get(f2_add(t[32 * h + 2 * k + 1], minus_m));
-            const float4 e = make_float4(exp2_fast(x.x), exp2_fast(x.y), exp2_fast(y.x), exp2_fast(y.y));
-            if (masked) {                                               // (what is not seen may be no number)
-              const int j = j0 + 64 * h + 4 * k;
-              if (j < low || j >= high) fr.x = 0.f;
-              if (j + 1 < low || j + 1 >= high) fr.y = 0.f;
-              if (j + 2 < low || j + 2 >= high) fr.z = 0.f;
-              if (j + 3 < low || j + 3 >= high) fr.w = 0.f;
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w[2][16];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              const float2 r = get8(consts + 4 * KEYS * 2 + 8 * (4 * (8 * h + g) + pair));
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 x = f2_get(f2_add(t[k][8 * h + g], minus_m[k]));
+                const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
+                float2 rk = r;
+                if constexpr (decltype(some_hidden)::value) {
+                  const int j = j0 + 64 * h + 8 * g + 2 * pair;
+                  if (j < low[k] || j >= high[k]) rk.x = 0.f;
+                  if (j + 1 < low[k] || j + 1 >= high[k]) rk.y = 0.f;
+                }
+                l[k] = f2_fma(f2(e0, e1), f2(rk.x, rk.y), l[k]);
+                w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
+              }
             }
-            l = f2_fma(f2(e.x, e.y), f2(fr.x, fr.y), l);
-            l = f2_fma(f2(e.z, e.w), f2(fr.z, fr.w), l);
-            w[2 * k] = pack2(static_cast<const __half*>(nullptr), e.x, e.y);
-            w[2 * k + 1] = pack2(static_cast<const __half*>(nullptr), e.z, e.w);
+            tmem_put_pairs(tS + 32 * h, w[0]);
+            tmem_put_pairs(tS + (16u << 16) + 32 * h, w[1]);
           }
-          tmem_st32(tS + 32 * h, w);
-        }
+        };
+        if (masked) weights(std::true_type());
+        else weights(std::false_type());
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(p_full + 8 * half);
+      }
+      // m and l of the lane's row: they lie with the lanes 4 (row % 8) .. + 3, the sums a quarter each
+      float row_m = 0.f, sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = f2_get(l[k]);
+        float x = v.x + v.y;
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        const float s2 = __shfl_sync(0xffffffffu, x, 4 * (lane & 7)), m2 = __shfl_sync(0xffffffffu, m[k], 4 * (lane & 7));
+        if (lane >> 3 == k) { sum = s2; row_m = m2; }
       }
       // ---- O out
       mbar_wait_warp(o_full + 8 * half, done & 1, abortp, p.status);
       ++done;
       tc_fence_after();
-      const float2 l2 = f2_get(l);
-      const float sum = l2.x + l2.y;
-      const bool cut = at.cut();
-      float* const part = p.parts + (2 * (int64_t)blockIdx.x + (at.first == 0 ? 1 : 0)) * L::PART;
+      const bool cut = at.part >= 0;
+      float* const part = p.parts + (int64_t)at.part * L::PART;
       const int pr = half * HALF + row;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;                   // (a row that sees nothing: zeros)
 #pragma unroll 1
@@ -479,35 +582,28 @@ kv_attend_tile_kernel(const TileP p) {
           put_out(p.a, static_cast<T*>(p.a.o) + out_row * p.a.o_row + out_head * p.a.o_head + 32 * k, v);
         }
       }
-      if (cut && there) { part[ROWS * DIM + pr] = m; part[ROWS * (DIM + 1) + pr] = sum; }
-      if (cut && at.first == 0 && threadIdx.x == 0) {
-        // parts up to the CTA that holds the unit's last block
-        const int64_t u0 = begin + (end - begin - at.left);
-        p.cuts[blockIdx.x] = Cut{at.seq, at.head, at.tile, (int)(((u0 + at.total) * n_ctas - 1) / total)};
-      }
+      if (cut && there) { part[ROWS * DIM + pr] = row_m; part[ROWS * (DIM + 1) + pr] = sum; }
     }
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     // A warp takes 32 positions of a block: a lane knows where one of them lies and forms its numbers; eight lanes load a row, four rows at a time
-    const int w = warp - 8, sub = lane & 7, quarter = lane >> 3;
+    const int w = warp - 8;
     constexpr int SUBS = DIM / 16;                                      // lanes of a row
     constexpr int LOADS = SUBS;                                         // rows that a lane takes part in: 32 / (32 / SUBS)
-    struct Ahead { uint4 k[LOADS], v[LOADS]; float ks, vs; bool seen; };
     const int lane_sub = lane % SUBS, lane_row = lane / SUBS;
-    (void)sub; (void)quarter;
-    Segments ld = at;                                                   // of the block that is loaded next
-    int ld_i = 0;
+    uint32_t seg = 0;
+    int count = 0, i = 0, seq = 0, head = 0, length = 0;                // of the segment of the block that is loaded next; that block in it
+    int64_t j = 0;                                                      // the lane's position in that block
     int64_t row_at = 0;
     bool seen = false;
     float ks = 0.f, vs = 0.f;
     auto find = [&]() {
-      const int64_t j = (int64_t)(ld.block + ld_i) * KEYS + w * 32 + lane;
       uint32_t page = 0, slot = 0;
-      seen = j < ld.s.length;
-      if (seen && !place(c, b, ld.seq, (uint32_t)j, page, slot)) { report(p.status); seen = false; }
+      seen = j < length;
+      if (seen && !place(c, b, seq, (uint32_t)j, page, slot)) { report(p.status); seen = false; }
       if (!seen) page = slot = 0;
-      row_at = page * c.page + ld.head * c.head + slot * c.slot;
-      const int64_t sc = page * c.spage + ld.head * c.shead + slot * c.sslot;
+      row_at = page * c.page + head * c.head + slot * c.slot;
+      const int64_t sc = page * c.spage + head * c.shead + slot * c.sslot;
       ks = c.ks[sc];
       vs = c.vs[sc];
     };
@@ -534,42 +630,45 @@ kv_attend_tile_kernel(const TileP p) {
       }
     };
     auto step = [&]() {                                                 // on to the next block; false behind the last one
-      if (++ld_i < ld.count) return true;
-      ld_i = 0;
-      ld.next();
-      return ld.more();
+      ++i;
+      j += KEYS;
+      if (i < count) return true;
+      const Segment at = segment(seg++);
+      count = at.count; seq = at.seq; head = at.head; length = at.length;
+      i = 0;
+      j = (int64_t)at.block * KEYS + w * 32 + lane;
+      return count > 0;
     };
-    bool more = ld.more();
+    bool more = step();
     if (more) { find(); load(c.k, kr); load(c.v, vr); }
-    uint32_t blocks = 0, seg = 0;
-    for (; at.more(); at.next(), ++seg) {
-      for (int i = 0; i < at.count; ++i, ++blocks) {
-        const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
-        mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abortp, p.status);
-        store(smem + L::K0 + st * L::BYTES, kr);
-        fence_proxy_async();
-        mbar_arrive(k_full + 8 * st);
-        // (the block's numbers, before the next one's come)
-        const bool mine = seen;
-        const float my_ks = ks, my_vs = vs < LEAST ? LEAST : vs;
-        more = step();
-        if (more) { find(); load(c.k, kr); }
-        if (i == 0) mbar_wait_warp(q_full, seg & 1, abortp, p.status);     // (the factor)
-        mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abortp, p.status);
-        {
-          const uint32_t to = smem + L::C0 + st * L::CONSTS + (w * 32 + lane) * 4;
-          const float fa = mine ? my_ks * *(volatile float*)&factors[seg & 1] : 0.f, fb = mine ? __log2f(my_vs) : minus_inf(),
-                      fr = mine ? __fdividef(1.f, my_vs) : 0.f;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(fb) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 2 * KEYS * 4), "f"(fr) : "memory");
-          mbar_arrive(c_full + 8 * st);
-        }
-        store(smem + L::V0 + st * L::BYTES, vr);
-        fence_proxy_async();
-        mbar_arrive(v_full + 8 * st);
-        if (more) load(c.v, vr);
+    for (uint32_t blocks = 0; more; ++blocks) {
+      const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
+      mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abortp, p.status);
+      store(smem + L::K0 + st * L::BYTES, kr);
+      fence_proxy_async();
+      mbar_arrive(k_full + 8 * st);
+      // (the block's numbers, before the next one's come)
+      const bool mine = seen;
+      const float my_ks = ks, my_vs = vs < LEAST ? LEAST : vs;
+      const uint32_t of = seg - 1;                                      // its segment
+      const bool first = i == 0;
+      more = step();
+      if (more) { find(); load(c.k, kr); }
+      if (first) mbar_wait_warp(q_full, of & 1, abortp, p.status);      // (the factor)
+      mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abortp, p.status);
+      {
+        const uint32_t at = smem + L::C0 + st * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
+        const float fa = mine ? my_ks * *(volatile float*)&factors[of & 1] : 0.f, fb = mine ? __log2f(my_vs) : minus_inf(),
+                    fr = mine ? __fdividef(1.f, my_vs) : 0.f;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
+        mbar_arrive(c_full + 8 * st);
       }
+      store(smem + L::V0 + st * L::BYTES, vr);
+      fence_proxy_async();
+      mbar_arrive(v_full + 8 * st);
+      if (more) load(c.v, vr);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -596,8 +695,13 @@ kv_attend_tile_kernel(const TileP p) {
           umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
       };
       uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
-      for (; at.more(); at.next(), ++seg) {
-        const int halves = at.rows() > HALF ? 2 : 1;
+      for (;; ++seg) {
+        int count, halves;
+        {
+          const Segment at = segment(seg);
+          count = at.count; halves = at.rows > HALF ? 2 : 1;
+        }
+        if (!count) break;
         wait(q_full, seg & 1);
         if (halves == 2) wait(q_full + 8, seg1++ & 1);
         wait(k_full + 8 * (n & 1), (n >> 1) & 1);
@@ -605,8 +709,8 @@ kv_attend_tile_kernel(const TileP p) {
         scores(0, n & 1);
         if (halves == 2) scores(1, n & 1);
         if (ok) umma_commit_w(leader, k_empty + 8 * (n & 1));
-        for (int i = 0; i < at.count; ++i, ++n) {
-          const bool last = i + 1 == at.count;
+        for (int i = 0; i < count; ++i, ++n) {
+          const bool last = i + 1 == count;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == halves) break;
@@ -624,6 +728,29 @@ kv_attend_tile_kernel(const TileP p) {
             }
           }
         }
+      }
+    } else if (warp == 13) {
+      Walk at(p, prefix);
+      at.start(begin, end, at_seq);
+      for (uint32_t n = 0;; ++n) {
+        mbar_wait_warp(r_empty + 8 * (n % RING), ((n / RING) & 1) ^ 1, abortp, p.status);
+        const bool cut = at.more() && at.count < at.total;
+        if (lane == 0) {
+          Segment g{};
+          if (at.more()) {
+            g.count = at.count; g.block = at.block;
+            g.rows = at.s.n * p.a.group - at.tile * ROWS; g.first_row = at.tile * ROWS;
+            g.seq = at.seq; g.head = at.head; g.row0 = at.s.first; g.n = at.s.n; g.length = at.s.length;
+            g.part = cut ? 2 * (int)blockIdx.x + (at.first == 0 ? 1 : 0) : -1;
+            if (cut && at.first == 0)                                   // parts up to the CTA that holds the unit's last block
+              p.cuts[blockIdx.x] = Cut{at.seq, at.head, at.tile, (int)(((end - at.left + at.total) * n_ctas - 1) / total)};
+          }
+          ring[n % RING] = g;
+          mbar_arrive(r_full + 8 * (n % RING));
+        }
+        __syncwarp();
+        if (!at.more() || *abortp) break;
+        at.next();
       }
     }
   }
