@@ -8,10 +8,10 @@
 //                    (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16).  A lane has 32 of
 //                    the block's columns in four rows, not a row (a lane a row reads all positions' numbers: 96 reads of 16 bytes a
 //                    warp, each of them 512 bytes into registers; blocks took 11,000 cycles)
-//   warps 8-11     : keys and values from their pages through registers to fp16 in shared memory, two blocks of each, loaded a block ahead; the
-//                    three numbers of a position (ks factor, log2 vs, 1 / vs)
-//   warp 12        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
-//   warp 13        : finds the units of the CTA's share, a few ahead of the others
+//   warps 8-11     : keys from their pages through registers to fp16 in shared memory, two blocks, loaded a block ahead
+//   warps 12-15    : values likewise, and the three numbers of a position (ks factor, log2 vs, 1 / vs)
+//   warp 16        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
+//   warp 17        : finds the units of the CTA's share, a few ahead of the others
 // Tensor memory: S of either half (128 columns each; W in its first 64), O of either half.
 //
 // All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
@@ -26,7 +26,7 @@ using namespace rows;
 using namespace kv;
 using namespace tc;
 
-constexpr int THREADS = 512, HALF = 128, ROWS = 2 * HALF, KEYS = 128;
+constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 128;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr float LEAST = 7.888609e-31f;
@@ -138,6 +138,13 @@ __device__ __forceinline__ void tmem_put_pairs(uint32_t taddr, const uint32_t* r
       "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_get_pairs(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x128b.x8.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -308,11 +315,11 @@ kv_attend_tile_kernel(const TileP p) {
     mbar_init(t_full, 8);
     for (int i = 0; i < RING; ++i) {
       mbar_init(r_full + 8 * i, 1);
-      mbar_init(r_empty + 8 * i, 13);
+      mbar_init(r_empty + 8 * i, 17);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_holder)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -360,7 +367,7 @@ kv_attend_tile_kernel(const TileP p) {
   const int64_t begin = idle ? 0 : (int64_t)blockIdx.x * total / n_ctas, end = idle ? 0 : (int64_t)(blockIdx.x + 1) * total / n_ctas;
   for (int i = threadIdx.x; i < b.n; i += THREADS)
     if (prefix[i] <= begin && begin < prefix[i + 1]) at_seq = i;
-  if (warp == 13 && lane == 0) p.cuts[blockIdx.x].last = -1;
+  if (warp == 17 && lane == 0) p.cuts[blockIdx.x].last = -1;
   __syncthreads();
 
   // the n-th segment of the share, by a whole warp; the ring has its place back
@@ -374,7 +381,7 @@ kv_attend_tile_kernel(const TileP p) {
     return g;
   };
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
     const int half = warp >> 2, row = threadIdx.x & 127, quad = lane >> 2, pair = lane & 3;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + half * 128 + lanes, tO = tmem + 256 + half * 128 + lanes;
@@ -426,122 +433,155 @@ kv_attend_tile_kernel(const TileP p) {
         }
       }
       if (rows <= 0) { blocks += at.count; continue; }
-      // ---- the positions that rows lane / 4 + {0, 8, 16, 24} of the warp's see: [low, high)
-      int low[4], high[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      // ---- the positions that rows lane / 4 + {0, 8, 16, 24} of the warp's see: [low, high); what all of them see
+      auto sees = [&](int k, int& low, int& high) {
         const int rr = (warp & 3) * 32 + quad + 8 * k;
-        low[k] = 0;
-        high[k] = 0x7fffffff;                                           // (a row that does not exist: whatever costs nothing)
+        low = 0;
+        high = 0x7fffffff;                                              // (a row that does not exist: whatever costs nothing)
         if (rr < rows) {
           const int64_t pos = (int64_t)at.length - at.n + (at.first_row + half * HALF + rr) / p.a.group;
-          high[k] = (int)max((int64_t)0, pos + 1);
-          low[k] = p.a.window ? (int)max((int64_t)0, pos + 1 - p.a.window) : 0;
+          high = (int)max((int64_t)0, pos + 1);
+          low = p.a.window ? (int)max((int64_t)0, pos + 1 - p.a.window) : 0;
         }
+      };
+      int inner_lo = 0, inner_hi = 0x7fffffff;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        int low, high;
+        sees(k, low, high);
+        inner_lo = max(inner_lo, low);
+        inner_hi = min(inner_hi, high);
       }
+      inner_lo = __reduce_max_sync(0xffffffffu, inner_lo);
+      inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
       float m[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
       F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
-      const int inner_lo = max(max(low[0], low[1]), max(low[2], low[3])), inner_hi = min(min(high[0], high[1]), min(high[2], high[3]));
       for (int i = 0; i < at.count; ++i, ++blocks, ++turn) {
         const int j0 = (at.block + i) * KEYS;
-        const uint32_t consts = smem + L::C0 + (blocks & 1) * L::CONSTS;
+        const uint32_t consts = smem + L::C0 + (blocks & 1) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
         mbar_wait_warp(c_full + 8 * (blocks & 1), (blocks >> 1) & 1, abortp, p.status);
         mbar_wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);
         tc_fence_after();
-        F2 t[4][16];
-        {
-          uint32_t raw[4][32];
+        // 64 columns at a time
+        auto pass = [&](int h, auto some_hidden) {
+          constexpr bool HIDDEN = decltype(some_hidden)::value;
+          F2 t[4][8];
+          {
+            uint32_t raw[2][32];
 #pragma unroll
-          for (int h = 0; h < 4; ++h) tmem_get_frag(tS + ((uint32_t)((h >> 1) * 16) << 16) + (h & 1) * 64, raw[h]);
-          tmem_wait_ld();
-#pragma unroll
-          for (int g = 0; g < 16; ++g) {
-            const float4 ab = get16(consts + 16 * (4 * g + pair));
-            const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t* const x = &raw[(k >> 1) * 2 + (g >> 3)][4 * (g & 7) + 2 * (k & 1)];
-              t[k][g] = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, fb);
-            }
-          }
-        }
-        const bool masked = __any_sync(0xffffffffu, j0 < inner_lo || j0 + KEYS > inner_hi);
-        if (masked) {
-#pragma unroll
-          for (int g = 0; g < 16; ++g)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int j = j0 + 8 * g + 2 * pair;
-              float2 v = f2_get(t[k][g]);
-              if (j < low[k] || j >= high[k]) v.x = minus_inf();
-              if (j + 1 < low[k] || j + 1 >= high[k]) v.y = minus_inf();
-              t[k][g] = f2(v.x, v.y);
-            }
-        }
-        float top[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          top[k] = minus_inf();
-#pragma unroll
-          for (int g = 0; g < 16; ++g) { const float2 v = f2_get(t[k][g]); top[k] = fmaxf(top[k], fmaxf(v.x, v.y)); }
-          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
-          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
-        }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
-          float f[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float to = fmaxf(m[k], top[k]);
-            f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
-            l[k] = f2_mul(l[k], f2(f[k]));
-            m[k] = to;
-          }
-          if (i > 0) {
-            // (S has come behind the product of the block before: O is at rest)
-#pragma unroll 1
-            for (int h = 0; h < DIM / 32; ++h) {
-              uint32_t o[32];
-              const float f0 = h & 1 ? f[2] : f[0], f1 = h & 1 ? f[3] : f[1];
-              const uint32_t where = tO + ((uint32_t)((h & 1) * 16) << 16) + (h >> 1) * 64;
-              tmem_get_frag(where, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (e & 2 ? f1 : f0));
-              tmem_put_frag(where, o);
-            }
-          }
-        }
-        F2 minus_m[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
-        // weights of 64 positions at a time; those of what is not seen, which may be no number, out of the sum
-        auto weights = [&](auto some_hidden) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w[2][16];
+            for (int e = 0; e < 2; ++e) tmem_get_frag(tS + ((uint32_t)(e * 16) << 16) + h * 64, raw[e]);
+            tmem_wait_ld();
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
-              const float2 r = get8(consts + 4 * KEYS * 2 + 8 * (4 * (8 * h + g) + pair));
+              const float4 ab = get16(consts + 64 * (8 * h + g));
+              const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
-                const float2 x = f2_get(f2_add(t[k][8 * h + g], minus_m[k]));
-                const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
-                float2 rk = r;
-                if constexpr (decltype(some_hidden)::value) {
-                  const int j = j0 + 64 * h + 8 * g + 2 * pair;
-                  if (j < low[k] || j >= high[k]) rk.x = 0.f;
-                  if (j + 1 < low[k] || j + 1 >= high[k]) rk.y = 0.f;
-                }
-                l[k] = f2_fma(f2(e0, e1), f2(rk.x, rk.y), l[k]);
-                w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
+                const uint32_t* const x = &raw[k >> 1][4 * g + 2 * (k & 1)];
+                t[k][g] = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, fb);
               }
             }
-            tmem_put_pairs(tS + 32 * h, w[0]);
-            tmem_put_pairs(tS + (16u << 16) + 32 * h, w[1]);
           }
+          uint32_t hidden[4] = {0u, 0u, 0u, 0u};                        // a bit a column of the lane's
+          if constexpr (HIDDEN) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              int low, high;
+              sees(k, low, high);
+#pragma unroll
+              for (int g = 0; g < 8; ++g) {
+                const int j = j0 + 64 * h + 8 * g + 2 * pair;
+                float2 v = f2_get(t[k][g]);
+                if (j < low || j >= high) { v.x = minus_inf(); hidden[k] |= 1u << (2 * g); }
+                if (j + 1 < low || j + 1 >= high) { v.y = minus_inf(); hidden[k] |= 2u << (2 * g); }
+                t[k][g] = f2(v.x, v.y);
+              }
+            }
+          }
+          float top[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float2 v[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) v[g] = f2_get(t[k][g]);
+            float x = fmaxf(fmaxf(v[0].x, v[0].y), v[1].x), y = fmaxf(fmaxf(v[4].x, v[4].y), v[5].x);
+            x = fmaxf(fmaxf(x, v[1].y), v[2].x); y = fmaxf(fmaxf(y, v[5].y), v[6].x);
+            x = fmaxf(fmaxf(x, v[2].y), v[3].x); y = fmaxf(fmaxf(y, v[6].y), v[7].x);
+            top[k] = fmaxf(fmaxf(x, v[3].y), fmaxf(y, v[7].y));
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+          if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
+            // To a whole number, so that what has been multiplied already, O and the block's first weights, moves by a power of two
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float to = fmaxf(m[k], floorf(top[k]));
+              f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
+              l[k] = f2_mul(l[k], f2(f[k]));
+              m[k] = to;
+            }
+            if (i > 0) {
+              // (S has come behind the product of the block before: O is at rest)
+#pragma unroll 1
+              for (int e = 0; e < DIM / 32; ++e) {
+                uint32_t o[32];
+                const float f0 = e & 1 ? f[2] : f[0], f1 = e & 1 ? f[3] : f[1];
+                const uint32_t where = tO + ((uint32_t)((e & 1) * 16) << 16) + (e >> 1) * 64;
+                tmem_get_frag(where, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (x & 2 ? f1 : f0));
+                tmem_put_frag(where, o);
+              }
+            }
+            if (h) {
+              tmem_wait_st();
+#pragma unroll 1
+              for (int e = 0; e < 2; ++e) {
+                uint32_t w[16];
+                const __half2 f0 = __float2half2_rn(e ? f[2] : f[0]), f1 = __float2half2_rn(e ? f[3] : f[1]);
+                tmem_get_pairs(tS + ((uint32_t)(e * 16) << 16), w);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&w[x]), x & 1 ? f1 : f0);
+                  w[x] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+                tmem_put_pairs(tS + ((uint32_t)(e * 16) << 16), w);
+              }
+            }
+          }
+          F2 minus_m[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
+          uint32_t w[2][16];
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            const float2 r = get8(inverses + 32 * (8 * h + g));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 x = f2_get(f2_add(t[k][g], minus_m[k]));
+              const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
+              float2 rk = r;                                            // (what is not seen may be no number: out of the sum)
+              if (HIDDEN && (hidden[k] >> (2 * g) & 1u)) rk.x = 0.f;
+              if (HIDDEN && (hidden[k] >> (2 * g) & 2u)) rk.y = 0.f;
+              l[k] = f2_fma(f2(e0, e1), f2(rk.x, rk.y), l[k]);
+              w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
+            }
+          }
+          tmem_put_pairs(tS + 32 * h, w[0]);
+          tmem_put_pairs(tS + (16u << 16) + 32 * h, w[1]);
         };
-        if (masked) weights(std::true_type());
-        else weights(std::false_type());
+        if (j0 < inner_lo || j0 + KEYS > inner_hi) {
+          pass(0, std::true_type());
+          pass(1, std::true_type());
+        } else {
+          pass(0, std::false_type());
+          pass(1, std::false_type());
+        }
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(p_full + 8 * half);
@@ -584,43 +624,69 @@ kv_attend_tile_kernel(const TileP p) {
       }
       if (cut && there) { part[ROWS * DIM + pr] = row_m; part[ROWS * (DIM + 1) + pr] = sum; }
     }
-  } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    // A warp takes 32 positions of a block: a lane knows where one of them lies and forms its numbers; eight lanes load a row, four rows at a time
-    const int w = warp - 8;
+  } else if (warp < 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    // Warps 8-11 have the keys, 12-15 the values and the numbers.  A warp takes 32 positions of a block: a lane knows where one of them lies, DIM / 16
+    // lanes load a row.  While a block is stored the next one's rows are on their way, and the page of the one after that.
+    const bool values = warp >= 12;
+    const int w = warp & 3;
     constexpr int SUBS = DIM / 16;                                      // lanes of a row
     constexpr int LOADS = SUBS;                                         // rows that a lane takes part in: 32 / (32 / SUBS)
     const int lane_sub = lane % SUBS, lane_row = lane / SUBS;
+    const int8_t* const from = (values ? c.v : c.k) + lane_sub * 16;
     uint32_t seg = 0;
-    int count = 0, i = 0, seq = 0, head = 0, length = 0;                // of the segment of the block that is loaded next; that block in it
-    int64_t j = 0;                                                      // the lane's position in that block
-    int64_t row_at = 0;
-    bool seen = false;
-    float ks = 0.f, vs = 0.f;
-    auto find = [&]() {
-      uint32_t page = 0, slot = 0;
-      seen = j < length;
-      if (seen && !place(c, b, seq, (uint32_t)j, page, slot)) { report(p.status); seen = false; }
-      if (!seen) page = slot = 0;
-      row_at = page * c.page + head * c.head + slot * c.slot;
-      const int64_t sc = page * c.spage + head * c.shead + slot * c.sslot;
-      ks = c.ks[sc];
-      vs = c.vs[sc];
+    // the block whose page is looked up: the segment's blocks behind it, its sequence, head, length, the lane's position
+    int behind = 0, seq = 0, head = 0, length = 0, j = 0;
+    bool begins = false;                                                // it is its segment's first
+    auto step = [&]() {                                                 // on to the next block; false behind the last one
+      j += KEYS;
+      begins = false;
+      if (behind-- > 0) return true;
+      const Segment at = segment(seg++);
+      if (!at.count) return false;
+      behind = at.count - 1; seq = at.seq; head = at.head; length = at.length;
+      j = at.block * KEYS + w * 32 + lane;
+      begins = true;
+      return true;
     };
-    uint4 kr[LOADS], vr[LOADS];
-    auto load = [&](const int8_t* from, uint4 (&to)[LOADS]) {
+    // page: the lane's, or one that there is for a position that has none
+    uint32_t page = 0, slot = 0;
+    bool seen = false;
+    auto look = [&]() {
+      page = slot = 0;
+      seen = j < length;
+      if (seen) {
+        const uint32_t i = quotient((uint32_t)j, c.mul, c.shift);
+        slot = (uint32_t)j - i * c.page_size;
+        page = i < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + i] : 0xffffffffu;
+      }
+    };
+    uint4 raw[LOADS];
+    float ks = 0.f, vs = 0.f;
+    bool there = false;
+    int of_head = 0;
+    auto load = [&]() {                                                 // of the block whose page has been looked up
+      there = seen && page < c.n_pages;
+      if (seen && !there) {
+        if (values) report(p.status);
+        page = slot = 0;
+      }
+      const int64_t row = page * c.page + of_head * c.head + slot * c.slot;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int64_t r = __shfl_sync(0xffffffffu, row_at, i * (32 / SUBS) + lane_row);
-        to[i] = *reinterpret_cast<const uint4*>(from + r + lane_sub * 16);
+      for (int i = 0; i < LOADS; ++i)
+        raw[i] = *reinterpret_cast<const uint4*>(from + __shfl_sync(0xffffffffu, row, i * (32 / SUBS) + lane_row));
+      if (values) {
+        const int64_t at = page * c.spage + of_head * c.shead + slot * c.sslot;
+        ks = c.ks[at];
+        vs = c.vs[at];
       }
     };
     // sixteen bytes of row i as fp16, two pieces of sixteen bytes (the second first in half of the lanes: eight lanes then meet in no bank)
-    auto store = [&](uint32_t base, const uint4 (&from)[LOADS]) {
+    auto store = [&](uint32_t base) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int r = w * 32 + i * (32 / SUBS) + lane_row;
-        const uint32_t a = from[i].x ^ 0x80808080u, d = from[i].y ^ 0x80808080u, e = from[i].z ^ 0x80808080u, f = from[i].w ^ 0x80808080u;
+        const uint32_t a = raw[i].x ^ 0x80808080u, d = raw[i].y ^ 0x80808080u, e = raw[i].z ^ 0x80808080u, f = raw[i].w ^ 0x80808080u;
         const uint4 lo = make_uint4(bytes_half(a, 0x4140), bytes_half(a, 0x4342), bytes_half(d, 0x4140), bytes_half(d, 0x4342));
         const uint4 hi = make_uint4(bytes_half(e, 0x4140), bytes_half(e, 0x4342), bytes_half(f, 0x4140), bytes_half(f, 0x4342));
         const uint32_t line = base + (lane_sub >> 2) * L::CHUNK + r * 128;
@@ -629,50 +695,46 @@ kv_attend_tile_kernel(const TileP p) {
         put16(line + (((x + 1 - swap) ^ k) << 4), swap ? lo : hi);
       }
     };
-    auto step = [&]() {                                                 // on to the next block; false behind the last one
-      ++i;
-      j += KEYS;
-      if (i < count) return true;
-      const Segment at = segment(seg++);
-      count = at.count; seq = at.seq; head = at.head; length = at.length;
-      i = 0;
-      j = (int64_t)at.block * KEYS + w * 32 + lane;
-      return count > 0;
-    };
-    bool more = step();
-    if (more) { find(); load(c.k, kr); load(c.v, vr); }
-    for (uint32_t blocks = 0; more; ++blocks) {
-      const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
-      mbar_wait_warp(k_empty + 8 * st, ph ^ 1, abortp, p.status);
-      store(smem + L::K0 + st * L::BYTES, kr);
-      fence_proxy_async();
-      mbar_arrive(k_full + 8 * st);
-      // (the block's numbers, before the next one's come)
-      const bool mine = seen;
-      const float my_ks = ks, my_vs = vs < LEAST ? LEAST : vs;
-      const uint32_t of = seg - 1;                                      // its segment
-      const bool first = i == 0;
+    bool more = step(), first = begins;                                 // of the block that is loaded
+    uint32_t of = 0;                                                    // its segment
+    if (more) {
+      look();
+      of_head = head;
+      load();
       more = step();
-      if (more) { find(); load(c.k, kr); }
-      if (first) mbar_wait_warp(q_full, of & 1, abortp, p.status);      // (the factor)
-      mbar_wait_warp(v_empty + 8 * st, ph ^ 1, abortp, p.status);
-      {
-        const uint32_t at = smem + L::C0 + st * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
-        const float fa = mine ? my_ks * *(volatile float*)&factors[of & 1] : 0.f, fb = mine ? __log2f(my_vs) : minus_inf(),
-                    fr = mine ? __fdividef(1.f, my_vs) : 0.f;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
-        mbar_arrive(c_full + 8 * st);
+      if (more) look();
+      bool one = true;                                                  // a block is loaded
+      const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, base = smem + (values ? L::V0 : L::K0);
+      for (uint32_t blocks = 0; one; ++blocks) {
+        const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
+        if (values && first) mbar_wait_warp(q_full, of & 1, abortp, p.status);      // (the factor)
+        mbar_wait_warp(empty + 8 * st, ph ^ 1, abortp, p.status);
+        if (values) {
+          const uint32_t at = smem + L::C0 + st * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
+          const float v = vs < LEAST ? LEAST : vs;
+          const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = there ? __fdividef(1.f, v) : 0.f;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
+          mbar_arrive(c_full + 8 * st);
+        }
+        store(base + st * L::BYTES);
+        fence_proxy_async();
+        mbar_arrive(full + 8 * st);
+        one = more;
+        if (more) {
+          first = begins;
+          of += first;
+          of_head = head;
+          load();
+          more = step();
+          if (more) look();
+        }
       }
-      store(smem + L::V0 + st * L::BYTES, vr);
-      fence_proxy_async();
-      mbar_arrive(v_full + 8 * st);
-      if (more) load(c.v, vr);
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp == 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 16) {
       const uint32_t leader = elect_lane();
       const uint32_t qk = idesc_f16(KEYS, 0), pv = idesc_f16(DIM, 1);
       bool ok = true;
@@ -729,7 +791,7 @@ kv_attend_tile_kernel(const TileP p) {
           }
         }
       }
-    } else if (warp == 13) {
+    } else if (warp == 17) {
       Walk at(p, prefix);
       at.start(begin, end, at_seq);
       for (uint32_t n = 0;; ++n) {
@@ -757,7 +819,7 @@ kv_attend_tile_kernel(const TileP p) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+  if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
 // The parts of units that were cut: CTA x takes the unit whose first part is that of CTA x, JOIN_ROWS rows of it.
