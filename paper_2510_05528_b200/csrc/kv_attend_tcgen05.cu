@@ -8,11 +8,12 @@
 //                    (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16).  A lane has 32 of
 //                    the block's columns in four rows, not a row (a lane a row reads all positions' numbers: 96 reads of 16 bytes a
 //                    warp, each of them 512 bytes into registers; blocks took 11,000 cycles)
-//   warps 8-11     : keys from their pages through registers to fp16 in shared memory, two blocks, loaded a block ahead
-//   warps 12-15    : values likewise, and the three numbers of a position (ks factor, log2 vs, 1 / vs)
+//   warps 8-11     : keys from their pages through registers to fp16 in shared memory, four blocks, and the three numbers of a
+//                    position (ks factor, log2 vs, 1 / vs)
+//   warps 12-15    : values likewise
 //   warp 16        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
 //   warp 17        : finds the units of the CTA's share, a few ahead of the others
-// Tensor memory: S of either half (128 columns each; W in its first 64), O of either half.
+// Tensor memory: for either half S of two blocks (64 columns each, the weights in their first 32) and O.
 //
 // All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
@@ -26,21 +27,23 @@ using namespace rows;
 using namespace kv;
 using namespace tc;
 
-constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 128;
+constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr float LEAST = 7.888609e-31f;
 constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
 
+constexpr int NUMBERS = 8;                  // blocks whose positions' numbers are kept
+
 template <int DIM>
 struct Tile {
-  static constexpr int CHUNK = 128 * 128;                       // 128 rows of 64 fp16
-  static constexpr int BYTES = DIM / 64 * CHUNK;                // 128 rows of q, keys or values
-  static constexpr int PART = ROWS * (DIM + 2);                 // floats of a part: O, m, l
-  // Q of both halves, two blocks of K, of V, two blocks of a position's three numbers
-  static constexpr int Q0 = 0, K0 = 2 * BYTES, V0 = 4 * BYTES, C0 = 6 * BYTES;
+  static constexpr int Q_CHUNK = HALF * 128, CHUNK = KEYS * 128;         // 64 dimensions of a half's rows, of a block's
+  static constexpr int Q_BYTES = DIM / 64 * Q_CHUNK, BYTES = DIM / 64 * CHUNK;
+  static constexpr int PART = ROWS * (DIM + 2);                 // floats of a part: O, four dimensions of all rows behind one another; m; l
+  // q of both halves (their outputs at the end), blocks of keys, of values, the numbers of blocks
+  static constexpr int Q0 = 0, K0 = 2 * Q_BYTES, V0 = K0 + STAGES * BYTES, C0 = V0 + STAGES * BYTES;
   static constexpr int CONSTS = 3 * KEYS * 4;                   // for two positions: factors, logarithms (16 bytes); behind those of all: inverses
-  static constexpr size_t SMEM = C0 + 2 * CONSTS + 1024;
+  static constexpr size_t SMEM = C0 + NUMBERS * CONSTS + 1024;
 };
 
 struct Cut { int seq, head, tile, last; };  // a unit whose first part is this CTA's; last: the CTA of its last part (-1: none)
@@ -139,15 +142,26 @@ __device__ __forceinline__ void tmem_put_pairs(uint32_t taddr, const uint32_t* r
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_get_pairs(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.16x128b.x8.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// mbar_wait_warp in a few instructions: there are twenty of them here, and the code of all roles has to stay in the instruction cache.  (With that
+// one, whose inner loop is unrolled, the kernel had 400 KB.)
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  bool ok = mbar_try(bar, parity);
+  if (!ok) {
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (!(ok = mbar_try(bar, parity)) && !*abort_flag) {
+      if (clock64() - t0 > WAIT_CYCLES) {
+        *abort_flag = 1;
+        atomicAdd(&status[ST_WAIT_TIMEOUTS], 1);
+        status[ST_LAST_ERR] = ARMOR_ERR_TIMEOUT;
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
 
 // ---------------------------------------------------------------- units
 // The blocks that a tile's rows see, from `block` on
@@ -251,42 +265,20 @@ struct Walk {
   __device__ __forceinline__ void next() { left -= count; advance(); }
 };
 
-// one row of q as fp16 in shared memory, rows of 128 bytes, swizzled
-template <typename T, int DIM>
-__device__ __forceinline__ void put_row(uint32_t base, int row, const uint4 (&raw)[DIM / 8], float up) {
-  const T* const t = nullptr;
-#pragma unroll
-  for (int c = 0; c < DIM / 8; ++c) {
-    uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
-    if (!std::is_same<T, __half>::value) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { const float2 v = unpack2(t, w[i]); w[i] = pack2(static_cast<const __half*>(nullptr), v.x * up, v.y * up); }
-    }
-    put16(base + (c >> 3) * Tile<DIM>::CHUNK + row * 128 + (((c & 7) ^ (row & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-  }
+// eight dimensions from 8 c on of a row of a half in shared memory: rows of 128 bytes, swizzled
+template <int DIM>
+__device__ __forceinline__ uint32_t row_at(uint32_t base, int row, int c) {
+  return base + (c >> 3) * Tile<DIM>::Q_CHUNK + row * 128 + (((c & 7) ^ (row & 7)) << 4);
 }
 
-template <typename T>
-__device__ __forceinline__ void put_out(const KvAttend& a, T* to, const float (&v)[32]) {
-  if (a.aligned) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float w[8] = {v[8 * c], v[8 * c + 1], v[8 * c + 2], v[8 * c + 3], v[8 * c + 4], v[8 * c + 5], v[8 * c + 6], v[8 * c + 7]};
-      store8(to + 8 * c, w);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) to[i] = from_f<T>(v[i]);
-  }
-}
-
-template <typename T, int DIM>
+// ALIGNED: rows of q and o start on 16-byte boundaries
+template <typename T, int DIM, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS, 1)
 kv_attend_tile_kernel(const TileP p) {
   using L = Tile<DIM>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) uint64_t bars[19 + 2 * RING];
+  __shared__ __align__(8) uint64_t bars[29 + 2 * RING];
   __shared__ Segment ring[RING];
   __shared__ int64_t prefix[SEQS + 1];
   __shared__ unsigned tops[2][8];
@@ -296,21 +288,24 @@ kv_attend_tile_kernel(const TileP p) {
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar0 = smem_u32(&bars[0]);
-  // (a pair each)
-  const uint32_t q_full = bar0, s_full = bar0 + 16, p_full = bar0 + 32, o_full = bar0 + 48, k_full = bar0 + 64, k_empty = bar0 + 80, v_full = bar0 + 96,
-                 v_empty = bar0 + 112, c_full = bar0 + 128, t_full = bar0 + 144, r_full = bar0 + 152, r_empty = r_full + 8 * RING;
+  // of either half: q, S and weights in two places, O; of the stages: keys, values
+  const uint32_t q_full = bar0, s_full = bar0 + 16, p_full = bar0 + 48, o_done = bar0 + 80, k_full = bar0 + 96, k_empty = bar0 + 128, v_full = bar0 + 160,
+                 v_empty = bar0 + 192, t_full = bar0 + 224, r_full = bar0 + 232, r_empty = r_full + 8 * RING;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full + 8 * i, HALF);
+      mbar_init(o_done + 8 * i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(s_full + 8 * i, 1);
       mbar_init(p_full + 8 * i, HALF);
-      mbar_init(o_full + 8 * i, 1);
-      mbar_init(k_full + 8 * i, 128);
+    }
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(k_full + 8 * i, 64);
       mbar_init(k_empty + 8 * i, 1);
-      mbar_init(v_full + 8 * i, 128);
+      mbar_init(v_full + 8 * i, 64);
       mbar_init(v_empty + 8 * i, 1);
-      mbar_init(c_full + 8 * i, 128);
     }
     mbar_init(t_full, 8);
     for (int i = 0; i < RING; ++i) {
@@ -374,7 +369,7 @@ kv_attend_tile_kernel(const TileP p) {
   auto segment = [&](uint32_t n) {
     const uint32_t i = n % RING;
     Segment g;
-    if (!mbar_wait_warp(r_full + 8 * i, (n / RING) & 1, abortp, p.status)) g.count = 0;
+    if (!wait_warp(r_full + 8 * i, (n / RING) & 1, abortp, p.status)) g.count = 0;
     else g = ring[i];
     __syncwarp();
     if (lane == 0) mbar_arrive(r_empty + 8 * i);
@@ -385,27 +380,32 @@ kv_attend_tile_kernel(const TileP p) {
     const int half = warp >> 2, row = threadIdx.x & 127, quad = lane >> 2, pair = lane & 3;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + half * 128 + lanes, tO = tmem + 256 + half * 128 + lanes;
-    uint32_t seg = 0, blocks = 0, turn = 0, done = 0;                   // segments, blocks of the CTA, blocks and segments of this half
+    uint32_t seg = 0, blocks = 0, turn = 0;                             // segments, blocks of the CTA, blocks of this half
+    constexpr int LANES = DIM / 8, MOVES = LANES;                       // a row by so many lanes; 32 rows by so many instructions
+    const int c8 = lane % LANES, sub_row = lane / LANES;
+    const uint32_t rows_at = smem + L::Q0 + half * L::Q_BYTES;
     for (;; ++seg) {
       const Segment at = segment(seg);
       if (!at.count) break;
       const int rows = at.rows - half * HALF;                           // of this half
-      const bool there = row < rows;
-      const int r = there ? at.first_row + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
+      const int r = row < rows ? at.first_row + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
       const int64_t out_row = (int64_t)(at.row0 + tok), out_head = (int64_t)(at.head * p.a.group + g);
       // ---- q
       {
-        uint4 raw[DIM / 8];
-        const T* const from = static_cast<const T*>(p.a.q) + out_row * p.a.q_row + out_head * p.a.q_head;
+        uint4 raw[MOVES];
+        const int64_t off = out_row * p.a.q_row + out_head * p.a.q_head;
 #pragma unroll
-        for (int i = 0; i < DIM / 8; ++i)
-          raw[i] = !there ? make_uint4(0u, 0u, 0u, 0u) : (p.a.aligned ? raw_load(from + 8 * i).w : row_load<false>(from, 8 * i, DIM).w);
+        for (int i = 0; i < MOVES; ++i) {
+          const int rr = i * (32 / LANES) + sub_row;
+          const T* const from = static_cast<const T*>(p.a.q) + __shfl_sync(0xffffffffu, off, rr) + 8 * c8;
+          raw[i] = (warp & 3) * 32 + rr >= rows ? make_uint4(0u, 0u, 0u, 0u) : row_load<ALIGNED>(from, 0, 8).w;
+        }
         int shift = 0;
         if (std::is_same<T, __nv_bfloat16>::value) {
           // by the power of two that brings the largest finite |q| of the tile to [2^14, 2^15): what is lost is below 2^-39 of it
           unsigned top = 0;
 #pragma unroll
-          for (int i = 0; i < DIM / 8; ++i) {
+          for (int i = 0; i < MOVES; ++i) {
             const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -419,7 +419,7 @@ kv_attend_tile_kernel(const TileP p) {
             tops[seg & 1][warp] = top;
             mbar_arrive(t_full);
           }
-          mbar_wait_warp(t_full, seg & 1, abortp, p.status);
+          wait_warp(t_full, seg & 1, abortp, p.status);
           top = 0;
 #pragma unroll
           for (int i = 0; i < 8; ++i) top = max(top, *(volatile unsigned*)&tops[seg & 1][i]);
@@ -427,7 +427,17 @@ kv_attend_tile_kernel(const TileP p) {
         }
         if (threadIdx.x == 0) factors[seg & 1] = p.a.scale * __int_as_float((127 - shift) << 23);
         if (rows > 0) {
-          put_row<T, DIM>(smem + L::Q0 + half * L::BYTES, row, raw, __int_as_float((127 + shift) << 23));
+          const float up = __int_as_float((127 + shift) << 23);
+          const T* const t = nullptr;
+#pragma unroll
+          for (int i = 0; i < MOVES; ++i) {
+            uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            if (!std::is_same<T, __half>::value) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) { const float2 v = unpack2(t, w[k]); w[k] = pack2(static_cast<const __half*>(nullptr), v.x * up, v.y * up); }
+            }
+            put16(row_at<DIM>(rows_at, (warp & 3) * 32 + i * (32 / LANES) + sub_row, c8), make_uint4(w[0], w[1], w[2], w[3]));
+          }
           fence_proxy_async();
           mbar_arrive(q_full + 8 * half);
         }
@@ -458,22 +468,20 @@ kv_attend_tile_kernel(const TileP p) {
       F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
       for (int i = 0; i < at.count; ++i, ++blocks, ++turn) {
         const int j0 = (at.block + i) * KEYS;
-        const uint32_t consts = smem + L::C0 + (blocks & 1) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
-        mbar_wait_warp(c_full + 8 * (blocks & 1), (blocks >> 1) & 1, abortp, p.status);
-        mbar_wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);
+        const uint32_t consts = smem + L::C0 + (blocks % NUMBERS) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
+        const uint32_t place = 2 * half + (turn & 1), tB = tS + (turn & 1) * 64;
+        wait_warp(s_full + 8 * place, (turn >> 1) & 1, abortp, p.status);       // (and the numbers: they are there before the keys)
         tc_fence_after();
-        // 64 columns at a time
-        auto pass = [&](int h, auto some_hidden) {
-          constexpr bool HIDDEN = decltype(some_hidden)::value;
+        {
           F2 t[4][8];
           {
             uint32_t raw[2][32];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) tmem_get_frag(tS + ((uint32_t)(e * 16) << 16) + h * 64, raw[e]);
+            for (int e = 0; e < 2; ++e) tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw[e]);
             tmem_wait_ld();
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
-              const float4 ab = get16(consts + 64 * (8 * h + g));
+              const float4 ab = get16(consts + 64 * g);
               const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
@@ -482,18 +490,18 @@ kv_attend_tile_kernel(const TileP p) {
               }
             }
           }
-          uint32_t hidden[4] = {0u, 0u, 0u, 0u};                        // a bit a column of the lane's
-          if constexpr (HIDDEN) {
+          if (j0 < inner_lo || j0 + KEYS > inner_hi) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               int low, high;
               sees(k, low, high);
+              low -= j0 + 2 * pair;
+              high -= j0 + 2 * pair;
 #pragma unroll
               for (int g = 0; g < 8; ++g) {
-                const int j = j0 + 64 * h + 8 * g + 2 * pair;
                 float2 v = f2_get(t[k][g]);
-                if (j < low || j >= high) { v.x = minus_inf(); hidden[k] |= 1u << (2 * g); }
-                if (j + 1 < low || j + 1 >= high) { v.y = minus_inf(); hidden[k] |= 2u << (2 * g); }
+                if (8 * g < low || 8 * g >= high) v.x = minus_inf();
+                if (8 * g + 1 < low || 8 * g + 1 >= high) v.y = minus_inf();
                 t[k][g] = f2(v.x, v.y);
               }
             }
@@ -514,17 +522,17 @@ kv_attend_tile_kernel(const TileP p) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
           if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
-            // To a whole number, so that what has been multiplied already, O and the block's first weights, moves by a power of two
             float f[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float to = fmaxf(m[k], floorf(top[k]));
+              const float to = fmaxf(m[k], top[k]);
               f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
               l[k] = f2_mul(l[k], f2(f[k]));
               m[k] = to;
             }
             if (i > 0) {
-              // (S has come behind the product of the block before: O is at rest)
+              wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);   // (the product of the block before)
+              tc_fence_after();
 #pragma unroll 1
               for (int e = 0; e < DIM / 32; ++e) {
                 uint32_t o[32];
@@ -537,22 +545,6 @@ kv_attend_tile_kernel(const TileP p) {
                 tmem_put_frag(where, o);
               }
             }
-            if (h) {
-              tmem_wait_st();
-#pragma unroll 1
-              for (int e = 0; e < 2; ++e) {
-                uint32_t w[16];
-                const __half2 f0 = __float2half2_rn(e ? f[2] : f[0]), f1 = __float2half2_rn(e ? f[3] : f[1]);
-                tmem_get_pairs(tS + ((uint32_t)(e * 16) << 16), w);
-                tmem_wait_ld();
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&w[x]), x & 1 ? f1 : f0);
-                  w[x] = *reinterpret_cast<const uint32_t*>(&v);
-                }
-                tmem_put_pairs(tS + ((uint32_t)(e * 16) << 16), w);
-              }
-            }
           }
           F2 minus_m[4];
 #pragma unroll
@@ -560,31 +552,21 @@ kv_attend_tile_kernel(const TileP p) {
           uint32_t w[2][16];
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
-            const float2 r = get8(inverses + 32 * (8 * h + g));
+            const float2 r = get8(inverses + 32 * g);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               const float2 x = f2_get(f2_add(t[k][g], minus_m[k]));
               const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
-              float2 rk = r;                                            // (what is not seen may be no number: out of the sum)
-              if (HIDDEN && (hidden[k] >> (2 * g) & 1u)) rk.x = 0.f;
-              if (HIDDEN && (hidden[k] >> (2 * g) & 2u)) rk.y = 0.f;
-              l[k] = f2_fma(f2(e0, e1), f2(rk.x, rk.y), l[k]);
+              l[k] = f2_fma(f2(e0, e1), f2(r.x, r.y), l[k]);
               w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
             }
           }
-          tmem_put_pairs(tS + 32 * h, w[0]);
-          tmem_put_pairs(tS + (16u << 16) + 32 * h, w[1]);
-        };
-        if (j0 < inner_lo || j0 + KEYS > inner_hi) {
-          pass(0, std::true_type());
-          pass(1, std::true_type());
-        } else {
-          pass(0, std::false_type());
-          pass(1, std::false_type());
+          tmem_put_pairs(tB, w[0]);
+          tmem_put_pairs(tB + (16u << 16), w[1]);
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(p_full + 8 * half);
+        mbar_arrive(p_full + 8 * place);
       }
       // m and l of the lane's row: they lie with the lanes 4 (row % 8) .. + 3, the sums a quarter each
       float row_m = 0.f, sum = 0.f;
@@ -598,38 +580,68 @@ kv_attend_tile_kernel(const TileP p) {
         if (lane >> 3 == k) { sum = s2; row_m = m2; }
       }
       // ---- O out
-      mbar_wait_warp(o_full + 8 * half, done & 1, abortp, p.status);
-      ++done;
+      wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);
       tc_fence_after();
-      const bool cut = at.part >= 0;
-      float* const part = p.parts + (int64_t)at.part * L::PART;
-      const int pr = half * HALF + row;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;                   // (a row that sees nothing: zeros)
+      if (at.part >= 0) {
+        float* const part = p.parts + (int64_t)at.part * L::PART + 4 * (half * HALF + row);
 #pragma unroll 1
-      for (int k = 0; k < DIM / 32; ++k) {
-        uint32_t o[32];
-        tmem_get32(tO + 32 * k, o);
-        tmem_wait_ld();
-        if (!there) continue;
-        if (cut) {
+        for (int k = 0; k < DIM / 32; ++k) {
+          uint32_t o[32];
+          tmem_get32(tO + 32 * k, o);
+          tmem_wait_ld();
+          if (row < rows) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            *reinterpret_cast<uint4*>(part + pr * DIM + 32 * k + 4 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-        } else {
-          float v[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * inv;
-          put_out(p.a, static_cast<T*>(p.a.o) + out_row * p.a.o_row + out_head * p.a.o_head + 32 * k, v);
+            for (int e = 0; e < 8; ++e)
+              *reinterpret_cast<uint4*>(part + (8 * k + e) * 4 * ROWS) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
         }
+        if (row < rows) {
+          float* const ml = p.parts + (int64_t)at.part * L::PART + ROWS * DIM + half * HALF + row;
+          ml[0] = row_m;
+          ml[ROWS] = sum;
+        }
+      } else {
+        // by way of q's place, so that rows go out whole
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;                 // (a row that sees nothing: zeros)
+        const T* const t = nullptr;
+#pragma unroll 1
+        for (int k = 0; k < DIM / 32; ++k) {
+          uint32_t o[32];
+          tmem_get32(tO + 32 * k, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[x] = pack2(t, __uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv);
+            put16(row_at<DIM>(rows_at, row, 4 * k + e), make_uint4(w[0], w[1], w[2], w[3]));
+          }
+        }
+        __syncwarp();
+        const int64_t off = out_row * p.a.o_row + out_head * p.a.o_head;
+#pragma unroll 4
+        for (int i = 0; i < MOVES; ++i) {
+          const int rr = i * (32 / LANES) + sub_row;
+          T* const to = static_cast<T*>(p.a.o) + __shfl_sync(0xffffffffu, off, rr) + 8 * c8;
+          const float4 v = get16(row_at<DIM>(rows_at, (warp & 3) * 32 + rr, c8));
+          if ((warp & 3) * 32 + rr >= rows) continue;
+          if (ALIGNED) *reinterpret_cast<float4*>(to) = v;
+          else {
+            const uint32_t w[4] = {__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
+#pragma unroll
+            for (int x = 0; x < 8; ++x) reinterpret_cast<unsigned short*>(to)[x] = (unsigned short)(w[x >> 1] >> (16 * (x & 1)));
+          }
+        }
+        __syncwarp();
       }
-      if (cut && there) { part[ROWS * DIM + pr] = row_m; part[ROWS * (DIM + 1) + pr] = sum; }
     }
   } else if (warp < 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    // Warps 8-11 have the keys, 12-15 the values and the numbers.  A warp takes 32 positions of a block: a lane knows where one of them lies, DIM / 16
-    // lanes load a row.  While a block is stored the next one's rows are on their way, and the page of the one after that.
+    // Warps 8-11 have the keys and the numbers, 12-15 the values; the first two of each the even blocks, the others the odd ones.  A warp takes 32
+    // positions: a lane knows where one of them lies, DIM / 16 lanes load a row.  While a block is stored the rows of the warp's next one
+    // are on their way, and the page of the one after that.
     const bool values = warp >= 12;
-    const int w = warp & 3;
+    const int w = warp & 1;
     constexpr int SUBS = DIM / 16;                                      // lanes of a row
     constexpr int LOADS = SUBS;                                         // rows that a lane takes part in: 32 / (32 / SUBS)
     const int lane_sub = lane % SUBS, lane_row = lane / SUBS;
@@ -637,17 +649,14 @@ kv_attend_tile_kernel(const TileP p) {
     uint32_t seg = 0;
     // the block whose page is looked up: the segment's blocks behind it, its sequence, head, length, the lane's position
     int behind = 0, seq = 0, head = 0, length = 0, j = 0;
-    bool begins = false;                                                // it is its segment's first
-    auto step = [&]() {                                                 // on to the next block; false behind the last one
+    bool more = true;
+    auto step = [&]() {                                                 // on to the next block; more: there is one
       j += KEYS;
-      begins = false;
-      if (behind-- > 0) return true;
+      if (behind-- > 0) return;
       const Segment at = segment(seg++);
-      if (!at.count) return false;
+      more = at.count > 0;
       behind = at.count - 1; seq = at.seq; head = at.head; length = at.length;
       j = at.block * KEYS + w * 32 + lane;
-      begins = true;
-      return true;
     };
     // page: the lane's, or one that there is for a position that has none
     uint32_t page = 0, slot = 0;
@@ -668,14 +677,14 @@ kv_attend_tile_kernel(const TileP p) {
     auto load = [&]() {                                                 // of the block whose page has been looked up
       there = seen && page < c.n_pages;
       if (seen && !there) {
-        if (values) report(p.status);
+        if (!values) report(p.status);
         page = slot = 0;
       }
       const int64_t row = page * c.page + of_head * c.head + slot * c.slot;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
         raw[i] = *reinterpret_cast<const uint4*>(from + __shfl_sync(0xffffffffu, row, i * (32 / SUBS) + lane_row));
-      if (values) {
+      if (!values) {
         const int64_t at = page * c.spage + of_head * c.shead + slot * c.sslot;
         ks = c.ks[at];
         vs = c.vs[at];
@@ -695,42 +704,44 @@ kv_attend_tile_kernel(const TileP p) {
         put16(line + (((x + 1 - swap) ^ k) << 4), swap ? lo : hi);
       }
     };
-    bool more = step(), first = begins;                                 // of the block that is loaded
-    uint32_t of = 0;                                                    // its segment
-    if (more) {
-      look();
-      of_head = head;
-      load();
-      more = step();
+    uint32_t of = 0, ahead = 0, waited = 0;                             // segments: of the loaded block, of the one that is looked up; q's that have been waited for
+    uint32_t n = ((uint32_t)(warp >> 1) & 1) - 2;                       // the loaded block (none yet)
+    bool one = false;                                                   // there is a loaded block
+    auto steps = [&](int times) {
+#pragma unroll 1
+      for (int e = 0; e < times && more; ++e) step();
+      ahead = seg - 1;
       if (more) look();
-      bool one = true;                                                  // a block is loaded
-      const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, base = smem + (values ? L::V0 : L::K0);
-      for (uint32_t blocks = 0; one; ++blocks) {
-        const uint32_t st = blocks & 1, ph = (blocks >> 1) & 1;
-        if (values && first) mbar_wait_warp(q_full, of & 1, abortp, p.status);      // (the factor)
-        mbar_wait_warp(empty + 8 * st, ph ^ 1, abortp, p.status);
-        if (values) {
-          const uint32_t at = smem + L::C0 + st * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
-          const float v = vs < LEAST ? LEAST : vs;
-          const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = there ? __fdividef(1.f, v) : 0.f;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
-          mbar_arrive(c_full + 8 * st);
-        }
-        store(base + st * L::BYTES);
-        fence_proxy_async();
-        mbar_arrive(full + 8 * st);
-        one = more;
-        if (more) {
-          first = begins;
-          of += first;
-          of_head = head;
-          load();
-          more = step();
-          if (more) look();
-        }
+    };
+    const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, base = smem + (values ? L::V0 : L::K0);
+    steps((int)n + 3);
+    for (;; n += 2) {
+     if (one) {
+      const uint32_t st = n % STAGES;
+      if (!values)                                                      // (the factor; phase by phase)
+        for (; waited <= of; ++waited) wait_warp(q_full, waited & 1, abortp, p.status);
+      wait_warp(empty + 8 * st, ((n / STAGES) & 1) ^ 1, abortp, p.status);
+      if (!values) {
+        // The numbers of block n - NUMBERS have been read: the keys of block n - STAGES have been multiplied, and those only behind the weights of
+        // block n - STAGES - 2
+        const uint32_t at = smem + L::C0 + (n % NUMBERS) * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
+        const float v = vs < LEAST ? LEAST : vs;
+        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
       }
+      store(base + st * L::BYTES);
+      fence_proxy_async();
+      mbar_arrive(full + 8 * st);
+     }
+     if (!more) break;
+     one = true;
+     // load the block that has been looked up, look up the next one
+     of_head = head;
+     of = ahead;
+     load();
+     steps(2);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
@@ -738,23 +749,23 @@ kv_attend_tile_kernel(const TileP p) {
       const uint32_t leader = elect_lane();
       const uint32_t qk = idesc_f16(KEYS, 0), pv = idesc_f16(DIM, 1);
       bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait_warp(bar, parity, abortp, p.status) && ok; };
-      auto scores = [&](int half, uint32_t st) {
+      auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(bar, parity, abortp, p.status) && ok; };
+      auto scores = [&](int half, uint32_t st, uint32_t place) {
         if (!ok) return;
-        const uint64_t dq = smem_desc_sw128(smem + L::Q0 + half * L::BYTES, 16, 1024), dk = smem_desc_sw128(smem + L::K0 + st * L::BYTES, 16, 1024);
+        const uint64_t dq = smem_desc_sw128(smem + L::Q0 + half * L::Q_BYTES, 16, 1024), dk = smem_desc_sw128(smem + L::K0 + st * L::BYTES, 16, 1024);
 #pragma unroll
-        for (int k = 0; k < DIM / 16; ++k) {
-          const uint64_t o = (uint64_t)(((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4);
-          umma_ss(leader, tmem + half * 128, dq + o, dk + o, qk, k > 0);
-        }
-        umma_commit_w(leader, s_full + 8 * half);
+        for (int k = 0; k < DIM / 16; ++k)
+          umma_ss(leader, tmem + half * 128 + place * 64, dq + (uint64_t)(((k >> 2) * L::Q_CHUNK + (k & 3) * 32) >> 4),
+                  dk + (uint64_t)(((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4), qk, k > 0);
+        umma_commit_w(leader, s_full + 8 * (2 * half + place));
       };
-      auto values = [&](int half, uint32_t st, bool acc) {
+      auto values = [&](int half, uint32_t st, uint32_t place, bool acc) {
         if (!ok) return;
         const uint64_t dv = smem_desc_sw128(smem + L::V0 + st * L::BYTES, L::CHUNK, 1024);
 #pragma unroll
         for (int k = 0; k < KEYS / 16; ++k)
-          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
+          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + place * 64 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
+        umma_commit_w(leader, o_done + 8 * half);
       };
       uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
       for (;; ++seg) {
@@ -766,28 +777,33 @@ kv_attend_tile_kernel(const TileP p) {
         if (!count) break;
         wait(q_full, seg & 1);
         if (halves == 2) wait(q_full + 8, seg1++ & 1);
-        wait(k_full + 8 * (n & 1), (n >> 1) & 1);
-        tc_fence_after();
-        scores(0, n & 1);
-        if (halves == 2) scores(1, n & 1);
-        if (ok) umma_commit_w(leader, k_empty + 8 * (n & 1));
+        // scores two blocks ahead of the values: a half's weights are formed from one while the other is multiplied
+        for (int e = 0; e < 2 && e < count; ++e) {
+          const uint32_t st = (n + e) % STAGES;
+          wait(k_full + 8 * st, ((n + e) / STAGES) & 1);
+          tc_fence_after();
+          scores(0, st, (turn[0] + e) & 1);
+          if (halves == 2) scores(1, st, (turn[1] + e) & 1);
+          if (ok) umma_commit_w(leader, k_empty + 8 * st);
+        }
         for (int i = 0; i < count; ++i, ++n) {
-          const bool last = i + 1 == count;
+          const uint32_t st = n % STAGES, st2 = (n + 2) % STAGES;
+          const bool ahead = i + 2 < count;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == halves) break;
-            wait(p_full + 8 * h, turn[h]++ & 1);
-            if (h == 0) wait(v_full + 8 * (n & 1), (n >> 1) & 1);
+            const uint32_t place = turn[h] & 1;
+            wait(p_full + 8 * (2 * h + place), (turn[h] >> 1) & 1);
+            if (h == 0) wait(v_full + 8 * st, (n / STAGES) & 1);
             tc_fence_after();
-            values(h, n & 1, i > 0);
-            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * (n & 1));
-            if (ok && last) umma_commit_w(leader, o_full + 8 * h);
-            if (!last) {
-              const uint32_t nn = n + 1;
-              if (h == 0) { wait(k_full + 8 * (nn & 1), (nn >> 1) & 1); tc_fence_after(); }
-              scores(h, nn & 1);
-              if (ok && h + 1 == halves) umma_commit_w(leader, k_empty + 8 * (nn & 1));
+            values(h, st, place, i > 0);
+            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * st);
+            if (ahead) {
+              if (h == 0) { wait(k_full + 8 * st2, ((n + 2) / STAGES) & 1); tc_fence_after(); }
+              scores(h, st2, place);
+              if (ok && h + 1 == halves) umma_commit_w(leader, k_empty + 8 * st2);
             }
+            ++turn[h];
           }
         }
       }
@@ -795,7 +811,7 @@ kv_attend_tile_kernel(const TileP p) {
       Walk at(p, prefix);
       at.start(begin, end, at_seq);
       for (uint32_t n = 0;; ++n) {
-        mbar_wait_warp(r_empty + 8 * (n % RING), ((n / RING) & 1) ^ 1, abortp, p.status);
+        wait_warp(r_empty + 8 * (n % RING), ((n / RING) & 1) ^ 1, abortp, p.status);
         const bool cut = at.more() && at.count < at.total;
         if (lane == 0) {
           Segment g{};
@@ -833,20 +849,19 @@ kv_join_kernel(const TileP p) {
   bool bad;
   const Seq s = sequence(p.a.b, cut.seq, bad);
   const int rows = s.n * p.a.group - cut.tile * ROWS, c0 = blockIdx.x;
-  constexpr int PER = DIM / 4;                                          // lanes of a row
-  const int end = min(rows, ((int)blockIdx.y + 1) * JOIN_ROWS);
-  for (int r = blockIdx.y * JOIN_ROWS + threadIdx.x / PER; r < end; r += 128 / PER) {
-    const int d = threadIdx.x % PER * 4;
-    auto part = [&](int k) { return p.parts + (2 * (int64_t)k + (k == c0)) * L::PART; };
-    float top = minus_inf();
-    for (int k = c0; k <= cut.last; ++k) top = fmaxf(top, part(k)[ROWS * DIM + r]);
+  const int r = blockIdx.y * JOIN_ROWS + threadIdx.x % JOIN_ROWS;
+  if (r >= rows) return;
+  auto part = [&](int k) { return p.parts + (2 * (int64_t)k + (k == c0)) * L::PART; };
+  float top = minus_inf();
+  for (int k = c0; k <= cut.last; ++k) top = fmaxf(top, part(k)[ROWS * DIM + r]);
+  for (int d = threadIdx.x / JOIN_ROWS * 4; d < DIM; d += 128 / JOIN_ROWS * 4) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
     for (int k = c0; k <= cut.last; ++k) {
       const float* const from = part(k);
       const float m = from[ROWS * DIM + r], f = m == minus_inf() ? 0.f : exp2_fast(m - top);
-      const float4 v = *reinterpret_cast<const float4*>(from + r * DIM + d);
+      const float4 v = *reinterpret_cast<const float4*>(from + d * ROWS + 4 * r);
       sum = fmaf(f, from[ROWS * (DIM + 1) + r], sum);
       o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
     }
@@ -859,11 +874,11 @@ kv_join_kernel(const TileP p) {
   }
 }
 
-template <typename T, int DIM>
+template <typename T, int DIM, bool ALIGNED>
 armor_status launch_typed(armor_ctx* c, TileP p, cudaStream_t s) {
   using L = Tile<DIM>;
   static PerDeviceOnce once;
-  if (ensure_dynamic_smem(once, c->device, kv_attend_tile_kernel<T, DIM>, L::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
+  if (ensure_dynamic_smem(once, c->device, kv_attend_tile_kernel<T, DIM, ALIGNED>, L::SMEM) != ARMOR_OK) return ARMOR_ERR_CUDA;
   const unsigned n = (unsigned)c->n_sm;
   const int64_t part_bytes = (int64_t)L::PART * 4, need = 2 * n * part_bytes;
   p.whole = ws_scratch_bytes(c) < need;
@@ -875,7 +890,7 @@ armor_status launch_typed(armor_ctx* c, TileP p, cudaStream_t s) {
     p.a.b.lengths = all.lengths + b0;
     p.a.b.starts = all.starts + b0;
     p.a.b.pages = all.pages + b0 * all.ld;
-    launch_dependent(kv_attend_tile_kernel<T, DIM>, dim3(n), dim3(THREADS), L::SMEM, s, p);
+    launch_dependent(kv_attend_tile_kernel<T, DIM, ALIGNED>, dim3(n), dim3(THREADS), L::SMEM, s, p);
     c->launches++;
     if (!p.whole) {
       launch_dependent(kv_join_kernel<T, DIM>, dim3(n, ROWS / JOIN_ROWS), dim3(128), 0, s, p);
@@ -883,6 +898,11 @@ armor_status launch_typed(armor_ctx* c, TileP p, cudaStream_t s) {
     }
   }
   return cudaGetLastError() == cudaSuccess ? ARMOR_OK : ARMOR_ERR_CUDA;
+}
+
+template <typename T, int DIM>
+armor_status launch_aligned(armor_ctx* c, const TileP& p, cudaStream_t s) {
+  return p.a.aligned ? launch_typed<T, DIM, true>(c, p, s) : launch_typed<T, DIM, false>(c, p, s);
 }
 
 }  // namespace
@@ -893,6 +913,6 @@ armor_status launch_kv_attend_tile(armor_ctx* c, const KvAttend& a, int64_t limi
   p.limit = limit;
   p.status = c->status;
   KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
-  if (a.dtype == ARMOR_DTYPE_BF16) return a.dim == 64 ? launch_typed<__nv_bfloat16, 64>(c, p, s) : launch_typed<__nv_bfloat16, 128>(c, p, s);
-  return a.dim == 64 ? launch_typed<__half, 64>(c, p, s) : launch_typed<__half, 128>(c, p, s);
+  if (a.dtype == ARMOR_DTYPE_BF16) return a.dim == 64 ? launch_aligned<__nv_bfloat16, 64>(c, p, s) : launch_aligned<__nv_bfloat16, 128>(c, p, s);
+  return a.dim == 64 ? launch_aligned<__half, 64>(c, p, s) : launch_aligned<__half, 128>(c, p, s);
 }
