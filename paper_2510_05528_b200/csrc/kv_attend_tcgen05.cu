@@ -29,7 +29,8 @@ using namespace tc;
 
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
-constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
+constexpr float MOST = 256.f;               // the weight that makes a row's maximum move (2^LAZY of kv_attend_few.cu)
+constexpr float NOWHERE = -1e38f;           // the logarithm of a position that there is not
 constexpr float LEAST = 7.888609e-31f;
 constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
 
@@ -365,15 +366,11 @@ kv_attend_tile_kernel(const TileP p) {
   if (warp == 17 && lane == 0) p.cuts[blockIdx.x].last = -1;
   __syncthreads();
 
-  // the n-th segment of the share, by a whole warp; the ring has its place back
-  auto segment = [&](uint32_t n) {
-    const uint32_t i = n % RING;
-    Segment g;
-    if (!wait_warp(r_full + 8 * i, (n / RING) & 1, abortp, p.status)) g.count = 0;
-    else g = ring[i];
+  // the n-th segment of the share, by a whole warp: false behind the last one.  done: the ring may have its place back
+  auto segment = [&](uint32_t n) { return wait_warp(r_full + 8 * (n % RING), (n / RING) & 1, abortp, p.status) && ring[n % RING].count > 0; };
+  auto done = [&](uint32_t n) {
     __syncwarp();
-    if (lane == 0) mbar_arrive(r_empty + 8 * i);
-    return g;
+    if (lane == 0) mbar_arrive(r_empty + 8 * (n % RING));
   };
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
@@ -384,16 +381,17 @@ kv_attend_tile_kernel(const TileP p) {
     constexpr int LANES = DIM / 8, MOVES = LANES;                       // a row by so many lanes; 32 rows by so many instructions
     const int c8 = lane % LANES, sub_row = lane / LANES;
     const uint32_t rows_at = smem + L::Q0 + half * L::Q_BYTES;
-    for (;; ++seg) {
-      const Segment at = segment(seg);
-      if (!at.count) break;
+    for (; segment(seg); ++seg) {
+      const Segment& at = ring[seg % RING];                             // (read where it is needed: registers are short)
       const int rows = at.rows - half * HALF;                           // of this half
-      const int r = row < rows ? at.first_row + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
-      const int64_t out_row = (int64_t)(at.row0 + tok), out_head = (int64_t)(at.head * p.a.group + g);
+      auto row_in = [&](int64_t stride, int64_t head_stride) {          // where the lane's row begins in q or o
+        const int r = row < rows ? at.first_row + half * HALF + row : 0, tok = r / p.a.group, g = r - tok * p.a.group;
+        return (int64_t)(at.row0 + tok) * stride + (int64_t)(at.head * p.a.group + g) * head_stride;
+      };
       // ---- q
       {
         uint4 raw[MOVES];
-        const int64_t off = out_row * p.a.q_row + out_head * p.a.q_head;
+        const int64_t off = row_in(p.a.q_row, p.a.q_head);
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
           const int rr = i * (32 / LANES) + sub_row;
@@ -442,7 +440,7 @@ kv_attend_tile_kernel(const TileP p) {
           mbar_arrive(q_full + 8 * half);
         }
       }
-      if (rows <= 0) { blocks += at.count; continue; }
+      if (rows <= 0) { blocks += at.count; done(seg); continue; }
       // ---- the positions that rows lane / 4 + {0, 8, 16, 24} of the warp's see: [low, high); what all of them see
       auto sees = [&](int k, int& low, int& high) {
         const int rr = (warp & 3) * 32 + quad + 8 * k;
@@ -465,105 +463,119 @@ kv_attend_tile_kernel(const TileP p) {
       inner_lo = __reduce_max_sync(0xffffffffu, inner_lo);
       inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
       float m[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
-      F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
-      for (int i = 0; i < at.count; ++i, ++blocks, ++turn) {
-        const int j0 = (at.block + i) * KEYS;
+      F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)}, minus_m[4];       // (-m, twice)
+      const int count = at.count, block0 = at.block;
+      for (int i = 0; i < count; ++i, ++blocks, ++turn) {
+        const int j0 = (block0 + i) * KEYS;
         const uint32_t consts = smem + L::C0 + (blocks % NUMBERS) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
         const uint32_t place = 2 * half + (turn & 1), tB = tS + (turn & 1) * 64;
-        wait_warp(s_full + 8 * place, (turn >> 1) & 1, abortp, p.status);       // (and the numbers: they are there before the keys)
+        const bool masked = j0 < inner_lo || j0 + KEYS > inner_hi;
+        wait_warp(s_full + 8 * place, (turn >> 1) & 1, abortp, p.status);            // (and the numbers: they are there before the keys)
         tc_fence_after();
-        {
-          F2 t[4][8];
-          {
-            uint32_t raw[2][32];
+        // m to the maximum of the block, where that is higher; O and l with it
+        auto raise = [&]() {
+          float top[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw[e]);
+          for (int e = 0; e < 2; ++e) {
+            uint32_t raw[32];
+            tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw);
             tmem_wait_ld();
 #pragma unroll
-            for (int g = 0; g < 8; ++g) {
-              const float4 ab = get16(consts + 64 * g);
-              const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t* const x = &raw[k >> 1][4 * g + 2 * (k & 1)];
-                t[k][g] = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, fb);
-              }
-            }
-          }
-          if (j0 < inner_lo || j0 + KEYS > inner_hi) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              int low, high;
-              sees(k, low, high);
+            for (int k = 0; k < 2; ++k) {
+              int low = 0, high = 0x7fffffff;
+              if (masked) sees(2 * e + k, low, high);
               low -= j0 + 2 * pair;
               high -= j0 + 2 * pair;
 #pragma unroll
               for (int g = 0; g < 8; ++g) {
-                float2 v = f2_get(t[k][g]);
-                if (8 * g < low || 8 * g >= high) v.x = minus_inf();
-                if (8 * g + 1 < low || 8 * g + 1 >= high) v.y = minus_inf();
-                t[k][g] = f2(v.x, v.y);
+                const float4 ab = get16(consts + 64 * g);
+                const float x = fmaf(__uint_as_float(raw[4 * g + 2 * k]), ab.x, ab.z), y = fmaf(__uint_as_float(raw[4 * g + 2 * k + 1]), ab.y, ab.w);
+                if (8 * g >= low && 8 * g < high) top[2 * e + k] = fmaxf(top[2 * e + k], x);
+                if (8 * g + 1 >= low && 8 * g + 1 < high) top[2 * e + k] = fmaxf(top[2 * e + k], y);
               }
             }
           }
-          float top[4];
+          float f[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            float2 v[8];
-#pragma unroll
-            for (int g = 0; g < 8; ++g) v[g] = f2_get(t[k][g]);
-            float x = fmaxf(fmaxf(v[0].x, v[0].y), v[1].x), y = fmaxf(fmaxf(v[4].x, v[4].y), v[5].x);
-            x = fmaxf(fmaxf(x, v[1].y), v[2].x); y = fmaxf(fmaxf(y, v[5].y), v[6].x);
-            x = fmaxf(fmaxf(x, v[2].y), v[3].x); y = fmaxf(fmaxf(y, v[6].y), v[7].x);
-            top[k] = fmaxf(fmaxf(x, v[3].y), fmaxf(y, v[7].y));
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+            const float to = fmaxf(m[k], top[k]);
+            f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
+            l[k] = f2_mul(l[k], f2(f[k]));
+            m[k] = to;
+            minus_m[k] = f2(-to);                                       // (no position yet: infinite, which the next one exceeds)
           }
+          if (i > 0) {
+            wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);          // (the product of the block before)
+            tc_fence_after();
+#pragma unroll 1
+            for (int e = 0; e < DIM / 32; ++e) {
+              uint32_t o[32];
+              const float f0 = e & 1 ? f[2] : f[0], f1 = e & 1 ? f[3] : f[1];
+              const uint32_t where = tO + ((uint32_t)((e & 1) * 16) << 16) + (e >> 1) * 64;
+              tmem_get_frag(where, o);
+              tmem_wait_ld();
 #pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+              for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (x & 2 ? f1 : f0));
+              tmem_put_frag(where, o);
+            }
+          }
+        };
+        uint32_t w[2][16];
+        // The weights by the m there is, which hardly ever moves behind a row's first blocks; true: one of them is above 2^LAZY
+        auto weights = [&](auto some_hidden) {
+          constexpr bool HIDDEN = decltype(some_hidden)::value;
+          uint32_t raw[2][32];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
-          if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
-            float f[4];
+          for (int e = 0; e < 2; ++e) tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw[e]);
+          int low[4], high[4];
+          if constexpr (HIDDEN) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float to = fmaxf(m[k], top[k]);
-              f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
-              l[k] = f2_mul(l[k], f2(f[k]));
-              m[k] = to;
-            }
-            if (i > 0) {
-              wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);   // (the product of the block before)
-              tc_fence_after();
-#pragma unroll 1
-              for (int e = 0; e < DIM / 32; ++e) {
-                uint32_t o[32];
-                const float f0 = e & 1 ? f[2] : f[0], f1 = e & 1 ? f[3] : f[1];
-                const uint32_t where = tO + ((uint32_t)((e & 1) * 16) << 16) + (e >> 1) * 64;
-                tmem_get_frag(where, o);
-                tmem_wait_ld();
-#pragma unroll
-                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (x & 2 ? f1 : f0));
-                tmem_put_frag(where, o);
-              }
+              sees(k, low[k], high[k]);
+              low[k] -= j0 + 2 * pair;
+              high[k] -= j0 + 2 * pair;
             }
           }
-          F2 minus_m[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
-          uint32_t w[2][16];
+          F2 sum[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
+          __half2 top[4];
+          tmem_wait_ld();
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
+            const float4 ab = get16(consts + 64 * g);
             const float2 r = get8(inverses + 32 * g);
+            const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w), fr = f2(r.x, r.y);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float2 x = f2_get(f2_add(t[k][g], minus_m[k]));
-              const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
-              l[k] = f2_fma(f2(e0, e1), f2(r.x, r.y), l[k]);
-              w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
+              const uint32_t* const x = &raw[k >> 1][4 * g + 2 * (k & 1)];
+              const float2 t = f2_get(f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, f2_add(fb, minus_m[k])));
+              float e0 = exp2_fast(t.x), e1 = exp2_fast(t.y);
+              if (HIDDEN && (8 * g < low[k] || 8 * g >= high[k])) e0 = 0.f;
+              if (HIDDEN && (8 * g + 1 < low[k] || 8 * g + 1 >= high[k])) e1 = 0.f;
+              sum[k] = f2_fma(f2(e0, e1), fr, sum[k]);
+              const __half2 h = __floats2half2_rn(e0, e1);
+              top[k] = g ? __hmax2(top[k], h) : h;
+              w[k >> 1][2 * g + (k & 1)] = *reinterpret_cast<const uint32_t*>(&h);
             }
           }
-          tmem_put_pairs(tB, w[0]);
-          tmem_put_pairs(tB + (16u << 16), w[1]);
+          const __half2 all = __hmax2(__hmax2(top[0], top[1]), __hmax2(top[2], top[3]));
+          const bool over = __any_sync(0xffffffffu, __half2float(__hmax(__low2half(all), __high2half(all))) > MOST);
+          if (!over) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) l[k] = f2_add(l[k], sum[k]);
+          }
+          return over;
+        };
+        if (i == 0) raise();
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+          const bool over = masked ? weights(std::true_type()) : weights(std::false_type());
+          if (!over) break;
+          raise();
         }
+        tmem_put_pairs(tB, w[0]);
+        tmem_put_pairs(tB + (16u << 16), w[1]);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(p_full + 8 * place);
@@ -618,7 +630,7 @@ kv_attend_tile_kernel(const TileP p) {
           }
         }
         __syncwarp();
-        const int64_t off = out_row * p.a.o_row + out_head * p.a.o_head;
+        const int64_t off = row_in(p.a.o_row, p.a.o_head);
 #pragma unroll 4
         for (int i = 0; i < MOVES; ++i) {
           const int rr = i * (32 / LANES) + sub_row;
@@ -632,8 +644,8 @@ kv_attend_tile_kernel(const TileP p) {
             for (int x = 0; x < 8; ++x) reinterpret_cast<unsigned short*>(to)[x] = (unsigned short)(w[x >> 1] >> (16 * (x & 1)));
           }
         }
-        __syncwarp();
       }
+      done(seg);
     }
   } else if (warp < 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -653,10 +665,13 @@ kv_attend_tile_kernel(const TileP p) {
     auto step = [&]() {                                                 // on to the next block; more: there is one
       j += KEYS;
       if (behind-- > 0) return;
-      const Segment at = segment(seg++);
-      more = at.count > 0;
-      behind = at.count - 1; seq = at.seq; head = at.head; length = at.length;
-      j = at.block * KEYS + w * 32 + lane;
+      more = segment(seg);
+      if (more) {
+        const Segment& at = ring[seg % RING];
+        behind = at.count - 1; seq = at.seq; head = at.head; length = at.length;
+        j = at.block * KEYS + w * 32 + lane;
+      }
+      done(seg++);
     };
     // page: the lane's, or one that there is for a position that has none
     uint32_t page = 0, slot = 0;
@@ -726,7 +741,7 @@ kv_attend_tile_kernel(const TileP p) {
         // block n - STAGES - 2
         const uint32_t at = smem + L::C0 + (n % NUMBERS) * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
         const float v = vs < LEAST ? LEAST : vs;
-        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
+        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : NOWHERE, fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
@@ -768,13 +783,9 @@ kv_attend_tile_kernel(const TileP p) {
         umma_commit_w(leader, o_done + 8 * half);
       };
       uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
-      for (;; ++seg) {
-        int count, halves;
-        {
-          const Segment at = segment(seg);
-          count = at.count; halves = at.rows > HALF ? 2 : 1;
-        }
-        if (!count) break;
+      for (; segment(seg); ++seg) {
+        const int count = ring[seg % RING].count, halves = ring[seg % RING].rows > HALF ? 2 : 1;
+        done(seg);
         wait(q_full, seg & 1);
         if (halves == 2) wait(q_full + 8, seg1++ & 1);
         // scores two blocks ahead of the values: a half's weights are formed from one while the other is multiplied
