@@ -13,7 +13,8 @@
 //   warps 12-15    : values likewise
 //   warp 16        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
 //   warp 17        : finds the units of the CTA's share, a few ahead of the others
-// Tensor memory: for either half S of two blocks (64 columns each, the weights in their first 32) and O.
+// Tensor memory: for either half S of a block (64 columns), the weights of two (32 each) and O.  S is read into registers at once, so that the next
+// block's scores are formed behind this one's exponentials.
 //
 // All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
@@ -29,8 +30,7 @@ using namespace tc;
 
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
-constexpr float MOST = 256.f;               // the weight that makes a row's maximum move (2^LAZY of kv_attend_few.cu)
-constexpr float NOWHERE = -1e38f;           // the logarithm of a position that there is not
+constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr float LEAST = 7.888609e-31f;
 constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
 
@@ -66,6 +66,11 @@ __device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 __device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
@@ -128,11 +133,19 @@ __device__ __forceinline__ void tmem_get_frag(uint32_t taddr, uint32_t* r) {
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_put_frag(uint32_t taddr, const uint32_t* r) {
+// the same of 32 columns
+__device__ __forceinline__ void tmem_get_frag32(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_put_frag32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 // the same of pairs of 16-bit numbers: 32 columns of 32 bits, r[2 g ..]: column 4 g + lane % 4 of row lane / 4, then of row lane / 4 + 8
@@ -279,7 +292,7 @@ kv_attend_tile_kernel(const TileP p) {
   using L = Tile<DIM>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) uint64_t bars[29 + 2 * RING];
+  __shared__ __align__(8) uint64_t bars[31 + 2 * RING];
   __shared__ Segment ring[RING];
   __shared__ int64_t prefix[SEQS + 1];
   __shared__ unsigned tops[2][8];
@@ -289,23 +302,24 @@ kv_attend_tile_kernel(const TileP p) {
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar0 = smem_u32(&bars[0]);
-  // of either half: q, S and weights in two places, O; of the stages: keys, values
-  const uint32_t q_full = bar0, s_full = bar0 + 16, p_full = bar0 + 48, o_done = bar0 + 80, k_full = bar0 + 96, k_empty = bar0 + 128, v_full = bar0 + 160,
-                 v_empty = bar0 + 192, t_full = bar0 + 224, r_full = bar0 + 232, r_empty = r_full + 8 * RING;
+  // of either half: q, S there and read, weights there and multiplied (two places); of the stages: keys, values
+  const uint32_t q_full = bar0, s_full = bar0 + 16, s_empty = bar0 + 32, p_full = bar0 + 48, o_done = bar0 + 80, k_full = bar0 + 112, k_empty = bar0 + 144,
+                 v_full = bar0 + 176, v_empty = bar0 + 208, t_full = bar0 + 240, r_full = bar0 + 248, r_empty = r_full + 8 * RING;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
-      mbar_init(q_full + 8 * i, HALF);
-      mbar_init(o_done + 8 * i, 1);
+      mbar_init(q_full + 8 * i, 4);
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(s_empty + 8 * i, 4);
     }
     for (int i = 0; i < 4; ++i) {
-      mbar_init(s_full + 8 * i, 1);
-      mbar_init(p_full + 8 * i, HALF);
+      mbar_init(p_full + 8 * i, 4);
+      mbar_init(o_done + 8 * i, 1);
     }
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(k_full + 8 * i, 64);
+      mbar_init(k_full + 8 * i, 2);
       mbar_init(k_empty + 8 * i, 1);
-      mbar_init(v_full + 8 * i, 64);
+      mbar_init(v_full + 8 * i, 2);
       mbar_init(v_empty + 8 * i, 1);
     }
     mbar_init(t_full, 8);
@@ -368,15 +382,16 @@ kv_attend_tile_kernel(const TileP p) {
 
   // the n-th segment of the share, by a whole warp: false behind the last one.  done: the ring may have its place back
   auto segment = [&](uint32_t n) { return wait_warp(r_full + 8 * (n % RING), (n / RING) & 1, abortp, p.status) && ring[n % RING].count > 0; };
-  auto done = [&](uint32_t n) {
+  auto arrive = [&](uint32_t bar) {                                     // of a warp
     __syncwarp();
-    if (lane == 0) mbar_arrive(r_empty + 8 * (n % RING));
+    if (lane == 0) mbar_arrive(bar);
   };
+  auto done = [&](uint32_t n) { arrive(r_empty + 8 * (n % RING)); };
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
     const int half = warp >> 2, row = threadIdx.x & 127, quad = lane >> 2, pair = lane & 3;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + half * 128 + lanes, tO = tmem + 256 + half * 128 + lanes;
+    const uint32_t tS = tmem + half * 128 + lanes, tP = tS + 64, tO = tmem + 256 + half * 128 + lanes;
     uint32_t seg = 0, blocks = 0, turn = 0;                             // segments, blocks of the CTA, blocks of this half
     constexpr int LANES = DIM / 8, MOVES = LANES;                       // a row by so many lanes; 32 rows by so many instructions
     const int c8 = lane % LANES, sub_row = lane / LANES;
@@ -437,7 +452,7 @@ kv_attend_tile_kernel(const TileP p) {
             put16(row_at<DIM>(rows_at, (warp & 3) * 32 + i * (32 / LANES) + sub_row, c8), make_uint4(w[0], w[1], w[2], w[3]));
           }
           fence_proxy_async();
-          mbar_arrive(q_full + 8 * half);
+          arrive(q_full + 8 * half);
         }
       }
       if (rows <= 0) { blocks += at.count; done(seg); continue; }
@@ -463,38 +478,59 @@ kv_attend_tile_kernel(const TileP p) {
       inner_lo = __reduce_max_sync(0xffffffffu, inner_lo);
       inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
       float m[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
-      F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)}, minus_m[4];       // (-m, twice)
+      F2 l[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
       const int count = at.count, block0 = at.block;
       for (int i = 0; i < count; ++i, ++blocks, ++turn) {
         const int j0 = (block0 + i) * KEYS;
         const uint32_t consts = smem + L::C0 + (blocks % NUMBERS) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
-        const uint32_t place = 2 * half + (turn & 1), tB = tS + (turn & 1) * 64;
-        const bool masked = j0 < inner_lo || j0 + KEYS > inner_hi;
-        wait_warp(s_full + 8 * place, (turn >> 1) & 1, abortp, p.status);            // (and the numbers: they are there before the keys)
+        const uint32_t place = turn & 1;
+        wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);       // (and the numbers: they are there before the keys)
         tc_fence_after();
-        // m to the maximum of the block, where that is higher; O and l with it
-        auto raise = [&]() {
-          float top[4] = {minus_inf(), minus_inf(), minus_inf(), minus_inf()};
+        F2 t[4][8];
+        {
+          uint32_t raw[2][32];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint32_t raw[32];
-            tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw);
-            tmem_wait_ld();
+          for (int e = 0; e < 2; ++e) tmem_get_frag(tS + ((uint32_t)(e * 16) << 16), raw[e]);
+          tmem_wait_ld();
+          tc_fence_before();
+          arrive(s_empty + 8 * half);                                   // (the next block's scores are formed behind this one's weights)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              int low = 0, high = 0x7fffffff;
-              if (masked) sees(2 * e + k, low, high);
-              low -= j0 + 2 * pair;
-              high -= j0 + 2 * pair;
+          for (int g = 0; g < 8; ++g) {
+            const float4 ab = get16(consts + 64 * g);
+            const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w);
 #pragma unroll
-              for (int g = 0; g < 8; ++g) {
-                const float4 ab = get16(consts + 64 * g);
-                const float x = fmaf(__uint_as_float(raw[4 * g + 2 * k]), ab.x, ab.z), y = fmaf(__uint_as_float(raw[4 * g + 2 * k + 1]), ab.y, ab.w);
-                if (8 * g >= low && 8 * g < high) top[2 * e + k] = fmaxf(top[2 * e + k], x);
-                if (8 * g + 1 >= low && 8 * g + 1 < high) top[2 * e + k] = fmaxf(top[2 * e + k], y);
-              }
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t* const x = &raw[k >> 1][4 * g + 2 * (k & 1)];
+              t[k][g] = f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, fb);
             }
           }
+        }
+        if (j0 < inner_lo || j0 + KEYS > inner_hi) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            int low, high;
+            sees(k, low, high);
+            low -= j0 + 2 * pair;
+            high -= j0 + 2 * pair;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              float2 v = f2_get(t[k][g]);
+              if (8 * g < low || 8 * g >= high) v.x = minus_inf();
+              if (8 * g + 1 < low || 8 * g + 1 >= high) v.y = minus_inf();
+              t[k][g] = f2(v.x, v.y);
+            }
+          }
+        }
+        float top[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 v = f2_get(t[k][0]);
+          top[k] = fmaxf(v.x, v.y);
+#pragma unroll
+          for (int g = 1; g < 8; ++g) { const float2 v = f2_get(t[k][g]); top[k] = max3(top[k], v.x, v.y); }
+        }
+        // m hardly ever moves behind a row's first blocks
+        if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
           float f[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -504,81 +540,45 @@ kv_attend_tile_kernel(const TileP p) {
             f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
             l[k] = f2_mul(l[k], f2(f[k]));
             m[k] = to;
-            minus_m[k] = f2(-to);                                       // (no position yet: infinite, which the next one exceeds)
           }
           if (i > 0) {
-            wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);          // (the product of the block before)
+            wait_warp(o_done + 8 * (2 * half + (place ^ 1)), ((turn - 1) >> 1) & 1, abortp, p.status);   // (the product of the block before)
             tc_fence_after();
 #pragma unroll 1
-            for (int e = 0; e < DIM / 32; ++e) {
-              uint32_t o[32];
+            for (int e = 0; e < DIM / 16; ++e) {
+              uint32_t o[16];
               const float f0 = e & 1 ? f[2] : f[0], f1 = e & 1 ? f[3] : f[1];
-              const uint32_t where = tO + ((uint32_t)((e & 1) * 16) << 16) + (e >> 1) * 64;
-              tmem_get_frag(where, o);
+              const uint32_t where = tO + ((uint32_t)((e & 1) * 16) << 16) + (e >> 1) * 32;
+              tmem_get_frag32(where, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (x & 2 ? f1 : f0));
-              tmem_put_frag(where, o);
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * (x & 2 ? f1 : f0));
+              tmem_put_frag32(where, o);
             }
           }
-        };
-        uint32_t w[2][16];
-        // The weights by the m there is, which hardly ever moves behind a row's first blocks; true: one of them is above 2^LAZY
-        auto weights = [&](auto some_hidden) {
-          constexpr bool HIDDEN = decltype(some_hidden)::value;
-          uint32_t raw[2][32];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) tmem_get_frag(tB + ((uint32_t)(e * 16) << 16), raw[e]);
-          int low[4], high[4];
-          if constexpr (HIDDEN) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              sees(k, low[k], high[k]);
-              low[k] -= j0 + 2 * pair;
-              high[k] -= j0 + 2 * pair;
-            }
-          }
-          F2 sum[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)};
-          __half2 top[4];
-          tmem_wait_ld();
-#pragma unroll
-          for (int g = 0; g < 8; ++g) {
-            const float4 ab = get16(consts + 64 * g);
-            const float2 r = get8(inverses + 32 * g);
-            const F2 fa = f2(ab.x, ab.y), fb = f2(ab.z, ab.w), fr = f2(r.x, r.y);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t* const x = &raw[k >> 1][4 * g + 2 * (k & 1)];
-              const float2 t = f2_get(f2_fma(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), fa, f2_add(fb, minus_m[k])));
-              float e0 = exp2_fast(t.x), e1 = exp2_fast(t.y);
-              if (HIDDEN && (8 * g < low[k] || 8 * g >= high[k])) e0 = 0.f;
-              if (HIDDEN && (8 * g + 1 < low[k] || 8 * g + 1 >= high[k])) e1 = 0.f;
-              sum[k] = f2_fma(f2(e0, e1), fr, sum[k]);
-              const __half2 h = __floats2half2_rn(e0, e1);
-              top[k] = g ? __hmax2(top[k], h) : h;
-              w[k >> 1][2 * g + (k & 1)] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-          }
-          const __half2 all = __hmax2(__hmax2(top[0], top[1]), __hmax2(top[2], top[3]));
-          const bool over = __any_sync(0xffffffffu, __half2float(__hmax(__low2half(all), __high2half(all))) > MOST);
-          if (!over) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) l[k] = f2_add(l[k], sum[k]);
-          }
-          return over;
-        };
-        if (i == 0) raise();
-#pragma unroll 1
-        for (int e = 0; e < 2; ++e) {
-          const bool over = masked ? weights(std::true_type()) : weights(std::false_type());
-          if (!over) break;
-          raise();
         }
-        tmem_put_pairs(tB, w[0]);
-        tmem_put_pairs(tB + (16u << 16), w[1]);
+        F2 minus_m[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
+        if (turn > 1) wait_warp(o_done + 8 * (2 * half + place), ((turn >> 1) & 1) ^ 1, abortp, p.status);   // (the weights that were here)
+        tc_fence_after();
+        uint32_t w[2][16];
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const float2 r = get8(inverses + 32 * g);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 x = f2_get(f2_add(t[k][g], minus_m[k]));
+            const float e0 = exp2_fast(x.x), e1 = exp2_fast(x.y);
+            l[k] = f2_fma(f2(e0, e1), f2(r.x, r.y), l[k]);
+            w[k >> 1][2 * g + (k & 1)] = pack2(static_cast<const __half*>(nullptr), e0, e1);
+          }
+        }
+        tmem_put_pairs(tP + 32 * place, w[0]);
+        tmem_put_pairs(tP + (16u << 16) + 32 * place, w[1]);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(p_full + 8 * place);
+        arrive(p_full + 8 * (2 * half + place));
       }
       // m and l of the lane's row: they lie with the lanes 4 (row % 8) .. + 3, the sums a quarter each
       float row_m = 0.f, sum = 0.f;
@@ -592,7 +592,7 @@ kv_attend_tile_kernel(const TileP p) {
         if (lane >> 3 == k) { sum = s2; row_m = m2; }
       }
       // ---- O out
-      wait_warp(o_done + 8 * half, (turn - 1) & 1, abortp, p.status);
+      wait_warp(o_done + 8 * (2 * half + ((turn - 1) & 1)), ((turn - 1) >> 1) & 1, abortp, p.status);
       tc_fence_after();
       if (at.part >= 0) {
         float* const part = p.parts + (int64_t)at.part * L::PART + 4 * (half * HALF + row);
@@ -737,18 +737,18 @@ kv_attend_tile_kernel(const TileP p) {
         for (; waited <= of; ++waited) wait_warp(q_full, waited & 1, abortp, p.status);
       wait_warp(empty + 8 * st, ((n / STAGES) & 1) ^ 1, abortp, p.status);
       if (!values) {
-        // The numbers of block n - NUMBERS have been read: the keys of block n - STAGES have been multiplied, and those only behind the weights of
-        // block n - STAGES - 2
+        // The numbers of block n - NUMBERS have been read: the keys of block n - STAGES have been multiplied, and those only when the scores of
+        // block n - STAGES - 1 had been read, behind the weights of the one before
         const uint32_t at = smem + L::C0 + (n % NUMBERS) * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
         const float v = vs < LEAST ? LEAST : vs;
-        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : NOWHERE, fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
+        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
       }
       store(base + st * L::BYTES);
       fence_proxy_async();
-      mbar_arrive(full + 8 * st);
+      arrive(full + 8 * st);
      }
      if (!more) break;
      one = true;
@@ -765,22 +765,22 @@ kv_attend_tile_kernel(const TileP p) {
       const uint32_t qk = idesc_f16(KEYS, 0), pv = idesc_f16(DIM, 1);
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(bar, parity, abortp, p.status) && ok; };
-      auto scores = [&](int half, uint32_t st, uint32_t place) {
+      auto scores = [&](int half, uint32_t st) {
         if (!ok) return;
         const uint64_t dq = smem_desc_sw128(smem + L::Q0 + half * L::Q_BYTES, 16, 1024), dk = smem_desc_sw128(smem + L::K0 + st * L::BYTES, 16, 1024);
 #pragma unroll
         for (int k = 0; k < DIM / 16; ++k)
-          umma_ss(leader, tmem + half * 128 + place * 64, dq + (uint64_t)(((k >> 2) * L::Q_CHUNK + (k & 3) * 32) >> 4),
+          umma_ss(leader, tmem + half * 128, dq + (uint64_t)(((k >> 2) * L::Q_CHUNK + (k & 3) * 32) >> 4),
                   dk + (uint64_t)(((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4), qk, k > 0);
-        umma_commit_w(leader, s_full + 8 * (2 * half + place));
+        umma_commit_w(leader, s_full + 8 * half);
       };
       auto values = [&](int half, uint32_t st, uint32_t place, bool acc) {
         if (!ok) return;
         const uint64_t dv = smem_desc_sw128(smem + L::V0 + st * L::BYTES, L::CHUNK, 1024);
 #pragma unroll
         for (int k = 0; k < KEYS / 16; ++k)
-          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + place * 64 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
-        umma_commit_w(leader, o_done + 8 * half);
+          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + 64 + place * 32 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
+        umma_commit_w(leader, o_done + 8 * (2 * half + place));
       };
       uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
       for (; segment(seg); ++seg) {
@@ -788,34 +788,32 @@ kv_attend_tile_kernel(const TileP p) {
         done(seg);
         wait(q_full, seg & 1);
         if (halves == 2) wait(q_full + 8, seg1++ & 1);
-        // scores two blocks ahead of the values: a half's weights are formed from one while the other is multiplied
-        for (int e = 0; e < 2 && e < count; ++e) {
-          const uint32_t st = (n + e) % STAGES;
-          wait(k_full + 8 * st, ((n + e) / STAGES) & 1);
-          tc_fence_after();
-          scores(0, st, (turn[0] + e) & 1);
-          if (halves == 2) scores(1, st, (turn[1] + e) & 1);
-          if (ok) umma_commit_w(leader, k_empty + 8 * st);
-        }
-        for (int i = 0; i < count; ++i, ++n) {
-          const uint32_t st = n % STAGES, st2 = (n + 2) % STAGES;
-          const bool ahead = i + 2 < count;
+        for (int i = -1; i < count; ++i) {
+          // the scores of block i + 1, once those of block i have been read; then the values of block i
+          const uint32_t next = n + (i < 0 ? 0 : 1), st2 = next % STAGES, st = n % STAGES;
+          if (i + 1 < count) wait(k_full + 8 * st2, (next / STAGES) & 1);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == halves) break;
-            const uint32_t place = turn[h] & 1;
-            wait(p_full + 8 * (2 * h + place), (turn[h] >> 1) & 1);
-            if (h == 0) wait(v_full + 8 * st, (n / STAGES) & 1);
-            tc_fence_after();
-            values(h, st, place, i > 0);
-            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * st);
-            if (ahead) {
-              if (h == 0) { wait(k_full + 8 * st2, ((n + 2) / STAGES) & 1); tc_fence_after(); }
-              scores(h, st2, place);
+            if (i >= 0) wait(s_empty + 8 * h, turn[h] & 1);
+            if (i + 1 < count) {
+              tc_fence_after();
+              scores(h, st2);
               if (ok && h + 1 == halves) umma_commit_w(leader, k_empty + 8 * st2);
             }
+          }
+          if (i < 0) continue;
+          wait(v_full + 8 * st, (n / STAGES) & 1);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h == halves) break;
+            wait(p_full + 8 * (2 * h + (turn[h] & 1)), (turn[h] >> 1) & 1);
+            tc_fence_after();
+            values(h, st, turn[h] & 1, i > 0);
+            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * st);
             ++turn[h];
           }
+          ++n;
         }
       }
     } else if (warp == 17) {
