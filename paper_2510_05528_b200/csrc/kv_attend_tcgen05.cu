@@ -560,8 +560,7 @@ kv_attend_tile_kernel(const TileP p) {
         F2 minus_m[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) minus_m[k] = f2(m[k] == minus_inf() ? 0.f : -m[k]);
-        if (turn > 1) wait_warp(o_done + 8 * (2 * half + place), ((turn >> 1) & 1) ^ 1, abortp, p.status);   // (the weights that were here)
-        tc_fence_after();
+        // (the weights that were here have been multiplied: before these scores, by the same warp)
         uint32_t w[2][16];
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
