@@ -8,13 +8,14 @@
 // fp16 is one of 2^-12 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
 // a multiplication by a power of two; products and sums are fp32.  l is summed from the unrounded weights.  No row: zeros.
 //
-// Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time from memory straight to registers, in the
-// layout that mma.sync m16n8k16 wants of its M side, where a product over the dimensions may take them in any order: positions are the M side of
-// the scores, S^T = K Q^T, dimensions the M side of O^T = V^T P^T, rows of q the N side of both, eight at a time, so that for up to eight rows
-// nothing is computed twice and O takes dim / 4 registers.  (tcgen05 would multiply 128 rows for these eight.)  A byte becomes fp16 by a
-// permutation, 1024 + (byte + 128), and a subtraction.  Two warps of eight never meet before the end of a CTA's share.
+// Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time, in the layout that mma.sync m16n8k16 wants of its
+// M side, where a product over the dimensions may take them in any order: positions are the M side of the scores, S^T = K Q^T, dimensions the M
+// side of O^T = V^T P^T, rows of q the N side of both, eight at a time, so that for up to eight rows nothing is computed twice
+// and O takes dim / 4 registers.  (tcgen05 would multiply 128 rows for these eight.)  A byte becomes fp16 by a permutation, 1024 + (byte + 128),
+// and a subtraction.  A lane copies the bytes that it multiplies itself, sixteen at a time, to a place of its own in shared memory, STAGES - 1
+// times sixteen positions ahead (cp.async): no registers wait, and no warp waits for another before the end of a CTA's share.
 //
-// All positions of all (sequence, key head, tile of rows) units, 64 at a time, stand in one line that is cut into equal
+// All positions of all (sequence, key head, tile of rows) units, 128 at a time, stand in one line that is cut into equal
 // shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
 // last, by a counter, adds them up in the order of the parts: no CTA waits for another and the bits do not depend on the run.
 #include "kv_cache.cuh"
@@ -24,7 +25,8 @@ namespace {
 using namespace rows;
 using namespace kv;
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, STEP = 16 * WARPS;      // positions a step of a CTA
+constexpr int WARPS = 8, THREADS = 32 * WARPS, STEP = 16 * WARPS;      // positions a step of a CTA
+constexpr int STAGES = 3;                   // of sixteen positions a warp
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
 constexpr float LEAST = 7.888609e-31f;      // 2^-100: scales of values below count as this (their values are below 1e-28)
@@ -35,8 +37,27 @@ struct Few {
   static constexpr int KW = DIM / 16;       // words of a key that a lane holds; steps of the scores' product
   static constexpr int VB = DIM / 8;        // bytes of a value that a lane holds
   static constexpr int PART = R * DIM + 2 * R;     // floats of a part: O, m, l
-  static constexpr int CTAS = NT == 1 ? 4 : 3;
+  static constexpr int CTAS = 2;            // an SM
+  static constexpr int K_BYTES = DIM / 64 * 2 * 512, V_BYTES = 4 * 32 * VB;        // of sixteen positions
+  static constexpr int STAGE = K_BYTES + V_BYTES + 128;                             // and their scales
+  static constexpr int SUMS = WARPS * R * (DIM + 4) * 4;                            // the warps' O, in the place of the stages
+  static constexpr int SMEM = STAGES * STAGE * WARPS > SUMS ? STAGES * STAGE * WARPS : SUMS;
 };
+// bytes that a lane copies for itself, complete with wait_copies
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LATER>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
@@ -88,22 +109,14 @@ __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   return u;
 }
 
-// Sixteen positions of a warp on their way: keys lane / 4 and lane / 4 + 8, values 2 (lane % 4) + {0, 1, 8, 9}
-template <int DIM>
-struct Load {
-  uint32_t k[2][DIM / 16], v[4][DIM / 32];
-  float ks[2], vs[2];
-};
-// where the sixteen from position j on lie, if they share a page: the first one's row and scale
-struct Where { int64_t row, scale; int j; bool none; };
-
 template <typename T, int DIM, int NT>
 __global__ void __launch_bounds__(THREADS, Few<DIM, NT>::CTAS)
 kv_attend_few_kernel(const FewP p) {
   grid_begin();
   using F = Few<DIM, NT>;
   constexpr int R = F::R;
-  __shared__ float sO[WARPS][R][DIM + 4];
+  extern __shared__ __align__(16) uint8_t smem[];
+  float (*const sO)[R][DIM + 4] = reinterpret_cast<float (*)[R][DIM + 4]>(smem);
   __shared__ float sM[WARPS][R], sL[WARPS][R];
   __shared__ int64_t scan[WARPS];
   __shared__ int64_t at_base;
@@ -244,51 +257,34 @@ kv_attend_few_kernel(const FewP p) {
     inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
 
     const int last = max(s.length - 1, 0);
-    const bool shared = (c.page_size & 15u) == 0;          // sixteen positions share a page
-    // the place of position j, or any place in the cache for one that has none
-    auto at = [&](int j, Where& w) {
-      uint32_t page = 0, slot = 0;
-      w.none = !place(c, b, seq, (uint32_t)min(j, last), page, slot);
-      if (w.none) page = slot = 0;
-      w.row = page * c.page + head * c.head + slot * c.slot;
-      w.scale = page * c.spage + head * c.shead + slot * c.sslot;
+    // ---- sixteen positions from j on: a lane looks up the place of j + lane % 16
+    uint8_t* const mine = smem + warp * (STAGES * F::STAGE);
+    const uint32_t lane_at = (uint32_t)__cvta_generic_to_shared(mine) + lane * 16;
+    uint32_t page = 0, slot = 0;
+    auto look = [&](int i) {                                // of step i
+      const uint32_t j = (uint32_t)min((step0 + i) * STEP + warp * 16 + (lane & 15), last);
+      const uint32_t x = quotient(j, c.mul, c.shift);
+      slot = j - x * c.page_size;
+      page = x < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + x] : 0xffffffffu;
     };
-    auto find = [&](int j0, Where& w) {
-      if (shared) at(min(j0, last & ~15), w);
-      w.j = j0;
-    };
-    auto load_k = [&](Where& w, Load<DIM>& x) {
-      bool none = false;
+    unsigned refused = 0;                                   // a bit a step under way: one of its positions has no page
+    auto fetch = [&](int i) {                               // what has been looked up, to the stage of step i
+      const bool none = page >= c.n_pages;
+      if (none) page = slot = 0;
+      refused = refused << 1 | (unsigned)__any_sync(0xffffffffu, none);
+      const int64_t row = page * c.page + head * c.head + slot * c.slot, scale = page * c.spage + head * c.shead + slot * c.sslot;
+      const uint32_t to = lane_at + (uint32_t)(i % STAGES) * F::STAGE;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int r = quad + 8 * e;
-        Where one{w.row + r * c.slot, w.scale + r * c.sslot, 0, false};
-        if (!shared) { at(w.j + r, one); none |= one.none; }
+        const int64_t r = __shfl_sync(0xffffffffu, row, quad + 8 * e);
 #pragma unroll
-        for (int h = 0; h < DIM / 64; ++h) {
-          const uint4 v = *reinterpret_cast<const uint4*>(c.k + one.row + h * 64 + part * 16);
-          x.k[e][4 * h] = v.x; x.k[e][4 * h + 1] = v.y; x.k[e][4 * h + 2] = v.z; x.k[e][4 * h + 3] = v.w;
-        }
-        x.ks[e] = c.ks[one.scale];
-        x.vs[e] = c.vs[one.scale];
+        for (int h = 0; h < DIM / 64; ++h) copy_async<16>(to + (e * (DIM / 64) + h) * 512, c.k + r + h * 64 + part * 16);
       }
-      if (!shared) w.none = __any_sync(0xffffffffu, none);
-    };
-    auto load_v = [&](const Where& w, Load<DIM>& x) {
+      const uint32_t to_v = to - lane * 16 + F::K_BYTES + lane * F::VB;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 2 * part + (e & 1) + (e >> 1) * 8;
-        Where one{w.row + r * c.slot, 0, 0, false};
-        if (!shared) at(w.j + r, one);
-        const int8_t* const from = c.v + one.row + quad * F::VB;
-        if constexpr (DIM == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(from);
-          x.v[e][0] = v.x; x.v[e][1] = v.y; x.v[e][2] = v.z; x.v[e][3] = v.w;
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(from);
-          x.v[e][0] = v.x; x.v[e][1] = v.y;
-        }
-      }
+      for (int e = 0; e < 4; ++e)
+        copy_async<F::VB>(to_v + e * 32 * F::VB, c.v + __shfl_sync(0xffffffffu, row, 2 * part + (e & 1) + (e >> 1) * 8) + quad * F::VB);
+      copy_async<4>(to - lane * 12 + F::K_BYTES + F::V_BYTES, (lane < 16 ? c.ks : c.vs) + scale);
     };
 
     float O[NT][DIM / 16][4], m[NT][2], l[NT][2];
@@ -296,42 +292,63 @@ kv_attend_few_kernel(const FewP p) {
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int d = 0; d < DIM / 16; ++d) O[n][d][0] = O[n][d][1] = O[n][d][2] = O[n][d][3] = 0.f;
-      m[n][0] = m[n][1] = -__int_as_float(0x7f800000);
+      m[n][0] = m[n][1] = minus_inf();
       l[n][0] = l[n][1] = 0.f;
     }
 
-    Where w, next;                                        // of the sixteen whose values are next, and of those after them
-    Load<DIM> x;
-    find(step0 * STEP + warp * 16, w);
-    load_k(w, x);
-    load_v(w, x);
-    next = w;
-    if (count > 1) find((step0 + 1) * STEP + warp * 16, next);
+    look(0);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+      if (i < count) {
+        fetch(i);
+        if (i + 1 < count) look(i + 1);
+      }
+      end_copies();
+    }
     for (int i = 0; i < count; ++i) {
-      const int j0 = w.j;
-      const bool bad_page = w.none;
+      wait_copies<STAGES - 2>();
+      __syncwarp();
+      unsigned behind = STAGES - 2;                         // steps fetched behind this one
+      if (i + STAGES - 1 < count) {
+        fetch(i + STAGES - 1);
+        if (i + STAGES < count) look(i + STAGES);
+        ++behind;
+      } else {
+        behind = (unsigned)(count - 1 - i);
+      }
+      end_copies();
+      const int j0 = (step0 + i) * STEP + warp * 16;
+      const bool bad_page = refused >> behind & 1u;
       if (bad_page && j0 < inner_hi && lane == 0) report(p.status);
+      const uint8_t* const stage = mine + (i % STAGES) * F::STAGE;
 
       // ---- scores
       float t[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) t[n][0] = t[n][1] = t[n][2] = t[n][3] = 0.f;
 #pragma unroll
-      for (int k = 0; k < F::KW; ++k) {
-        const uint32_t a0 = x.k[0][k] ^ 0x80808080u, a1 = x.k[1][k] ^ 0x80808080u;
-        const uint32_t a[4] = {bytes_half(a0, 0x4140), bytes_half(a1, 0x4140), bytes_half(a0, 0x4342), bytes_half(a1, 0x4342)};
+      for (int h = 0; h < DIM / 64; ++h) {
+        const uint4 x = *reinterpret_cast<const uint4*>(stage + h * 512 + lane * 16), y = *reinterpret_cast<const uint4*>(stage + (DIM / 64 + h) * 512 + lane * 16);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma(t[n], a, q[n][k][0], q[n][k][1]);
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t a0 = xs[k] ^ 0x80808080u, a1 = ys[k] ^ 0x80808080u;
+          const uint32_t a[4] = {bytes_half(a0, 0x4140), bytes_half(a1, 0x4140), bytes_half(a0, 0x4342), bytes_half(a1, 0x4342)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma(t[n], a, q[n][4 * h + k][0], q[n][4 * h + k][1]);
+        }
       }
       float ka[2], kb[2], kr[2];
+      {
+        const float* const scales = reinterpret_cast<const float*>(stage + F::K_BYTES + F::V_BYTES);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float vs = x.vs[e] < LEAST ? LEAST : x.vs[e];
-        ka[e] = x.ks[e] * factor;
-        kb[e] = __log2f(vs);
-        kr[e] = __fdividef(1.f, vs);
+        for (int e = 0; e < 2; ++e) {
+          const float v = scales[16 + quad + 8 * e], vs = v < LEAST ? LEAST : v;
+          ka[e] = scales[quad + 8 * e] * factor;
+          kb[e] = __log2f(vs);
+          kr[e] = __fdividef(1.f, vs);
+        }
       }
-      if (i + 1 < count) load_k(next, x);                 // the next keys set out
       const bool whole = !bad_page && j0 >= inner_lo && j0 + 16 <= inner_hi;
       uint32_t P[NT][2];
 #pragma unroll
@@ -343,20 +360,17 @@ kv_attend_few_kernel(const FewP p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = j0 + quad + 8 * (e >> 1);
-            if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) { t[n][e] = -__int_as_float(0x7f800000); r[e] = 0.f; }
+            if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) { t[n][e] = minus_inf(); r[e] = 0.f; }
           }
         }
-        // the sixteen's maxima, and m with them where it is passed by far
+        // m to the sixteen's maximum, where that passes it by far
         float top[2] = {fmaxf(t[n][0], t[n][2]), fmaxf(t[n][1], t[n][3])};
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], o));
-          top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], o));
-        }
         if (__any_sync(0xffffffffu, top[0] > m[n][0] + LAZY || top[1] > m[n][1] + LAZY)) {
           float f[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
             const float to = fmaxf(m[n][e], top[e]);
             f[e] = m[n][e] == to ? 1.f : exp2_fast(m[n][e] - to);       // (nothing yet: 2^-inf)
             m[n][e] = to;
@@ -368,7 +382,7 @@ kv_attend_few_kernel(const FewP p) {
         float wgt[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float mm = m[n][e & 1] == -__int_as_float(0x7f800000) ? 0.f : m[n][e & 1];
+          const float mm = m[n][e & 1] == minus_inf() ? 0.f : m[n][e & 1];
           wgt[e] = exp2_fast(t[n][e] - mm);
           l[n][e & 1] = fmaf(wgt[e], r[e], l[n][e & 1]);
         }
@@ -377,13 +391,25 @@ kv_attend_few_kernel(const FewP p) {
       }
 
       // ---- O^T += V^T P^T: a lane's dimensions quad DIM / 8 + 2 d, + 1
+      uint32_t V[4][DIM / 32];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint8_t* const from = stage + F::K_BYTES + e * 32 * F::VB + lane * F::VB;
+        if constexpr (DIM == 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(from);
+          V[e][0] = v.x; V[e][1] = v.y; V[e][2] = v.z; V[e][3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(from);
+          V[e][0] = v.x; V[e][1] = v.y;
+        }
+      }
 #pragma unroll
       for (int h = 0; h < DIM / 32; ++h) {
-        uint32_t V[4];
+        uint32_t v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) V[e] = x.v[e][h] ^ 0x80808080u;
-        const uint32_t a01 = __byte_perm(V[0], V[1], 0x5140), b01 = __byte_perm(V[0], V[1], 0x7362);
-        const uint32_t a23 = __byte_perm(V[2], V[3], 0x5140), b23 = __byte_perm(V[2], V[3], 0x7362);
+        for (int e = 0; e < 4; ++e) v[e] = V[e][h] ^ 0x80808080u;
+        const uint32_t a01 = __byte_perm(v[0], v[1], 0x5140), b01 = __byte_perm(v[0], v[1], 0x7362);
+        const uint32_t a23 = __byte_perm(v[2], v[3], 0x5140), b23 = __byte_perm(v[2], v[3], 0x7362);
         const uint32_t lo[4] = {bytes_half(a01, 0x4140), bytes_half(a01, 0x4342), bytes_half(a23, 0x4140), bytes_half(a23, 0x4342)};
         const uint32_t hi[4] = {bytes_half(b01, 0x4140), bytes_half(b01, 0x4342), bytes_half(b23, 0x4140), bytes_half(b23, 0x4342)};
 #pragma unroll
@@ -392,15 +418,11 @@ kv_attend_few_kernel(const FewP p) {
           mma(O[n][2 * h + 1], hi, P[n][0], P[n][1]);
         }
       }
-      if (i + 1 < count) {                                // and the next values
-        w = next;
-        load_v(w, x);
-        if (i + 2 < count) find((step0 + i + 2) * STEP + warp * 16, next);
-      }
     }
+    wait_copies<0>();
 
-    // ---- the four warps' sums to one
-    __syncthreads();                                      // (what a previous unit left has been read)
+    // ---- the warps' sums to one
+    __syncthreads();                                      // (the stages have been read)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -417,7 +439,7 @@ kv_attend_few_kernel(const FewP p) {
     __syncthreads();
     const bool cut = count < un.steps;
     float* const parts = p.parts;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first == 0 ? 1 : 0);
+    const int64_t part_at = 2 * (int64_t)blockIdx.x + (first == 0 ? 1 : 0);
     auto put = [&](int r, int d, float4 o, float l) {     // four dimensions of a row of the output
       const float inv = l == 0.f ? 0.f : 1.f / l;         // (a row that sees nothing: zeros)
       const int rr = tile * R + r, i = rr / p.a.group, g = rr - i * p.a.group;
@@ -446,7 +468,7 @@ kv_attend_few_kernel(const FewP p) {
         o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
       }
       if (!cut) { put(r, d, o, sum); continue; }
-      float* const to = parts + slot * F::PART;
+      float* const to = parts + part_at * F::PART;
       *reinterpret_cast<float4*>(to + r * DIM + d) = o;
       if (d == 0) { to[R * DIM + r] = top; to[R * DIM + R + r] = sum; }
     }
@@ -462,26 +484,72 @@ kv_attend_few_kernel(const FewP p) {
       }
       __syncthreads();
       if (last_one) {
+        // Each warp adds every WARPS-th part, eight of its rows or more at a time; then the warps' sums as above
         __threadfence();
+        const int n_parts = (int)(c1 - c0) + 1;
+        auto at = [&](int k) { return parts + (2 * (c0 + k) + (k == 0)) * F::PART; };
+        float top[R / 8], sum[R / 8];                     // of rows lane % 8 + 8 k, over the lane's parts
+#pragma unroll
+        for (int k = 0; k < R / 8; ++k) {
+          top[k] = minus_inf();
+          for (int x = threadIdx.x >> 3; x < n_parts; x += THREADS / 8) top[k] = fmaxf(top[k], __ldcg(at(x) + R * DIM + 8 * k + (lane & 7)));
+          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 8));
+          top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 16));
+          if (lane < 8) sM[warp][8 * k + lane] = top[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < R / 8; ++k) {
+#pragma unroll
+          for (int w2 = 0; w2 < WARPS; ++w2) top[k] = fmaxf(top[k], sM[w2][8 * k + (lane & 7)]);
+          sum[k] = 0.f;
+        }
+        __syncthreads();
+        float4 o[R * DIM / 128];                          // four numbers of every 128
+#pragma unroll
+        for (int u = 0; u < R * DIM / 128; ++u) o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int x = warp; x < n_parts; x += WARPS) {
+          const float* const from = at(x);
+          float4 v[R * DIM / 128];
+#pragma unroll
+          for (int u = 0; u < R * DIM / 128; ++u) v[u] = __ldcg(reinterpret_cast<const float4*>(from + u * 128) + lane);
+          float f[R / 8];
+#pragma unroll
+          for (int k = 0; k < R / 8; ++k) {
+            f[k] = weight(__ldcg(from + R * DIM + 8 * k + (lane & 7)), top[k]);
+            sum[k] = fmaf(f[k], __ldcg(from + R * DIM + R + 8 * k + (lane & 7)), sum[k]);
+          }
+#pragma unroll
+          for (int u = 0; u < R * DIM / 128; ++u) {
+            const int r = u * (128 / DIM) + (DIM == 64 ? lane >> 4 : 0);
+            const float g = __shfl_sync(0xffffffffu, f[u * (128 / DIM) / 8], r & 7);
+            o[u].x = fmaf(g, v[u].x, o[u].x); o[u].y = fmaf(g, v[u].y, o[u].y); o[u].z = fmaf(g, v[u].z, o[u].z); o[u].w = fmaf(g, v[u].w, o[u].w);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < R * DIM / 128; ++u)
+          *reinterpret_cast<float4*>(&sO[warp][u * (128 / DIM) + (DIM == 64 ? lane >> 4 : 0)][DIM == 64 ? (lane & 15) * 4 : lane * 4]) = o[u];
+#pragma unroll
+        for (int k = 0; k < R / 8; ++k)
+          if (lane < 8) sL[warp][8 * k + lane] = sum[k];
+        __syncthreads();
         for (int u = threadIdx.x; u < R * (DIM / 4); u += THREADS) {
           const int r = u / (DIM / 4), d = u % (DIM / 4) * 4;
           if (r >= rows) break;
-          float top = -__int_as_float(0x7f800000);
-          for (int64_t k = c0; k <= c1; ++k) top = fmaxf(top, __ldcg(parts + (2 * k + (k == c0)) * F::PART + R * DIM + r));
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-          float sum = 0.f;
-#pragma unroll 4
-          for (int64_t k = c0; k <= c1; ++k) {
-            const float* const from = parts + (2 * k + (k == c0)) * F::PART;
-            const float f = weight(__ldcg(from + R * DIM + r), top);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(from + r * DIM + d));
-            sum = fmaf(f, __ldcg(from + R * DIM + R + r), sum);
-            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+          float4 s4 = make_float4(0.f, 0.f, 0.f, 0.f);
+          float ls = 0.f;
+#pragma unroll
+          for (int w2 = 0; w2 < WARPS; ++w2) {
+            const float4 v = *reinterpret_cast<const float4*>(&sO[w2][r][d]);
+            ls += sL[w2][r];
+            s4.x += v.x; s4.y += v.y; s4.z += v.z; s4.w += v.w;
           }
-          put(r, d, o, sum);
+          put(r, d, s4, ls);
         }
       }
     }
+    __syncthreads();                                      // (the stages' place is free)
     begin += count;
   }
 }
@@ -493,6 +561,8 @@ namespace {
 template <typename T, int DIM, int NT>
 void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
   using F = Few<DIM, NT>;
+  static PerDeviceOnce once;
+  if (ensure_dynamic_smem(once, c->device, kv_attend_few_kernel<T, DIM, NT>, F::SMEM) != ARMOR_OK) { c->host_err = ARMOR_ERR_CUDA; return; }
   // two parts a CTA have to find room in the workspace (a single CTA leaves none)
   int64_t n = (int64_t)c->n_sm * F::CTAS;
   const int64_t room = ws_scratch_bytes(c) / (2 * F::PART * (int64_t)sizeof(float));
@@ -505,7 +575,7 @@ void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
     p.a.b.lengths = all.lengths + b0;
     p.a.b.starts = all.starts + b0;
     p.a.b.pages = all.pages + b0 * all.ld;
-    launch_dependent(kv_attend_few_kernel<T, DIM, NT>, dim3((unsigned)n), dim3(THREADS), 0, s, p);
+    launch_dependent(kv_attend_few_kernel<T, DIM, NT>, dim3((unsigned)n), dim3(THREADS), F::SMEM, s, p);
     c->launches++;
   }
 }
