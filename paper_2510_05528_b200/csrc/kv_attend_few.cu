@@ -8,14 +8,14 @@
 // fp16 is one of 2^-12 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
 // a multiplication by a power of two; products and sums are fp32.  l is summed from the unrounded weights.  No row: zeros.
 //
-// Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time, in the layout that mma.sync m16n8k16 wants of its
+// Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time, twice, in the layout that mma.sync m16n8k16 wants of its
 // M side, where a product over the dimensions may take them in any order: positions are the M side of the scores, S^T = K Q^T, dimensions the M
 // side of O^T = V^T P^T, rows of q the N side of both, eight at a time, so that for up to eight rows nothing is computed twice
 // and O takes dim / 4 registers.  (tcgen05 would multiply 128 rows for these eight.)  A byte becomes fp16 by a permutation, 1024 + (byte + 128),
-// and a subtraction.  A lane copies the bytes that it multiplies itself, sixteen at a time, to a place of its own in shared memory, STAGES - 1
-// times sixteen positions ahead (cp.async): no registers wait, and no warp waits for another before the end of a CTA's share.
+// and a subtraction.  A lane copies the bytes that it multiplies itself, sixteen at a time, to a place of its own in shared memory, 32
+// positions ahead (cp.async): no registers wait, and no warp waits for another before the end of a CTA's share.
 //
-// All positions of all (sequence, key head, tile of rows) units, 128 at a time, stand in one line that is cut into equal
+// All positions of all (sequence, key head, tile of rows) units, 192 at a time, stand in one line that is cut into equal
 // shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
 // last, by a counter, adds them up in the order of the parts: no CTA waits for another and the bits do not depend on the run.
 #include "kv_cache.cuh"
@@ -25,8 +25,8 @@ namespace {
 using namespace rows;
 using namespace kv;
 
-constexpr int WARPS = 8, THREADS = 32 * WARPS, STEP = 16 * WARPS;      // positions a step of a CTA
-constexpr int STAGES = 3;                   // of sixteen positions a warp
+constexpr int WARPS = 6, THREADS = 32 * WARPS, STEP = 32 * WARPS;      // positions a step of a CTA
+constexpr int STAGES = 2;                   // of 32 positions a warp
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
 constexpr float LEAST = 7.888609e-31f;      // 2^-100: scales of values below count as this (their values are below 1e-28)
@@ -39,9 +39,10 @@ struct Few {
   static constexpr int PART = R * DIM + 2 * R;     // floats of a part: O, m, l
   static constexpr int CTAS = 2;            // an SM
   static constexpr int K_BYTES = DIM / 64 * 2 * 512, V_BYTES = 4 * 32 * VB;        // of sixteen positions
-  static constexpr int STAGE = K_BYTES + V_BYTES + 128;                             // and their scales
+  static constexpr int SCALES = 2 * (K_BYTES + V_BYTES), STAGE = SCALES + 256;      // of 32
+  static constexpr bool Q_SHARED = NT > 1;                                          // q in shared memory (registers hold eight rows of it)
   static constexpr int SUMS = WARPS * R * (DIM + 4) * 4;                            // the warps' O, in the place of the stages
-  static constexpr int SMEM = STAGES * STAGE * WARPS > SUMS ? STAGES * STAGE * WARPS : SUMS;
+  static constexpr int Q_AT = STAGES * STAGE * WARPS > SUMS ? STAGES * STAGE * WARPS : SUMS, SMEM = Q_AT + (Q_SHARED ? NT * KW * 32 * 8 : 0);
 };
 // bytes that a lane copies for itself, complete with wait_copies
 template <int BYTES>
@@ -52,11 +53,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
 __device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LATER>
 __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory"); }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 __device__ __forceinline__ float minus_inf() { return -__int_as_float(0x7f800000); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -109,7 +105,8 @@ __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   return u;
 }
 
-template <typename T, int DIM, int NT>
+// TOGETHER: sixteen positions that begin at a multiple of sixteen share a page
+template <typename T, int DIM, int NT, bool TOGETHER>
 __global__ void __launch_bounds__(THREADS, Few<DIM, NT>::CTAS)
 kv_attend_few_kernel(const FewP p) {
   grid_begin();
@@ -183,7 +180,8 @@ kv_attend_few_kernel(const FewP p) {
     const int step0 = (int)(lo_all / STEP) + first;
 
     // ---- q: rows lane / 4 of each eight, four dimensions for each step of the product, in the order that keys come in
-    uint32_t q[NT][F::KW][2];
+    uint32_t q[F::Q_SHARED ? 1 : NT][F::Q_SHARED ? 1 : F::KW][2];
+    uint2* const q_shared = reinterpret_cast<uint2*>(smem + F::Q_AT) + lane;
     float factor;
     {
       const T* const t = nullptr;
@@ -228,12 +226,16 @@ kv_attend_few_kernel(const FewP p) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int k = 0; k < F::KW; ++k)
+        for (int k = 0; k < F::KW; ++k) {
+          uint32_t x[2] = {raw[n][k][0], raw[n][k][1]};
+          if (!std::is_same<T, __half>::value) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (std::is_same<T, __half>::value) q[n][k][e] = raw[n][k][e];
-            else { const float2 v = unpack2(t, raw[n][k][e]); q[n][k][e] = half2_bits(v.x * up, v.y * up); }
+            for (int e = 0; e < 2; ++e) { const float2 v = unpack2(t, x[e]); x[e] = half2_bits(v.x * up, v.y * up); }
           }
+          if constexpr (!F::Q_SHARED) { q[n][k][0] = x[0]; q[n][k][1] = x[1]; }
+          else if (warp == 0) q_shared[(n * F::KW + k) * 32] = make_uint2(x[0], x[1]);
+        }
+      if (F::Q_SHARED) __syncthreads();
     }
 
     // ---- the positions that rows 2 part and 2 part + 1 of each eight see: [low, high)
@@ -257,34 +259,45 @@ kv_attend_few_kernel(const FewP p) {
     inner_hi = __reduce_min_sync(0xffffffffu, inner_hi);
 
     const int last = max(s.length - 1, 0);
-    // ---- sixteen positions from j on: a lane looks up the place of j + lane % 16
+    // ---- 32 positions of a step: a lane looks up the place of one of them, or of the first of its sixteen
     uint8_t* const mine = smem + warp * (STAGES * F::STAGE);
-    const uint32_t lane_at = (uint32_t)__cvta_generic_to_shared(mine) + lane * 16;
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
     uint32_t page = 0, slot = 0;
     auto look = [&](int i) {                                // of step i
-      const uint32_t j = (uint32_t)min((step0 + i) * STEP + warp * 16 + (lane & 15), last);
-      const uint32_t x = quotient(j, c.mul, c.shift);
-      slot = j - x * c.page_size;
+      int j = (step0 + i) * STEP + warp * 32 + lane;
+      j = TOGETHER ? min(j & ~15, last & ~15) : min(j, last);
+      const uint32_t x = quotient((uint32_t)j, c.mul, c.shift);
+      slot = (uint32_t)j - x * c.page_size;
       page = x < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + x] : 0xffffffffu;
     };
     unsigned refused = 0;                                   // a bit a step under way: one of its positions has no page
+    const int64_t to_k = quad * c.slot + part * 16, to_v = 2 * part * c.slot + quad * F::VB;
     auto fetch = [&](int i) {                               // what has been looked up, to the stage of step i
       const bool none = page >= c.n_pages;
       if (none) page = slot = 0;
       refused = refused << 1 | (unsigned)__any_sync(0xffffffffu, none);
-      const int64_t row = page * c.page + head * c.head + slot * c.slot, scale = page * c.spage + head * c.shead + slot * c.sslot;
-      const uint32_t to = lane_at + (uint32_t)(i % STAGES) * F::STAGE;
+      const int64_t row = page * c.page + head * c.head + slot * c.slot;
+      int64_t scale = page * c.spage + head * c.shead + slot * c.sslot;
+      if (TOGETHER) scale += (lane & 15) * c.sslot;
+      const uint32_t to = mine_at + (uint32_t)(i % STAGES) * F::STAGE, k_at = to + lane * 16, v_at = to + 2 * F::K_BYTES + lane * F::VB;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int64_t r = __shfl_sync(0xffffffffu, row, quad + 8 * e);
+      for (int g = 0; g < 2; ++g) {
+        const int64_t first = TOGETHER ? __shfl_sync(0xffffffffu, row, 16 * g) : 0;
 #pragma unroll
-        for (int h = 0; h < DIM / 64; ++h) copy_async<16>(to + (e * (DIM / 64) + h) * 512, c.k + r + h * 64 + part * 16);
+        for (int e = 0; e < 2; ++e) {
+          const int8_t* const from = c.k + (TOGETHER ? first + to_k + 8 * e * c.slot : __shfl_sync(0xffffffffu, row, 16 * g + quad + 8 * e) + part * 16);
+#pragma unroll
+          for (int h = 0; h < DIM / 64; ++h) copy_async<16>(k_at + ((g * 2 + e) * (DIM / 64) + h) * 512, from + h * 64);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = (e & 1) + (e >> 1) * 8;
+          copy_async<F::VB>(v_at + (g * 4 + e) * 32 * F::VB,
+                            c.v + (TOGETHER ? first + to_v + r * c.slot : __shfl_sync(0xffffffffu, row, 16 * g + 2 * part + r) + quad * F::VB));
+        }
       }
-      const uint32_t to_v = to - lane * 16 + F::K_BYTES + lane * F::VB;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        copy_async<F::VB>(to_v + e * 32 * F::VB, c.v + __shfl_sync(0xffffffffu, row, 2 * part + (e & 1) + (e >> 1) * 8) + quad * F::VB);
-      copy_async<4>(to - lane * 12 + F::K_BYTES + F::V_BYTES, (lane < 16 ? c.ks : c.vs) + scale);
+      copy_async<4>(to + F::SCALES + lane * 4, c.ks + scale);
+      copy_async<4>(to + F::SCALES + 128 + lane * 4, c.vs + scale);
     };
 
     float O[NT][DIM / 16][4], m[NT][2], l[NT][2];
@@ -317,61 +330,97 @@ kv_attend_few_kernel(const FewP p) {
         behind = (unsigned)(count - 1 - i);
       }
       end_copies();
-      const int j0 = (step0 + i) * STEP + warp * 16;
+      const int j0 = (step0 + i) * STEP + warp * 32;
       const bool bad_page = refused >> behind & 1u;
       if (bad_page && j0 < inner_hi && lane == 0) report(p.status);
       const uint8_t* const stage = mine + (i % STAGES) * F::STAGE;
 
-      // ---- scores
-      float t[NT][4];
+      // ---- scores of twice sixteen positions
+      float t[2][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) t[n][0] = t[n][1] = t[n][2] = t[n][3] = 0.f;
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) t[g][n][0] = t[g][n][1] = t[g][n][2] = t[g][n][3] = 0.f;
 #pragma unroll
       for (int h = 0; h < DIM / 64; ++h) {
-        const uint4 x = *reinterpret_cast<const uint4*>(stage + h * 512 + lane * 16), y = *reinterpret_cast<const uint4*>(stage + (DIM / 64 + h) * 512 + lane * 16);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+        uint4 x[2][2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) x[g][e] = *reinterpret_cast<const uint4*>(stage + ((g * 2 + e) * (DIM / 64) + h) * 512 + lane * 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t a0 = xs[k] ^ 0x80808080u, a1 = ys[k] ^ 0x80808080u;
-          const uint32_t a[4] = {bytes_half(a0, 0x4140), bytes_half(a1, 0x4140), bytes_half(a0, 0x4342), bytes_half(a1, 0x4342)};
+          uint32_t b0[NT], b1[NT];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma(t[n], a, q[n][4 * h + k][0], q[n][4 * h + k][1]);
-        }
-      }
-      float ka[2], kb[2], kr[2];
-      {
-        const float* const scales = reinterpret_cast<const float*>(stage + F::K_BYTES + F::V_BYTES);
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (F::Q_SHARED) {
+              const uint2 v = q_shared[(n * F::KW + 4 * h + k) * 32];
+              b0[n] = v.x; b1[n] = v.y;
+            } else { b0[n] = q[n][4 * h + k][0]; b1[n] = q[n][4 * h + k][1]; }
+          }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float v = scales[16 + quad + 8 * e], vs = v < LEAST ? LEAST : v;
-          ka[e] = scales[quad + 8 * e] * factor;
-          kb[e] = __log2f(vs);
-          kr[e] = __fdividef(1.f, vs);
-        }
-      }
-      const bool whole = !bad_page && j0 >= inner_lo && j0 + 16 <= inner_hi;
-      uint32_t P[NT][2];
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t x0 = k == 0 ? x[g][0].x : k == 1 ? x[g][0].y : k == 2 ? x[g][0].z : x[g][0].w;
+            const uint32_t x1 = k == 0 ? x[g][1].x : k == 1 ? x[g][1].y : k == 2 ? x[g][1].z : x[g][1].w;
+            const uint32_t a0 = x0 ^ 0x80808080u, a1 = x1 ^ 0x80808080u;
+            const uint32_t a[4] = {bytes_half(a0, 0x4140), bytes_half(a1, 0x4140), bytes_half(a0, 0x4342), bytes_half(a1, 0x4342)};
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[n][e] = fmaf(t[n][e], ka[e >> 1], kb[e >> 1]);
-        float r[4] = {kr[0], kr[0], kr[1], kr[1]};
-        if (!whole) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = j0 + quad + 8 * (e >> 1);
-            if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) { t[n][e] = minus_inf(); r[e] = 0.f; }
+            for (int n = 0; n < NT; ++n) mma(t[g][n], a, b0[n], b1[n]);
           }
         }
-        // m to the sixteen's maximum, where that passes it by far
-        float top[2] = {fmaxf(t[n][0], t[n][2]), fmaxf(t[n][1], t[n][3])};
-        if (__any_sync(0xffffffffu, top[0] > m[n][0] + LAZY || top[1] > m[n][1] + LAZY)) {
+      }
+      float kr[2][2];
+      {
+        const float* const scales = reinterpret_cast<const float*>(stage + F::SCALES);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float v = scales[32 + 16 * g + quad + 8 * e], vs = v < LEAST ? LEAST : v;
+            const float ka = scales[16 * g + quad + 8 * e] * factor, kb = __log2f(vs);
+            kr[g][e] = __fdividef(1.f, vs);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) t[g][n][2 * e + x] = fmaf(t[g][n][2 * e + x], ka, kb);
+          }
+      }
+      const bool some_hidden = bad_page || j0 < inner_lo || j0 + 32 > inner_hi;
+      if (some_hidden) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = j0 + 16 * g + quad + 8 * (e >> 1);
+              if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) t[g][n][e] = minus_inf();
+            }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (!(kr[g][e] == kr[g][e])) kr[g][e] = 1.f;    // (no number: the weight is none either, and 0 where it is not seen)
+      }
+      // m to their maximum, where that passes it by far
+      bool over = false;
+      float top[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          top[n][e] = fmaxf(fmaxf(t[0][n][e], t[0][n][e + 2]), fmaxf(t[1][n][e], t[1][n][e + 2]));
+          over |= top[n][e] > m[n][e] + LAZY;
+        }
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
           float f[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], o));
-            const float to = fmaxf(m[n][e], top[e]);
+            for (int o = 4; o < 32; o <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], o));
+            const float to = fmaxf(m[n][e], top[n][e]);
             f[e] = m[n][e] == to ? 1.f : exp2_fast(m[n][e] - to);       // (nothing yet: 2^-inf)
             m[n][e] = to;
             l[n][e] *= f[e];
@@ -379,43 +428,51 @@ kv_attend_few_kernel(const FewP p) {
 #pragma unroll
           for (int d = 0; d < DIM / 16; ++d) { O[n][d][0] *= f[0]; O[n][d][1] *= f[1]; O[n][d][2] *= f[0]; O[n][d][3] *= f[1]; }
         }
-        float wgt[4];
+      }
+      uint32_t P[2][NT][2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float mm = m[n][e & 1] == minus_inf() ? 0.f : m[n][e & 1];
-          wgt[e] = exp2_fast(t[n][e] - mm);
-          l[n][e & 1] = fmaf(wgt[e], r[e], l[n][e & 1]);
-        }
-        P[n][0] = transpose8(half2_bits(wgt[0], wgt[1]));
-        P[n][1] = transpose8(half2_bits(wgt[2], wgt[3]));
+      for (int n = 0; n < NT; ++n) {
+        const float m0 = m[n][0] == minus_inf() ? 0.f : m[n][0], m1 = m[n][1] == minus_inf() ? 0.f : m[n][1];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float w0 = exp2_fast(t[g][n][2 * e] - m0), w1 = exp2_fast(t[g][n][2 * e + 1] - m1);
+            l[n][0] = fmaf(w0, kr[g][e], l[n][0]);
+            l[n][1] = fmaf(w1, kr[g][e], l[n][1]);
+            P[g][n][e] = transpose8(half2_bits(w0, w1));
+          }
       }
 
       // ---- O^T += V^T P^T: a lane's dimensions quad DIM / 8 + 2 d, + 1
-      uint32_t V[4][DIM / 32];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint8_t* const from = stage + F::K_BYTES + e * 32 * F::VB + lane * F::VB;
-        if constexpr (DIM == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(from);
-          V[e][0] = v.x; V[e][1] = v.y; V[e][2] = v.z; V[e][3] = v.w;
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(from);
-          V[e][0] = v.x; V[e][1] = v.y;
+      for (int g = 0; g < 2; ++g) {
+        uint32_t V[4][DIM / 32];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint8_t* const from = stage + 2 * F::K_BYTES + (g * 4 + e) * 32 * F::VB + lane * F::VB;
+          if constexpr (DIM == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(from);
+            V[e][0] = v.x; V[e][1] = v.y; V[e][2] = v.z; V[e][3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(from);
+            V[e][0] = v.x; V[e][1] = v.y;
+          }
         }
-      }
 #pragma unroll
-      for (int h = 0; h < DIM / 32; ++h) {
-        uint32_t v[4];
+        for (int h = 0; h < DIM / 32; ++h) {
+          uint32_t v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = V[e][h] ^ 0x80808080u;
-        const uint32_t a01 = __byte_perm(v[0], v[1], 0x5140), b01 = __byte_perm(v[0], v[1], 0x7362);
-        const uint32_t a23 = __byte_perm(v[2], v[3], 0x5140), b23 = __byte_perm(v[2], v[3], 0x7362);
-        const uint32_t lo[4] = {bytes_half(a01, 0x4140), bytes_half(a01, 0x4342), bytes_half(a23, 0x4140), bytes_half(a23, 0x4342)};
-        const uint32_t hi[4] = {bytes_half(b01, 0x4140), bytes_half(b01, 0x4342), bytes_half(b23, 0x4140), bytes_half(b23, 0x4342)};
+          for (int e = 0; e < 4; ++e) v[e] = V[e][h] ^ 0x80808080u;
+          const uint32_t a01 = __byte_perm(v[0], v[1], 0x5140), b01 = __byte_perm(v[0], v[1], 0x7362);
+          const uint32_t a23 = __byte_perm(v[2], v[3], 0x5140), b23 = __byte_perm(v[2], v[3], 0x7362);
+          const uint32_t lo[4] = {bytes_half(a01, 0x4140), bytes_half(a01, 0x4342), bytes_half(a23, 0x4140), bytes_half(a23, 0x4342)};
+          const uint32_t hi[4] = {bytes_half(b01, 0x4140), bytes_half(b01, 0x4342), bytes_half(b23, 0x4140), bytes_half(b23, 0x4342)};
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma(O[n][2 * h], lo, P[n][0], P[n][1]);
-          mma(O[n][2 * h + 1], hi, P[n][0], P[n][1]);
+          for (int n = 0; n < NT; ++n) {
+            mma(O[n][2 * h], lo, P[g][n][0], P[g][n][1]);
+            mma(O[n][2 * h + 1], hi, P[g][n][0], P[g][n][1]);
+          }
         }
       }
     }
@@ -558,11 +615,11 @@ kv_attend_few_kernel(const FewP p) {
 
 namespace {
 
-template <typename T, int DIM, int NT>
+template <typename T, int DIM, int NT, bool TOGETHER>
 void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
   using F = Few<DIM, NT>;
   static PerDeviceOnce once;
-  if (ensure_dynamic_smem(once, c->device, kv_attend_few_kernel<T, DIM, NT>, F::SMEM) != ARMOR_OK) { c->host_err = ARMOR_ERR_CUDA; return; }
+  if (ensure_dynamic_smem(once, c->device, kv_attend_few_kernel<T, DIM, NT, TOGETHER>, F::SMEM) != ARMOR_OK) { c->host_err = ARMOR_ERR_CUDA; return; }
   // two parts a CTA have to find room in the workspace (a single CTA leaves none)
   int64_t n = (int64_t)c->n_sm * F::CTAS;
   const int64_t room = ws_scratch_bytes(c) / (2 * F::PART * (int64_t)sizeof(float));
@@ -575,14 +632,15 @@ void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
     p.a.b.lengths = all.lengths + b0;
     p.a.b.starts = all.starts + b0;
     p.a.b.pages = all.pages + b0 * all.ld;
-    launch_dependent(kv_attend_few_kernel<T, DIM, NT>, dim3((unsigned)n), dim3(THREADS), F::SMEM, s, p);
+    launch_dependent(kv_attend_few_kernel<T, DIM, NT, TOGETHER>, dim3((unsigned)n), dim3(THREADS), F::SMEM, s, p);
     c->launches++;
   }
 }
 template <typename T, int DIM>
 void launch_by_rows(armor_ctx* c, const FewP& p, int64_t rows, cudaStream_t s) {
-  if (rows <= 8) launch_typed<T, DIM, 1>(c, p, s);
-  else launch_typed<T, DIM, 2>(c, p, s);
+  const bool together = p.a.c.page_size % 16 == 0;
+  if (rows <= 8) together ? launch_typed<T, DIM, 1, true>(c, p, s) : launch_typed<T, DIM, 1, false>(c, p, s);
+  else together ? launch_typed<T, DIM, 2, true>(c, p, s) : launch_typed<T, DIM, 2, false>(c, p, s);
 }
 
 }  // namespace
@@ -594,7 +652,7 @@ armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit
   p.status = c->status;
   p.counters = c->kv_counters;
   p.parts = c->T;
-  p.min_steps = 2;
+  p.min_steps = 1;
   const int64_t rows = (a.max_chunk ? a.max_chunk : (a.b.rows + a.b.n - 1) / a.b.n) * a.group;
   KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
   if (a.dtype == ARMOR_DTYPE_BF16) {
