@@ -19,6 +19,7 @@
 // shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
 // last, by a counter, adds them up in the order of the parts: no CTA waits for another and the bits do not depend on the run.
 #include "kv_cache.cuh"
+#include "tc_common.cuh"
 
 namespace {
 
@@ -39,10 +40,12 @@ struct Few {
   static constexpr int PART = R * DIM + 2 * R;     // floats of a part: O, m, l
   static constexpr int CTAS = 2;            // an SM
   static constexpr int K_BYTES = DIM / 64 * 2 * 512, V_BYTES = 4 * 32 * VB;        // of sixteen positions
-  static constexpr int SCALES = 2 * (K_BYTES + V_BYTES), STAGE = SCALES + 256;      // of 32
+  static constexpr int STAGE = 2 * (K_BYTES + V_BYTES);                             // of 32: keys, values
+  static constexpr int SCALES = WARPS * STAGES * STAGE;                             // behind all stages: 256 bytes of scales for each
   static constexpr bool Q_SHARED = NT > 1;                                          // q in shared memory (registers hold eight rows of it)
   static constexpr int SUMS = WARPS * R * (DIM + 4) * 4;                            // the warps' O, in the place of the stages
-  static constexpr int Q_AT = STAGES * STAGE * WARPS > SUMS ? STAGES * STAGE * WARPS : SUMS, SMEM = Q_AT + (Q_SHARED ? NT * KW * 32 * 8 : 0);
+  static constexpr int Q_AT = SCALES + WARPS * STAGES * 256, SMEM = Q_AT + (Q_SHARED ? NT * KW * 32 * 8 : 0) + 1024;
+  static_assert(SUMS <= SCALES, "");
 };
 // bytes that a lane copies for itself, complete with wait_copies
 template <int BYTES>
@@ -105,23 +108,51 @@ __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   return u;
 }
 
-// TOGETHER: sixteen positions that begin at a multiple of sixteen share a page
+// sixteen rows of a page's head, swizzled: the bank of a row's sixteen bytes moves with the row
+template <int DIM>
+__device__ __forceinline__ void copy_rows(uint32_t dst, const CUtensorMap* map, uint32_t slot, int head, uint32_t page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(0), "r"(slot), "r"(head), "r"(page), "r"(bar)
+      : "memory");
+}
+// where sixteen bytes (chunk) of a row lie then
+template <int DIM>
+__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) {
+  return DIM == 128 ? row * 128 + ((chunk ^ (row & 7)) << 4) : row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+}
+
+// TOGETHER: sixteen positions that begin at a multiple of sixteen share a page: one lane of a warp asks for all of their keys, or values, at once.
+// (Every lane asking for its own sixteen bytes took 1,000 to 1,300 cycles of a step's 3,900.)  Else every lane copies what it reads itself.
 template <typename T, int DIM, int NT, bool TOGETHER>
 __global__ void __launch_bounds__(THREADS, Few<DIM, NT>::CTAS)
-kv_attend_few_kernel(const FewP p) {
+kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const FewP p) {
   grid_begin();
   using F = Few<DIM, NT>;
   constexpr int R = F::R;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
+  __shared__ int abort_flag;
   float (*const sO)[R][DIM + 4] = reinterpret_cast<float (*)[R][DIM + 4]>(smem);
   __shared__ float sM[WARPS][R], sL[WARPS][R];
   __shared__ int64_t scan[WARPS];
   __shared__ int64_t at_base;
   __shared__ int at_seq, last_one;
+  __shared__ Seq at_s;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, part = lane & 3;
   const Cache& c = p.a.c;
   const Batch& b = p.a.b;
+  const uint32_t my_bars = tc::smem_u32(&bars[warp * STAGES]);
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (TOGETHER && lane == 0) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) tc::mbar_init(my_bars + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  uint32_t turn = 0;                                      // steps of this warp so far
+  bool ok = true;                                         // all copies came
 
   // ---- the line of all steps, this CTA's share of it and the sequence that it begins in
   int64_t total, begin, end;
@@ -158,20 +189,25 @@ kv_attend_few_kernel(const FewP p) {
     if (base <= begin && begin < base + mine)
       for (int i = s0; i < s1; ++i) {
         bool bad;
-        const int64_t w = units_of<R>(p, sequence(b, i, bad)).per;
-        if (begin < base + w) { at_seq = i; at_base = base; break; }
+        const Seq s = sequence(b, i, bad);
+        const int64_t w = units_of<R>(p, s).per;
+        if (begin < base + w) { at_seq = i; at_base = base; at_s = s; break; }
         base += w;
       }
     __syncthreads();
   }
   int seq = at_seq;
   int64_t base = at_base;
+  Seq s = at_s;
 
   while (begin < end) {
-    bool bad;
-    const Seq s = sequence(b, seq, bad);
     const Unit un = units_of<R>(p, s);
-    if (begin >= base + un.per) { base += un.per; ++seq; continue; }
+    if (begin >= base + un.per) {
+      bool bad;
+      base += un.per;
+      s = sequence(b, ++seq, bad);
+      continue;
+    }
     const int64_t unit = (begin - base) / un.steps, u0 = base + unit * un.steps;
     const int first = (int)(begin - u0), count = (int)(min(end, u0 + un.steps) - begin);
     const int head = (int)(unit / un.tiles), tile = (int)(unit - (int64_t)head * un.tiles);
@@ -195,7 +231,7 @@ kv_attend_few_kernel(const FewP p) {
         const T* const row = static_cast<const T*>(p.a.q) + (int64_t)(s.first + i) * p.a.q_row + (int64_t)(head * p.a.group + g) * p.a.q_head;
 #pragma unroll
         for (int h = 0; h < DIM / 64; ++h) {
-          const int d = h * 64 + part * 16;
+          const int d = TOGETHER ? part * (DIM / 4) + h * 16 : h * 64 + part * 16;
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const Raw8<T> x = !there ? raw_zero<T>() : (p.a.aligned ? raw_load(row + d + 8 * e) : row_load<false>(row, d + 8 * e, DIM));
@@ -261,7 +297,8 @@ kv_attend_few_kernel(const FewP p) {
     const int last = max(s.length - 1, 0);
     // ---- 32 positions of a step: a lane looks up the place of one of them, or of the first of its sixteen
     uint8_t* const mine = smem + warp * (STAGES * F::STAGE);
-    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    float* const my_scales = reinterpret_cast<float*>(smem + F::SCALES + warp * (STAGES * 256));
+    const uint32_t mine_at = tc::smem_u32(mine), scales_at = tc::smem_u32(my_scales) + lane * 4;
     uint32_t page = 0, slot = 0;
     auto look = [&](int i) {                                // of step i
       int j = (step0 + i) * STEP + warp * 32 + lane;
@@ -271,33 +308,39 @@ kv_attend_few_kernel(const FewP p) {
       page = x < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + x] : 0xffffffffu;
     };
     unsigned refused = 0;                                   // a bit a step under way: one of its positions has no page
-    const int64_t to_k = quad * c.slot + part * 16, to_v = 2 * part * c.slot + quad * F::VB;
-    auto fetch = [&](int i) {                               // what has been looked up, to the stage of step i
+    auto fetch = [&](uint32_t turn) {                       // what has been looked up, to the stage of that step
       const bool none = page >= c.n_pages;
       if (none) page = slot = 0;
       refused = refused << 1 | (unsigned)__any_sync(0xffffffffu, none);
-      const int64_t row = page * c.page + head * c.head + slot * c.slot;
-      int64_t scale = page * c.spage + head * c.shead + slot * c.sslot;
-      if (TOGETHER) scale += (lane & 15) * c.sslot;
-      const uint32_t to = mine_at + (uint32_t)(i % STAGES) * F::STAGE, k_at = to + lane * 16, v_at = to + 2 * F::K_BYTES + lane * F::VB;
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int64_t first = TOGETHER ? __shfl_sync(0xffffffffu, row, 16 * g) : 0;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int8_t* const from = c.k + (TOGETHER ? first + to_k + 8 * e * c.slot : __shfl_sync(0xffffffffu, row, 16 * g + quad + 8 * e) + part * 16);
-#pragma unroll
-          for (int h = 0; h < DIM / 64; ++h) copy_async<16>(k_at + ((g * 2 + e) * (DIM / 64) + h) * 512, from + h * 64);
+      const uint32_t st = turn % STAGES, to = mine_at + st * F::STAGE;
+      if constexpr (TOGETHER) {
+        const uint32_t page1 = __shfl_sync(0xffffffffu, page, 16), slot1 = __shfl_sync(0xffffffffu, slot, 16), bar = my_bars + 8 * st;
+        if (lane == 0) {
+          tc::mbar_expect_tx(bar, F::STAGE);
+          copy_rows<DIM>(to, &k_map, slot, head, page, bar);
+          copy_rows<DIM>(to + F::K_BYTES, &k_map, slot1, head, page1, bar);
+          copy_rows<DIM>(to + 2 * F::K_BYTES, &v_map, slot, head, page, bar);
+          copy_rows<DIM>(to + 2 * F::K_BYTES + F::V_BYTES, &v_map, slot1, head, page1, bar);
         }
+      } else {
+        const int64_t row = page * c.page + head * c.head + slot * c.slot;
+        const uint32_t k_at = to + lane * 16, v_at = to + 2 * F::K_BYTES + lane * F::VB;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = (e & 1) + (e >> 1) * 8;
-          copy_async<F::VB>(v_at + (g * 4 + e) * 32 * F::VB,
-                            c.v + (TOGETHER ? first + to_v + r * c.slot : __shfl_sync(0xffffffffu, row, 16 * g + 2 * part + r) + quad * F::VB));
+        for (int g = 0; g < 2; ++g) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int8_t* const from = c.k + __shfl_sync(0xffffffffu, row, 16 * g + quad + 8 * e) + part * 16;
+#pragma unroll
+            for (int h = 0; h < DIM / 64; ++h) copy_async<16>(k_at + ((g * 2 + e) * (DIM / 64) + h) * 512, from + h * 64);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            copy_async<F::VB>(v_at + (g * 4 + e) * 32 * F::VB, c.v + __shfl_sync(0xffffffffu, row, 16 * g + 2 * part + (e & 1) + (e >> 1) * 8) + quad * F::VB);
         }
       }
-      copy_async<4>(to + F::SCALES + lane * 4, c.ks + scale);
-      copy_async<4>(to + F::SCALES + 128 + lane * 4, c.vs + scale);
+      const int64_t scale = page * c.spage + head * c.shead + (slot + (TOGETHER ? lane & 15 : 0)) * c.sslot;
+      copy_async<4>(scales_at + st * 256, c.ks + scale);
+      copy_async<4>(scales_at + st * 256 + 128, c.vs + scale);
     };
 
     float O[NT][DIM / 16][4], m[NT][2], l[NT][2];
@@ -310,30 +353,32 @@ kv_attend_few_kernel(const FewP p) {
     }
 
     look(0);
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) {
-      if (i < count) {
-        fetch(i);
-        if (i + 1 < count) look(i + 1);
+    if (TOGETHER && lane == 0) tc::fence_proxy_async();     // (sums of the unit before lay in the stages)
+    if (ok) fetch(turn);
+    if (count > 1) look(1);
+    end_copies();
+    for (int i = 0; i < count; ++i, ++turn) {
+      wait_copies<0>();
+      if (TOGETHER && ok) {
+        const uint32_t bar = my_bars + 8 * (turn % STAGES), parity = (turn / STAGES) & 1;
+        if (!tc::mbar_wait_warp(bar, parity, &abort_flag, p.status)) {
+          // what comes out is worthless, as the status says; no more copies, and this one once more
+          ok = false;
+          const long long t0 = clock64();
+          while (!tc::mbar_try(bar, parity) && clock64() - t0 < 20000000ll) {}
+        }
       }
-      end_copies();
-    }
-    for (int i = 0; i < count; ++i) {
-      wait_copies<STAGES - 2>();
       __syncwarp();
-      unsigned behind = STAGES - 2;                         // steps fetched behind this one
-      if (i + STAGES - 1 < count) {
-        fetch(i + STAGES - 1);
-        if (i + STAGES < count) look(i + STAGES);
-        ++behind;
-      } else {
-        behind = (unsigned)(count - 1 - i);
+      const bool ahead = i + 1 < count && ok;
+      if (ahead) {
+        fetch(turn + 1);
+        if (i + 2 < count) look(i + 2);
+        end_copies();
       }
-      end_copies();
       const int j0 = (step0 + i) * STEP + warp * 32;
-      const bool bad_page = refused >> behind & 1u;
+      const bool bad_page = refused >> (ahead ? 1 : 0) & 1u;
       if (bad_page && j0 < inner_hi && lane == 0) report(p.status);
-      const uint8_t* const stage = mine + (i % STAGES) * F::STAGE;
+      const uint8_t* const stage = mine + (turn % STAGES) * F::STAGE;
 
       // ---- scores of twice sixteen positions
       float t[2][NT][4];
@@ -347,7 +392,8 @@ kv_attend_few_kernel(const FewP p) {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) x[g][e] = *reinterpret_cast<const uint4*>(stage + ((g * 2 + e) * (DIM / 64) + h) * 512 + lane * 16);
+          for (int e = 0; e < 2; ++e) x[g][e] = *reinterpret_cast<const uint4*>(TOGETHER ? stage + g * F::K_BYTES + swizzled<DIM>(quad + 8 * e, part * (DIM / 64) + h)
+                                                              : stage + ((g * 2 + e) * (DIM / 64) + h) * 512 + lane * 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t b0[NT], b1[NT];
@@ -371,7 +417,7 @@ kv_attend_few_kernel(const FewP p) {
       }
       float kr[2][2];
       {
-        const float* const scales = reinterpret_cast<const float*>(stage + F::SCALES);
+        const float* const scales = my_scales + (turn % STAGES) * 64;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -450,7 +496,9 @@ kv_attend_few_kernel(const FewP p) {
         uint32_t V[4][DIM / 32];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint8_t* const from = stage + 2 * F::K_BYTES + (g * 4 + e) * 32 * F::VB + lane * F::VB;
+          const uint32_t r = 2 * part + (e & 1) + (e >> 1) * 8;
+          const uint8_t* const from = stage + 2 * F::K_BYTES +
+                                      (TOGETHER ? g * F::V_BYTES + swizzled<DIM>(r, quad * F::VB / 16) + (quad * F::VB & 15) : (g * 4 + e) * 32 * F::VB + lane * F::VB);
           if constexpr (DIM == 128) {
             const uint4 v = *reinterpret_cast<const uint4*>(from);
             V[e][0] = v.x; V[e][1] = v.y; V[e][2] = v.z; V[e][3] = v.w;
@@ -476,7 +524,6 @@ kv_attend_few_kernel(const FewP p) {
         }
       }
     }
-    wait_copies<0>();
 
     // ---- the warps' sums to one
     __syncthreads();                                      // (the stages have been read)
@@ -615,11 +662,24 @@ kv_attend_few_kernel(const FewP p) {
 
 namespace {
 
+// [pages][heads][slots][DIM] of keys or values, sixteen slots at a time
+template <int DIM>
+bool make_map(CUtensorMap* map, const Cache& c, int8_t* base) {
+  PFN_cuTensorMapEncodeTiled_v12000 enc = tc::get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[4] = {DIM, c.page_size, (cuuint64_t)c.heads, c.n_pages}, strides[3] = {(cuuint64_t)c.slot, (cuuint64_t)c.head, (cuuint64_t)c.page};
+  cuuint32_t box[4] = {DIM, 16, 1, 1}, step[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             DIM == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int DIM, int NT, bool TOGETHER>
 void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
   using F = Few<DIM, NT>;
   static PerDeviceOnce once;
   if (ensure_dynamic_smem(once, c->device, kv_attend_few_kernel<T, DIM, NT, TOGETHER>, F::SMEM) != ARMOR_OK) { c->host_err = ARMOR_ERR_CUDA; return; }
+  CUtensorMap k_map{}, v_map{};
+  if (TOGETHER && (!make_map<DIM>(&k_map, p.a.c, p.a.c.k) || !make_map<DIM>(&v_map, p.a.c, p.a.c.v))) { c->host_err = ARMOR_ERR_CUDA; return; }
   // two parts a CTA have to find room in the workspace (a single CTA leaves none)
   int64_t n = (int64_t)c->n_sm * F::CTAS;
   const int64_t room = ws_scratch_bytes(c) / (2 * F::PART * (int64_t)sizeof(float));
@@ -632,13 +692,14 @@ void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
     p.a.b.lengths = all.lengths + b0;
     p.a.b.starts = all.starts + b0;
     p.a.b.pages = all.pages + b0 * all.ld;
-    launch_dependent(kv_attend_few_kernel<T, DIM, NT, TOGETHER>, dim3((unsigned)n), dim3(THREADS), F::SMEM, s, p);
+    launch_dependent(kv_attend_few_kernel<T, DIM, NT, TOGETHER>, dim3((unsigned)n), dim3(THREADS), F::SMEM, s, k_map, v_map, p);
     c->launches++;
   }
 }
 template <typename T, int DIM>
 void launch_by_rows(armor_ctx* c, const FewP& p, int64_t rows, cudaStream_t s) {
-  const bool together = p.a.c.page_size % 16 == 0;
+  // (a copy of rows takes strides below 2^40)
+  const bool together = p.a.c.page_size % 16 == 0 && (uint64_t)(p.a.c.page | p.a.c.head | p.a.c.slot) < (1ull << 40);
   if (rows <= 8) together ? launch_typed<T, DIM, 1, true>(c, p, s) : launch_typed<T, DIM, 1, false>(c, p, s);
   else together ? launch_typed<T, DIM, 2, true>(c, p, s) : launch_typed<T, DIM, 2, false>(c, p, s);
 }
