@@ -2,8 +2,10 @@
 //
 // In: a row x (one token, one head, keys or values) becomes q = round(127 x / a), s = a / 127, a = max |x| (rows_io.cuh has the exact
 // rounding).  Out: q s in fp32, rounded once to the output's type.  Both are bound by HBM: in, an element is read once and one byte
-// written; out, the reverse.  A row is taken by dim / 8 lanes, eight elements each, so that its bytes go out whole and its maximum needs
-// three or four shuffles and no barrier; a lane has ITEMS rows under way.
+// written; out, the reverse.  A warp has some tokens and some heads of each.  Its lanes look up the places of all its tokens at once, then
+// take the rows, dim / 8 lanes and eight elements each, so that a row's bytes go out whole and its maximum needs three or four
+// shuffles and no barrier; UNROLL rows of a lane are under way together.  (With a search for every row, 8,188 tokens of 8 heads took 63 us in and out, so
+// {NEW}.)
 #include "kv_cache.cuh"
 
 namespace {
@@ -11,23 +13,59 @@ namespace {
 using namespace rows;
 using namespace kv;
 
-constexpr int THREADS = 256, ITEMS = 4;
+constexpr int THREADS = 128, UNROLL = 4;
 
 struct Packed {                             // rows [n][heads][dim] of keys and of values
   const void *k, *v;
   int64_t k_row, k_head, v_row, v_head;
 };
+struct Split { int tokens, heads, head_groups; };      // of a warp; groups of heads
 
-// Item i: keys (even) or values (odd) of head i / 2 % heads in row i / 2 / heads.
-struct Item { int64_t row; int head, values; };
-__device__ __forceinline__ Item item(int64_t i, int heads) {
-  Item r;
-  r.values = (int)(i & 1);
-  const uint64_t u = (uint64_t)i >> 1;
-  r.row = u < (1ull << 32) ? (uint32_t)u / (uint32_t)heads : (int64_t)(u / (uint32_t)heads);
-  r.head = (int)(u - (uint64_t)r.row * heads);
-  return r;
-}
+// What a warp has: tokens first .. first + n - 1, heads head .. head + heads - 1; lane u knows where token u lies.
+// found: 0: nowhere (a row of no sequence); 1: at `at` (its scale at `scale`) of head 0; 2: refused; 3: padding
+struct Share {
+  int64_t first; int n, head, heads;
+  int64_t at, scale; int found;
+  __device__ __forceinline__ Share(const Cache& c, const Batch& b, const Split& s, int32_t* status) {
+    const int64_t w = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5), group = w % s.head_groups;
+    const int lane = threadIdx.x & 31;
+    first = w / s.head_groups * s.tokens;
+    n = (int)max((int64_t)0, min((int64_t)s.tokens, b.rows - first));
+    head = (int)group * s.heads;
+    heads = min(s.heads, c.heads - head);
+    at = scale = 0;
+    found = 0;
+    if (n < 1) return;
+    const int64_t row = first + min(lane, n - 1);
+    const int seq = sequence_of(b, row);
+    if (seq < 0 || lane >= n) return;
+    bool bad;
+    const Seq q = sequence(b, seq, bad);
+    const int64_t off = row - q.first, p = (int64_t)q.length - q.n + off;
+    uint32_t page = 0, slot = 0;
+    if (bad || off < 0 || off >= q.n) found = 2;
+    else if (p < 0) found = 3;
+    else found = place(c, b, seq, (uint32_t)p, page, slot) ? 1 : 2;
+    if (found == 2 && head == 0) report(status);
+    if (found == 1) {
+      at = page * c.page + slot * c.slot;
+      scale = page * c.spage + slot * c.sslot;
+    }
+  }
+};
+
+// How the lanes stand: DIM / 8 to a row, the first half of the warp's rows keys and the second values, or by turns (DIM 64: two heads)
+template <int DIM>
+struct Lane {
+  static constexpr int LANES = DIM / 8, HEADS = 16 / LANES;               // of a row; heads at once
+  int e, values, head;
+  __device__ __forceinline__ Lane() {
+    const int r = (threadIdx.x & 31) / LANES;
+    e = (threadIdx.x % LANES) * 8;
+    values = r & 1;
+    head = r >> 1;
+  }
+};
 
 template <int DIM>
 __device__ __forceinline__ unsigned row_top(unsigned v) {
@@ -36,91 +74,95 @@ __device__ __forceinline__ unsigned row_top(unsigned v) {
   return v;
 }
 
-// Position and place of the rows that a lane has under way.  place 0: nothing to do; 1: found; 2: a position with no page; 3: padding
-template <int DIM>
-struct Rows {
-  Item it[ITEMS];
-  uint32_t page[ITEMS], slot[ITEMS];
-  int found[ITEMS];
-  __device__ __forceinline__ void find(const Cache& c, const Batch& b, int64_t n_items, int32_t* status) {
-    constexpr int LANES = DIM / 8, PER = THREADS / LANES;
-    const int64_t i0 = (int64_t)blockIdx.x * (PER * ITEMS) + threadIdx.x / LANES;
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int64_t i = i0 + u * PER;
-      it[u] = item(i < n_items ? i : 0, c.heads);
-      found[u] = 0;
-      const int at = sequence_of(b, it[u].row);
-      if (i < n_items && at >= 0) {
-        bool bad;
-        const Seq s = sequence(b, at, bad);
-        const int64_t off = it[u].row - s.first, p = (int64_t)s.length - s.n + off;
-        if (bad || off < 0 || off >= s.n) found[u] = 2;
-        else if (p < 0) found[u] = 3;
-        else found[u] = place(c, b, at, (uint32_t)p, page[u], slot[u]) ? 1 : 2;
-        if (found[u] == 2 && threadIdx.x % LANES == 0) report(status);
-      }
-    }
-  }
-};
-
 template <typename T, int DIM, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS)
-kv_write_kernel(const Cache c, const Batch b, const Packed x, int64_t n_items, int32_t* status) {
+kv_write_kernel(const Cache c, const Batch b, const Packed x, const Split split, int32_t* status) {
   grid_begin();
-  const int e = (threadIdx.x % (DIM / 8)) * 8;
-  Rows<DIM> r;
-  r.find(c, b, n_items, status);
-  Raw8<T> raw[ITEMS];
+  using L = Lane<DIM>;
+  const L lane;
+  const Share s(c, b, split, status);
+  const int64_t x_head = lane.values ? x.v_head : x.k_head, x_row = lane.values ? x.v_row : x.k_row;
+  const T* const from = static_cast<const T*>(lane.values ? x.v : x.k) + s.first * x_row + (s.head + lane.head) * x_head;
+  int8_t* const to = (lane.values ? c.v : c.k) + (s.head + lane.head) * c.head + lane.e;
+  float* const to_scale = (lane.values ? c.vs : c.ks) + (s.head + lane.head) * c.shead;
+  for (int t = 0; t < s.n; ++t) {
+    const int64_t at = __shfl_sync(0xffffffffu, s.at, t), scale = __shfl_sync(0xffffffffu, s.scale, t);
+    if (__shfl_sync(0xffffffffu, s.found, t) != 1) continue;
+    for (int h = 0; h < s.heads; h += UNROLL * L::HEADS) {
+      Raw8<T> raw[UNROLL];
+      unsigned top[UNROLL], own = 0;
 #pragma unroll
-  for (int u = 0; u < ITEMS; ++u) {
-    const Item& it = r.it[u];
-    const T* const at = it.values ? static_cast<const T*>(x.v) + it.row * x.v_row + it.head * x.v_head
-                                  : static_cast<const T*>(x.k) + it.row * x.k_row + it.head * x.k_head;
-    raw[u] = r.found[u] == 1 ? row_load<ALIGNED>(at, e, DIM) : raw_zero<T>();
-  }
+      for (int u = 0; u < UNROLL; ++u) {
+        const int head = h + u * L::HEADS;
+        raw[u] = head + lane.head < s.heads ? row_load<ALIGNED>(from + t * x_row + head * x_head, lane.e, DIM) : raw_zero<T>();
+      }
 #pragma unroll
-  for (int u = 0; u < ITEMS; ++u) {
-    const RowScale s = row_scale<sizeof(T) == 2>(row_top<DIM>(raw_top(raw[u])));
-    if (r.found[u] != 1) continue;
-    float v[8];
-    raw_get(raw[u], v);
-    const Item& it = r.it[u];
-    *reinterpret_cast<uint2*>((it.values ? c.v : c.k) + r.page[u] * c.page + it.head * c.head + r.slot[u] * c.slot + e) = row_round8<sizeof(T) == 2>(v, s);
-    if (e == 0) (it.values ? c.vs : c.ks)[r.page[u] * c.spage + it.head * c.shead + r.slot[u] * c.sslot] = s.s;
+      for (int u = 0; u < UNROLL; ++u) {
+        top[u] = row_top<DIM>(raw_top(raw[u]));
+        if (threadIdx.x % UNROLL == u) own = top[u];
+      }
+      // a row's scale and inverse by one of its lanes, four rows at once
+      const RowScale mine = row_scale<sizeof(T) == 2>(own);
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        RowScale r;
+        r.pre = __shfl_sync(0xffffffffu, mine.pre, u, L::LANES);
+        r.inv = __shfl_sync(0xffffffffu, mine.inv, u, L::LANES);
+        r.top = __shfl_sync(0xffffffffu, mine.top, u, L::LANES);
+        r.edge = __shfl_sync(0xffffffffu, mine.edge, u, L::LANES);
+        const int head = h + u * L::HEADS;
+        if (head + lane.head >= s.heads) continue;
+        float v[8];
+        raw_get(raw[u], v);
+        *reinterpret_cast<uint2*>(to + at + head * c.head) = row_round8<sizeof(T) == 2>(v, r);
+        if (lane.e == 8 * u) to_scale[scale + head * c.shead] = mine.s;
+      }
+    }
   }
 }
 
 // (positions that have no page, and padding, read as zeros; rows behind the last sequence are left as they are)
 template <typename T, int DIM, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS)
-kv_read_kernel(const Cache c, const Batch b, const Packed y, int64_t n_items, int32_t* status) {
+kv_read_kernel(const Cache c, const Batch b, const Packed y, const Split split, int32_t* status) {
   grid_begin();
-  const int e = (threadIdx.x % (DIM / 8)) * 8;
-  Rows<DIM> r;
-  r.find(c, b, n_items, status);
-  uint2 q[ITEMS];
-  float s[ITEMS];
+  using L = Lane<DIM>;
+  const L lane;
+  const Share s(c, b, split, status);
+  const int64_t y_head = lane.values ? y.v_head : y.k_head, y_row = lane.values ? y.v_row : y.k_row;
+  T* const to = const_cast<T*>(static_cast<const T*>(lane.values ? y.v : y.k)) + s.first * y_row + (s.head + lane.head) * y_head;
+  const int8_t* const from = (lane.values ? c.v : c.k) + (s.head + lane.head) * c.head + lane.e;
+  const float* const from_scale = (lane.values ? c.vs : c.ks) + (s.head + lane.head) * c.shead;
+  for (int t = 0; t < s.n; ++t) {
+    const int64_t at = __shfl_sync(0xffffffffu, s.at, t), at_scale = __shfl_sync(0xffffffffu, s.scale, t);
+    const int found = __shfl_sync(0xffffffffu, s.found, t);
+    if (!found) continue;
+    for (int h = 0; h < s.heads; h += UNROLL * L::HEADS) {
+      uint2 q[UNROLL];
+      float scale[UNROLL];
 #pragma unroll
-  for (int u = 0; u < ITEMS; ++u) {
-    const Item& it = r.it[u];
-    q[u] = make_uint2(0u, 0u);
-    s[u] = 0.f;
-    if (r.found[u] == 1) {
-      q[u] = *reinterpret_cast<const uint2*>((it.values ? c.v : c.k) + r.page[u] * c.page + it.head * c.head + r.slot[u] * c.slot + e);
-      s[u] = (it.values ? c.vs : c.ks)[r.page[u] * c.spage + it.head * c.shead + r.slot[u] * c.sslot];
+      for (int u = 0; u < UNROLL; ++u) {
+        const int head = h + u * L::HEADS;
+        q[u] = make_uint2(0u, 0u);
+        scale[u] = 0.f;
+        if (found == 1 && head + lane.head < s.heads) {
+          q[u] = *reinterpret_cast<const uint2*>(from + at + head * c.head);
+          scale[u] = from_scale[at_scale + head * c.shead];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int head = h + u * L::HEADS;
+        if (head + lane.head >= s.heads) continue;
+        // a byte in the last place of 2^23 + (byte + 128), less 2^23 + 128: the number, exactly, without the conversions' few units
+        const uint32_t w[2] = {q[u].x ^ 0x80808080u, q[u].y ^ 0x80808080u};
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          v[k] = (__uint_as_float(__byte_perm(w[k >> 2], 0x4b000000u, 0x7440 + (k & 3))) - 8388736.f) * scale[u];
+        row_store<ALIGNED>(to + t * y_row + head * y_head, lane.e, DIM, v);
+      }
     }
-  }
-#pragma unroll
-  for (int u = 0; u < ITEMS; ++u) {
-    if (!r.found[u]) continue;
-    const Item& it = r.it[u];
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? q[u].x : q[u].y) >> (8 * (i & 3))) * s[u];
-    T* const at = const_cast<T*>(it.values ? static_cast<const T*>(y.v) + it.row * y.v_row + it.head * y.v_head
-                                           : static_cast<const T*>(y.k) + it.row * y.k_row + it.head * y.k_head);
-    row_store<ALIGNED>(at, e, DIM, v);
   }
 }
 
@@ -187,10 +229,16 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
   const Packed x{g->k, g->v, g->k_row_stride, g->k_head_stride, g->v_row_stride, g->v_head_stride};
   const bool al = aligned16(g->k, g->k_row_stride, es) && aligned16(g->v, g->v_row_stride, es) && g->k_head_stride * es % 16 == 0 &&
                   g->v_head_stride * es % 16 == 0;
-  const int64_t items = 2 * g->n_rows * cache->kv_heads;
-  const int64_t per = THREADS / (cache->head_dim / 8) * ITEMS;
+  // Few tokens: a warp has one and four heads of it, so that many SMs have some; many: four tokens and all heads, whose search and places are
+  // paid for once.
+  const int64_t heads = cache->kv_heads, items = 2 * g->n_rows * heads;
+  Split split;
+  const bool many = g->n_rows * heads >= 16 * 1024;
+  split.tokens = many ? 4 : 1;
+  split.heads = many ? (int)heads : 4;
+  split.head_groups = (int)((heads + split.heads - 1) / split.heads);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t blocks = (items + per - 1) / per;
+  const int64_t warps = (g->n_rows + split.tokens - 1) / split.tokens * split.head_groups, blocks = (warps + THREADS / 32 - 1) / (THREADS / 32);
   if (blocks > MOST) return ARMOR_ERR_TOO_LARGE;
   KTimer kt(c, ARMOR_KC_FORWARD, (double)items * (double)(cache->head_dim * (es + 1) + 4), s);
   st = by_row_type(g->dtype, [&](auto t) {
@@ -199,11 +247,11 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
     auto go = [&](auto dim) {
       constexpr int DIM = decltype(dim)::value;
       if (WHAT == WRITE) {
-        if (al) launch_dependent(kv_write_kernel<T, DIM, true>, grid, block, 0, s, cv, bv, x, items, c->status);
-        else launch_dependent(kv_write_kernel<T, DIM, false>, grid, block, 0, s, cv, bv, x, items, c->status);
+        if (al) launch_dependent(kv_write_kernel<T, DIM, true>, grid, block, 0, s, cv, bv, x, split, c->status);
+        else launch_dependent(kv_write_kernel<T, DIM, false>, grid, block, 0, s, cv, bv, x, split, c->status);
       } else {
-        if (al) launch_dependent(kv_read_kernel<T, DIM, true>, grid, block, 0, s, cv, bv, x, items, c->status);
-        else launch_dependent(kv_read_kernel<T, DIM, false>, grid, block, 0, s, cv, bv, x, items, c->status);
+        if (al) launch_dependent(kv_read_kernel<T, DIM, true>, grid, block, 0, s, cv, bv, x, split, c->status);
+        else launch_dependent(kv_read_kernel<T, DIM, false>, grid, block, 0, s, cv, bv, x, split, c->status);
       }
     };
     if (cache->head_dim == 64) go(std::integral_constant<int, 64>());
