@@ -6,6 +6,8 @@
 // take the rows, dim / 8 lanes and eight elements each, so that a row's bytes go out whole and its maximum needs three or four
 // shuffles and no barrier; UNROLL rows of a lane are under way together.  (With a search for every row, 8,188 tokens of 8 heads took 63 us in and out, so
 // {NEW}.)
+#include <algorithm>
+
 #include "kv_cache.cuh"
 
 namespace {
@@ -13,7 +15,7 @@ namespace {
 using namespace rows;
 using namespace kv;
 
-constexpr int THREADS = 128, UNROLL = 4;
+constexpr int THREADS = 128, UNROLL = 4, WARPS_RESIDENT = 32, MOST_TOKENS = 4;
 
 struct Packed {                             // rows [n][heads][dim] of keys and of values
   const void *k, *v;
@@ -229,13 +231,14 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
   const Packed x{g->k, g->v, g->k_row_stride, g->k_head_stride, g->v_row_stride, g->v_head_stride};
   const bool al = aligned16(g->k, g->k_row_stride, es) && aligned16(g->v, g->v_row_stride, es) && g->k_head_stride * es % 16 == 0 &&
                   g->v_head_stride * es % 16 == 0;
-  // Few tokens: a warp has one and four heads of it, so that many SMs have some; many: four tokens and all heads, whose search and places are
+  // As many warps as the SMs hold: with few tokens some heads of one to a warp, with many several tokens and all heads, whose search and places are
   // paid for once.
-  const int64_t heads = cache->kv_heads, items = 2 * g->n_rows * heads;
+  const int64_t heads = cache->kv_heads, items = 2 * g->n_rows * heads, resident = (int64_t)c->n_sm * WARPS_RESIDENT;
+  const int64_t batch_heads = UNROLL * 16 / (cache->head_dim / 8);        // heads under way at once
   Split split;
-  const bool many = g->n_rows * heads >= 16 * 1024;
-  split.tokens = many ? 4 : 1;
-  split.heads = many ? (int)heads : 4;
+  split.tokens = (int)std::min<int64_t>(MOST_TOKENS, std::max<int64_t>(1, g->n_rows / resident));
+  const int64_t groups = std::min((heads + batch_heads - 1) / batch_heads, std::max<int64_t>(1, resident / g->n_rows));
+  split.heads = (int)((heads + groups - 1) / groups);
   split.head_groups = (int)((heads + split.heads - 1) / split.heads);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const int64_t warps = (g->n_rows + split.tokens - 1) / split.tokens * split.head_groups, blocks = (warps + THREADS / 32 - 1) / (THREADS / 32);
