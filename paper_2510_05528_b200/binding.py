@@ -646,20 +646,30 @@ def armor_kv_read(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
         _check(code, "armor_kv_read")
 
 
-def armor_kv_attend(ctx, cache: KvCache, batch: KvBatch, q, o, scale: float, window: int = 0, max_chunk: int = 0) -> None:
-    """o [rows, heads, head_dim] = attention of q over the cache (see armor.h)."""
-    here = _cuda_index(q, "q")
+def _kv_attend(ctx, here, cache, batch, q, o, scale, window, max_chunk) -> torch.Tensor:
     if cache.index != here or batch.index != here:
-        raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, q on cuda:{here}")
+        raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, the call's device is cuda:{here}")
     code = _row_dtype(q, "q")
     dim = cache.head_dim
     qp, qr, qh = _heads_at(q, q.dtype, None, None, dim, "q", here)
     rows, heads, _ = q.shape
-    op, orow, oh = _heads_at(o, q.dtype, rows, heads, dim, "o", here)
+    if o is None:
+        o = q.new_empty((rows, heads, dim))
+        op, orow, oh = o.data_ptr(), heads * dim, dim
+    else:
+        op, orow, oh = _heads_at(o, q.dtype, rows, heads, dim, "o", here)
     code = lib().armor_kv_attend(ctx, cache.args, batch.args, armor_kv_attend_args(qp, op, rows, heads, qr, qh, orow, oh, window, max_chunk, scale, code),
                                  _stream())
     if code:
         _check(code, "armor_kv_attend")
+    return o
+
+
+def armor_kv_attend(ctx, cache: KvCache, batch: KvBatch, q, o, scale: float, window: int = 0, max_chunk: int = 0) -> None:
+    """o [rows, heads, head_dim] = attention of q over the cache (see armor.h)."""
+    if o is None:
+        raise ValueError("o is missing")
+    _kv_attend(ctx, _cuda_index(q, "q"), cache, batch, q, o, scale, window, max_chunk)
 
 
 def armor_get_device_status(ctx, n: int = 16) -> list[int]:
@@ -1015,7 +1025,8 @@ class ArmorContext:
         they are (in new tensors: not set)."""
         here = self._current()
         if out is None:
-            k, v = out = tuple(torch.empty(rows, cache.kv_heads, cache.head_dim, dtype=dtype, device=self.device) for _ in range(2))
+            size = (rows, cache.kv_heads, cache.head_dim)
+            k, v = out = cache.k.new_empty(size, dtype=dtype), cache.k.new_empty(size, dtype=dtype)
         else:
             k, v = out
             if k.size(0) != rows or k.dtype is not dtype:
@@ -1031,11 +1042,7 @@ class ArmorContext:
         last `window` of them if that is not 0; scale: head_dim ** -0.5.  The new rows' keys and values have been written.  Heads
         share keys in groups of heads / kv_heads.  max_chunk: the most rows of a sequence, where the caller knows it (a hint).  Rows
         behind the last sequence are left as they are (in a new tensor: not set)."""
-        self._current()
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        armor_kv_attend(self.ctx, cache, batch, q, out, cache.head_dim ** -0.5 if scale is None else scale, window, max_chunk)
-        return out
+        return _kv_attend(self.ctx, self._current(), cache, batch, q, out, cache.head_dim ** -0.5 if scale is None else scale, window, max_chunk)
 
     def device_status(self) -> list[int]:
         torch.cuda.current_stream().synchronize()
