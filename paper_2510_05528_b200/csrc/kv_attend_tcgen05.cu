@@ -83,15 +83,16 @@ __device__ __forceinline__ uint32_t bytes_half(uint32_t x, uint32_t sel) {      
 __device__ __forceinline__ void put16(uint32_t at, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// (behind the wait for the numbers, which is volatile too)
+// (the address is made behind the wait for what it holds: see `behind`)
+__device__ __forceinline__ void behind(uint32_t& at) { asm volatile("" : "+r"(at)::"memory"); }
 __device__ __forceinline__ float4 get16(uint32_t at) {
   float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+  asm("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
   return v;
 }
 __device__ __forceinline__ float2 get8(uint32_t at) {
   float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at));
+  asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at));
   return v;
 }
 
@@ -482,10 +483,12 @@ kv_attend_tile_kernel(const TileP p) {
       const int count = at.count, block0 = at.block;
       for (int i = 0; i < count; ++i, ++blocks, ++turn) {
         const int j0 = (block0 + i) * KEYS;
-        const uint32_t consts = smem + L::C0 + (blocks % NUMBERS) * L::CONSTS + 16 * pair, inverses = consts - 8 * pair + 8 * KEYS;
         const uint32_t place = turn & 1;
         wait_warp(s_full + 8 * half, turn & 1, abortp, p.status);       // (and the numbers: they are there before the keys)
         tc_fence_after();
+        uint32_t consts = smem + L::C0 + (blocks % NUMBERS) * L::CONSTS + 16 * pair;
+        behind(consts);
+        const uint32_t inverses = consts - 8 * pair + 8 * KEYS;
         F2 t[4][8];
         {
           uint32_t raw[2][32];
@@ -634,7 +637,9 @@ kv_attend_tile_kernel(const TileP p) {
         for (int i = 0; i < MOVES; ++i) {
           const int rr = i * (32 / LANES) + sub_row;
           T* const to = static_cast<T*>(p.a.o) + __shfl_sync(0xffffffffu, off, rr) + 8 * c8;
-          const float4 v = get16(row_at<DIM>(rows_at, (warp & 3) * 32 + rr, c8));
+          uint32_t at16 = row_at<DIM>(rows_at, (warp & 3) * 32 + rr, c8);
+          behind(at16);
+          const float4 v = get16(at16);
           if ((warp & 3) * 32 + rr >= rows) continue;
           if (ALIGNED) *reinterpret_cast<float4*>(to) = v;
           else {
