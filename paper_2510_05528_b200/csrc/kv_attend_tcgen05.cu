@@ -80,6 +80,8 @@ __device__ __forceinline__ uint32_t bytes_half(uint32_t x, uint32_t sel) {      
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));
   return r;
 }
+// upper half of a descriptor of rows of 128 bytes, swizzled, groups of eight 1024 bytes apart (smem_desc_sw128)
+constexpr uint32_t SW128_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 __device__ __forceinline__ void put16(uint32_t at, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -160,22 +162,31 @@ __device__ __forceinline__ void tmem_put_pairs(uint32_t taddr, const uint32_t* r
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+static __device__ __forceinline__ bool wait_warp_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  const long long t0 = clock64();
+  bool ok;
+#pragma unroll 1
+  while (!(ok = mbar_try(bar, parity)) && !*abort_flag) {
+    if (clock64() - t0 > WAIT_CYCLES) {
+      *abort_flag = 1;
+      atomicAdd(&status[ST_WAIT_TIMEOUTS], 1);
+      status[ST_LAST_ERR] = ARMOR_ERR_TIMEOUT;
+    }
+  }
+  return ok;
+}
 // mbar_wait_warp in a few instructions: there are twenty of them here, and the code of all roles has to stay in the instruction cache.  (With that
 // one, whose inner loop is unrolled, the kernel had 400 KB.)
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
   bool ok = mbar_try(bar, parity);
-  if (!ok) {
-    const long long t0 = clock64();
-#pragma unroll 1
-    while (!(ok = mbar_try(bar, parity)) && !*abort_flag) {
-      if (clock64() - t0 > WAIT_CYCLES) {
-        *abort_flag = 1;
-        atomicAdd(&status[ST_WAIT_TIMEOUTS], 1);
-        status[ST_LAST_ERR] = ARMOR_ERR_TIMEOUT;
-      }
-    }
-  }
+  if (!ok) ok = wait_warp_slow(bar, parity, abort_flag, status);
   return __all_sync(0xffffffffu, ok);
+}
+
+// The same without an answer, for the warp that issues the products: one that goes on after a wait ran out multiplies what is there.
+__device__ __forceinline__ void wait_short(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  if (!mbar_try(bar, parity)) wait_warp_slow(bar, parity, abort_flag, status);
+  __syncwarp();
 }
 
 // ---------------------------------------------------------------- units
@@ -767,23 +778,23 @@ kv_attend_tile_kernel(const TileP p) {
     if (warp == 16) {
       const uint32_t leader = elect_lane();
       const uint32_t qk = idesc_f16(KEYS, 0), pv = idesc_f16(DIM, 1);
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(bar, parity, abortp, p.status) && ok; };
+      auto wait = [&](uint32_t bar, uint32_t parity) { wait_short(bar, parity, abortp, p.status); };
+      // (Descriptors begin from a value that the compiler knows to be the same in all lanes, so that they are formed in uniform registers.)
+      const uint32_t tm = uniform(tmem);
+      auto desc = [&](uint32_t at, uint32_t leading) { return (uint64_t)SW128_HI << 32 | (leading >> 4) << 16 | (at >> 4); };
+      const uint32_t q0 = smem + L::Q0;
       auto scores = [&](int half, uint32_t st) {
-        if (!ok) return;
-        const uint64_t dq = smem_desc_sw128(smem + L::Q0 + half * L::Q_BYTES, 16, 1024), dk = smem_desc_sw128(smem + L::K0 + st * L::BYTES, 16, 1024);
+        const uint32_t k0 = uniform(smem + L::K0 + st * L::BYTES), qh = uniform(q0 + half * L::Q_BYTES);
 #pragma unroll
         for (int k = 0; k < DIM / 16; ++k)
-          umma_ss(leader, tmem + half * 128, dq + (uint64_t)(((k >> 2) * L::Q_CHUNK + (k & 3) * 32) >> 4),
-                  dk + (uint64_t)(((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4), qk, k > 0);
+          umma_ss(leader, tm + half * 128, desc(qh + (k >> 2) * L::Q_CHUNK + (k & 3) * 32, 16), desc(k0 + (k >> 2) * L::CHUNK + (k & 3) * 32, 16), qk, k > 0);
         umma_commit_w(leader, s_full + 8 * half);
       };
       auto values = [&](int half, uint32_t st, uint32_t place, bool acc) {
-        if (!ok) return;
-        const uint64_t dv = smem_desc_sw128(smem + L::V0 + st * L::BYTES, L::CHUNK, 1024);
+        const uint32_t v = uniform(smem + L::V0 + st * L::BYTES), w = uniform(tm + half * 128 + 64 + place * 32);
 #pragma unroll
         for (int k = 0; k < KEYS / 16; ++k)
-          umma_ts(leader, tmem + 256 + half * 128, tmem + half * 128 + 64 + place * 32 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), pv, acc || k > 0);
+          umma_ts(leader, tm + 256 + half * 128, w + k * 8, desc(v + k * 2048, L::CHUNK), pv, acc || k > 0);
         umma_commit_w(leader, o_done + 8 * (2 * half + place));
       };
       uint32_t seg = 0, seg1 = 0, n = 0, turn[2] = {0, 0};
@@ -803,7 +814,7 @@ kv_attend_tile_kernel(const TileP p) {
             if (i + 1 < count) {
               tc_fence_after();
               scores(h, st2);
-              if (ok && h + 1 == halves) umma_commit_w(leader, k_empty + 8 * st2);
+              if (h + 1 == halves) umma_commit_w(leader, k_empty + 8 * st2);
             }
           }
           if (i < 0) continue;
@@ -814,7 +825,7 @@ kv_attend_tile_kernel(const TileP p) {
             wait(p_full + 8 * (2 * h + (turn[h] & 1)), (turn[h] >> 1) & 1);
             tc_fence_after();
             values(h, st, turn[h] & 1, i > 0);
-            if (ok && h + 1 == halves) umma_commit_w(leader, v_empty + 8 * st);
+            if (h + 1 == halves) umma_commit_w(leader, v_empty + 8 * st);
             ++turn[h];
           }
           ++n;
