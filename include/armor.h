@@ -324,8 +324,9 @@ armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_gr
  * last n_b of the lengths[b] positions of sequence b: its row i has position p = lengths[b] - n_b + i, which lies in slot p % page_size
  * of page pages[b * ld_pages + p / page_size].  Positions below zero are padding.  Rows from starts[n_seqs] on belong to no sequence and
  * are left as they are.  Nothing of a batch is read on the host: a captured call follows what the arrays hold when it is replayed.
- * A page out of [0, n_pages), a position behind the table's max_pages and a sequence whose rows are out of range are counted in device
- * status word 11 and neither read nor written.  n_rows (of the packed arrays) 0 or n_seqs 0: a no-op. */
+ * A page out of [0, n_pages), a sequence whose rows are out of range and one longer than its max_pages hold are counted in device status
+ * word 11 and neither read nor written: positions on such a page are not there, the rows of such a sequence are left as they are (by
+ * armor_kv_read: zeros).  n_rows (of the packed arrays) 0 or n_seqs 0: a no-op. */
 typedef struct {
   int8_t *k, *v;
   float *k_scale, *v_scale;

@@ -30,7 +30,6 @@ constexpr int WARPS = 6, THREADS = 32 * WARPS, STEP = 32 * WARPS;      // positi
 constexpr int STAGES = 2;                   // of 32 positions a warp
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
-constexpr float LEAST = 7.888609e-31f;      // 2^-100: scales of values below count as this (their values are below 1e-28)
 
 template <int DIM, int NT>
 struct Few {
@@ -422,7 +421,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         for (int g = 0; g < 2; ++g)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float v = scales[32 + 16 * g + quad + 8 * e], vs = v < LEAST ? LEAST : v;
+            const float vs = measure(scales[32 + 16 * g + quad + 8 * e]);
             const float ka = scales[16 * g + quad + 8 * e] * factor, kb = __log2f(vs);
             kr[g][e] = __fdividef(1.f, vs);
 #pragma unroll

@@ -31,7 +31,6 @@ using namespace tc;
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
-constexpr float LEAST = 7.888609e-31f;
 constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
 
 constexpr int NUMBERS = 8;                  // blocks whose positions' numbers are kept
@@ -755,7 +754,7 @@ kv_attend_tile_kernel(const TileP p) {
         // The numbers of block n - NUMBERS have been read: the keys of block n - STAGES have been multiplied, and those only when the scores of
         // block n - STAGES - 1 had been read, behind the weights of the one before
         const uint32_t at = smem + L::C0 + (n % NUMBERS) * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
-        const float v = vs < LEAST ? LEAST : vs;
+        const float v = measure(vs);
         const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");

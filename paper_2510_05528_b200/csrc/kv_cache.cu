@@ -204,10 +204,11 @@ Cache view(const armor_kv_cache* g) {
   divisor(c.page_size, c.mul, c.shift);
   return c;
 }
-Batch view(const armor_kv_batch* g, int64_t rows) {
+Batch view(const armor_kv_batch* g, const armor_kv_cache* c, int64_t rows) {
   Batch b;
   b.pages = g->pages; b.lengths = g->lengths; b.starts = g->starts; b.ld = g->ld_pages;
   b.n = (int)g->n_seqs; b.max_pages = (int)g->max_pages; b.rows = rows;
+  b.capacity = g->max_pages * c->page_size;
   return b;
 }
 
@@ -227,7 +228,7 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
   if (g->n_rows == 0 || batch->n_seqs == 0) return ARMOR_OK;
   if (!g->k || !g->v) return ARMOR_ERR_INVALID_ARG;
   const Cache cv = view(cache);
-  const Batch bv = view(batch, g->n_rows);
+  const Batch bv = view(batch, cache, g->n_rows);
   const Packed x{g->k, g->v, g->k_row_stride, g->k_head_stride, g->v_row_stride, g->v_head_stride};
   const bool al = aligned16(g->k, g->k_row_stride, es) && aligned16(g->v, g->v_row_stride, es) && g->k_head_stride * es % 16 == 0 &&
                   g->v_head_stride * es % 16 == 0;
@@ -295,7 +296,7 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   if (reinterpret_cast<uintptr_t>(g->q) % 2 || reinterpret_cast<uintptr_t>(g->o) % 2) return ARMOR_ERR_SHAPE;
   KvAttend a;
   a.c = view(cache);
-  a.b = view(batch, g->n_rows);
+  a.b = view(batch, cache, g->n_rows);
   a.q = g->q; a.q_row = g->q_row_stride; a.q_head = g->q_head_stride;
   a.o = g->o; a.o_row = g->o_row_stride; a.o_head = g->o_head_stride;
   a.group = (int)(g->heads / cache->kv_heads); a.dim = (int)cache->head_dim; a.dtype = g->dtype;

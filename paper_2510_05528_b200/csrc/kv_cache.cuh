@@ -20,6 +20,7 @@ struct Batch {
   int64_t ld;
   int n, max_pages;
   int64_t rows;                             // rows of the packed arrays
+  int64_t capacity;                         // positions that a table holds
 };
 
 // (the rounded-up reciprocal: with 2^(s-1) < d <= 2^s, m = ceil(2^(31+s) / d) is at most 2^32 - 1 for d > 1 and
@@ -39,7 +40,7 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int at, bool& bad) {
   s.first = b.starts[at];
   const int64_t n = (int64_t)b.starts[at + 1] - s.first;
   s.length = max(b.lengths[at], 0);
-  bad = s.first < 0 || n < 0 || s.first + n > b.rows;
+  bad = s.first < 0 || n < 0 || s.first + n > b.rows || s.length > b.capacity;
   s.n = bad ? 0 : (int)n;
   return s;
 }
@@ -81,6 +82,11 @@ __device__ __forceinline__ bool place(const Cache& c, const Batch& b, int at, ui
   page = (uint32_t)b.pages[(int64_t)at * b.ld + i];
   return page < c.n_pages;
 }
+
+// The scale that a position's contribution is measured with, sv itself for all that matter.  A row of zeros may have any: 2^-60, so that neither its own
+// weight, which the sum of the weights needs, nor the others' contributions fall below what fp32 holds.  Scales below 2^-100 count as that (their values
+// are below 1e-28).  A scale that is no number stays what it is.
+__device__ __forceinline__ float measure(float sv) { return sv == 0.f ? 8.6736174e-19f : (sv < 7.8886091e-31f ? 7.8886091e-31f : sv); }
 
 }  // namespace kv
 

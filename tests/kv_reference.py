@@ -72,7 +72,8 @@ class Case:
         """(o, tolerance of each of its elements) in 64 bits.
 
         Beside the output's own half step, off is: a weight by its rounding to fp16, 2^-11 of it, or 2^-25 of the largest (weight times scale
-        of the value) where it is small; and by what fp32 does to its exponent: a dot product of `dim` products in any order, each
+        of the value) where it is small (a row of zeros counts with the scale 2^-60, scales below 2^-100 as that: such a position may have all of the weight and be the
+        largest by it); and by what fp32 does to its exponent: a dot product of `dim` products in any order, each
         addition off by 2^-23 of the sum of the moduli at most (tensor cores cut off), then a product with two rounded factors, an added logarithm and
         the subtraction of the maximum (2^-22 of the largest of the numbers in hand, in log2 units), the exponential, the inverse of the
         scale and the sum of the weights over up to `positions` terms in fp32, each of these to 2^-22 (sum: 2^-24 for each of the terms added one by one)."""
@@ -105,7 +106,7 @@ class Case:
                 off = 0.6932 * (torch.where(seen, moduli, 0.0).amax(1, keepdim=True) * dim * 2.0 ** -23 +
                                 (torch.where(seen, s, 0.0).abs().amax(1, keepdim=True) * 1.4427 + vs[c].clamp(min=1e-30).log2().abs().max() + 16) * 2.0 ** -22)
                 off = off + 4 * 2.0 ** -22 + min(length, 4096) * 2.0 ** -24
-                big = (w * vs[c]).amax(1, keepdim=True) * 127
+                big = (w * torch.where(vs[c] == 0, 2.0 ** -60, vs[c].clamp(min=2.0 ** -100))).amax(1, keepdim=True) * 127
                 near = (2.0 ** -11 + 2 * off) * (w @ V[c].abs()) + seen.sum(1, keepdim=True) * 2.0 ** -25 * big
                 rows = slice(self.first[b], self.first[b] + n)
                 out[rows, h] = o
