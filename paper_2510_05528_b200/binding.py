@@ -623,32 +623,43 @@ def _heads_at(t: torch.Tensor, dtype, rows: int | None, heads: int | None, dim: 
     return t.data_ptr(), row if shape[0] > 1 else max(row, dim), head if shape[1] > 1 else max(head, dim)
 
 
-def _kv_rows(cache: KvCache, batch: KvBatch, k, v, here) -> armor_kv_rows:
+def _kv_here(cache: KvCache, batch: KvBatch, here: int) -> None:
     if cache.index != here or batch.index != here:
         raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, the call's device is cuda:{here}")
+
+
+def _kv_rows(cache: KvCache, batch: KvBatch, k, v, here) -> armor_kv_rows:
+    _kv_here(cache, batch, here)
     code = _row_dtype(k, "k")
     kp, kr, kh = _heads_at(k, k.dtype, None, cache.kv_heads, cache.head_dim, "k", here)
     vp, vr, vh = _heads_at(v, k.dtype, k.size(0), cache.kv_heads, cache.head_dim, "v", here)
     return armor_kv_rows(kp, vp, k.size(0), kr, kh, vr, vh, code)
 
 
-def armor_kv_write(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
-    """The rows of k and v [rows, kv_heads, head_dim] rounded into the cache's pages (see armor.h)."""
-    code = lib().armor_kv_write(ctx, cache.args, batch.args, _kv_rows(cache, batch, k, v, _cuda_index(k, "k")), _stream())
+def _kv_write(ctx, here, cache, batch, k, v) -> None:
+    code = lib().armor_kv_write(ctx, cache.args, batch.args, _kv_rows(cache, batch, k, v, here), _stream())
     if code:
         _check(code, "armor_kv_write")
 
 
-def armor_kv_read(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
-    """The same rows of the cache, to k and v."""
-    code = lib().armor_kv_read(ctx, cache.args, batch.args, _kv_rows(cache, batch, k, v, _cuda_index(k, "k")), _stream())
+def _kv_read(ctx, cache, batch, rows) -> None:
+    code = lib().armor_kv_read(ctx, cache.args, batch.args, rows, _stream())
     if code:
         _check(code, "armor_kv_read")
 
 
+def armor_kv_write(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
+    """The rows of k and v [rows, kv_heads, head_dim] rounded into the cache's pages (see armor.h)."""
+    _kv_write(ctx, _cuda_index(k, "k"), cache, batch, k, v)
+
+
+def armor_kv_read(ctx, cache: KvCache, batch: KvBatch, k, v) -> None:
+    """The same rows of the cache, to k and v."""
+    _kv_read(ctx, cache, batch, _kv_rows(cache, batch, k, v, _cuda_index(k, "k")))
+
+
 def _kv_attend(ctx, here, cache, batch, q, o, scale, window, max_chunk) -> torch.Tensor:
-    if cache.index != here or batch.index != here:
-        raise ValueError(f"the cache is on cuda:{cache.index}, the batch on cuda:{batch.index}, the call's device is cuda:{here}")
+    _kv_here(cache, batch, here)
     code = _row_dtype(q, "q")
     dim = cache.head_dim
     qp, qr, qh = _heads_at(q, q.dtype, None, None, dim, "q", here)
@@ -1016,8 +1027,7 @@ class ArmorContext:
 
     def kv_write(self, cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor) -> None:
         """Puts the new rows k and v [rows, kv_heads, head_dim] (fp32, bf16 or fp16) into the cache, rounded to int8 with a scale each."""
-        self._current()
-        armor_kv_write(self.ctx, cache, batch, k, v)
+        _kv_write(self.ctx, self._current(), cache, batch, k, v)
 
     def kv_read(self, cache: KvCache, batch: KvBatch, rows: int, dtype: torch.dtype = torch.bfloat16, *,
                 out: tuple[torch.Tensor, torch.Tensor] | None = None) -> tuple[torch.Tensor, torch.Tensor]:
@@ -1025,15 +1035,18 @@ class ArmorContext:
         they are (in new tensors: not set)."""
         here = self._current()
         if out is None:
-            size = (rows, cache.kv_heads, cache.head_dim)
-            k, v = out = cache.k.new_empty(size, dtype=dtype), cache.k.new_empty(size, dtype=dtype)
-        else:
-            k, v = out
-            if k.size(0) != rows or k.dtype is not dtype:
-                raise ValueError(f"out must have {rows} rows of {dtype}, got {k.size(0)} of {k.dtype}")
-        if k.get_device() != here:
-            raise ValueError(f"out must be on {self.device}")
-        armor_kv_read(self.ctx, cache, batch, k, v)
+            # one allocation for both
+            _kv_here(cache, batch, here)
+            heads, dim = cache.kv_heads, cache.head_dim
+            both = cache.k.new_empty((2, rows, heads, dim), dtype=dtype)
+            at, row = both.data_ptr(), heads * dim
+            args = armor_kv_rows(at, at + rows * row * both.element_size(), rows, row, dim, row, dim, _row_dtype(both, "dtype"))
+            _kv_read(self.ctx, cache, batch, args)
+            return both.unbind(0)
+        k, v = out
+        if k.size(0) != rows or k.dtype is not dtype:
+            raise ValueError(f"out must have {rows} rows of {dtype}, got {k.size(0)} of {k.dtype}")
+        _kv_read(self.ctx, cache, batch, _kv_rows(cache, batch, k, v, here))
         return out
 
     def kv_attend(self, cache: KvCache, batch: KvBatch, q: torch.Tensor, *, scale: float | None = None, window: int = 0, max_chunk: int = 0,

@@ -90,7 +90,7 @@ struct FewP {
   int64_t limit;                            // rows of a sequence at most: those with more are left out
   float* parts;                             // two of every CTA
   int* counters;                            // one of every CTA, zero between calls
-  int min_steps;
+  int wide;                                 // 32 positions that begin at a multiple of 32 share a page: one copy for them
   int32_t* status;
 };
 
@@ -102,13 +102,12 @@ __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   if (rows < 1 || rows > p.limit) return u;
   u.tiles = (int)((rows + R - 1) / R);
   const int64_t lo = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
-  u.steps = max((int64_t)1, ((int64_t)s.length + STEP - 1) / STEP - lo / STEP);
+  u.steps = max((int64_t)1, divide((int64_t)s.length + STEP - 1, STEP) - divide(lo, STEP));
   u.per = u.steps * u.tiles * p.a.c.heads;
   return u;
 }
 
-// sixteen rows of a page's head, swizzled: the bank of a row's sixteen bytes moves with the row
-template <int DIM>
+// sixteen rows of a page's head, or 32, swizzled: the bank of a row's sixteen bytes moves with the row
 __device__ __forceinline__ void copy_rows(uint32_t dst, const CUtensorMap* map, uint32_t slot, int head, uint32_t page, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -144,7 +143,13 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   const Cache& c = p.a.c;
   const Batch& b = p.a.b;
   const uint32_t my_bars = tc::smem_u32(&bars[warp * STAGES]);
-  if (threadIdx.x == 0) abort_flag = 0;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    if (TOGETHER) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
+  }
   if (TOGETHER && lane == 0) {
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) tc::mbar_init(my_bars + 8 * i, 1);
@@ -180,10 +185,10 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       if (w < warp) before += scan[w];
       total += scan[w];
     }
-    n_ctas = (int)min((int64_t)gridDim.x, (total + p.min_steps - 1) / p.min_steps);
+    n_ctas = (int)min((int64_t)gridDim.x, total);
     if ((int)blockIdx.x >= n_ctas) return;
-    begin = (int64_t)blockIdx.x * total / n_ctas;
-    end = (int64_t)(blockIdx.x + 1) * total / n_ctas;
+    begin = divide((int64_t)blockIdx.x * total, n_ctas);
+    end = divide((int64_t)(blockIdx.x + 1) * total, n_ctas);
     int64_t base = before + up_to - mine;
     if (base <= begin && begin < base + mine)
       for (int i = s0; i < s1; ++i) {
@@ -207,12 +212,12 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       s = sequence(b, ++seq, bad);
       continue;
     }
-    const int64_t unit = (begin - base) / un.steps, u0 = base + unit * un.steps;
+    const int64_t unit = divide(begin - base, un.steps), u0 = base + unit * un.steps;
     const int first = (int)(begin - u0), count = (int)(min(end, u0 + un.steps) - begin);
-    const int head = (int)(unit / un.tiles), tile = (int)(unit - (int64_t)head * un.tiles);
+    const int head = (int)divide(unit, un.tiles), tile = (int)(unit - (int64_t)head * un.tiles);
     const int rows = s.n * p.a.group - tile * R;        // of this tile, if fewer than R
     const int64_t lo_all = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
-    const int step0 = (int)(lo_all / STEP) + first;
+    const int step0 = (int)divide(lo_all, STEP) + first;
 
     // ---- q: rows lane / 4 of each eight, four dimensions for each step of the product, in the order that keys come in
     uint32_t q[F::Q_SHARED ? 1 : NT][F::Q_SHARED ? 1 : F::KW][2];
@@ -301,7 +306,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     uint32_t page = 0, slot = 0;
     auto look = [&](int i) {                                // of step i
       int j = (step0 + i) * STEP + warp * 32 + lane;
-      j = TOGETHER ? min(j & ~15, last & ~15) : min(j, last);
+      j = TOGETHER ? (p.wide ? min(j & ~31, last & ~31) + (lane & 16) : min(j & ~15, last & ~15)) : min(j, last);
       const uint32_t x = quotient((uint32_t)j, c.mul, c.shift);
       slot = (uint32_t)j - x * c.page_size;
       page = x < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + x] : 0xffffffffu;
@@ -316,10 +321,12 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         const uint32_t page1 = __shfl_sync(0xffffffffu, page, 16), slot1 = __shfl_sync(0xffffffffu, slot, 16), bar = my_bars + 8 * st;
         if (lane == 0) {
           tc::mbar_expect_tx(bar, F::STAGE);
-          copy_rows<DIM>(to, &k_map, slot, head, page, bar);
-          copy_rows<DIM>(to + F::K_BYTES, &k_map, slot1, head, page1, bar);
-          copy_rows<DIM>(to + 2 * F::K_BYTES, &v_map, slot, head, page, bar);
-          copy_rows<DIM>(to + 2 * F::K_BYTES + F::V_BYTES, &v_map, slot1, head, page1, bar);
+          copy_rows(to, &k_map, slot, head, page, bar);
+          copy_rows(to + 2 * F::K_BYTES, &v_map, slot, head, page, bar);
+          if (!p.wide) {
+            copy_rows(to + F::K_BYTES, &k_map, slot1, head, page1, bar);
+            copy_rows(to + 2 * F::K_BYTES + F::V_BYTES, &v_map, slot1, head, page1, bar);
+          }
         }
       } else {
         const int64_t row = page * c.page + head * c.head + slot * c.slot;
@@ -579,7 +586,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       // ---- the parts of the unit: those of the CTAs from the one that holds its first step to the one that holds its last
       __threadfence();
       __syncthreads();
-      const int64_t c0 = ((u0 + 1) * n_ctas - 1) / total, c1 = ((u0 + un.steps) * n_ctas - 1) / total;
+      const int64_t c0 = divide((u0 + 1) * n_ctas - 1, total), c1 = divide((u0 + un.steps) * n_ctas - 1, total);
       if (threadIdx.x == 0) {
         const int had = atomicAdd(&p.counters[c0], 1);
         last_one = had == (int)(c1 - c0);
@@ -661,13 +668,13 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 
 namespace {
 
-// [pages][heads][slots][DIM] of keys or values, sixteen slots at a time
+// [pages][heads][slots][DIM] of keys or values, so many slots at a time
 template <int DIM>
-bool make_map(CUtensorMap* map, const Cache& c, int8_t* base) {
+bool make_map(CUtensorMap* map, const Cache& c, int8_t* base, cuuint32_t rows) {
   PFN_cuTensorMapEncodeTiled_v12000 enc = tc::get_encode();
   if (!enc) return false;
   cuuint64_t dims[4] = {DIM, c.page_size, (cuuint64_t)c.heads, c.n_pages}, strides[3] = {(cuuint64_t)c.slot, (cuuint64_t)c.head, (cuuint64_t)c.page};
-  cuuint32_t box[4] = {DIM, 16, 1, 1}, step[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {DIM, rows, 1, 1}, step[4] = {1, 1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
              DIM == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -678,7 +685,8 @@ void launch_typed(armor_ctx* c, FewP p, cudaStream_t s) {
   static PerDeviceOnce once;
   if (ensure_dynamic_smem(once, c->device, kv_attend_few_kernel<T, DIM, NT, TOGETHER>, F::SMEM) != ARMOR_OK) { c->host_err = ARMOR_ERR_CUDA; return; }
   CUtensorMap k_map{}, v_map{};
-  if (TOGETHER && (!make_map<DIM>(&k_map, p.a.c, p.a.c.k) || !make_map<DIM>(&v_map, p.a.c, p.a.c.v))) { c->host_err = ARMOR_ERR_CUDA; return; }
+  p.wide = p.a.c.page_size % 32 == 0;
+  if (TOGETHER && (!make_map<DIM>(&k_map, p.a.c, p.a.c.k, p.wide ? 32 : 16) || !make_map<DIM>(&v_map, p.a.c, p.a.c.v, p.wide ? 32 : 16))) { c->host_err = ARMOR_ERR_CUDA; return; }
   // two parts a CTA have to find room in the workspace (a single CTA leaves none)
   int64_t n = (int64_t)c->n_sm * F::CTAS;
   const int64_t room = ws_scratch_bytes(c) / (2 * F::PART * (int64_t)sizeof(float));
@@ -712,7 +720,6 @@ armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit
   p.status = c->status;
   p.counters = c->kv_counters;
   p.parts = c->T;
-  p.min_steps = 1;
   const int64_t rows = (a.max_chunk ? a.max_chunk : (a.b.rows + a.b.n - 1) / a.b.n) * a.group;
   KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
   if (a.dtype == ARMOR_DTYPE_BF16) {

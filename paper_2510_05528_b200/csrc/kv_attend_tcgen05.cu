@@ -245,8 +245,8 @@ struct Walk {
     if (left <= 0) return;
     seq = seq_;
     load();
-    const int64_t a_head = (prefix[seq + 1] - prefix[seq]) / p.a.c.heads, off = begin - prefix[seq];
-    head = (int)(off / a_head);
+    const int64_t a_head = divide(prefix[seq + 1] - prefix[seq], p.a.c.heads), off = begin - prefix[seq];
+    head = (int)divide(off, a_head);
     int64_t rem = off - head * a_head;
     const int lane = threadIdx.x & 31;
     for (int t0 = 0;; t0 += 32) {
@@ -385,7 +385,7 @@ kv_attend_tile_kernel(const TileP p) {
   const int64_t total = prefix[b.n];
   const int n_ctas = (int)min((int64_t)gridDim.x, total);
   const bool idle = (int)blockIdx.x >= n_ctas;
-  const int64_t begin = idle ? 0 : (int64_t)blockIdx.x * total / n_ctas, end = idle ? 0 : (int64_t)(blockIdx.x + 1) * total / n_ctas;
+  const int64_t begin = idle ? 0 : divide((int64_t)blockIdx.x * total, n_ctas), end = idle ? 0 : divide((int64_t)(blockIdx.x + 1) * total, n_ctas);
   for (int i = threadIdx.x; i < b.n; i += THREADS)
     if (prefix[i] <= begin && begin < prefix[i + 1]) at_seq = i;
   if (warp == 17 && lane == 0) p.cuts[blockIdx.x].last = -1;
@@ -844,7 +844,7 @@ kv_attend_tile_kernel(const TileP p) {
             g.seq = at.seq; g.head = at.head; g.row0 = at.s.first; g.n = at.s.n; g.length = at.s.length;
             g.part = cut ? 2 * (int)blockIdx.x + (at.first == 0 ? 1 : 0) : -1;
             if (cut && at.first == 0)                                   // parts up to the CTA that holds the unit's last block
-              p.cuts[blockIdx.x] = Cut{at.seq, at.head, at.tile, (int)(((end - at.left + at.total) * n_ctas - 1) / total)};
+              p.cuts[blockIdx.x] = Cut{at.seq, at.head, at.tile, (int)divide((end - at.left + at.total) * n_ctas - 1, total)};
           }
           ring[n % RING] = g;
           mbar_arrive(r_full + 8 * (n % RING));

@@ -33,6 +33,13 @@ inline void divisor(uint32_t d, uint32_t& mul, int& shift) {
 }
 __device__ __forceinline__ uint32_t quotient(uint32_t p, uint32_t mul, int shift) { return (uint32_t)(((uint64_t)p * mul) >> shift); }
 
+// a / b of numbers that are not negative: in 32 bits where they fit (a 64-bit division is a hundred instructions or so, and a call of 10 us has ten of them
+// one behind the other)
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  if (((uint64_t)a | (uint64_t)b) >> 32 == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+  return a / b;
+}
+
 // what a sequence is made of: n new rows from row `first` on, the last n of `length` positions
 struct Seq { int first, n, length; };
 __device__ __forceinline__ Seq sequence(const Batch& b, int at, bool& bad) {
