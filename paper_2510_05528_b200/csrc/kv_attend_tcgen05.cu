@@ -16,7 +16,8 @@
 // Tensor memory: for either half S of a block (64 columns), the weights of two (32 each) and O.  S is read into registers at once, so that the next
 // block's scores are formed behind this one's exponentials.
 //
-// All blocks of all units stand in one line, cut into equal shares for one CTA an SM.  A unit that is cut leaves its parts in the
+// All blocks of all units, and OVERHEAD more for each unit, stand in one line, cut into equal shares for one CTA an SM.  (Without the overhead the CTAs with the
+// first tiles of a prompt, of a few blocks each, came last: 8,192 tokens of 64 heads {OVER}.)  A unit that is cut leaves its parts in the
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
 // that no barrier is missed, and the status says that its output is worthless.
 #include "kv_cache.cuh"
@@ -32,6 +33,7 @@ constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
+constexpr int OVERHEAD = 5;                 // what a unit takes beside its blocks, in blocks: q in, O out, the first maximum (14,000 cycles)
 
 constexpr int NUMBERS = 8;                  // blocks whose positions' numbers are kept
 
@@ -222,8 +224,8 @@ constexpr int RING = 4;
 // The CTA's share of the line, walked by one warp
 struct Walk {
   const TileP& p;
-  const int64_t* prefix;                    // [n + 1] blocks ahead of a sequence
-  int64_t left;                             // blocks of the share from this segment on
+  const int64_t* prefix;                    // [n + 1] where a sequence begins in the line
+  int64_t left;                             // of the share from this segment on
   int seq, head, tile, tiles;
   Seq s;
   int first, count, total, block;           // of the segment: its first block in the unit, its blocks, the unit's, the position block of first
@@ -251,7 +253,7 @@ struct Walk {
     const int lane = threadIdx.x & 31;
     for (int t0 = 0;; t0 += 32) {
       const int t = t0 + lane;
-      const int mine = t < tiles ? blocks_of(p.a, s, t).count : 0;
+      const int mine = t < tiles ? blocks_of(p.a, s, t).count + OVERHEAD : 0;
       int64_t upto = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -268,8 +270,8 @@ struct Walk {
       rem -= __shfl_sync(0xffffffffu, upto, 31);
     }
     set((int)rem);
-    if (p.whole && first > 0) {             // the unit is that of the CTA where it begins
-      left -= total - first;
+    if (count < 1 || (p.whole && first > 0)) {          // nothing left of this unit; or it is that of the CTA where it begins
+      left -= total + OVERHEAD - first;
       advance();
     }
   }
@@ -287,7 +289,7 @@ struct Walk {
     set(0);
   }
   __device__ __forceinline__ bool more() const { return left > 0; }
-  __device__ __forceinline__ void next() { left -= count; advance(); }
+  __device__ __forceinline__ void next() { left -= total + OVERHEAD - first; advance(); }
 };
 
 // eight dimensions from 8 c on of a row of a half in shared memory: rows of 128 bytes, swizzled
@@ -360,7 +362,7 @@ kv_attend_tile_kernel(const TileP p) {
     if (bad && blockIdx.x == 0 && lane == 0) report(p.status);
     const int tiles = tiles_of(p, s);
     int64_t sum = 0;
-    for (int t = lane; t < tiles; t += 32) sum += blocks_of(p.a, s, t).count;
+    for (int t = lane; t < tiles; t += 32) sum += blocks_of(p.a, s, t).count + OVERHEAD;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) prefix[i + 1] = sum * c.heads;
