@@ -28,6 +28,7 @@ using namespace kv;
 
 constexpr int WARPS = 6, THREADS = 32 * WARPS, STEP = 32 * WARPS;      // positions a step of a CTA
 constexpr int STAGES = 2;                   // of 32 positions a warp
+constexpr int OVERHEAD = 2;                 // what a unit takes beside its steps, in steps: its sequence, q, the first copies, the warps' sums
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
 
@@ -94,7 +95,7 @@ struct FewP {
   int32_t* status;
 };
 
-struct Unit { int64_t per, steps; int tiles; };       // steps in all, of one unit; tiles of rows
+struct Unit { int64_t per, steps; int tiles; };       // what all units take, steps of one; tiles of rows
 template <int R>
 __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   Unit u{0, 0, 0};
@@ -103,7 +104,7 @@ __device__ __forceinline__ Unit units_of(const FewP& p, const Seq& s) {
   u.tiles = (int)((rows + R - 1) / R);
   const int64_t lo = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
   u.steps = max((int64_t)1, divide((int64_t)s.length + STEP - 1, STEP) - divide(lo, STEP));
-  u.per = u.steps * u.tiles * p.a.c.heads;
+  u.per = (u.steps + OVERHEAD) * u.tiles * p.a.c.heads;
   return u;
 }
 
@@ -212,8 +213,10 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       s = sequence(b, ++seq, bad);
       continue;
     }
-    const int64_t unit = divide(begin - base, un.steps), u0 = base + unit * un.steps;
+    const int64_t unit = divide(begin - base, un.steps + OVERHEAD), u0 = base + unit * (un.steps + OVERHEAD);
     const int first = (int)(begin - u0), count = (int)(min(end, u0 + un.steps) - begin);
+    begin = u0 + un.steps + OVERHEAD;                     // of the unit that comes
+    if (count < 1) continue;                              // (the share begins behind its last step)
     const int head = (int)divide(unit, un.tiles), tile = (int)(unit - (int64_t)head * un.tiles);
     const int rows = s.n * p.a.group - tile * R;        // of this tile, if fewer than R
     const int64_t lo_all = p.a.window ? max((int64_t)0, (int64_t)s.length - s.n + 1 - p.a.window) : 0;
@@ -660,7 +663,6 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       }
     }
     __syncthreads();                                      // (the stages' place is free)
-    begin += count;
   }
 }
 
