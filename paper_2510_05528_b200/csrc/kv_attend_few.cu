@@ -5,18 +5,20 @@
 //   t_j = (q . kq_j) ks_j scale log2 e + log2 vs_j     over j <= p (and j > p - window)
 //   w_j = 2^(t_j - m),  O = sum w_j vq_j,  l = sum w_j / vs_j,  o = O / l
 // m is a maximum of the t_j seen so far, so that w_j, the weight a value's bytes are taken with, is a factor of at most 2^LAZY and its rounding to
-// fp16 is one of 2^-12 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
+// fp16 is one of 2^-11 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
 // a multiplication by a power of two; products and sums are fp32.  l is summed from the unrounded weights.  No row: zeros.
 //
 // Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time, twice, in the layout that mma.sync m16n8k16 wants of its
 // M side, where a product over the dimensions may take them in any order: positions are the M side of the scores, S^T = K Q^T, dimensions the M
 // side of O^T = V^T P^T, rows of q the N side of both, eight at a time, so that for up to eight rows nothing is computed twice
 // and O takes dim / 4 registers.  (tcgen05 would multiply 128 rows for these eight.)  A byte becomes fp16 by a permutation, 1024 + (byte + 128),
-// and a subtraction.  A lane copies the bytes that it multiplies itself, sixteen at a time, to a place of its own in shared memory, 32
-// positions ahead (cp.async): no registers wait, and no warp waits for another before the end of a CTA's share.
+// and a subtraction.  A warp's rows come to shared memory a stage of 32
+// positions ahead by tensor copies (TMA) that one lane asks for, 16 rows each, or 32 where pages hold a multiple of 32; pages of other sizes take
+// cp.async, each lane the sixteen bytes that it multiplies.  (Always so, the asking took 1,000 to 1,300 of a step's 3,900 cycles, 64 streams 152 us
+// for 123.)  No registers wait, and no warp waits for another before the end of a CTA's share.
 //
-// All positions of all (sequence, key head, tile of rows) units, 192 at a time, stand in one line that is cut into equal
-// shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
+// All positions of all (sequence, key head, tile of rows) units, 192 at a time, and OVERHEAD more steps for each unit, stand in one line that is
+// cut into equal shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
 // last, by a counter, adds them up in the order of the parts: no CTA waits for another and the bits do not depend on the run.
 #include "kv_cache.cuh"
 #include "tc_common.cuh"

@@ -2,12 +2,12 @@
 // kv_attend_few.cu: S = Q Kq^T in fp32, t = S ks factor + log2 vs, weights 2^(t - m) in fp16, O = W Vq, l = sum w / vs, o = O / l.
 //
 // A unit is a tile of 256 rows (a token and a head of the group each; the heads of a group share keys) of one sequence and key head against the
-// blocks of 128 positions that its rows see.  A CTA takes it as two halves of 128 rows, so that the tensor cores have the one half's
+// blocks of 64 positions that its rows see.  A CTA takes it as two halves of 128 rows, so that the tensor cores have the one half's
 // products while the other's weights are formed:
-//   warps 0-3, 4-7 : the rows of a half each: S from tensor memory, weights back in its place, O rescaled there when the maximum moves by far
-//                    (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16).  A lane has 32 of
+//   warps 0-3, 4-7 : the rows of a half each: S from tensor memory, weights back to places of their own, O rescaled there when the maximum moves by far
+//                    (rarely), O out at the end; they also bring q in (fp16, scaled by a power of two where it was bf16).  A lane has 16 of
 //                    the block's columns in four rows, not a row (a lane a row reads all positions' numbers: 96 reads of 16 bytes a
-//                    warp, each of them 512 bytes into registers; blocks took 11,000 cycles)
+//                    warp for 128 positions, each of them 512 bytes into registers, and those took 11,000 cycles; now 64 take 2,900)
 //   warps 8-11     : keys from their pages through registers to fp16 in shared memory, four blocks, and the three numbers of a
 //                    position (ks factor, log2 vs, 1 / vs)
 //   warps 12-15    : values likewise
@@ -16,8 +16,11 @@
 // Tensor memory: for either half S of a block (64 columns), the weights of two (32 each) and O.  S is read into registers at once, so that the next
 // block's scores are formed behind this one's exponentials.
 //
+// Bound by the products' operands: M 128 N 64 from shared memory takes 80 to 90 cycles here (32 by the rate), and the warp that issues them
+// stands meanwhile.  8,192 tokens of 64 heads, causal: 1.45 ms, 757 TFLOP/s; 2,048 after 14,336 of 32 heads, each its own keys: 0.66 ms, 778.
+//
 // All blocks of all units, and OVERHEAD more for each unit, stand in one line, cut into equal shares for one CTA an SM.  (Without the overhead the CTAs with the
-// first tiles of a prompt, of a few blocks each, came last: 8,192 tokens of 64 heads {OVER}.)  A unit that is cut leaves its parts in the
+// first tiles of a prompt, of a few blocks each, came last: 8,192 tokens of 64 heads 1.82 ms.)  A unit that is cut leaves its parts in the
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
 // that no barrier is missed, and the status says that its output is worthless.
 #include "kv_cache.cuh"
@@ -32,7 +35,7 @@ using namespace tc;
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
-constexpr int JOIN_ROWS = 16;               // rows of a CTA of the join
+constexpr int JOIN_ROWS = 16, JOIN_THREADS = 256;   // rows and threads of a CTA of the join (16 x 5 tokens: 128 threads 70.0 us, 256 67.7; 32 rows of 128 threads 77)
 constexpr int OVERHEAD = 5;                 // what a unit takes beside its blocks, in blocks: q in, O out, the first maximum (14,000 cycles)
 
 constexpr int NUMBERS = 8;                  // blocks whose positions' numbers are kept
@@ -865,7 +868,7 @@ kv_attend_tile_kernel(const TileP p) {
 
 // The parts of units that were cut: CTA x takes the unit whose first part is that of CTA x, JOIN_ROWS rows of it.
 template <typename T, int DIM>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(JOIN_THREADS)
 kv_join_kernel(const TileP p) {
   grid_begin();
   using L = Tile<DIM>;
@@ -879,7 +882,7 @@ kv_join_kernel(const TileP p) {
   auto part = [&](int k) { return p.parts + (2 * (int64_t)k + (k == c0)) * L::PART; };
   float top = minus_inf();
   for (int k = c0; k <= cut.last; ++k) top = fmaxf(top, part(k)[ROWS * DIM + r]);
-  for (int d = threadIdx.x / JOIN_ROWS * 4; d < DIM; d += 128 / JOIN_ROWS * 4) {
+  for (int d = threadIdx.x / JOIN_ROWS * 4; d < DIM; d += JOIN_THREADS / JOIN_ROWS * 4) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
@@ -918,7 +921,7 @@ armor_status launch_typed(armor_ctx* c, TileP p, cudaStream_t s) {
     launch_dependent(kv_attend_tile_kernel<T, DIM, ALIGNED>, dim3(n), dim3(THREADS), L::SMEM, s, p);
     c->launches++;
     if (!p.whole) {
-      launch_dependent(kv_join_kernel<T, DIM>, dim3(n, ROWS / JOIN_ROWS), dim3(128), 0, s, p);
+      launch_dependent(kv_join_kernel<T, DIM>, dim3(n, ROWS / JOIN_ROWS), dim3(JOIN_THREADS), 0, s, p);
       c->launches++;
     }
   }

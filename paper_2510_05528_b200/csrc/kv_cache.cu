@@ -4,8 +4,10 @@
 // rounding).  Out: q s in fp32, rounded once to the output's type.  Both are bound by HBM: in, an element is read once and one byte
 // written; out, the reverse.  A warp has some tokens and some heads of each.  Its lanes look up the places of all its tokens at once, then
 // take the rows, dim / 8 lanes and eight elements each, so that a row's bytes go out whole and its maximum needs three or four
-// shuffles and no barrier; UNROLL rows of a lane are under way together.  (With a search for every row, 8,188 tokens of 8 heads took 63 us in and out, so
-// {NEW}.)
+// shuffles and no barrier; UNROLL rows of a lane are under way together.  With a search for every row, 8,188 tokens of 8
+// heads of 128 took 63 us in and out; so 31, in 18.4 (51 MB, 2.8 TB/s) and out 12.4 (4.1 TB/s).  What is left
+// of long calls: 16 sequences of 8,000 go in at 3.7 TB/s (issue slots half taken) and out at 4.5, reads and writes mixed; of short ones: the
+// chain of loads, from the table to the page to the row.
 #include <algorithm>
 
 #include "kv_cache.cuh"
