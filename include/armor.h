@@ -324,9 +324,10 @@ armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_gr
  * last n_b of the lengths[b] positions of sequence b: its row i has position p = lengths[b] - n_b + i, which lies in slot p % page_size
  * of page pages[b * ld_pages + p / page_size].  Positions below zero are padding.  Rows from starts[n_seqs] on belong to no sequence and
  * are left as they are.  Nothing of a batch is read on the host: a captured call follows what the arrays hold when it is replayed.
- * A page out of [0, n_pages), a sequence whose rows are out of range and one longer than its max_pages hold are counted in device status
- * word 11 and neither read nor written: positions on such a page are not there, the rows of such a sequence are left as they are (by
- * armor_kv_read: zeros).  n_rows (of the packed arrays) 0 or n_seqs 0: a no-op. */
+ * A page out of [0, n_pages), a sequence whose rows are out of range and one longer than its max_pages hold or 2^31 - 4096 are counted in
+ * device status word 11 and neither read nor written: positions on such a page are not there, the rows of such a sequence are left as
+ * they are (by armor_kv_read: zeros).  Pages that nothing of a call reads (those before all windows) may be out of range.  n_rows (of the
+ * packed arrays) 0 or n_seqs 0: a no-op. */
 typedef struct {
   int8_t *k, *v;
   float *k_scale, *v_scale;
@@ -342,7 +343,7 @@ typedef struct {
  * their rows.  armor_kv_write rounds them into the cache; two rows of one call must not have the same place (pages that sequences share are
  * complete, or each is written by one).  armor_kv_read writes what the cache holds, rounded once from fp32 (rows of padding, and
  * those refused: zeros).  Errors: INVALID_ARG (missing arrays, negative counts), SHAPE (sizes, strides, alignment), UNSUPPORTED (dtype, head_dim),
- * TOO_LARGE (2^31 pages, slots, rows). */
+ * TOO_LARGE (2^31 pages, slots, rows; rows times heads of a group above 2^31 - 4096). */
 typedef struct {
   const void *k, *v;                       /* written to by armor_kv_read */
   int64_t n_rows;

@@ -15,7 +15,7 @@
 // and a subtraction.  A warp's rows come to shared memory a stage of 32
 // positions ahead by tensor copies (TMA) that one lane asks for, 16 rows each, or 32 where pages hold a multiple of 32; pages of other sizes take
 // cp.async, each lane the sixteen bytes that it multiplies.  (Always so, the asking took 1,000 to 1,300 of a step's 3,900 cycles, 64 streams 152 us
-// for 123.)  No registers wait, and no warp waits for another before the end of a CTA's share.
+// for 117.)  No registers wait, and no warp waits for another before the end of a CTA's share.
 //
 // All positions of all (sequence, key head, tile of rows) units, 192 at a time, and OVERHEAD more steps for each unit, stand in one line that is
 // cut into equal shares, one a CTA, whatever the lengths.  A unit that is cut leaves its parts (m, l, O in fp32) in the workspace, and the CTA that comes
@@ -316,11 +316,11 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       slot = (uint32_t)j - x * c.page_size;
       page = x < (uint32_t)b.max_pages ? (uint32_t)b.pages[(int64_t)seq * b.ld + x] : 0xffffffffu;
     };
-    unsigned refused = 0;                                   // a bit a step under way: one of its positions has no page
+    unsigned refused = 0;                                   // a bit a position of the step fetched last: it has no page
     auto fetch = [&](uint32_t turn) {                       // what has been looked up, to the stage of that step
       const bool none = page >= c.n_pages;
       if (none) page = slot = 0;
-      refused = refused << 1 | (unsigned)__any_sync(0xffffffffu, none);
+      refused = __ballot_sync(0xffffffffu, none);
       const uint32_t st = turn % STAGES, to = mine_at + st * F::STAGE;
       if constexpr (TOGETHER) {
         const uint32_t page1 = __shfl_sync(0xffffffffu, page, 16), slot1 = __shfl_sync(0xffffffffu, slot, 16), bar = my_bars + 8 * st;
@@ -380,15 +380,19 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
       }
       __syncwarp();
-      const bool ahead = i + 1 < count && ok;
-      if (ahead) {
+      const unsigned bad = refused;                         // of this step
+      if (i + 1 < count && ok) {
         fetch(turn + 1);
         if (i + 2 < count) look(i + 2);
         end_copies();
       }
       const int j0 = (step0 + i) * STEP + warp * 32;
-      const bool bad_page = refused >> (ahead ? 1 : 0) & 1u;
-      if (bad_page && j0 < inner_hi && lane == 0) report(p.status);
+      if (bad) {
+        // (what no row sees may lie on pages that are gone)
+        const int64_t at = (int64_t)s.length - s.n, hi = at + (tile * R + min(rows, R) - 1) / p.a.group + 1;
+        const int64_t lo = p.a.window ? at + tile * R / p.a.group + 1 - p.a.window : 0;
+        if (bad >> lane & 1u && j0 + lane >= lo && j0 + lane < hi) report(p.status);
+      }
       const uint8_t* const stage = mine + (turn % STAGES) * F::STAGE;
 
       // ---- scores of twice sixteen positions
@@ -442,7 +446,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
               for (int x = 0; x < 2; ++x) t[g][n][2 * e + x] = fmaf(t[g][n][2 * e + x], ka, kb);
           }
       }
-      const bool some_hidden = bad_page || j0 < inner_lo || j0 + 32 > inner_hi;
+      const bool some_hidden = bad || j0 < inner_lo || j0 + 32 > inner_hi;
       if (some_hidden) {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
@@ -451,7 +455,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int j = j0 + 16 * g + quad + 8 * (e >> 1);
-              if (bad_page || j < low[n][e & 1] || j >= high[n][e & 1]) t[g][n][e] = minus_inf();
+              if (bad >> (16 * g + quad + 8 * (e >> 1)) & 1u || j < low[n][e & 1] || j >= high[n][e & 1]) t[g][n][e] = minus_inf();
             }
 #pragma unroll
         for (int g = 0; g < 2; ++g)

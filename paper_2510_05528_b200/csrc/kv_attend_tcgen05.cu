@@ -195,13 +195,14 @@ __device__ __forceinline__ void wait_short(uint32_t bar, uint32_t parity, volati
 
 // ---------------------------------------------------------------- units
 // The blocks that a tile's rows see, from `block` on
-struct Blocks { int block, count; };
+struct Blocks { int block, count, low; };
 __device__ __forceinline__ Blocks blocks_of(const KvAttend& a, const Seq& s, int tile) {
   const int rows = s.n * a.group, r0 = tile * ROWS, r1 = min(rows, r0 + ROWS) - 1;
   const int64_t at = (int64_t)s.length - s.n;
   const int64_t hi = max((int64_t)0, at + r1 / a.group + 1);
   const int64_t lo = a.window ? max((int64_t)0, at + r0 / a.group + 1 - a.window) : 0;
   Blocks b;
+  b.low = (int)lo;
   b.block = (int)(lo / KEYS);
   b.count = max(1, (int)((hi + KEYS - 1) / KEYS) - b.block);
   return b;
@@ -220,7 +221,8 @@ struct __align__(16) Segment {
   int row0;                                 // the sequence's first row in the packed arrays
   int n, length;                            // its new tokens, its positions
   int part;                                 // the place of the part that is left; -1: the unit is done here
-  int pad[2];
+  int low;                                  // the first position that a row of the tile sees
+  int pad;
 };
 constexpr int RING = 4;
 
@@ -231,7 +233,7 @@ struct Walk {
   int64_t left;                             // of the share from this segment on
   int seq, head, tile, tiles;
   Seq s;
-  int first, count, total, block;           // of the segment: its first block in the unit, its blocks, the unit's, the position block of first
+  int first, count, total, block, low;      // of the segment: its first block in the unit, its blocks, the unit's, the position block of first; the tile's first position
   __device__ __forceinline__ Walk(const TileP& p_, const int64_t* prefix_) : p(p_), prefix(prefix_) {}
   __device__ __forceinline__ void load() {
     bool bad;
@@ -241,6 +243,7 @@ struct Walk {
   __device__ __forceinline__ void set(int off) {
     const Blocks b = blocks_of(p.a, s, tile);
     total = b.count;
+    low = b.low;
     first = off;
     block = b.block + off;
     count = p.whole ? b.count : (int)min(left, (int64_t)(b.count - off));
@@ -678,8 +681,8 @@ kv_attend_tile_kernel(const TileP p) {
     const int lane_sub = lane % SUBS, lane_row = lane / SUBS;
     const int8_t* const from = (values ? c.v : c.k) + lane_sub * 16;
     uint32_t seg = 0;
-    // the block whose page is looked up: the segment's blocks behind it, its sequence, head, length, the lane's position
-    int behind = 0, seq = 0, head = 0, length = 0, j = 0;
+    // the block whose page is looked up: the segment's blocks behind it, its sequence, head, first position, length, the lane's position
+    int behind = 0, seq = 0, head = 0, low = 0, length = 0, j = 0;
     bool more = true;
     auto step = [&]() {                                                 // on to the next block; more: there is one
       j += KEYS;
@@ -687,7 +690,7 @@ kv_attend_tile_kernel(const TileP p) {
       more = segment(seg);
       if (more) {
         const Segment& at = ring[seg % RING];
-        behind = at.count - 1; seq = at.seq; head = at.head; length = at.length;
+        behind = at.count - 1; seq = at.seq; head = at.head; low = at.low; length = at.length;
         j = at.block * KEYS + w * 32 + lane;
       }
       done(seg++);
@@ -697,7 +700,7 @@ kv_attend_tile_kernel(const TileP p) {
     bool seen = false;
     auto look = [&]() {
       page = slot = 0;
-      seen = j < length;
+      seen = j >= low && j < length;                                    // (what no row sees may lie on pages that are gone)
       if (seen) {
         const uint32_t i = quotient((uint32_t)j, c.mul, c.shift);
         slot = (uint32_t)j - i * c.page_size;
@@ -844,7 +847,7 @@ kv_attend_tile_kernel(const TileP p) {
         if (lane == 0) {
           Segment g{};
           if (at.more()) {
-            g.count = at.count; g.block = at.block;
+            g.count = at.count; g.block = at.block; g.low = at.low;
             g.rows = at.s.n * p.a.group - at.tile * ROWS; g.first_row = at.tile * ROWS;
             g.seq = at.seq; g.head = at.head; g.row0 = at.s.first; g.n = at.s.n; g.length = at.s.length;
             g.part = cut ? 2 * (int)blockIdx.x + (at.first == 0 ? 1 : 0) : -1;

@@ -176,7 +176,7 @@ armor_status by_row_type(int32_t dtype, F&& f) {
   return dtype == ARMOR_DTYPE_BF16 ? f(__nv_bfloat16()) : f(__half());
 }
 
-constexpr int64_t MOST = 0x7fffffff;
+constexpr int64_t MOST = 0x7fffffff, MOST_POSITIONS = MOST + 1 - 4096;      // (a step that begins in a sequence ends below 2^31)
 
 armor_status check_cache(const armor_kv_cache* g) {
   if (!g) return ARMOR_ERR_INVALID_ARG;
@@ -210,7 +210,7 @@ Batch view(const armor_kv_batch* g, const armor_kv_cache* c, int64_t rows) {
   Batch b;
   b.pages = g->pages; b.lengths = g->lengths; b.starts = g->starts; b.ld = g->ld_pages;
   b.n = (int)g->n_seqs; b.max_pages = (int)g->max_pages; b.rows = rows;
-  b.capacity = g->max_pages * c->page_size;
+  b.capacity = std::min(g->max_pages * c->page_size, MOST_POSITIONS);
   return b;
 }
 
@@ -291,7 +291,7 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   if (g->heads < 1 || g->heads % cache->kv_heads) return ARMOR_ERR_SHAPE;
   if (g->q_row_stride < 0 || g->q_head_stride < 0 || g->o_row_stride < cache->head_dim || g->o_head_stride < cache->head_dim) return ARMOR_ERR_SHAPE;
   if (g->window < 0 || g->max_chunk < 0 || !(g->scale >= 0.f) || g->scale > 1e30f) return ARMOR_ERR_INVALID_ARG;
-  if (g->n_rows * (g->heads / cache->kv_heads) > MOST) return ARMOR_ERR_TOO_LARGE;
+  if (g->n_rows > 0 && g->heads / cache->kv_heads > MOST_POSITIONS / g->n_rows) return ARMOR_ERR_TOO_LARGE;
   if (!c) return ARMOR_ERR_INVALID_ARG;
   if (g->n_rows == 0 || batch->n_seqs == 0) return ARMOR_OK;
   if (!g->q || !g->o) return ARMOR_ERR_INVALID_ARG;
@@ -302,13 +302,13 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   a.q = g->q; a.q_row = g->q_row_stride; a.q_head = g->q_head_stride;
   a.o = g->o; a.o_row = g->o_row_stride; a.o_head = g->o_head_stride;
   a.group = (int)(g->heads / cache->kv_heads); a.dim = (int)cache->head_dim; a.dtype = g->dtype;
-  a.window = g->window; a.max_chunk = g->max_chunk;
+  a.window = g->window; a.max_chunk = std::min(g->max_chunk, g->n_rows);
   a.scale = g->scale * 1.4426950408889634f;
   a.aligned = aligned16(a.q, a.q_row, 2) && aligned16(a.o, a.o_row, 2) && a.q_head % 8 == 0 && a.o_head % 8 == 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   // Which kernels: the one for few rows a sequence reads keys and values once for every KV_FEW_ROWS of them, the other one once for 256.  Where
   // the host cannot tell (lengths are on the device), both run, each on its sequences.
-  const int64_t chunk = g->max_chunk ? g->max_chunk : (a.b.n == 1 ? g->n_rows : 0), rows = chunk * a.group;
+  const int64_t chunk = a.max_chunk ? a.max_chunk : (a.b.n == 1 ? g->n_rows : 0), rows = chunk * a.group;
   if (chunk ? rows <= KV_FEW_ROWS : g->n_rows <= batch->n_seqs && a.group <= KV_FEW_ROWS) st = launch_kv_attend_few(c, a, MOST, s);
   else if (a.b.n == 1 || a.group > KV_FEW_ROWS) st = launch_kv_attend_tile(c, a, 0, s);
   else {

@@ -68,8 +68,8 @@ class Case:
         q, s = getattr(self, t)[at, :, slot], getattr(self, t + "_scale")[at, :, slot]
         return q.transpose(0, 1).double(), s.transpose(0, 1).double()
 
-    def attention(self, q, scale=None, window=0):
-        """(o, tolerance of each of its elements) in 64 bits.
+    def attention(self, q, scale=None, window=0, gone=None):
+        """(o, tolerance of each of its elements) in 64 bits; gone: positions of the first sequence that are not there.
 
         Beside the output's own half step, off is: a weight by its rounding to fp16, 2^-11 of it, or 2^-25 of the largest (weight times scale
         of the value) where it is small (a row of zeros counts with the scale 2^-60, scales below 2^-100 as that: such a position may have all of the weight and be the
@@ -92,6 +92,8 @@ class Case:
             seen = j <= at
             if window:
                 seen &= j > at - window
+            if gone is not None and b == 0:
+                seen[:, gone] = False
             for h in range(heads):
                 c = h // group
                 x = q[self.first[b]:self.first[b] + n, h].double()

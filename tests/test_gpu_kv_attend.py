@@ -331,3 +331,103 @@ def test_a_block_of_a_served_model(ctx):
         assert torch.equal(getattr(case, t)[at, :, slot], getattr(steps, t)[at2, :, slot2])
     assert ((torch.cat([g[1] for g in got]).double() - want).abs() <= tol).all()
     assert torch.isfinite(torch.cat([g[2][0] for g in got])).all() and torch.isfinite(h).all() and torch.isfinite(n).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page", [1, 16, 17, 48, 64])
+@pytest.mark.parametrize("sizes", [[(1, 300), (1, 50)], [(100, 300), (20, 50)]])
+def test_only_the_positions_of_a_page_that_is_not_there_are_missed(sizes, page, dim):
+    with_status = Bd.ArmorContext(256, 256, 32, device=DEV)
+    case = Case(sizes, kv_heads=2, dim=dim, page=page, seed=2)
+    q = case.new(6, BF, size=2.0)
+    at = 70 // page
+    want, tol = case.attention(q, gone=slice(at * page, (at + 1) * page))
+    case.pages[0, at] = -1
+    got = with_status.kv_attend(case.cache, case.batch, q)
+    assert ((got.double() - want).abs() <= tol).all()
+    assert with_status.device_status()[11] > 0
+    with_status.close()
+
+
+@pytest.mark.parametrize("page", [1, 16, 17, 48, 64])
+@pytest.mark.parametrize("sizes", [[(1, 700), (1, 500)], [(100, 700), (20, 500)]])
+def test_pages_before_a_window_may_be_gone(ctx, sizes, page):
+    """(and count as none that is refused: the fixture looks)"""
+    case = Case(sizes, kv_heads=2, dim=64, page=page, seed=3)
+    q = case.new(6, BF, size=2.0)
+    window = 150
+    want = check(ctx, case, q, window=window)
+    for b, (n, length) in enumerate(sizes):
+        case.pages[b, :(length - n + 1 - window) // page] = -1
+    assert torch.equal(ctx.kv_attend(case.cache, case.batch, q, window=window), want)
+
+
+@pytest.mark.parametrize("chunk", [1, 40])
+def test_a_sequence_too_long_for_any_call_is_refused(chunk):
+    c = Bd.ArmorContext(256, 256, 32, device=DEV)
+    cache = c.new_kv_cache(1, 4096, 1, 64)
+    batch = Bd.KvBatch(torch.zeros(1, 2 ** 19, dtype=torch.int32, device=DEV), torch.tensor([2 ** 31 - 4095], dtype=torch.int32, device=DEV),
+                       torch.tensor([0, chunk], dtype=torch.int32, device=DEV))
+    k = torch.ones(chunk, 1, 64, dtype=BF, device=DEV)
+    c.kv_write(cache, batch, k, k)
+    assert (cache.k == 0).all() and (c.kv_read(cache, batch, chunk)[0] == 0).all()
+    out = torch.full_like(k, 4.0)
+    before = c.device_status()[11]
+    c.kv_attend(cache, batch, k, out=out)
+    assert (out == 4.0).all() and c.device_status()[11] > before
+    c.close()
+
+
+def test_a_hint_of_any_size(ctx):
+    case = Case([(5, 300), (1, 50)], kv_heads=2, dim=64, page=16, seed=4)
+    check(ctx, case, case.new(8, BF), max_chunk=2 ** 62)
+
+
+def test_binding_refuses(ctx):
+    case = Case([(2, 20)], kv_heads=2, dim=64, page=16)
+    cache, batch, q = case.cache, case.batch, case.new(4, BF)
+
+    def refused(match, f, *args, **kw):
+        with pytest.raises(ValueError, match=match):
+            f(*args, **kw)
+
+    k, s = torch.zeros(3, 2, 16, 64, dtype=torch.int8, device=DEV), torch.zeros(3, 2, 16, device=DEV)
+    for args, match in [((k.float(), k, s, s), "int8"), ((k, k, s, s.half()), "float32"), ((k[:2], k, s, s), r"\[2, 2, 16, 64\]"),
+                        ((k, k, s[:, :1], s), r"\[3, 2, 16\]"), ((k, k.transpose(1, 2).contiguous().transpose(1, 2), s, s), "alike"),
+                        ((k, k, s, s.transpose(1, 2).contiguous().transpose(1, 2)), "alike"), ((k[:0], k[:0], s[:0], s[:0]), "hold a page"),
+                        ((k, k.expand(3, 2, 16, 64)[..., ::1].cpu(), s, s), "CUDA"), ((k[:, :1].expand(3, 2, 16, 64),) * 2 + (s, s), "overlap")]:
+        refused(match, Bd.KvCache, *args)
+    wide = torch.zeros(3, 2, 16, 80 + 8, dtype=torch.int8, device=DEV)
+    refused("16-byte", Bd.KvCache, wide[..., :64], wide[..., :64], s, s)
+    refused("16-byte", Bd.KvCache, wide[..., 8:72], wide[..., 8:72], s, s)
+    refused("contiguous", Bd.KvCache, k.transpose(2, 3), k.transpose(2, 3), torch.zeros(3, 2, 64, device=DEV), torch.zeros(3, 2, 64, device=DEV))
+
+    pages, lengths, starts = case.pages, case.lengths, case.starts
+    for args, match in [((pages.long(), lengths, starts), "int32"), ((pages, lengths, starts[:1]), "2 starts"), ((pages, starts, starts), "1 lengths"),
+                        ((pages[0], lengths, starts), "2 dimensions"), ((pages, lengths, starts.cpu()), "CUDA"),
+                        ((pages.repeat(2, 1).T.contiguous().T, starts, torch.zeros(3, dtype=torch.int32, device=DEV)), "contiguous")]:
+        refused(match, Bd.KvBatch, *args)
+
+    refused("dtype", ctx.kv_attend, cache, batch, q.float(), out=q)
+    with pytest.raises(Bd.ArmorError):
+        ctx.kv_attend(cache, batch, q.float())
+    with pytest.raises(Bd.ArmorError):                      # heads that share no whole groups
+        ctx.kv_attend(cache, batch, case.new(3, BF))
+    for kw in ({"window": -1}, {"max_chunk": -1}, {"scale": -1.0}, {"scale": float("nan")}):
+        with pytest.raises(Bd.ArmorError):
+            ctx.kv_attend(cache, batch, q, **kw)
+    refused("rows, heads, 64", ctx.kv_attend, cache, batch, q[..., :32])
+    refused(r"\[2, 4, 64\]", ctx.kv_attend, cache, batch, q, out=q[:1])
+    refused("dtype", ctx.kv_attend, cache, batch, q, out=q.half())
+    refused("CUDA", ctx.kv_attend, cache, batch, q, out=q.cpu())
+    refused("CUDA", ctx.kv_attend, cache, batch, q.cpu())
+    new = case.new(2, BF)
+    refused("2, 64", ctx.kv_write, cache, batch, q, q)
+    refused("dtype", ctx.kv_write, cache, batch, new, new.half())
+    refused(r"\[2, 2, 64\]", ctx.kv_write, cache, batch, new, new[:1])
+    refused("2 rows", ctx.kv_read, cache, batch, 2, BF, out=(new[:1], new[:1]))
+    refused("float16", ctx.kv_read, cache, batch, 2, torch.float16, out=(new, new))
+    with pytest.raises((ValueError, Bd.ArmorError)):
+        ctx.kv_read(cache, batch, 2, torch.float64)
+    with pytest.raises((ValueError, Bd.ArmorError)):        # rows that overlap are not written
+        ctx.kv_read(cache, batch, 2, BF, out=(new[:1].expand(2, 2, 64), new))
