@@ -4,10 +4,12 @@
 // rounding).  Out: q s in fp32, rounded once to the output's type.  Both are bound by HBM: in, an element is read once and one byte
 // written; out, the reverse.  A warp has some tokens and some heads of each.  Its lanes look up the places of all its tokens at once, then
 // take the rows, dim / 8 lanes and eight elements each, so that a row's bytes go out whole and its maximum needs three or four
-// shuffles and no barrier; UNROLL rows of a lane are under way together.  With a search for every row, 8,188 tokens of 8
-// heads of 128 took 63 us in and out; so 31, in 18.4 (51 MB, 2.8 TB/s) and out 12.4 (4.1 TB/s).  What is left
-// of long calls: 16 sequences of 8,000 go in at 3.7 TB/s (issue slots half taken) and out at 4.5, reads and writes mixed; of short ones: the
-// chain of loads, from the table to the page to the row.
+// shuffles and no barrier; UNROLL rows of a lane are under way together (out: UNROLL_OUT; with four there 12.6 us for 10.8).
+//
+// With a search for every row, 8,188 tokens of 8 heads of 128 took 63 us in and out; so 29, in 18.2 (51 MB, 2.8 TB/s) and out 10.8
+// (4.7 TB/s).  What is left of long calls: 16 sequences of 8,000 go in at 3.7 TB/s (issue slots half taken; rows asked for ahead of the search,
+// fewer registers or more tokens a warp change 5 % either way) and out at 4.5, reads and writes mixed; of short ones: the chain of
+// loads, from the table to the page to the row.
 #include <algorithm>
 
 #include "kv_cache.cuh"
@@ -17,7 +19,7 @@ namespace {
 using namespace rows;
 using namespace kv;
 
-constexpr int THREADS = 128, UNROLL = 4, WARPS_RESIDENT = 32, MOST_TOKENS = 4;
+constexpr int THREADS = 128, UNROLL = 4, UNROLL_OUT = 2, WARPS_RESIDENT = 32, MOST_TOKENS = 4;
 
 struct Packed {                             // rows [n][heads][dim] of keys and of values
   const void *k, *v;
@@ -141,11 +143,11 @@ kv_read_kernel(const Cache c, const Batch b, const Packed y, const Split split, 
     const int64_t at = __shfl_sync(0xffffffffu, s.at, t), at_scale = __shfl_sync(0xffffffffu, s.scale, t);
     const int found = __shfl_sync(0xffffffffu, s.found, t);
     if (!found) continue;
-    for (int h = 0; h < s.heads; h += UNROLL * L::HEADS) {
-      uint2 q[UNROLL];
-      float scale[UNROLL];
+    for (int h = 0; h < s.heads; h += UNROLL_OUT * L::HEADS) {
+      uint2 q[UNROLL_OUT];
+      float scale[UNROLL_OUT];
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
+      for (int u = 0; u < UNROLL_OUT; ++u) {
         const int head = h + u * L::HEADS;
         q[u] = make_uint2(0u, 0u);
         scale[u] = 0.f;
@@ -155,7 +157,7 @@ kv_read_kernel(const Cache c, const Batch b, const Packed y, const Split split, 
         }
       }
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
+      for (int u = 0; u < UNROLL_OUT; ++u) {
         const int head = h + u * L::HEADS;
         if (head + lane.head >= s.heads) continue;
         // a byte in the last place of 2^23 + (byte + 128), less 2^23 + 128: the number, exactly, without the conversions' few units
@@ -237,7 +239,7 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
   // As many warps as the SMs hold: with few tokens some heads of one to a warp, with many several tokens and all heads, whose search and places are
   // paid for once.
   const int64_t heads = cache->kv_heads, items = 2 * g->n_rows * heads, resident = (int64_t)c->n_sm * WARPS_RESIDENT;
-  const int64_t batch_heads = UNROLL * 16 / (cache->head_dim / 8);        // heads under way at once
+  const int64_t batch_heads = (WHAT == READ ? UNROLL_OUT : UNROLL) * 16 / (cache->head_dim / 8);        // heads under way at once
   Split split;
   split.tokens = (int)std::min<int64_t>(MOST_TOKENS, std::max<int64_t>(1, g->n_rows / resident));
   const int64_t groups = std::min((heads + batch_heads - 1) / batch_heads, std::max<int64_t>(1, resident / g->n_rows));
