@@ -728,7 +728,9 @@ armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit
   p.status = c->status;
   p.counters = c->kv_counters;
   p.parts = c->T;
-  const int64_t rows = (a.max_chunk ? a.max_chunk : (a.b.rows + a.b.n - 1) / a.b.n) * a.group;
+  // rows a sequence: as expected, or on average; with a batch of which others have most rows, single tokens
+  int64_t rows = (a.max_chunk ? a.max_chunk : (a.b.rows + a.b.n - 1) / a.b.n) * a.group;
+  if (rows > limit) rows = a.group;
   KTimer kt(c, ARMOR_KC_FORWARD, 0.0, s);
   if (a.dtype == ARMOR_DTYPE_BF16) {
     if (a.dim == 64) launch_by_rows<__nv_bfloat16, 64>(c, p, rows, s);

@@ -308,8 +308,9 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   a.scale = g->scale * 1.4426950408889634f;
   a.aligned = aligned16(a.q, a.q_row, 2) && aligned16(a.o, a.o_row, 2) && a.q_head % 8 == 0 && a.o_head % 8 == 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  // Which kernels: the one for few rows a sequence reads keys and values once for every KV_FEW_ROWS of them, the other one once for 256.  Where
-  // the host cannot tell (lengths are on the device), both run, each on its sequences.
+  // Which kernels: the one for few rows a sequence reads keys and values once for every 16 of them, the other one once for 256, of which a few cost what all
+  // do.  (16 sequences of 4,003, 8 key heads: 25 rows each 73 us and 86, 40 rows 102 and 86; 64 of 8,000: 32 rows 432 and 489, 48 rows 644 and
+  // 499.)  Where the host cannot tell (lengths are on the device), both run, each on its sequences.
   const int64_t chunk = a.max_chunk ? a.max_chunk : (a.b.n == 1 ? g->n_rows : 0), rows = chunk * a.group;
   if (chunk ? rows <= KV_FEW_ROWS : g->n_rows <= batch->n_seqs && a.group <= KV_FEW_ROWS) st = launch_kv_attend_few(c, a, MOST, s);
   else if (a.b.n == 1 || a.group > KV_FEW_ROWS) st = launch_kv_attend_tile(c, a, 0, s);

@@ -114,4 +114,4 @@ struct KvAttend {
 armor_status launch_kv_attend_few(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s);
 // sequences of more
 armor_status launch_kv_attend_tile(armor_ctx* c, const KvAttend& a, int64_t limit, cudaStream_t s);
-constexpr int64_t KV_FEW_ROWS = 16;
+constexpr int64_t KV_FEW_ROWS = 32;

@@ -431,3 +431,12 @@ def test_binding_refuses(ctx):
         ctx.kv_read(cache, batch, 2, torch.float64)
     with pytest.raises((ValueError, Bd.ArmorError)):        # rows that overlap are not written
         ctx.kv_read(cache, batch, 2, BF, out=(new[:1].expand(2, 2, 64), new))
+
+
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 17), (128, 64)])
+@pytest.mark.parametrize("group,max_chunk", [(1, 0), (1, 33), (4, 0), (8, 0), (17, 0), (32, 1), (33, 0)])
+def test_rows_on_either_side_of_a_choice_of_kernels(ctx, group, max_chunk, dim, page):
+    case = Case([(n, 37 + 61 * n) for n in (1, 2, 4, 5, 8, 9, 15, 16, 17, 31, 32, 33)], kv_heads=2, dim=dim, page=page, seed=6)
+    check(ctx, case, case.new(2 * group, BF), max_chunk=max_chunk)
+    one = Case([(4, 300)], kv_heads=2, dim=dim, page=page, seed=7)
+    check(ctx, one, one.new(2 * group, BF), max_chunk=max_chunk)
