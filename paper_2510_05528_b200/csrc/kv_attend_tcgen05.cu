@@ -35,7 +35,8 @@ using namespace tc;
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
-constexpr int JOIN_ROWS = 16, JOIN_THREADS = 256;   // rows and threads of a CTA of the join (16 x 5 tokens: 128 threads 70.0 us, 256 67.7; 32 rows of 128 threads 77)
+constexpr int JOIN_ROWS = 16, JOIN_THREADS = 256, JOIN_PARTS = 4;   // rows and threads of a CTA of the join, parts under way (16 x 5 tokens: 128 threads 70 us,
+                                            // 256 68, 32 rows of 128 77; 64 tokens after 29,936: 16 CTAs a unit 68 us, 4 127; its maxima first 68, with the sums 64)
 constexpr int OVERHEAD = 5;                 // what a unit takes beside its blocks, in blocks: q in, O out, the first maximum (14,000 cycles)
 
 constexpr int NUMBERS = 8;                  // blocks whose positions' numbers are kept
@@ -883,18 +884,31 @@ kv_join_kernel(const TileP p) {
   const int r = blockIdx.y * JOIN_ROWS + threadIdx.x % JOIN_ROWS;
   if (r >= rows) return;
   auto part = [&](int k) { return p.parts + (2 * (int64_t)k + (k == c0)) * L::PART; };
-  float top = minus_inf();
-  for (int k = c0; k <= cut.last; ++k) top = fmaxf(top, part(k)[ROWS * DIM + r]);
   for (int d = threadIdx.x / JOIN_ROWS * 4; d < DIM; d += JOIN_THREADS / JOIN_ROWS * 4) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int k = c0; k <= cut.last; ++k) {
-      const float* const from = part(k);
-      const float m = from[ROWS * DIM + r], f = m == minus_inf() ? 0.f : exp2_fast(m - top);
-      const float4 v = *reinterpret_cast<const float4*>(from + d * ROWS + 4 * r);
-      sum = fmaf(f, from[ROWS * (DIM + 1) + r], sum);
-      o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+    float top = minus_inf(), sum = 0.f;
+    for (int k0 = c0; k0 <= cut.last; k0 += JOIN_PARTS) {
+      float m[JOIN_PARTS], l[JOIN_PARTS], to = top;
+      float4 v[JOIN_PARTS];
+#pragma unroll
+      for (int u = 0; u < JOIN_PARTS; ++u) {
+        const float* const from = part(min(k0 + u, cut.last));
+        m[u] = k0 + u <= cut.last ? from[ROWS * DIM + r] : minus_inf();
+        l[u] = from[ROWS * (DIM + 1) + r];
+        v[u] = *reinterpret_cast<const float4*>(from + d * ROWS + 4 * r);
+      }
+#pragma unroll
+      for (int u = 0; u < JOIN_PARTS; ++u) to = fmaxf(to, m[u]);
+      const float f0 = top == to ? 1.f : exp2_fast(top - to);             // (nothing yet: 2^-inf)
+      top = to;
+      sum *= f0;
+      o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+      for (int u = 0; u < JOIN_PARTS; ++u) {
+        const float f = m[u] == minus_inf() ? 0.f : exp2_fast(m[u] - top);
+        sum = fmaf(f, l[u], sum);
+        o.x = fmaf(f, v[u].x, o.x); o.y = fmaf(f, v[u].y, o.y); o.z = fmaf(f, v[u].z, o.z); o.w = fmaf(f, v[u].w, o.w);
+      }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int rr = cut.tile * ROWS + r, tok = rr / p.a.group, g = rr - tok * p.a.group;
