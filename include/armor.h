@@ -359,7 +359,8 @@ armor_status armor_kv_read(armor_ctx* ctx, const armor_kv_cache* cache, const ar
  * own keys and values are in the cache already (armor_kv_write).  q and o [n_rows][heads][head_dim], BF16 or F16, strides in elements, any alignment;
  * o must not overlap q.  Weights are rounded to fp16 on their way to the tensor cores, q's values, keys and values are exact; sums are fp32.
  * max_chunk: how many rows a sequence is expected to have at most (0: not known); a hint for the choice of the kernel, never of the
- * result's meaning.  Runs give the same bits.  Uses the context's workspace.  Errors as above; SHAPE also where kv_heads does not divide
+ * result's meaning.  Runs give the same bits.  Uses the context's workspace (that of 1024 x 1024 or more has room for all parts of long sequences; with
+ * less they are cut into fewer or none, which is slower).  Errors as above; SHAPE also where kv_heads does not divide
  * heads, INVALID_ARG for a negative or infinite scale, window or max_chunk. */
 typedef struct {
   const void* q;
