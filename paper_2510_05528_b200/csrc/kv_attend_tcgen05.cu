@@ -24,6 +24,7 @@
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
 // that no barrier is missed, and the status says that its output is worthless.
 #include "kv_cache.cuh"
+#include "kv_order.h"
 #include "tc_common.cuh"
 
 namespace {
@@ -32,7 +33,7 @@ using namespace rows;
 using namespace kv;
 using namespace tc;
 
-constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64, STAGES = 4;
+constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64;
 constexpr int SEQS = 1024;                  // sequences a launch
 constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr int JOIN_ROWS = 16, JOIN_THREADS = 256, JOIN_PARTS = 4;   // rows and threads of a CTA of the join, parts under way (16 x 5 tokens: 128 threads 70 us,
@@ -225,7 +226,7 @@ struct __align__(16) Segment {
   int low;                                  // the first position that a row of the tile sees
   int pad;
 };
-constexpr int RING = 4;
+constexpr int RING = UNIT_PLACES;
 
 // The CTA's share of the line, walked by one warp
 struct Walk {
@@ -312,7 +313,7 @@ kv_attend_tile_kernel(const TileP p) {
   using L = Tile<DIM>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  __shared__ __align__(8) uint64_t bars[31 + 2 * RING];
+  __shared__ __align__(8) uint64_t bars[32 + 2 * RING];
   __shared__ Segment ring[RING];
   __shared__ int64_t prefix[SEQS + 1];
   __shared__ unsigned tops[2][8];
@@ -322,13 +323,16 @@ kv_attend_tile_kernel(const TileP p) {
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bar0 = smem_u32(&bars[0]);
-  // of either half: q, S there and read, weights there and multiplied (two places); of the stages: keys, values
-  const uint32_t q_full = bar0, s_full = bar0 + 16, s_empty = bar0 + 32, p_full = bar0 + 48, o_done = bar0 + 80, k_full = bar0 + 112, k_empty = bar0 + 144,
-                 v_full = bar0 + 176, v_empty = bar0 + 208, t_full = bar0 + 240, r_full = bar0 + 248, r_empty = r_full + 8 * RING;
+  // q of the upper half (Q_PLACES) and of the lower; of either half: S there and read, weights there and multiplied (two places); of the stages: keys,
+  // values; the units
+  const uint32_t q_full = bar0, q1_full = q_full + 8 * Q_PLACES, s_full = bar0 + 24, s_empty = bar0 + 40, p_full = bar0 + 56, o_done = bar0 + 88,
+                 k_full = bar0 + 120, k_empty = bar0 + 152, v_full = bar0 + 184, v_empty = bar0 + 216, t_full = bar0 + 248, r_full = bar0 + 256,
+                 r_empty = r_full + 8 * RING;
   if (threadIdx.x == 0) {
     abort_flag = 0;
+    for (int i = 0; i < Q_PLACES; ++i) mbar_init(q_full + 8 * i, 4);
+    mbar_init(q1_full, 4);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(q_full + 8 * i, 4);
       mbar_init(s_full + 8 * i, 1);
       mbar_init(s_empty + 8 * i, 4);
     }
@@ -400,8 +404,9 @@ kv_attend_tile_kernel(const TileP p) {
   if (warp == 17 && lane == 0) p.cuts[blockIdx.x].last = -1;
   __syncthreads();
 
+  auto q_bar = [&](uint32_t n) { return q_full + 8 * ring_place(n, Q_PLACES); };      // of unit n
   // the n-th segment of the share, by a whole warp: false behind the last one.  done: the ring may have its place back
-  auto segment = [&](uint32_t n) { return wait_warp(r_full + 8 * (n % RING), (n / RING) & 1, abortp, p.status) && ring[n % RING].count > 0; };
+  auto segment = [&](uint32_t n) { return wait_warp(r_full + 8 * ring_place(n, RING), ring_parity(n, RING), abortp, p.status) && ring[n % RING].count > 0; };
   auto arrive = [&](uint32_t bar) {                                     // of a warp
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
@@ -472,7 +477,7 @@ kv_attend_tile_kernel(const TileP p) {
             put16(row_at<DIM>(rows_at, (warp & 3) * 32 + i * (32 / LANES) + sub_row, c8), make_uint4(w[0], w[1], w[2], w[3]));
           }
           fence_proxy_async();
-          arrive(q_full + 8 * half);
+          arrive(half ? q1_full : q_bar(seg));
         }
       }
       if (rows <= 0) { blocks += at.count; done(seg); continue; }
@@ -742,7 +747,7 @@ kv_attend_tile_kernel(const TileP p) {
         put16(line + (((x + 1 - swap) ^ k) << 4), swap ? lo : hi);
       }
     };
-    uint32_t of = 0, ahead = 0, waited = 0;                             // segments: of the loaded block, of the one that is looked up; q's that have been waited for
+    uint32_t of = 0, ahead = 0;                                         // segments: of the loaded block, of the one that is looked up
     uint32_t n = ((uint32_t)(warp >> 1) & 1) - 2;                       // the loaded block (none yet)
     bool one = false;                                                   // there is a loaded block
     auto steps = [&](int times) {
@@ -756,8 +761,7 @@ kv_attend_tile_kernel(const TileP p) {
     for (;; n += 2) {
      if (one) {
       const uint32_t st = n % STAGES;
-      if (!values)                                                      // (the factor; phase by phase)
-        for (; waited <= of; ++waited) wait_warp(q_full, waited & 1, abortp, p.status);
+      if (!values) wait_warp(q_bar(of), ring_parity(of, Q_PLACES), abortp, p.status);        // (the factor)
       wait_warp(empty + 8 * st, ((n / STAGES) & 1) ^ 1, abortp, p.status);
       if (!values) {
         // The numbers of block n - NUMBERS have been read: the keys of block n - STAGES have been multiplied, and those only when the scores of
@@ -809,8 +813,8 @@ kv_attend_tile_kernel(const TileP p) {
       for (; segment(seg); ++seg) {
         const int count = ring[seg % RING].count, halves = ring[seg % RING].rows > HALF ? 2 : 1;
         done(seg);
-        wait(q_full, seg & 1);
-        if (halves == 2) wait(q_full + 8, seg1++ & 1);
+        wait(q_bar(seg), ring_parity(seg, Q_PLACES));
+        if (halves == 2) wait(q1_full, seg1++ & 1);
         for (int i = -1; i < count; ++i) {
           // the scores of block i + 1, once those of block i have been read; then the values of block i
           const uint32_t next = n + (i < 0 ? 0 : 1), st2 = next % STAGES, st = n % STAGES;
@@ -843,7 +847,7 @@ kv_attend_tile_kernel(const TileP p) {
       Walk at(p, prefix);
       at.start(begin, end, at_seq);
       for (uint32_t n = 0;; ++n) {
-        wait_warp(r_empty + 8 * (n % RING), ((n / RING) & 1) ^ 1, abortp, p.status);
+        wait_warp(r_empty + 8 * ring_place(n, RING), ring_parity(n, RING) ^ 1, abortp, p.status);
         const bool cut = at.more() && at.count < at.total;
         if (lane == 0) {
           Segment g{};
