@@ -73,3 +73,59 @@ def test_prompts_far_apart(ctx):
     case = Case(sizes, kv_heads=16, dim=64, page=16, seed=4)
     check(ctx, case, case.new(16, BF, size=2.0))
     check(ctx, case, case.new(32, HF, size=2.0))
+
+
+# ---- many units, many blocks
+def mixed(n):
+    """Units of one block and of several, tiles of a half and of both, one behind the other."""
+    return [((33, 33), (64, 64), (65, 300), (40, 41), (128, 200), (129, 129), (300, 300), (257, 500), (34, 64))[i % 9] for i in range(n)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim,page,layout", [(64, 16, "heads"), (128, 17, "slots"), (128, 64, "heads")])
+@pytest.mark.parametrize("sizes,kv_heads,group,window,least", [
+    ([(9 + i % 56, 9 + i % 56) for i in range(120)], 8, 4, 0, (6, 6)),           # one block each
+    (mixed(108), 8, 1, 0, (6, 17)),
+    (mixed(54), 4, 5, 0, (6, 17)),
+    ([(1400, 2500), (1200, 1200), (1800, 2200)], 16, 2, 256, (6, 17)),               # a window
+    (mixed(72), 8, 2, 70, (6, 17)),
+])
+def test_many_units_a_cta(ctx, sizes, kv_heads, group, window, least, dim, page, layout, dtype):
+    got = most(sizes, kv_heads, group, window=window, n_ctas=sms())
+    assert got[0] >= least[0] and got[1] >= least[1], got
+    case = Case(sizes, kv_heads=kv_heads, dim=dim, page=page, layout=layout, seed=2)
+    check(ctx, case, case.new(kv_heads * group, dtype, size=2.0), window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("sizes,kv_heads,group,least", [
+    ([(1700, 1700)], 8, 8, (6, 40)),                      # a whole prompt
+    ([(300, 30000), (40, 60000)], 4, 4, (2, 90)),         # long pieces of cut units
+    ([(256, 12000)] * 5, 32, 1, (2, 150)),
+])
+def test_many_blocks_a_cta(ctx, sizes, kv_heads, group, least, dtype):
+    got = most(sizes, kv_heads, group, n_ctas=sms())
+    assert got[0] >= least[0] and got[1] >= least[1], got
+    case = Case(sizes, kv_heads=kv_heads, dim=128, page=64, seed=3)
+    check(ctx, case, case.new(kv_heads * group, dtype, size=2.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_units_where_there_is_no_room_for_parts(dim, dtype):
+    sizes = mixed(90)
+    assert most(sizes, 8, 1, n_ctas=sms(), whole=True)[0] >= 5
+    small = Bd.ArmorContext(64, 64, 32, device=DEV, h_mode=Bd.H_DIAG)
+    case = Case(sizes, kv_heads=8, dim=dim, page=16, seed=6)
+    check(small, case, case.new(8, dtype, size=2.0))
+    small.close()
+
+
+@pytest.mark.parametrize("sizes,kv_heads,group", [(mixed(108), 8, 1), ([(16, 16)] * 100, 8, 4), ([(1700, 1700)], 8, 8)])
+def test_runs_give_the_same_bits(ctx, sizes, kv_heads, group):
+    case = Case(sizes, kv_heads=kv_heads, dim=128, page=32, seed=8)
+    for dtype in (BF, HF):
+        q = case.new(kv_heads * group, dtype, size=2.0)
+        first = ctx.kv_attend(case.cache, case.batch, q)
+        for _ in range(10):
+            assert torch.equal(ctx.kv_attend(case.cache, case.batch, q), first)
