@@ -322,8 +322,9 @@ armor_status armor_block_norm_backward(armor_ctx* ctx, const armor_block_norm_gr
  * values; any order of pages, heads and slots.
  * A batch of n_seqs sequences (device, int32): rows starts[b] .. starts[b + 1] - 1 of the packed arrays (n_b of them; starts rise) stand for the
  * last n_b of the lengths[b] positions of sequence b: its row i has position p = lengths[b] - n_b + i, which lies in slot p % page_size
- * of page pages[b * ld_pages + p / page_size].  Positions below zero are padding.  Rows from starts[n_seqs] on belong to no sequence and
- * are left as they are.  Nothing of a batch is read on the host: a captured call follows what the arrays hold when it is replayed.
+ * of page pages[b * ld_pages + p / page_size].  Positions below zero are padding.  Rows before starts[0] and from starts[n_seqs] on
+ * belong to no sequence and are left as they are by every call (so a batch may be some of another's sequences: its arrays from one of them on).
+ * Nothing of a batch is read on the host: a captured call follows what the arrays hold when it is replayed.
  * A page out of [0, n_pages), a sequence whose rows are out of range and one longer than its max_pages hold or 2^31 - 4096 are counted in
  * device status word 11 and neither read nor written: positions on such a page are not there, the rows of such a sequence are left as
  * they are (by armor_kv_read: zeros).  Pages that nothing of a call reads (those before all windows) may be out of range.  n_rows (of the

@@ -1031,8 +1031,8 @@ class ArmorContext:
 
     def kv_read(self, cache: KvCache, batch: KvBatch, rows: int, dtype: torch.dtype = torch.bfloat16, *,
                 out: tuple[torch.Tensor, torch.Tensor] | None = None) -> tuple[torch.Tensor, torch.Tensor]:
-        """(k, v) [rows, kv_heads, head_dim] of the batch's positions as the cache holds them.  Rows behind the last sequence are left as
-        they are (in new tensors: not set)."""
+        """(k, v) [rows, kv_heads, head_dim] of the batch's positions as the cache holds them.  Rows before the first sequence's
+        and behind the last one's are left as they are (in new tensors: not set)."""
         here = self._current()
         if out is None:
             # one allocation for both
@@ -1054,7 +1054,7 @@ class ArmorContext:
         """Attention of q [rows, heads, head_dim] (bf16 or fp16) over the cache, each row over the positions of its sequence up to its own, the
         last `window` of them if that is not 0; scale: head_dim ** -0.5.  The new rows' keys and values have been written.  Heads
         share keys in groups of heads / kv_heads.  max_chunk: the most rows of a sequence, where the caller knows it (a hint).  Rows
-        behind the last sequence are left as they are (in a new tensor: not set)."""
+        before the first sequence's and behind the last one's are left as they are (in a new tensor: not set)."""
         return _kv_attend(self.ctx, self._current(), cache, batch, q, out, cache.head_dim ** -0.5 if scale is None else scale, window, max_chunk)
 
     def device_status(self) -> list[int]:

@@ -127,7 +127,7 @@ kv_write_kernel(const Cache c, const Batch b, const Packed x, const Split split,
   }
 }
 
-// (positions that have no page, and padding, read as zeros; rows behind the last sequence are left as they are)
+// (positions that have no page, and padding, read as zeros; rows of no sequence are left as they are)
 template <typename T, int DIM, bool ALIGNED>
 __global__ void __launch_bounds__(THREADS)
 kv_read_kernel(const Cache c, const Batch b, const Packed y, const Split split, int32_t* status) {

@@ -56,7 +56,8 @@ __device__ __forceinline__ void report(int32_t* status) {
   status[ST_LAST_ERR] = ARMOR_ERR_INVALID_ARG;
 }
 
-// The sequence of row t, by a whole warp (t may differ between lanes): 32 offsets are compared at a time.  -1: behind the last one.
+// The sequence of row t, by a whole warp (t may differ between lanes): 32 offsets are compared at a time.  -1: before the first
+// one's rows or behind the last one's.
 __device__ __forceinline__ int sequence_of(const Batch& b, int64_t t) {
   const int lane = threadIdx.x & 31;
   int mine = -2;
@@ -75,8 +76,8 @@ __device__ __forceinline__ int sequence_of(const Batch& b, int64_t t) {
       if (step == 1) break;
       hi = min(hi, lo + step - 1);
     }
-    const int found = lo < b.n ? lo : -1;
-    const int64_t first = found < 0 ? 0 : b.starts[found], last = found < 0 ? 0 : b.starts[found + 1];
+    const int64_t first = lo < b.n ? b.starts[lo] : 0, last = lo < b.n ? b.starts[lo + 1] : 0;
+    const int found = lo < b.n && (lo > 0 || row >= first) ? lo : -1;
     if (mine == -2 && (t == row || (found >= 0 && t >= first && t < last))) mine = found;
   }
 }
