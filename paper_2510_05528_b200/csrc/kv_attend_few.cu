@@ -4,8 +4,8 @@
 // scales, for a row of position p:
 //   t_j = (q . kq_j) ks_j scale log2 e + log2 vs_j     over j <= p (and j > p - window)
 //   w_j = 2^(t_j - m),  O = sum w_j vq_j,  l = sum w_j / vs_j,  o = O / l
-// m is a maximum of the t_j seen so far, so that w_j, the weight a value's bytes are taken with, is a factor of at most 2^LAZY and its rounding to
-// fp16 is one of 2^-11 of what the value contributes (a weight below 2^-14 of the largest loses bits, 2^-25 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
+// m is a maximum of the t_j seen so far, less RAISED, so that w_j, the weight a value's bytes are taken with, is at most 2^15 and its rounding to
+// fp16 is one of 2^-11 of what the value contributes (a weight below 2^-21 of the largest loses bits, 2^-32 of the largest at most).  The bytes themselves are exact in fp16, and so are q's 16-bit numbers after
 // a multiplication by a power of two; products and sums are fp32.  l is summed from the unrounded weights.  No row: zeros.
 //
 // Bound by HBM: 2 (dim + 4) bytes a position and key head.  Each warp takes 16 positions at a time, twice, in the layout that mma.sync m16n8k16 wants of its
@@ -32,7 +32,6 @@ constexpr int WARPS = 6, THREADS = 32 * WARPS, STEP = 32 * WARPS;      // positi
 constexpr int STAGES = 2;                   // of 32 positions a warp
 constexpr int OVERHEAD = 2;                 // what a unit takes beside its steps, in steps: its sequence, q, the first copies, the warps' sums
 constexpr int SEQS = 1024;                  // sequences a launch
-constexpr float LAZY = 8.f;                 // the maximum moves when it is exceeded by this much (log2)
 
 template <int DIM, int NT>
 struct Few {
@@ -439,7 +438,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           for (int e = 0; e < 2; ++e) {
             const float vs = measure(scales[32 + 16 * g + quad + 8 * e]);
             const float ka = scales[16 * g + quad + 8 * e] * factor, kb = __log2f(vs);
-            kr[g][e] = __fdividef(1.f, vs);
+            kr[g][e] = __fdividef(LOWERED, vs);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -470,7 +469,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          top[n][e] = fmaxf(fmaxf(t[0][n][e], t[0][n][e + 2]), fmaxf(t[1][n][e], t[1][n][e + 2]));
+          top[n][e] = fmaxf(fmaxf(t[0][n][e], t[0][n][e + 2]), fmaxf(t[1][n][e], t[1][n][e + 2])) - RAISED;
           over |= top[n][e] > m[n][e] + LAZY;
         }
       if (__any_sync(0xffffffffu, over)) {
@@ -560,7 +559,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     float* const parts = p.parts;
     const int64_t part_at = 2 * (int64_t)blockIdx.x + (first == 0 ? 1 : 0);
     auto put = [&](int r, int d, float4 o, float l) {     // four dimensions of a row of the output
-      const float inv = l == 0.f ? 0.f : 1.f / l;         // (a row that sees nothing: zeros)
+      const float inv = l == 0.f ? 0.f : LOWERED / l;     // (a row that sees nothing: zeros)
       const int rr = tile * R + r, i = rr / p.a.group, g = rr - i * p.a.group;
       T* const to = static_cast<T*>(p.a.o) + (int64_t)(s.first + i) * p.a.o_row + (int64_t)(head * p.a.group + g) * p.a.o_head + d;
       if (p.a.aligned) {

@@ -35,7 +35,6 @@ using namespace tc;
 
 constexpr int THREADS = 640, HALF = 128, ROWS = 2 * HALF, KEYS = 64;
 constexpr int SEQS = 1024;                  // sequences a launch
-constexpr float LAZY = 8.f;                 // as in kv_attend_few.cu
 constexpr int JOIN_ROWS = 16, JOIN_THREADS = 256, JOIN_PARTS = 4;   // rows and threads of a CTA of the join, parts under way (16 x 5 tokens: 128 threads 70 us,
                                             // 256 68, 32 rows of 128 77; 64 tokens after 29,936: 16 CTAs a unit 68 us, 4 127; its maxima first 68, with the sums 64)
 constexpr int OVERHEAD = 5;                 // what a unit takes beside its blocks, in blocks: q in, O out, the first maximum (14,000 cycles)
@@ -555,6 +554,7 @@ kv_attend_tile_kernel(const TileP p) {
           top[k] = fmaxf(v.x, v.y);
 #pragma unroll
           for (int g = 1; g < 8; ++g) { const float2 v = f2_get(t[k][g]); top[k] = max3(top[k], v.x, v.y); }
+          top[k] -= RAISED;
         }
         // m hardly ever moves behind a row's first blocks
         if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
@@ -640,7 +640,7 @@ kv_attend_tile_kernel(const TileP p) {
         }
       } else {
         // by way of q's place, so that rows go out whole
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;                 // (a row that sees nothing: zeros)
+        const float inv = sum == 0.f ? 0.f : LOWERED / sum;             // (a row that sees nothing: zeros)
         const T* const t = nullptr;
 #pragma unroll 1
         for (int k = 0; k < DIM / 32; ++k) {
@@ -768,7 +768,7 @@ kv_attend_tile_kernel(const TileP p) {
         // block n - STAGES - 1 had been read, behind the weights of the one before
         const uint32_t at = smem + L::C0 + (n % NUMBERS) * L::CONSTS, k = w * 32 + lane, to = at + (k >> 1) * 16 + (k & 1) * 4;
         const float v = measure(vs);
-        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(1.f, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
+        const float fa = there ? ks * *(volatile float*)&factors[of & 1] : 0.f, fb = there ? __log2f(v) : minus_inf(), fr = !there ? 0.f : (v == v ? __fdividef(LOWERED, v) : 1.f);    // (no number: the weight is none either, and 0 where it is not seen)
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(fa) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 8), "f"(fb) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * KEYS + 4 * k), "f"(fr) : "memory");
@@ -914,7 +914,7 @@ kv_join_kernel(const TileP p) {
         o.x = fmaf(f, v[u].x, o.x); o.y = fmaf(f, v[u].y, o.y); o.z = fmaf(f, v[u].z, o.z); o.w = fmaf(f, v[u].w, o.w);
       }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sum == 0.f ? 0.f : LOWERED / sum;
     const int rr = cut.tile * ROWS + r, tok = rr / p.a.group, g = rr - tok * p.a.group;
     T* const to = static_cast<T*>(p.a.o) + (int64_t)(s.first + tok) * p.a.o_row + (int64_t)(cut.head * p.a.group + g) * p.a.o_head + d;
     const T* const t = nullptr;

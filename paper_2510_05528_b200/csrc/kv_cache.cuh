@@ -96,6 +96,14 @@ __device__ __forceinline__ bool place(const Cache& c, const Batch& b, int at, ui
 // are below 1e-28).  A scale that is no number stays what it is.
 __device__ __forceinline__ float measure(float sv) { return sv == 0.f ? 8.6736174e-19f : (sv < 7.8886091e-31f ? 7.8886091e-31f : sv); }
 
+// A row's weights are 2^(t - m), m its largest t so far less RAISED, and they are rounded to fp16.  So the largest is 2^RAISED, or 2^(RAISED + LAZY) = 2^15
+// before m moves, and one is off by half of fp16's smallest step, 2^-25 or 2^-32 of the largest, at most where it is small.  (With RAISED 0 weights below
+// 2^-25 of the largest were zeros in O, but not in l: with one position far above 131,071 others, 2^-9 of the output was missing.)  l takes the
+// weights unrounded, in fp32, and without the 2^RAISED, which rides on the inverse scales and comes out of O with 1 / l: 2^15 of scales of 2^-100
+// over all positions would come near the end of fp32's range.
+constexpr float RAISED = 7.f, LOWERED = 0.0078125f;   // 2^-RAISED
+constexpr float LAZY = 8.f;                 // m moves when it is exceeded by this much (log2)
+
 }  // namespace kv
 
 // kv_attend_few.cu, kv_attend_tcgen05.cu
