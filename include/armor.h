@@ -343,8 +343,9 @@ typedef struct {
 /* Packed rows [n_rows][kv_heads][head_dim] of keys and values (dtype F32, BF16, F16), strides in elements, any alignment of
  * their rows.  armor_kv_write rounds them into the cache; two rows of one call must not have the same place (pages that sequences share are
  * complete, or each is written by one).  armor_kv_read writes what the cache holds, rounded once from fp32 (rows of padding, and
- * those refused: zeros).  Errors: INVALID_ARG (missing arrays, negative counts), SHAPE (sizes, strides, alignment), UNSUPPORTED (dtype, head_dim),
- * TOO_LARGE (2^31 pages, slots, rows; rows times heads of a group above 2^31 - 4096). */
+ * those refused: zeros).  Errors: INVALID_ARG (missing arrays, negative counts), SHAPE (sizes, strides, arrays that are not on their elements'
+ * boundaries), UNSUPPORTED (dtype, head_dim), TOO_LARGE (2^31 pages, slots, sequences, rows; kv_heads above 65,535; rows times heads of a
+ * group above 2^31 - 4096). */
 typedef struct {
   const void *k, *v;                       /* written to by armor_kv_read */
   int64_t n_rows;
@@ -361,11 +362,11 @@ armor_status armor_kv_read(armor_ctx* ctx, const armor_kv_cache* cache, const ar
  * o must not overlap q.  A weight is rounded to fp16 on its way to the values: by 2^-11 of it, or by 2^-32 of the row's largest contribution (weight
  * times the value's scale, times 127) where it is small, so that over n positions up to n times that may be missing; their sum takes them
  * unrounded.  Exponentials, logarithms and quotients are good to 2^-22; keys, values and q are exact (of a bf16 q what is below 2^-39
- * of the largest near it is lost); sums are fp32.
+ * of the largest near it is lost; scales of values between 0 and 2^-100 count as 2^-100); sums are fp32.
  * max_chunk: how many rows a sequence is expected to have at most (0: not known); a hint for the choice of the kernel, never of the
  * result's meaning.  Runs give the same bits.  Uses the context's workspace (that of 1024 x 1024 or more has room for all parts of long sequences; with
  * less they are cut into fewer or none, which is slower).  Errors as above; SHAPE also where kv_heads does not divide
- * heads, INVALID_ARG for a negative or infinite scale, window or max_chunk. */
+ * heads, INVALID_ARG for a negative window or max_chunk and a scale that is negative, no number or above 1e30. */
 typedef struct {
   const void* q;
   void* o;

@@ -180,6 +180,9 @@ armor_status by_row_type(int32_t dtype, F&& f) {
 
 constexpr int64_t MOST = 0x7fffffff, MOST_POSITIONS = MOST + 1 - 4096;      // (a step that begins in a sequence ends below 2^31)
 
+template <typename... P>
+bool on_boundary(size_t bytes, P... p) { return ((reinterpret_cast<uintptr_t>(p) % bytes == 0) && ...); }
+
 armor_status check_cache(const armor_kv_cache* g) {
   if (!g) return ARMOR_ERR_INVALID_ARG;
   if (g->n_pages < 1 || g->page_size < 1 || g->kv_heads < 1 || g->head_dim < 1) return ARMOR_ERR_SHAPE;
@@ -188,7 +191,7 @@ armor_status check_cache(const armor_kv_cache* g) {
   if (g->slot_stride < g->head_dim || g->page_stride < g->head_dim || g->head_stride < g->head_dim || g->scale_page_stride < 1 ||
       g->scale_head_stride < 1 || g->scale_slot_stride < 1)
     return ARMOR_ERR_SHAPE;
-  if (g->page_stride % 16 || g->head_stride % 16 || g->slot_stride % 16 || reinterpret_cast<uintptr_t>(g->k) % 16 || reinterpret_cast<uintptr_t>(g->v) % 16)
+  if (g->page_stride % 16 || g->head_stride % 16 || g->slot_stride % 16 || !on_boundary(16, g->k, g->v) || !on_boundary(4, g->k_scale, g->v_scale))
     return ARMOR_ERR_SHAPE;
   return g->k && g->v && g->k_scale && g->v_scale ? ARMOR_OK : ARMOR_ERR_INVALID_ARG;
 }
@@ -196,8 +199,9 @@ armor_status check_batch(const armor_kv_batch* g, int64_t rows) {
   if (!g || g->n_seqs < 0 || rows < 0) return ARMOR_ERR_INVALID_ARG;
   if (g->max_pages < 0 || g->ld_pages < g->max_pages) return ARMOR_ERR_SHAPE;
   if (g->n_seqs > MOST || g->max_pages > MOST || rows > MOST) return ARMOR_ERR_TOO_LARGE;
-  if (g->n_seqs > 0 && rows > 0 && (!g->lengths || !g->starts || (g->max_pages > 0 && !g->pages))) return ARMOR_ERR_INVALID_ARG;
-  return ARMOR_OK;
+  if (g->n_seqs == 0 || rows == 0) return ARMOR_OK;       // (nothing is read)
+  if (!g->lengths || !g->starts || (g->max_pages > 0 && !g->pages)) return ARMOR_ERR_INVALID_ARG;
+  return on_boundary(4, g->lengths, g->starts, g->pages) ? ARMOR_OK : ARMOR_ERR_SHAPE;
 }
 Cache view(const armor_kv_cache* g) {
   Cache c;
@@ -225,6 +229,7 @@ armor_status move_rows(armor_ctx* c, const armor_kv_cache* cache, const armor_kv
   if ((st = check_batch(batch, g->n_rows)) != ARMOR_OK) return st;
   const int es = rows_dtype_bytes(g->dtype);
   if (!es) return ARMOR_ERR_UNSUPPORTED;
+  if (g->n_rows > 0 && batch->n_seqs > 0 && !on_boundary(es, g->k, g->v)) return ARMOR_ERR_SHAPE;
   // (what is written must not overlap; what is read may: heads may share a row)
   const int64_t least = WHAT == READ ? cache->head_dim : 0;
   if (g->k_row_stride < least || g->k_head_stride < least || g->v_row_stride < least || g->v_head_stride < least) return ARMOR_ERR_SHAPE;
@@ -293,11 +298,11 @@ extern "C" armor_status armor_kv_attend(armor_ctx* c, const armor_kv_cache* cach
   if (g->heads < 1 || g->heads % cache->kv_heads) return ARMOR_ERR_SHAPE;
   if (g->q_row_stride < 0 || g->q_head_stride < 0 || g->o_row_stride < cache->head_dim || g->o_head_stride < cache->head_dim) return ARMOR_ERR_SHAPE;
   if (g->window < 0 || g->max_chunk < 0 || !(g->scale >= 0.f) || g->scale > 1e30f) return ARMOR_ERR_INVALID_ARG;
+  if (g->n_rows > 0 && batch->n_seqs > 0 && !on_boundary(2, g->q, g->o)) return ARMOR_ERR_SHAPE;
   if (g->n_rows > 0 && g->heads / cache->kv_heads > MOST_POSITIONS / g->n_rows) return ARMOR_ERR_TOO_LARGE;
   if (!c) return ARMOR_ERR_INVALID_ARG;
   if (g->n_rows == 0 || batch->n_seqs == 0) return ARMOR_OK;
   if (!g->q || !g->o) return ARMOR_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(g->q) % 2 || reinterpret_cast<uintptr_t>(g->o) % 2) return ARMOR_ERR_SHAPE;
   KvAttend a;
   a.c = view(cache);
   a.b = view(batch, cache, g->n_rows);
