@@ -24,7 +24,6 @@
 // workspace, and kv_join_kernel adds them in their order.  Every wait is bounded; a CTA whose wait ran out goes on without waiting, so
 // that no barrier is missed, and the status says that its output is worthless.
 #include "kv_cache.cuh"
-#include "kv_order.h"
 #include "tc_common.cuh"
 
 namespace {

@@ -2,6 +2,7 @@
 // packed arrays are whose.  Nothing that a table or an offset holds is trusted: what it names outside of the arrays is neither read nor
 // written, and raises a status word.
 #pragma once
+#include "kv_order.h"
 #include "rows_io.cuh"
 
 namespace kv {
@@ -22,16 +23,6 @@ struct Batch {
   int64_t rows;                             // rows of the packed arrays
   int64_t capacity;                         // positions that a table holds
 };
-
-// (the rounded-up reciprocal: with 2^(s-1) < d <= 2^s, m = ceil(2^(31+s) / d) is at most 2^32 - 1 for d > 1 and
-// exceeds 2^(31+s) / d by less than one, so that p m >> (31 + s) is p / d for all p < 2^31; d = 1: m = 2^31, s = 0)
-inline void divisor(uint32_t d, uint32_t& mul, int& shift) {
-  int s = 0;
-  while ((1ull << s) < d) ++s;
-  mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
-  shift = 31 + s;
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t p, uint32_t mul, int shift) { return (uint32_t)(((uint64_t)p * mul) >> shift); }
 
 // a / b of numbers that are not negative: in 32 bits where they fit (a 64-bit division is a hundred instructions or so, and a call of 10 us has ten of them
 // one behind the other)
