@@ -362,7 +362,8 @@ armor_status armor_kv_read(armor_ctx* ctx, const armor_kv_cache* cache, const ar
  * o must not overlap q.  A weight is rounded to fp16 on its way to the values: by 2^-11 of it, or by 2^-32 of the row's largest contribution (weight
  * times the value's scale, times 127) where it is small, so that over n positions up to n times that may be missing; their sum takes them
  * unrounded.  Exponentials, logarithms and quotients are good to 2^-22; keys, values and q are exact (of a bf16 q what is below 2^-39
- * of the largest near it is lost; scales of values between 0 and 2^-100 count as 2^-100); sums are fp32.
+ * of the largest near it is lost; scales of values between 0 and 2^-100 count as 2^-100, and 0 as
+ * 2^-60, which is right where the row is zeros); sums are fp32.
  * max_chunk: how many rows a sequence is expected to have at most (0: not known); a hint for the choice of the kernel, never of the
  * result's meaning.  Runs give the same bits.  Uses the context's workspace (that of 1024 x 1024 or more has room for all parts of long sequences; with
  * less they are cut into fewer or none, which is slower).  Errors as above; SHAPE also where kv_heads does not divide

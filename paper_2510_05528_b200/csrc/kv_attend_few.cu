@@ -469,8 +469,8 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          top[n][e] = fmaxf(fmaxf(t[0][n][e], t[0][n][e + 2]), fmaxf(t[1][n][e], t[1][n][e + 2])) - RAISED;
-          over |= top[n][e] > m[n][e] + LAZY;
+          top[n][e] = fmaxf(fmaxf(t[0][n][e], t[0][n][e + 2]), fmaxf(t[1][n][e], t[1][n][e + 2]));
+          over |= top[n][e] > m[n][e] + (LAZY + RAISED);
         }
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -480,7 +480,7 @@ kv_attend_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], o));
-            const float to = fmaxf(m[n][e], top[n][e]);
+            const float to = fmaxf(m[n][e], top[n][e] - RAISED);
             f[e] = m[n][e] == to ? 1.f : exp2_fast(m[n][e] - to);       // (nothing yet: 2^-inf)
             m[n][e] = to;
             l[n][e] *= f[e];

@@ -553,16 +553,16 @@ kv_attend_tile_kernel(const TileP p) {
           top[k] = fmaxf(v.x, v.y);
 #pragma unroll
           for (int g = 1; g < 8; ++g) { const float2 v = f2_get(t[k][g]); top[k] = max3(top[k], v.x, v.y); }
-          top[k] -= RAISED;
         }
         // m hardly ever moves behind a row's first blocks
-        if (__any_sync(0xffffffffu, top[0] > m[0] + LAZY || top[1] > m[1] + LAZY || top[2] > m[2] + LAZY || top[3] > m[3] + LAZY)) {
+        constexpr float OVER = LAZY + RAISED;
+        if (__any_sync(0xffffffffu, top[0] > m[0] + OVER || top[1] > m[1] + OVER || top[2] > m[2] + OVER || top[3] > m[3] + OVER)) {
           float f[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
             top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
-            const float to = fmaxf(m[k], top[k]);
+            const float to = fmaxf(m[k], top[k] - RAISED);
             f[k] = m[k] == to ? 1.f : exp2_fast(m[k] - to);
             l[k] = f2_mul(l[k], f2(f[k]));
             m[k] = to;

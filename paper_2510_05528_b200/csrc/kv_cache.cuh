@@ -93,7 +93,7 @@ __device__ __forceinline__ float measure(float sv) { return sv == 0.f ? 8.673617
 // weights unrounded, in fp32, and without the 2^RAISED, which rides on the inverse scales and comes out of O with 1 / l: 2^15 of scales of 2^-100
 // over all positions would come near the end of fp32's range.
 constexpr float RAISED = 7.f, LOWERED = 0.0078125f;   // 2^-RAISED
-constexpr float LAZY = 8.f;                 // m moves when it is exceeded by this much (log2)
+constexpr float LAZY = 8.f;                 // m moves when the largest t is above m + RAISED by this much (log2)
 
 }  // namespace kv
 
