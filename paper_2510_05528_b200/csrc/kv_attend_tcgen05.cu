@@ -9,7 +9,7 @@
 //                    the block's columns in four rows, not a row (a lane a row reads all positions' numbers: 96 reads of 16 bytes a
 //                    warp for 128 positions, each of them 512 bytes into registers, and those took 11,000 cycles; now 64 take 2,900)
 //   warps 8-11     : keys from their pages through registers to fp16 in shared memory, four blocks, and the three numbers of a
-//                    position (ks factor, log2 vs, 1 / vs)
+//                    position (ks factor, log2 vs, 2^-RAISED / vs)
 //   warps 12-15    : values likewise
 //   warp 16        : the products: Q K^T (both from shared memory), W V (W from tensor memory, V as it lies, contiguous along the dimensions)
 //   warp 17        : finds the units of the CTA's share, a few ahead of the others
@@ -17,7 +17,8 @@
 // block's scores are formed behind this one's exponentials.
 //
 // Bound by the products' operands: M 128 N 64 from shared memory takes 80 to 90 cycles here (32 by the rate), and the warp that issues them
-// stands meanwhile.  8,192 tokens of 64 heads, causal: 1.45 ms, 757 TFLOP/s; 2,048 after 14,336 of 32 heads, each its own keys: 0.66 ms, 778.
+// stands meanwhile.  8,192 tokens of 64 heads, causal: 1.45 to 1.48 ms between GPUs, 743 to 760 TFLOP/s; 2,048 after 14,337 of 32 heads, each its own keys: 0.66 to
+// 0.70 ms, 738 to 778.
 //
 // All blocks of all units, and OVERHEAD more for each unit, stand in one line, cut into equal shares for one CTA an SM.  (Without the overhead the CTAs with the
 // first tiles of a prompt, of a few blocks each, came last: 8,192 tokens of 64 heads 1.82 ms.)  A unit that is cut leaves its parts in the
